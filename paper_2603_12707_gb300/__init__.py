@@ -8,4 +8,4 @@ seeded synthetic inputs and ``harness`` drives a decode session through the
 C ABI.  Importing this package loads nothing; the library is loaded on first
 use and its absence is an error.
 """
-__all__ = ["kvdecode", "workloads", "harness"]
+__all__ = ["kvdecode", "kv4", "workloads", "harness"]

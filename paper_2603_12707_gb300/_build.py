@@ -16,7 +16,8 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libkvdecode.so")
-SOURCES = ["kvd_host.cpp", "kvd_rules.cpp", "kvd_cache.cu", "kvd_decode.cu", "kvd_merge.cu", "kvd_cluster.cu", "kvd_noalloc.cu"]
+SOURCES = ["kvd_host.cpp", "kvd_rules.cpp", "kvd_cache.cu", "kvd_decode.cu", "kvd_merge.cu", "kvd_cluster.cu", "kvd_noalloc.cu",
+           "kvd_tables.cu", "kvd_kv4_rows.cu", "kvd_kv4_attention.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -29,7 +30,7 @@ def nvcc() -> str:
 
 def _inputs():
     files = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
-    files.append(os.path.join(INCLUDE, "kvdecode.h"))
+    files += [os.path.join(INCLUDE, f) for f in ("kvdecode.h", "kvdecode4.h")]
     files.append(os.path.abspath(__file__))
     return files
 
