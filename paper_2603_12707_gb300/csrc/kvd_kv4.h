@@ -8,6 +8,7 @@
 #include <stdint.h>
 
 #include "kvd_internal.h"
+#include "kvd_ptx.cuh"
 #include "kvdecode4.h"
 
 namespace kvd {
@@ -73,22 +74,12 @@ __host__ inline int64_t kv4_block_bytes(const kv4_pool& p) { return 16 * p.head_
 struct Bf16 {
     static __device__ __forceinline__ float lo(uint32_t w) { return __uint_as_float(w << 16); }
     static __device__ __forceinline__ float hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-    static __device__ __forceinline__ uint32_t pack(float a, float b)
-    {
-        uint32_t r;
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
-        return r;
-    }
+    static __device__ __forceinline__ uint32_t pack(float a, float b) { return pack_bf16(a, b); }
 };
 struct Fp16 {
     static __device__ __forceinline__ float lo(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w & 0xffffu))); }
     static __device__ __forceinline__ float hi(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w >> 16))); }
-    static __device__ __forceinline__ uint32_t pack(float a, float b)
-    {
-        uint32_t r;
-        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
-        return r;
-    }
+    static __device__ __forceinline__ uint32_t pack(float a, float b) { return pack_f16(a, b); }
 };
 
 __device__ __forceinline__ void kv4_error(int32_t* err, int32_t bit)

@@ -1,9 +1,36 @@
 // kv4_decode_attention: single-token decode attention over the 4-bit paged
 // cache (layout: kvdecode4.h).
 //
-// One CTA per (row, KV head).  Its warps take tokens in turn; each keeps a
-// running maximum, sum and output (an online softmax) for the G query heads of
-// the KV head, and the warps' results are merged in shared memory.
+// With K_td = s_t (c_td - 8) + z_t and V_td = s'_t (c'_td - 8) + z'_t over the
+// elements d of a scale group, a query row n (scaled to log2 units) has
+//
+//     S_tn = sum_groups s_t * sum_d q_nd (c_td - 8) + z_t * sum_d q_nd
+//     o_nd = sum_t (p_tn s'_t) (c'_td - 8) + sum_t p_tn z'_t,   p_tn = 2^(S_tn - m_n)
+//
+// so scales and middles multiply scores and weights, 16 per page, and the codes
+// go into the tensor cores as they are: a 4-bit code under a mask is an fp16
+// subnormal, c * 2^-24 in bits 0-3 and c * 2^-20 in bits 4-7, whose product with
+// another fp16 is exact.  Eight codes take five instructions to become four
+// operands.  The other operand is q, scaled by a power of two into fp16's range
+// (divided by 16 where it meets bits 4-7), or p * s', relative to a power of
+// two 2^E that follows the largest s'.  The 8 is subtracted by starting QK's
+// accumulators at -8 sum q, and for PV by one more product with rows of -8 (so
+// that p * s' is rounded once for both).
+//
+// Schedule.  The work is the list of all (row, KV head, page) tiles, a row's
+// heads in turn and a head's pages in order.  Every warp of a persistent grid
+// takes an equal, consecutive share of it, found from a scan over the rows'
+// lengths in shared memory: no plan, no host lengths, and rows of any
+// raggedness give equal shares.  A tile is one consecutive block of the pool,
+// streamed by one bulk copy into the warp's ring of shared memory; K is the
+// MMA's 16-row operand (its rows are the 16 tokens of the page), V^T's rows are
+// elements, the G <= 8 query heads are the 8 columns of both.
+//
+// A (row, KV head) that lies in one warp's share is written by that warp.
+// Others leave (o, m, l) per warp in shared memory, where the CTA merges what
+// it holds; what crosses CTAs goes through the workspace and the last CTA to
+// arrive (a counter per first CTA, which it sets back to zero) merges the parts in
+// the order of the list.
 #include <cmath>
 
 #include "kvd_kv4.h"
@@ -12,7 +39,12 @@
 namespace kvd {
 namespace {
 
-constexpr int kAttnWarps = 4;
+constexpr uint64_t kWaitLimitNs = 1000000000ull;
+constexpr float kLn2 = 0.6931471805599453f;
+// Tiles that a warp takes at least: a small call uses fewer warps rather than merge more parts.
+constexpr int kMinTiles = 2;
+
+constexpr int kCtasPerSm = 2;
 
 struct AttnArgs {
     const uint8_t* pool;
@@ -26,97 +58,673 @@ struct AttnArgs {
     uint16_t* out;
     int64_t q_stride, out_stride;
     float* lse;
-    float scale_log2;
+    float scale;         // softmax scale * log2(e) * 2^24 (the accumulators' unit)
+    int32_t* counters;   // [grid]: CTAs that have left their part of the row that starts in CTA i; zero between calls
+    float* parts;        // [grid][2][G][D + 2]: a CTA's part of the row that began before it, and of the one that goes on
     int32_t* err;
 };
 
+// The shape of a variant: warps per CTA, CTAs per SM, ring stages per warp.
+template <int D, int NG>
+struct AttnShape {
+    static constexpr int kWarps = NG == 4 ? 6 : 8;
+    static constexpr int kCtas = kCtasPerSm;
+    static constexpr int kStages = D == 64 ? 8 : 4;
+    static constexpr int kRing = kStages * Kv4Block<D, NG>::kBytes;   // of one warp
+};
+
+// A warp's part of a (row, KV head) that other warps hold parts of, too.
+struct PartInfo {
+    int32_t b, h;       // b < 0: none
+    int32_t begins, ends;
+};
+
+__host__ __device__ constexpr int part_floats(int G, int D) { return G * (D + 2); }   // o [G][D], m [G], l [G]
+
+template <int D, int NG>
+struct AttnSmem {   // byte offsets in dynamic shared memory
+    using S = AttnShape<D, NG>;
+    static constexpr int kBars = S::kWarps * S::kRing;
+    static constexpr int kInfo = kBars + S::kWarps * S::kStages * 8;
+    static constexpr int kHeads = kInfo + S::kWarps * 2 * (int)sizeof(PartInfo);   // a warp's first part: [kWarps][part_floats]
+    __host__ __device__ static constexpr int pages(int G) { return kHeads + S::kWarps * part_floats(G, D) * 4; }   // [batch + 1]
+    __host__ __device__ static constexpr int last(int G, int batch) { return pages(G) + (batch + 1) * 4; }         // [batch] bytes
+    __host__ __device__ static constexpr int bytes(int G, int batch) { return last(G, batch) + batch; }
+};
+
+// What a lane knows of one tile.
+struct Tile {
+    const uint8_t* src;
+    int32_t b, h;
+    int32_t bits;     // valid tokens (0 .. 16), kFirst / kLast page of its (row, KV head)
+    static constexpr int kFirst = 32, kLast = 64;
+};
+
+// The running state of a warp for one (row, KV head): lane (g = lane / 4, j =
+// lane % 4) holds columns n = 2j and 2j + 1 of everything, tokens g and g + 8 of a
+// page's scores, elements 16 mt + g and 16 mt + g + 8 of the output.
 template <int D, int NG, class T>
-__global__ void __launch_bounds__(kAttnWarps * 32) attention_kernel(AttnArgs a)
-{
+struct State {
     using B = Kv4Block<D, NG>;
-    constexpr int E = D / 32, NW = D / 32, GL = 32 / NG;
-    __shared__ float so[kAttnWarps][kMaxGroup][D];
-    __shared__ float sm[kAttnWarps][kMaxGroup], sl[kAttnWarps][kMaxGroup];
-    griddep_wait();
-    griddep_launch_dependents();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int b = blockIdx.x / a.H, h = blockIdx.x % a.H;
-    const int seq = a.seq_ids ? a.seq_ids[b] : b;
-    int len = seq >= 0 && seq < a.max_seqs ? a.lens[seq] : -1;
-    if (len < 0 || len > (int64_t)a.max_pages * kPageSize) {
-        if (threadIdx.x == 0) kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
-        len = 0;
-    }
-    float q[kMaxGroup][E], o[kMaxGroup][E], m[kMaxGroup], l[kMaxGroup];
-    for (int n = 0; n < kMaxGroup; ++n) {
-        m[n] = -INFINITY;
-        l[n] = 0.f;
-        for (int i = 0; i < E; ++i) {
-            o[n][i] = 0.f;
-            const uint16_t x = n < a.G ? a.q[b * a.q_stride + (int64_t)(h * a.G + n) * D + lane * E + i] : 0;
-            q[n][i] = T::lo(x) * a.scale_log2;
+    static constexpr int NW = D / 32;     // code words of a lane per 8 tokens
+    static constexpr int MT = D / 16;     // 16-element tiles of the output
+    uint32_t qf[2 * NW][2];               // q as the K product's column operand
+    float qsum[NG][2];                    // sum of q over a group, in the accumulators' units
+    float qback[2];                       // undoes q's power of two
+    float m[2], l[2];
+    float o[MT][4], e[NG][4], z[NG][2];
+    float vs, vlimit;                     // 2^-E, and the scale above which E moves
+
+    __device__ __forceinline__ void start(const AttnArgs& a, int b, int h, int lane)
+    {
+        const int n = lane >> 2, j = lane & 3;
+        uint4 w[NW];
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+            w[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (n < a.G)
+                w[i] = *reinterpret_cast<const uint4*>(a.q + b * a.q_stride + (int64_t)(h * a.G + n) * D + 32 * i + 8 * j);
         }
-    }
-    for (int t = warp; t < len; t += kAttnWarps) {
-        const int32_t page = a.block_table[(int64_t)seq * a.max_pages + t / kPageSize];
-        if (page < 0 || page >= a.num_pages) {
-            if (lane == 0) kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
-            continue;
+        float x[NW][8], top = 0.f;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+            const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                x[i][2 * k] = T::lo(u[k]);
+                x[i][2 * k + 1] = T::hi(u[k]);
+                top = fmaxf(top, fmaxf(fabsf(x[i][2 * k]), fabsf(x[i][2 * k + 1])));
+            }
         }
-        const uint8_t* block = a.pool + ((int64_t)page * a.H + h) * B::kBytes;
-        const int s = t % kPageSize;
-        const uint32_t* scales = reinterpret_cast<const uint32_t*>(block + 2 * B::kCodes) + s * NG + lane / GL;
-        const uint32_t mk = scales[0], mv = scales[kPageSize * NG];
-        float k[E], v[E];
-        for (int i = 0; i < E; ++i) {
-            const int d = lane * E + i, e = d % 8, j = (d / 8) % 4, w = d / 32;
-            const uint32_t kw = reinterpret_cast<const uint32_t*>(block)[(s * 4 + j) * NW + w];
-            k[i] = T::lo(mk) * ((float)((kw >> (16 * (e & 1) + 4 * (e >> 1))) & 15) - 8.f) + T::hi(mk);
-            const uint32_t vw = reinterpret_cast<const uint32_t*>(block + B::kCodes)[((s / 8 * 8 + e) * 4 + (s % 8) / 2) * NW + w];
-            v[i] = T::lo(mv) * ((float)((vw >> (16 * (s & 1) + 4 * j)) & 15) - 8.f) + T::hi(mv);
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // 2^up takes the row's largest |q| into [2^14, 2^15); a row of zeros, or one that is not finite, stays as it is.
+        const int ex = (int)(__float_as_uint(top) >> 23);
+        const int up = top == 0.f || ex == 255 ? 0 : max(-126, min(126, 14 + 127 - ex));
+        const float mul = __uint_as_float((uint32_t)(127 + up) << 23), back = __uint_as_float((uint32_t)(127 - up) << 23);
+        float sums[NG];
+#pragma unroll
+        for (int k = 0; k < NG; ++k) sums[k] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                // pair k of a word: elements 2k and 2k + 1, at bits 4k; odd k meets c * 2^-20
+                const float f = k & 1 ? mul * 0.0625f : mul;
+                const uint32_t p = pack_f16(x[i][2 * k] * f, x[i][2 * k + 1] * f);
+                qf[2 * i + (k >> 1)][k & 1] = p;
+                sums[i / (NW / NG)] += (Fp16::lo(p) + Fp16::hi(p)) * (k & 1 ? 16.f : 1.f);
+            }
         }
 #pragma unroll
-        for (int n = 0; n < kMaxGroup; ++n) {
-            if (n >= a.G) break;
-            float x = 0.f;
-            for (int i = 0; i < E; ++i) x += q[n][i] * k[i];
-            for (int mask = 1; mask < 32; mask <<= 1) x += __shfl_xor_sync(0xffffffffu, x, mask);
-            const float top = fmaxf(m[n], x), al = exp2f(m[n] - top), p = exp2f(x - top);
-            m[n] = top;
-            l[n] = l[n] * al + p;
-            for (int i = 0; i < E; ++i) o[n][i] = o[n][i] * al + p * v[i];
+        for (int k = 0; k < NG; ++k) {
+            sums[k] += __shfl_xor_sync(0xffffffffu, sums[k], 1);
+            sums[k] += __shfl_xor_sync(0xffffffffu, sums[k], 2);
+            sums[k] *= 0x1p-24f;
+            qsum[k][0] = __shfl_sync(0xffffffffu, sums[k], 8 * j);
+            qsum[k][1] = __shfl_sync(0xffffffffu, sums[k], 8 * j + 4);
+        }
+        qback[0] = __shfl_sync(0xffffffffu, back, 8 * j);
+        qback[1] = __shfl_sync(0xffffffffu, back, 8 * j + 4);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            m[c] = -INFINITY;
+            l[c] = 0.f;
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) o[mt][c] = 0.f;
+#pragma unroll
+        for (int k = 0; k < NG; ++k) {
+            z[k][0] = z[k][1] = 0.f;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) e[k][c] = 0.f;
+        }
+        vs = 0x1p100f;
+        vlimit = -1.f;   // below any |s'|: the first page sets E
+    }
+
+    static __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[NW])
+    {
+        if constexpr (NW == 4) {
+            const uint4 u = *reinterpret_cast<const uint4*>(p);
+            w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+        } else {
+            const uint2 u = *reinterpret_cast<const uint2*>(p);
+            w[0] = u.x, w[1] = u.y;
         }
     }
-    for (int n = 0; n < kMaxGroup; ++n) {
-        for (int i = 0; i < E; ++i) so[warp][n][lane * E + i] = o[n][i];
-        if (lane == 0) {
-            sm[warp][n] = m[n];
-            sl[warp][n] = l[n];
+
+    static __device__ __forceinline__ void load_scales(const uint8_t* p, uint32_t (&w)[NG])
+    {
+        if constexpr (NG == 4) {
+            const uint4 u = *reinterpret_cast<const uint4*>(p);
+            w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+        } else if constexpr (NG == 2) {
+            const uint2 u = *reinterpret_cast<const uint2*>(p);
+            w[0] = u.x, w[1] = u.y;
+        } else {
+            w[0] = *reinterpret_cast<const uint32_t*>(p);
+        }
+    }
+
+    // One page in shared memory, `valid` of whose tokens count (1 .. 16).
+    __device__ __forceinline__ void page(const uint8_t* st, int valid, float scale, int lane)
+    {
+        const int g = lane >> 2;
+        uint32_t ka[NW], kb[NW], mk[2][NG], mv[2][NG];
+        load_words(st + lane * NW * 4, ka);
+        load_words(st + (32 + lane) * NW * 4, kb);
+        const uint8_t* sc = st + 2 * B::kCodes + g * NG * 4;
+        load_scales(sc, mk[0]);
+        load_scales(sc + 8 * NG * 4, mk[1]);
+        load_scales(sc + B::kScales, mv[0]);
+        load_scales(sc + B::kScales + 8 * NG * 4, mv[1]);
+
+        float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < NG; ++k) {
+            const float c0 = -8.f * qsum[k][0], c1 = -8.f * qsum[k][1];
+            float acc[4] = {c0, c1, c0, c1};
+#pragma unroll
+            for (int i = k * (NW / NG); i < (k + 1) * (NW / NG); ++i) {
+                const uint32_t a8 = ka[i] >> 8, b8 = kb[i] >> 8;
+                mma_f16_16816(acc, ka[i] & 0x000f000fu, kb[i] & 0x000f000fu, ka[i] & 0x00f000f0u, kb[i] & 0x00f000f0u,
+                              qf[2 * i][0], qf[2 * i][1]);
+                mma_f16_16816(acc, a8 & 0x000f000fu, b8 & 0x000f000fu, a8 & 0x00f000f0u, b8 & 0x00f000f0u,
+                              qf[2 * i + 1][0], qf[2 * i + 1][1]);
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const float ss = T::lo(mk[t][k]), sz = T::hi(mk[t][k]);
+                s[2 * t] += ss * acc[2 * t] + sz * qsum[k][0];
+                s[2 * t + 1] += ss * acc[2 * t + 1] + sz * qsum[k][1];
+            }
+        }
+        uint32_t va[NW], vb[NW];
+        load_words(st + B::kCodes + lane * NW * 4, va);
+        load_words(st + B::kCodes + (32 + lane) * NW * 4, vb);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) s[c] = (s[c] * scale) * qback[c & 1];
+        if (valid < kPageSize) {   // slots past the end may hold anything
+            if (g >= valid) {
+                s[0] = s[1] = -INFINITY;
+#pragma unroll
+                for (int k = 0; k < NG; ++k) mv[0][k] = 0u;
+            }
+            if (g + 8 >= valid) {
+                s[2] = s[3] = -INFINITY;
+#pragma unroll
+                for (int k = 0; k < NG; ++k) mv[1][k] = 0u;
+            }
+        }
+        // The references m and E move only when a score passes m by more than
+        // 8 (log2 units) or a scale its limit: weights stay below 2^8, weights times scales
+        // below 2^15, and most pages skip the reductions and the rescale.
+        float vmax = 0.f;
+#pragma unroll
+        for (int k = 0; k < NG; ++k) vmax = fmaxf(vmax, fmaxf(fabsf(T::lo(mv[0][k])), fabsf(T::lo(mv[1][k]))));
+        float pm0 = fmaxf(s[0], s[2]), pm1 = fmaxf(s[1], s[3]);
+        if (__any_sync(0xffffffffu, pm0 > m[0] + 8.f || pm1 > m[1] + 8.f || vmax > vlimit)) {
+#pragma unroll
+            for (int mask = 4; mask < 32; mask <<= 1) {
+                pm0 = fmaxf(pm0, __shfl_xor_sync(0xffffffffu, pm0, mask));
+                pm1 = fmaxf(pm1, __shfl_xor_sync(0xffffffffu, pm1, mask));
+                vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, mask));
+            }
+            const float n0 = fmaxf(m[0], pm0), n1 = fmaxf(m[1], pm1);
+            const float al0 = n0 == m[0] ? 1.f : ex2(m[0] - n0), al1 = n1 == m[1] ? 1.f : ex2(m[1] - n1);
+            m[0] = n0;
+            m[1] = n1;
+            float r = 1.f;
+            if (vmax > vlimit) {   // the same in all lanes
+                const int ex = max(-100, (int)(__float_as_uint(vmax) >> 23) - 127);
+                const float next = __uint_as_float((uint32_t)(127 + 6 - ex) << 23);   // takes vmax into [2^6, 2^7)
+                r = next / vs;
+                vs = next;
+                vlimit = 128.f / next;
+            }
+            l[0] *= al0;
+            l[1] *= al1;
+#pragma unroll
+            for (int k = 0; k < NG; ++k) {
+                z[k][0] *= al0;
+                z[k][1] *= al1;
+                e[k][0] *= al0 * r;
+                e[k][1] *= al1 * r;
+            }
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                o[mt][0] *= al0 * r;
+                o[mt][1] *= al1 * r;
+                o[mt][2] *= al0 * r;
+                o[mt][3] *= al1 * r;
+            }
+        }
+        const float p0 = ex2(s[0] - m[0]), p1 = ex2(s[1] - m[1]), p2 = ex2(s[2] - m[0]), p3 = ex2(s[3] - m[1]);
+        l[0] += p0 + p2;
+        l[1] += p1 + p3;
+#pragma unroll
+        for (int k = 0; k < NG; ++k) {
+            const float s0 = T::lo(mv[0][k]) * vs, s1 = T::lo(mv[1][k]) * vs;
+            const float z0 = T::hi(mv[0][k]), z1 = T::hi(mv[1][k]);
+            z[k][0] += p0 * z0 + p2 * z1;
+            z[k][1] += p1 * z0 + p3 * z1;
+            // (p s')^T as the column operand: the packed pairs are 8x8 tiles
+            // [token][n] in the fragment layout, their transposes are the operand.
+            const uint32_t b0 = movmatrix_trans(pack_f16(p0 * s0, p1 * s0));
+            const uint32_t b1 = movmatrix_trans(pack_f16(p2 * s1, p3 * s1));
+            mma_f16_16816(e[k], 0xc800c800u, 0xc800c800u, 0xc800c800u, 0xc800c800u, b0, b1);   // -8 everywhere
+#pragma unroll
+            for (int i = k * (NW / NG); i < (k + 1) * (NW / NG); ++i) {
+                const uint32_t a8 = va[i] >> 8, b8 = vb[i] >> 8;
+                mma_f16_16816(o[2 * i], va[i] & 0x000f000fu, va[i] & 0x00f000f0u, vb[i] & 0x000f000fu, vb[i] & 0x00f000f0u, b0, b1);
+                mma_f16_16816(o[2 * i + 1], a8 & 0x000f000fu, a8 & 0x00f000f0u, b8 & 0x000f000fu, b8 & 0x00f000f0u, b0, b1);
+            }
+        }
+    }
+
+    // The sums over all lanes' tokens; o is then the unnormalised output.
+    __device__ __forceinline__ void finish()
+    {
+#pragma unroll
+        for (int mask = 4; mask < 32; mask <<= 1) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                l[c] += __shfl_xor_sync(0xffffffffu, l[c], mask);
+#pragma unroll
+                for (int k = 0; k < NG; ++k) z[k][c] += __shfl_xor_sync(0xffffffffu, z[k][c], mask);
+            }
+        }
+        const float back = 1.f / vs;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int k = mt / (MT / NG);
+                o[mt][c] = (o[mt][c] * (c < 2 ? 0x1p24f : 0x1p20f) + e[k][c & 1]) * back + z[k][c & 1];
+            }
+    }
+
+    __device__ __forceinline__ void write_out(const AttnArgs& a, int b, int h, int lane) const
+    {
+        const int g = lane >> 2;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int n = 2 * (lane & 3) + c;
+            if (n >= a.G) continue;
+            const float inv = l[c] == 0.f ? 0.f : 1.f / l[c];
+            uint16_t* out = a.out + b * a.out_stride + (int64_t)(h * a.G + n) * D + g;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                const uint32_t w = T::pack(o[mt][c] * inv, o[mt][c + 2] * inv);
+                out[16 * mt] = (uint16_t)w;
+                out[16 * mt + 8] = (uint16_t)(w >> 16);
+            }
+            if (a.lse && g == 0) a.lse[(int64_t)b * a.Hq + h * a.G + n] = (m[c] + log2f(l[c])) * kLn2;
+        }
+    }
+
+    __device__ __forceinline__ void write_part(float* part, int G, int lane) const
+    {
+        const int g = lane >> 2;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int n = 2 * (lane & 3) + c;
+            if (n >= G) continue;
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                part[n * D + 16 * mt + g] = o[mt][c];
+                part[n * D + 16 * mt + 8 + g] = o[mt][c + 2];
+            }
+            if (g == 0) {
+                part[G * D + n] = m[c];
+                part[G * (D + 1) + n] = l[c];
+            }
+        }
+    }
+};
+
+// One query row of a part: o elements lane * E .. of this lane, m and l.
+template <int D>
+struct RowSum {
+    static constexpr int E = D / 32;
+    float o[E], m, l;
+    __device__ __forceinline__ RowSum() : m(-INFINITY), l(0.f)
+    {
+#pragma unroll
+        for (int i = 0; i < E; ++i) o[i] = 0.f;
+    }
+    __device__ __forceinline__ void add(const float (&x)[E], float mx, float lx)
+    {
+        const float top = fmaxf(m, mx);
+        const float a = m == top ? 1.f : ex2(m - top), b = mx == top ? 1.f : ex2(mx - top);
+        m = top;
+        l = l * a + lx * b;
+#pragma unroll
+        for (int i = 0; i < E; ++i) o[i] = o[i] * a + x[i] * b;
+    }
+    template <class T>
+    __device__ __forceinline__ void write_out(const AttnArgs& a, int b, int h, int n, int lane) const
+    {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        uint16_t* out = a.out + b * a.out_stride + (int64_t)(h * a.G + n) * D + lane * E;
+#pragma unroll
+        for (int i = 0; i < E; i += 2) *reinterpret_cast<uint32_t*>(out + i) = T::pack(o[i] * inv, o[i + 1] * inv);
+        if (a.lse && lane == 0) a.lse[(int64_t)b * a.Hq + h * a.G + n] = (m + log2f(l)) * kLn2;
+    }
+};
+
+template <int D, int NG, class T>
+__global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, AttnShape<D, NG>::kCtas) attention_kernel(AttnArgs a)
+{
+    using S = AttnShape<D, NG>;
+    using B = Kv4Block<D, NG>;
+    using M = AttnSmem<D, NG>;
+    constexpr int W = S::kWarps, R = S::kStages, E = D / 32;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ uint32_t warp_pages[W];
+    __shared__ int arrived[2];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    uint8_t* ring = smem + warp * S::kRing;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + M::kBars) + warp * R;
+    PartInfo* infos = reinterpret_cast<PartInfo*>(smem + M::kInfo);
+    float* heads = reinterpret_cast<float*>(smem + M::kHeads);
+    uint32_t* pages = reinterpret_cast<uint32_t*>(smem + M::pages(a.G));   // pages of the rows before each row
+    uint8_t* last = smem + M::last(a.G, a.batch);                          // tokens on each row's last page
+    if (lane < R) mbar_init(smem_addr(bars + lane), 1);
+    fence_mbar_init();
+    if (tid < 2 * W) infos[tid].b = -1;
+    griddep_wait();
+    griddep_launch_dependents();
+
+    // Pages of the rows before each row.
+    if (tid == 0) pages[0] = 0;
+    uint64_t before = 0;
+    for (int r0 = 0; r0 < a.batch; r0 += W * 32) {
+        const int r = r0 + tid;
+        uint32_t n = 0;
+        if (r < a.batch) {
+            const int seq = a.seq_ids ? a.seq_ids[r] : r;
+            int len = seq >= 0 && seq < a.max_seqs ? a.lens[seq] : -1;
+            if (len < 0 || len > a.max_pages * kPageSize) {
+                if (blockIdx.x == 0) kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
+                len = 0;
+            }
+            n = (uint32_t)(len + kPageSize - 1) / kPageSize;
+            last[r] = (uint8_t)(len - ((int)n - 1) * kPageSize);
+        }
+        uint32_t sum = n;
+#pragma unroll
+        for (int k = 1; k < 32; k <<= 1) {
+            const uint32_t up = __shfl_up_sync(0xffffffffu, sum, k);
+            if (lane >= k) sum += up;
+        }
+        if (lane == 31) warp_pages[warp] = sum;
+        __syncthreads();
+        uint64_t mine = before;
+#pragma unroll
+        for (int w = 0; w < W; ++w) {
+            if (w < warp) mine += warp_pages[w];
+            before += warp_pages[w];
+        }
+        if (r < a.batch) pages[r + 1] = (uint32_t)(mine + sum);
+        __syncthreads();
+    }
+
+    if (before > 0xffffffffull) {   // the same in all threads
+        if (blockIdx.x == 0 && tid == 0) kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
+        return;
+    }
+
+    // Shares: the first `extra` warps take one tile more than the others.
+    const int64_t total = (int64_t)before * a.H;
+    const int64_t warps = min((int64_t)gridDim.x * W, (total + kMinTiles - 1) / kMinTiles);
+    const int64_t base = warps ? total / warps : 0, extra = warps ? total % warps : 0;
+    const int64_t me = (int64_t)blockIdx.x * W + warp;
+    const int64_t lo = me * base + min(me, extra);
+    const int64_t count = me < warps ? base + (me < extra) : 0;
+    auto cta_of = [&](int64_t at) {   // the CTA whose share holds a tile
+        const int64_t long_ones = extra * (base + 1);
+        return (int)((at < long_ones ? at / (base + 1) : extra + (at - long_ones) / base) / W);
+    };
+    const uint64_t policy = l2_policy_evict_first();
+
+    auto tile_of = [&](int64_t i) {   // tile i of this warp's share
+        Tile t{a.pool, 0, 0, 0};
+        if (i >= count) return t;
+        const int64_t at = lo + i, page_row = at / a.H;
+        int r0 = 0, r1 = a.batch;     // the last row with pages[row] <= page_row that is not empty
+        while (r1 - r0 > 1) {
+            const int mid = (r0 + r1) >> 1;
+            if ((int64_t)pages[mid] <= page_row) r0 = mid;
+            else r1 = mid;
+        }
+        const uint32_t first = pages[r0], n = pages[r0 + 1] - first;
+        const int64_t in_row = at - (int64_t)first * a.H;
+        const int p = (int)(in_row % n);
+        t.b = r0;
+        t.h = (int)(in_row / n);
+        const int seq = a.seq_ids ? a.seq_ids[r0] : r0;
+        const int32_t page = a.block_table[(int64_t)seq * a.max_pages + p];
+        int valid = p == (int)n - 1 ? last[r0] : kPageSize;
+        if (page >= 0 && page < a.num_pages) {
+            t.src = a.pool + ((int64_t)page * a.H + t.h) * B::kBytes;
+        } else {                      // read page 0 in its place, and leave its tokens out
+            kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
+            valid = 0;
+        }
+        t.bits = valid | (p == 0 ? Tile::kFirst : 0) | (p == (int)n - 1 ? Tile::kLast : 0);
+        return t;
+    };
+    uint32_t pending = 0, phase = 0;
+    auto issue = [&](const Tile& t, int stage) {   // by the lane that holds the tile
+        const uint32_t bar = smem_addr(bars + stage);
+        mbar_arrive_expect_tx(bar, B::kBytes);
+        bulk_load(smem_addr(ring + stage * B::kBytes), t.src, B::kBytes, bar, policy);
+    };
+
+    __syncwarp();
+    Tile cur = tile_of(lane), next = cur;
+    if (lane < R && lane < count) issue(cur, lane);
+    pending = (1u << (count < R ? (int)count : R)) - 1u;
+    State<D, NG, T> st;
+    bool ok = true, begins = true;
+    for (int64_t i = 0; i < count; ++i) {
+        const int src = (int)i & 31, stage = (int)(i % R);
+        if (src == 0) {
+            if (i) cur = next;
+            next = tile_of(i + 32 + lane);
+        }
+        const int bits = __shfl_sync(0xffffffffu, cur.bits, src);
+        const bool first = (bits & Tile::kFirst) || i == 0, end = (bits & Tile::kLast) || i == count - 1;
+        const int b = __shfl_sync(0xffffffffu, cur.b, src), h = __shfl_sync(0xffffffffu, cur.h, src);
+        if (first) {
+            begins = bits & Tile::kFirst;
+            st.start(a, b, h, lane);
+        }
+        if (ok && !__all_sync(0xffffffffu, mbar_wait_bounded(smem_addr(bars + stage), (phase >> stage) & 1u, kWaitLimitNs))) {
+            ok = false;   // the rest of the share is left out
+            if (lane == 0) kv4_error(a.err, KVC_DEVERR_WAIT_TIMEOUT);
+        }
+        if (ok) {
+            phase ^= 1u << stage;
+            pending &= ~(1u << stage);
+            if (bits & 31) st.page(ring + stage * B::kBytes, bits & 31, a.scale, lane);
+            __syncwarp();
+            if (i + R < count) {
+                if (lane == ((int)(i + R) & 31)) issue(src + R < 32 ? cur : next, stage);
+                pending |= 1u << stage;
+            }
+        }
+        if (end) {
+            st.finish();
+            const bool ends = bits & Tile::kLast;
+            if (begins && ends) {
+                st.write_out(a, b, h, lane);
+            } else {
+                // A part that is not the share's last one began before it.
+                if (i == count - 1) {
+                    for (int s = 0; s < R; ++s)   // (only after a wait that gave up)
+                        if (pending & (1u << s)) mbar_wait_bounded(smem_addr(bars + s), (phase >> s) & 1u, kWaitLimitNs);
+                    pending = 0;
+                    __syncwarp();
+                }
+                const int k = i == count - 1 ? 1 : 0;
+                st.write_part(k ? reinterpret_cast<float*>(ring) : heads + warp * part_floats(a.G, D), a.G, lane);
+                if (lane == 0) infos[2 * warp + k] = {b, h, begins, ends};
+            }
+        }
+    }
+    for (int s = 0; s < R; ++s)
+        if (pending & (1u << s)) mbar_wait_bounded(smem_addr(bars + s), (phase >> s) & 1u, kWaitLimitNs);
+
+    // Rows without tokens.
+    for (int r = blockIdx.x; r < a.batch; r += gridDim.x)
+        if (pages[r] == pages[r + 1]) {
+            for (int i = tid; i < a.Hq * (D / 8); i += W * 32)
+                *reinterpret_cast<uint4*>(a.out + r * a.out_stride + i * 8) = make_uint4(0u, 0u, 0u, 0u);
+            if (a.lse)
+                for (int i = tid; i < a.Hq; i += W * 32) a.lse[(int64_t)r * a.Hq + i] = -INFINITY;
+        }
+    __syncthreads();
+
+    // Merge this CTA's parts: one (group of adjacent parts, query row) per warp and turn.
+    const int PF = part_floats(a.G, D);
+    auto part_of = [&](int e) {
+        return e & 1 ? reinterpret_cast<const float*>(smem + (e >> 1) * S::kRing) : heads + (e >> 1) * PF;
+    };
+    int turn = 0, open[2] = {-1, -1};   // entries of the groups that go on before and after this CTA
+    for (int e = 0; e < 2 * W;) {
+        if (infos[e].b < 0) {
+            ++e;
+            continue;
+        }
+        int f = e + 1, ends = infos[e].ends;
+        for (; f < 2 * W && !ends; ++f)
+            if (infos[f].b >= 0) ends = infos[f].ends;
+        const PartInfo& in = infos[e];
+        const int slot = in.begins ? 1 : 0;
+        const bool whole = in.begins && ends;
+        if (!whole) open[slot] = e;
+        for (int n = 0; n < a.G; ++n, ++turn) {
+            if (turn % W != warp) continue;
+            RowSum<D> sum;
+            for (int k = e; k < f; ++k) {
+                if (infos[k].b < 0) continue;
+                const float* p = part_of(k);
+                float x[E];
+#pragma unroll
+                for (int i = 0; i < E; ++i) x[i] = p[n * D + lane * E + i];
+                sum.add(x, p[a.G * D + n], p[a.G * (D + 1) + n]);
+            }
+            if (whole) {
+                sum.template write_out<T>(a, in.b, in.h, n, lane);
+            } else {
+                float* to = a.parts + ((int64_t)blockIdx.x * 2 + slot) * PF;
+#pragma unroll
+                for (int i = 0; i < E; ++i) to[n * D + lane * E + i] = sum.o[i];
+                if (lane == 0) {
+                    to[a.G * D + n] = sum.m;
+                    to[a.G * (D + 1) + n] = sum.l;
+                }
+            }
+        }
+        e = f;
+    }
+    if (open[0] < 0 && open[1] < 0) return;
+
+    // What crosses CTAs: the last one to arrive merges it.
+    auto ctas_of = [&](const PartInfo& in, int* c0, int* c1) {
+        const int64_t n = pages[in.b + 1] - pages[in.b], first = (int64_t)pages[in.b] * a.H + in.h * n;
+        *c0 = cta_of(first);
+        *c1 = cta_of(first + n - 1);
+    };
+    __syncthreads();
+    if (tid < 2) {
+        arrived[tid] = 0;
+        if (open[tid] >= 0) {
+            int c0, c1;
+            ctas_of(infos[open[tid]], &c0, &c1);
+            __threadfence();
+            if (atomicAdd(a.counters + c0, 1) == c1 - c0) {
+                a.counters[c0] = 0;
+                arrived[tid] = 1;
+            }
+            __threadfence();
         }
     }
     __syncthreads();
-    for (int n = warp; n < a.G; n += kAttnWarps) {
-        float top = -INFINITY, sum = 0.f, x[E] = {};
-        for (int w = 0; w < kAttnWarps; ++w) top = fmaxf(top, sm[w][n]);
-        for (int w = 0; w < kAttnWarps; ++w) {
-            const float al = sl[w][n] == 0.f ? 0.f : exp2f(sm[w][n] - top);
-            sum += al * sl[w][n];
-            for (int i = 0; i < E; ++i) x[i] += al * so[w][n][lane * E + i];
+    for (int k = 0; k < 2; ++k) {
+        if (!arrived[k]) continue;
+        const PartInfo& in = infos[open[k]];
+        int c0, c1;
+        ctas_of(in, &c0, &c1);
+        for (int n = warp; n < a.G; n += W) {
+            RowSum<D> sum;
+            for (int c = c0; c <= c1; ++c) {
+                const float* p = a.parts + ((int64_t)c * 2 + (c == c0 ? 1 : 0)) * PF;
+                float x[E];
+#pragma unroll
+                for (int i = 0; i < E; ++i) x[i] = __ldcg(p + n * D + lane * E + i);
+                sum.add(x, __ldcg(p + a.G * D + n), __ldcg(p + a.G * (D + 1) + n));
+            }
+            sum.template write_out<T>(a, in.b, in.h, n, lane);
         }
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        uint16_t* out = a.out + b * a.out_stride + (int64_t)(h * a.G + n) * D + lane * E;
-        for (int i = 0; i < E; ++i) out[i] = (uint16_t)T::pack(x[i] * inv, 0.f);
-        if (a.lse && lane == 0) a.lse[(int64_t)b * a.Hq + h * a.G + n] = (top + log2f(sum)) * 0.6931471805599453f;
     }
 }
 
+int device_sms()
+{
+    static std::atomic<int> known[OncePerDevice::kDevices] = {};
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    if (dev < OncePerDevice::kDevices && (n = known[dev].load(std::memory_order_relaxed))) return n;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    if (dev < OncePerDevice::kDevices) known[dev].store(n, std::memory_order_relaxed);
+    return n;
+}
+
+constexpr int kSmemPerSm = 228 * 1024, kSmemPerCta = 1024 + 128;   // what an SM has, what a CTA takes beside its dynamic part
+
+template <int D, int NG>
+struct AttnPlan {
+    using S = AttnShape<D, NG>;
+    static int ctas_per_sm(int G, int batch)
+    {
+        const int fit = kSmemPerSm / (AttnSmem<D, NG>::bytes(G, batch) + kSmemPerCta);
+        return fit < S::kCtas ? fit : S::kCtas;
+    }
+};
+
+struct WorkspaceOf {
+    int sms, G;
+    template <int D, int NG, class T>
+    int64_t operator()() const
+    {
+        const int64_t ctas = (int64_t)sms * AttnShape<D, NG>::kCtas;
+        return 256 * ((ctas * 4 + 255) / 256) + ctas * 2 * part_floats(G, D) * 4;
+    }
+};
+
 struct LaunchAttention {
-    const AttnArgs& a;
+    AttnArgs& a;
+    int sms;
     cudaStream_t st;
     template <int D, int NG, class T>
     cudaError_t operator()() const
     {
-        return kv4_launch(attention_kernel<D, NG, T>, dim3((unsigned)(a.batch * a.H)), kAttnWarps * 32, 0, st, a);
+        using S = AttnShape<D, NG>;
+        static OncePerDevice once;
+        const int smem = AttnSmem<D, NG>::bytes(a.G, a.batch);
+        constexpr int most = AttnSmem<D, NG>::bytes(kMaxGroup, kKv4MaxBatch);
+        static_assert(2 * part_floats(kMaxGroup, D) * 4 <= 2 * S::kRing && part_floats(kMaxGroup, D) * 4 <= S::kRing, "");
+        static_assert(most <= 227 * 1024, "shared memory of a CTA");
+        cudaError_t e = once.set_attribute(attention_kernel<D, NG, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+        if (e != cudaSuccess) return e;
+        const int grid = sms * AttnPlan<D, NG>::ctas_per_sm(a.G, a.batch);
+        return kv4_launch(attention_kernel<D, NG, T>, dim3((unsigned)grid), S::kWarps * 32, (size_t)smem, st, a);
     }
 };
 
@@ -129,8 +737,6 @@ int check_heads(const kv4_pool* pool, int32_t num_q_heads) noexcept
     return KVC_OK;
 }
 
-int64_t workspace_bytes_of(const kv4_pool&, int32_t) { return 256; }
-
 }  // namespace
 }  // namespace kvd
 
@@ -140,7 +746,9 @@ extern "C" KVC_API int64_t kv4_workspace_bytes(const kv4_pool* pool, int32_t num
 {
     if (int rc = kv4_check_pool(pool, false)) return rc;
     if (int rc = check_heads(pool, num_q_heads)) return rc;
-    return workspace_bytes_of(*pool, num_q_heads);
+    const int sms = device_sms();
+    if (!sms) return kv4_fail(KVC_ERR_CUDA, "kv4_workspace_bytes: cannot query the current device");
+    return kv4_dispatch(*pool, WorkspaceOf{sms, num_q_heads / pool->num_kv_heads});
 }
 
 extern "C" KVC_API int kv4_decode_attention(const kv4_pool* pool, const kv_tables* tables, int32_t batch,
@@ -161,15 +769,20 @@ extern "C" KVC_API int kv4_decode_attention(const kv4_pool* pool, const kv_table
         return kv4_fail(KVC_ERR_INVALID, "kv4_decode_attention: q_stride must be >= 0, out rows must not overlap");
     if (!(softmax_scale <= 0.f) && !std::isfinite(softmax_scale))
         return kv4_fail(KVC_ERR_INVALID, "kv4_decode_attention: softmax_scale must be finite");
-    if (!kv4_aligned(workspace, 256) || workspace_bytes < workspace_bytes_of(*pool, num_q_heads))
+    if (!kv4_aligned(workspace, 256) || workspace_bytes < 256)
         return kv4_fail(KVC_ERR_INVALID, "kv4_decode_attention: workspace must be 256-byte aligned and of kv4_workspace_bytes()");
+    const int sms = device_sms();
+    if (!sms) return kv4_fail(KVC_ERR_CUDA, "kv4_decode_attention: cannot query the current device");
+    const int G = num_q_heads / pool->num_kv_heads;
+    if (workspace_bytes < kv4_dispatch(*pool, WorkspaceOf{sms, G}))
+        return kv4_fail(KVC_ERR_INVALID, "kv4_decode_attention: the workspace is smaller than kv4_workspace_bytes()");
     const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)pool->head_dim);
     AttnArgs a{};
     a.pool = static_cast<const uint8_t*>(pool->data);
     a.num_pages = pool->num_pages;
     a.H = pool->num_kv_heads;
     a.Hq = num_q_heads;
-    a.G = num_q_heads / pool->num_kv_heads;
+    a.G = G;
     a.block_table = tables->block_table;
     a.lens = tables->lens;
     a.max_seqs = tables->max_seqs;
@@ -181,7 +794,10 @@ extern "C" KVC_API int kv4_decode_attention(const kv4_pool* pool, const kv_table
     a.q_stride = q_stride;
     a.out_stride = out_stride;
     a.lse = lse;
-    a.scale_log2 = scale * 1.4426950408889634f;
+    a.scale = scale * 1.4426950408889634f * 0x1p24f;
     a.err = device_error;
-    return kv4_launch_result(kv4_dispatch(*pool, LaunchAttention{a, static_cast<cudaStream_t>(stream)}));
+    const int64_t most = (int64_t)sms * kCtasPerSm * 4;
+    a.counters = static_cast<int32_t*>(workspace);
+    a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + 256 * ((most + 255) / 256));
+    return kv4_launch_result(kv4_dispatch(*pool, LaunchAttention{a, sms, static_cast<cudaStream_t>(stream)}));
 }
