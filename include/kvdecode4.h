@@ -151,7 +151,7 @@ KVC_API int64_t kv4_workspace_bytes(const kv4_pool *pool, int32_t num_q_heads);
  * zeros and lse = -infinity; so does one whose id is out of range or whose length is
  * negative or above max_pages * 16, with KVC_DEVERR_SEQ_RANGE.  The tokens of a
  * page id outside the pool are left out, with KVC_DEVERR_PAGE_RANGE.  Rows that
- * together pass 2^32 pages set KVC_DEVERR_SEQ_RANGE and nothing is written.  Scores,
+ * together pass 2^31 pages times KV heads set KVC_DEVERR_SEQ_RANGE and nothing is written.  Scores,
  * softmax statistics and sums are held in 32 bits; a q that is not finite
  * gives NaN.  The result of a call does not depend on timing: partial results
  * are merged in the order of their tokens. */

@@ -73,6 +73,12 @@ struct AttnShape {
     static constexpr int kRing = kStages * Kv4Block<D, NG>::kBytes;   // of one warp
 };
 
+// The rest of a wait that has not ended at once (out of line).
+__device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity)
+{
+    return mbar_wait_bounded(bar, parity, kWaitLimitNs);
+}
+
 // A warp's part of a (row, KV head) that other warps hold parts of, too.
 struct PartInfo {
     int32_t b, h;       // b < 0: none
@@ -209,119 +215,137 @@ struct State {
         }
     }
 
-    // One page in shared memory, `valid` of whose tokens count (1 .. 16).
-    __device__ __forceinline__ void page(const uint8_t* st, int valid, float scale, int lane)
+    // NP pages in shared memory; `valid` (1 .. 16) of a single page's tokens
+    // count, all of a pair's.  Two at a time share the checks and keep two chains of products in flight.
+    template <int NP>
+    __device__ __forceinline__ void pages(const uint8_t* const (&st)[NP], int valid, float scale, int lane)
     {
         const int g = lane >> 2;
-        uint32_t ka[NW], kb[NW], mk[2][NG], mv[2][NG];
-        load_words(st + lane * NW * 4, ka);
-        load_words(st + (32 + lane) * NW * 4, kb);
-        const uint8_t* sc = st + 2 * B::kCodes + g * NG * 4;
-        load_scales(sc, mk[0]);
-        load_scales(sc + 8 * NG * 4, mk[1]);
-        load_scales(sc + B::kScales, mv[0]);
-        load_scales(sc + B::kScales + 8 * NG * 4, mv[1]);
-
-        float s[4] = {0.f, 0.f, 0.f, 0.f};
+        float s[NP][4];
+        uint32_t mv[NP][2][NG];
 #pragma unroll
-        for (int k = 0; k < NG; ++k) {
-            const float c0 = -8.f * qsum[k][0], c1 = -8.f * qsum[k][1];
-            float acc[4] = {c0, c1, c0, c1};
+        for (int p = 0; p < NP; ++p) {
+            uint32_t ka[NW], kb[NW], mk[2][NG];
+            load_words(st[p] + lane * NW * 4, ka);
+            load_words(st[p] + (32 + lane) * NW * 4, kb);
+            const uint8_t* sc = st[p] + 2 * B::kCodes + g * NG * 4;
+            load_scales(sc, mk[0]);
+            load_scales(sc + 8 * NG * 4, mk[1]);
+            load_scales(sc + B::kScales, mv[p][0]);
+            load_scales(sc + B::kScales + 8 * NG * 4, mv[p][1]);
 #pragma unroll
-            for (int i = k * (NW / NG); i < (k + 1) * (NW / NG); ++i) {
-                const uint32_t a8 = ka[i] >> 8, b8 = kb[i] >> 8;
-                mma_f16_16816(acc, ka[i] & 0x000f000fu, kb[i] & 0x000f000fu, ka[i] & 0x00f000f0u, kb[i] & 0x00f000f0u,
-                              qf[2 * i][0], qf[2 * i][1]);
-                mma_f16_16816(acc, a8 & 0x000f000fu, b8 & 0x000f000fu, a8 & 0x00f000f0u, b8 & 0x00f000f0u,
-                              qf[2 * i + 1][0], qf[2 * i + 1][1]);
+            for (int c = 0; c < 4; ++c) s[p][c] = 0.f;
+#pragma unroll
+            for (int k = 0; k < NG; ++k) {
+                const float c0 = -8.f * qsum[k][0], c1 = -8.f * qsum[k][1];
+                float acc[4] = {c0, c1, c0, c1};
+#pragma unroll
+                for (int i = k * (NW / NG); i < (k + 1) * (NW / NG); ++i) {
+                    const uint32_t a8 = ka[i] >> 8, b8 = kb[i] >> 8;
+                    mma_f16_16816(acc, ka[i] & 0x000f000fu, kb[i] & 0x000f000fu, ka[i] & 0x00f000f0u, kb[i] & 0x00f000f0u,
+                                  qf[2 * i][0], qf[2 * i][1]);
+                    mma_f16_16816(acc, a8 & 0x000f000fu, b8 & 0x000f000fu, a8 & 0x00f000f0u, b8 & 0x00f000f0u,
+                                  qf[2 * i + 1][0], qf[2 * i + 1][1]);
+                }
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const float ss = T::lo(mk[t][k]), sz = T::hi(mk[t][k]);
+                    s[p][2 * t] += ss * acc[2 * t] + sz * qsum[k][0];
+                    s[p][2 * t + 1] += ss * acc[2 * t + 1] + sz * qsum[k][1];
+                }
             }
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const float ss = T::lo(mk[t][k]), sz = T::hi(mk[t][k]);
-                s[2 * t] += ss * acc[2 * t] + sz * qsum[k][0];
-                s[2 * t + 1] += ss * acc[2 * t + 1] + sz * qsum[k][1];
-            }
-        }
-        uint32_t va[NW], vb[NW];
-        load_words(st + B::kCodes + lane * NW * 4, va);
-        load_words(st + B::kCodes + (32 + lane) * NW * 4, vb);
+            for (int c = 0; c < 4; ++c) s[p][c] = (s[p][c] * scale) * qback[c & 1];
+            if (NP == 1 && valid < kPageSize) {   // slots past the end may hold anything
+                if (g >= valid) {
+                    s[p][0] = s[p][1] = -INFINITY;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) s[c] = (s[c] * scale) * qback[c & 1];
-        if (valid < kPageSize) {   // slots past the end may hold anything
-            if (g >= valid) {
-                s[0] = s[1] = -INFINITY;
+                    for (int k = 0; k < NG; ++k) mv[p][0][k] = 0u;
+                }
+                if (g + 8 >= valid) {
+                    s[p][2] = s[p][3] = -INFINITY;
 #pragma unroll
-                for (int k = 0; k < NG; ++k) mv[0][k] = 0u;
-            }
-            if (g + 8 >= valid) {
-                s[2] = s[3] = -INFINITY;
-#pragma unroll
-                for (int k = 0; k < NG; ++k) mv[1][k] = 0u;
+                    for (int k = 0; k < NG; ++k) mv[p][1][k] = 0u;
+                }
             }
         }
         // The references m and E move only when a score passes m by more than
         // 8 (log2 units) or a scale its limit: weights stay below 2^8, weights times scales
         // below 2^15, and most pages skip the reductions and the rescale.
-        float vmax = 0.f;
+        float vmax = 0.f, pm0 = -INFINITY, pm1 = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < NG; ++k) vmax = fmaxf(vmax, fmaxf(fabsf(T::lo(mv[0][k])), fabsf(T::lo(mv[1][k]))));
-        float pm0 = fmaxf(s[0], s[2]), pm1 = fmaxf(s[1], s[3]);
-        if (__any_sync(0xffffffffu, pm0 > m[0] + 8.f || pm1 > m[1] + 8.f || vmax > vlimit)) {
+        for (int p = 0; p < NP; ++p) {
+            pm0 = fmaxf(pm0, fmaxf(s[p][0], s[p][2]));
+            pm1 = fmaxf(pm1, fmaxf(s[p][1], s[p][3]));
 #pragma unroll
-            for (int mask = 4; mask < 32; mask <<= 1) {
-                pm0 = fmaxf(pm0, __shfl_xor_sync(0xffffffffu, pm0, mask));
-                pm1 = fmaxf(pm1, __shfl_xor_sync(0xffffffffu, pm1, mask));
-                vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, mask));
-            }
-            const float n0 = fmaxf(m[0], pm0), n1 = fmaxf(m[1], pm1);
-            const float al0 = n0 == m[0] ? 1.f : ex2(m[0] - n0), al1 = n1 == m[1] ? 1.f : ex2(m[1] - n1);
-            m[0] = n0;
-            m[1] = n1;
-            float r = 1.f;
-            if (vmax > vlimit) {   // the same in all lanes
-                const int ex = max(-100, (int)(__float_as_uint(vmax) >> 23) - 127);
-                const float next = __uint_as_float((uint32_t)(127 + 6 - ex) << 23);   // takes vmax into [2^6, 2^7)
-                r = next / vs;
-                vs = next;
-                vlimit = 128.f / next;
-            }
-            l[0] *= al0;
-            l[1] *= al1;
+            for (int k = 0; k < NG; ++k) vmax = fmaxf(vmax, fmaxf(fabsf(T::lo(mv[p][0][k])), fabsf(T::lo(mv[p][1][k]))));
+        }
+        if (__any_sync(0xffffffffu, pm0 > m[0] + 8.f || pm1 > m[1] + 8.f || vmax > vlimit)) move_references(pm0, pm1, vmax);
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            const float p0 = ex2(s[p][0] - m[0]), p1 = ex2(s[p][1] - m[1]), p2 = ex2(s[p][2] - m[0]), p3 = ex2(s[p][3] - m[1]);
+            l[0] += p0 + p2;
+            l[1] += p1 + p3;
+            uint32_t va[NW], vb[NW];
+            load_words(st[p] + B::kCodes + lane * NW * 4, va);
+            load_words(st[p] + B::kCodes + (32 + lane) * NW * 4, vb);
 #pragma unroll
             for (int k = 0; k < NG; ++k) {
-                z[k][0] *= al0;
-                z[k][1] *= al1;
-                e[k][0] *= al0 * r;
-                e[k][1] *= al1 * r;
-            }
+                const float s0 = T::lo(mv[p][0][k]) * vs, s1 = T::lo(mv[p][1][k]) * vs;
+                const float z0 = T::hi(mv[p][0][k]), z1 = T::hi(mv[p][1][k]);
+                z[k][0] += p0 * z0 + p2 * z1;
+                z[k][1] += p1 * z0 + p3 * z1;
+                // (p s')^T as the column operand: the packed pairs are 8x8 tiles
+                // [token][n] in the fragment layout, their transposes are the operand.
+                const uint32_t b0 = movmatrix_trans(pack_f16(p0 * s0, p1 * s0));
+                const uint32_t b1 = movmatrix_trans(pack_f16(p2 * s1, p3 * s1));
+                mma_f16_16816(e[k], 0xc800c800u, 0xc800c800u, 0xc800c800u, 0xc800c800u, b0, b1);   // -8 everywhere
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-                o[mt][0] *= al0 * r;
-                o[mt][1] *= al1 * r;
-                o[mt][2] *= al0 * r;
-                o[mt][3] *= al1 * r;
+                for (int i = k * (NW / NG); i < (k + 1) * (NW / NG); ++i) {
+                    const uint32_t a8 = va[i] >> 8, b8 = vb[i] >> 8;
+                    mma_f16_16816(o[2 * i], va[i] & 0x000f000fu, va[i] & 0x00f000f0u, vb[i] & 0x000f000fu, vb[i] & 0x00f000f0u, b0, b1);
+                    mma_f16_16816(o[2 * i + 1], a8 & 0x000f000fu, a8 & 0x00f000f0u, b8 & 0x000f000fu, b8 & 0x00f000f0u, b0, b1);
+                }
             }
         }
-        const float p0 = ex2(s[0] - m[0]), p1 = ex2(s[1] - m[1]), p2 = ex2(s[2] - m[0]), p3 = ex2(s[3] - m[1]);
-        l[0] += p0 + p2;
-        l[1] += p1 + p3;
+    }
+
+    // m and E follow the lanes' largest scores and scale.
+    __device__ __forceinline__ void move_references(float pm0, float pm1, float vmax)
+    {
+#pragma unroll
+        for (int mask = 4; mask < 32; mask <<= 1) {
+            pm0 = fmaxf(pm0, __shfl_xor_sync(0xffffffffu, pm0, mask));
+            pm1 = fmaxf(pm1, __shfl_xor_sync(0xffffffffu, pm1, mask));
+            vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, mask));
+        }
+        const float n0 = fmaxf(m[0], pm0), n1 = fmaxf(m[1], pm1);
+        const float al0 = n0 == m[0] ? 1.f : ex2(m[0] - n0), al1 = n1 == m[1] ? 1.f : ex2(m[1] - n1);
+        m[0] = n0;
+        m[1] = n1;
+        float r = 1.f;
+        if (vmax > vlimit) {   // the same in all lanes
+            const int ex = max(-100, (int)(__float_as_uint(vmax) >> 23) - 127);
+            const float next = __uint_as_float((uint32_t)(127 + 6 - ex) << 23);   // takes vmax into [2^6, 2^7)
+            r = next / vs;
+            vs = next;
+            vlimit = 128.f / next;
+        }
+        l[0] *= al0;
+        l[1] *= al1;
 #pragma unroll
         for (int k = 0; k < NG; ++k) {
-            const float s0 = T::lo(mv[0][k]) * vs, s1 = T::lo(mv[1][k]) * vs;
-            const float z0 = T::hi(mv[0][k]), z1 = T::hi(mv[1][k]);
-            z[k][0] += p0 * z0 + p2 * z1;
-            z[k][1] += p1 * z0 + p3 * z1;
-            // (p s')^T as the column operand: the packed pairs are 8x8 tiles
-            // [token][n] in the fragment layout, their transposes are the operand.
-            const uint32_t b0 = movmatrix_trans(pack_f16(p0 * s0, p1 * s0));
-            const uint32_t b1 = movmatrix_trans(pack_f16(p2 * s1, p3 * s1));
-            mma_f16_16816(e[k], 0xc800c800u, 0xc800c800u, 0xc800c800u, 0xc800c800u, b0, b1);   // -8 everywhere
+            z[k][0] *= al0;
+            z[k][1] *= al1;
+            e[k][0] *= al0 * r;
+            e[k][1] *= al1 * r;
+        }
 #pragma unroll
-            for (int i = k * (NW / NG); i < (k + 1) * (NW / NG); ++i) {
-                const uint32_t a8 = va[i] >> 8, b8 = vb[i] >> 8;
-                mma_f16_16816(o[2 * i], va[i] & 0x000f000fu, va[i] & 0x00f000f0u, vb[i] & 0x000f000fu, vb[i] & 0x00f000f0u, b0, b1);
-                mma_f16_16816(o[2 * i + 1], a8 & 0x000f000fu, a8 & 0x00f000f0u, b8 & 0x000f000fu, b8 & 0x00f000f0u, b0, b1);
-            }
+        for (int mt = 0; mt < MT; ++mt) {
+            o[mt][0] *= al0 * r;
+            o[mt][1] *= al1 * r;
+            o[mt][2] *= al0 * r;
+            o[mt][3] *= al1 * r;
         }
     }
 
@@ -473,39 +497,38 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, AttnShape<D, NG
         __syncthreads();
     }
 
-    if (before > 0xffffffffull) {   // the same in all threads
+    if (before * a.H > 0x7fffffffull) {   // the same in all threads
         if (blockIdx.x == 0 && tid == 0) kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
         return;
     }
 
     // Shares: the first `extra` warps take one tile more than the others.
-    const int64_t total = (int64_t)before * a.H;
-    const int64_t warps = min((int64_t)gridDim.x * W, (total + kMinTiles - 1) / kMinTiles);
-    const int64_t base = warps ? total / warps : 0, extra = warps ? total % warps : 0;
-    const int64_t me = (int64_t)blockIdx.x * W + warp;
-    const int64_t lo = me * base + min(me, extra);
-    const int64_t count = me < warps ? base + (me < extra) : 0;
-    auto cta_of = [&](int64_t at) {   // the CTA whose share holds a tile
-        const int64_t long_ones = extra * (base + 1);
+    const uint32_t H = a.H, total = (uint32_t)before * H;
+    const uint32_t warps = min(gridDim.x * W, (total + kMinTiles - 1) / kMinTiles);
+    const uint32_t base = warps ? total / warps : 0, extra = warps ? total % warps : 0;
+    const uint32_t me = blockIdx.x * W + warp;
+    const uint32_t lo = me * base + min(me, extra);
+    const int count = me < warps ? (int)(base + (me < extra)) : 0;
+    auto cta_of = [&](uint32_t at) {   // the CTA whose share holds a tile
+        const uint32_t long_ones = extra * (base + 1);
         return (int)((at < long_ones ? at / (base + 1) : extra + (at - long_ones) / base) / W);
     };
     const uint64_t policy = l2_policy_evict_first();
 
-    auto tile_of = [&](int64_t i) {   // tile i of this warp's share
+    auto tile_of = [&](int i) {   // tile i of this warp's share
         Tile t{a.pool, 0, 0, 0};
         if (i >= count) return t;
-        const int64_t at = lo + i, page_row = at / a.H;
+        const uint32_t at = lo + i, page_row = at / H;
         int r0 = 0, r1 = a.batch;     // the last row with pages[row] <= page_row that is not empty
         while (r1 - r0 > 1) {
             const int mid = (r0 + r1) >> 1;
-            if ((int64_t)pages[mid] <= page_row) r0 = mid;
+            if (pages[mid] <= page_row) r0 = mid;
             else r1 = mid;
         }
-        const uint32_t first = pages[r0], n = pages[r0 + 1] - first;
-        const int64_t in_row = at - (int64_t)first * a.H;
-        const int p = (int)(in_row % n);
+        const uint32_t first = pages[r0], n = pages[r0 + 1] - first, in_row = at - first * H;
         t.b = r0;
         t.h = (int)(in_row / n);
+        const int p = (int)(in_row - t.h * n);
         const int seq = a.seq_ids ? a.seq_ids[r0] : r0;
         const int32_t page = a.block_table[(int64_t)seq * a.max_pages + p];
         int valid = p == (int)n - 1 ? last[r0] : kPageSize;
@@ -525,60 +548,90 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, AttnShape<D, NG
         bulk_load(smem_addr(ring + stage * B::kBytes), t.src, B::kBytes, bar, policy);
     };
 
+    auto drain = [&] {   // copies in flight (only after a wait that gave up)
+        for (int s = 0; pending; ++s, pending >>= 1)
+            if (pending & 1u) mbar_wait_bounded(smem_addr(bars + s), (phase >> s) & 1u, kWaitLimitNs);
+        __syncwarp();
+    };
     __syncwarp();
     Tile cur = tile_of(lane), next = cur;
     if (lane < R && lane < count) issue(cur, lane);
-    pending = (1u << (count < R ? (int)count : R)) - 1u;
+    pending = (1u << min(count, R)) - 1u;
     State<D, NG, T> st;
     bool ok = true, begins = true;
-    for (int64_t i = 0; i < count; ++i) {
-        const int src = (int)i & 31, stage = (int)(i % R);
+    uint32_t firsts = 0, lasts = 0, fulls = 0;   // of the 32 tiles in cur
+    int stage = 0;
+    // The next stage's copy has landed.
+    auto wait = [&](int s) {
+        const uint32_t bar = smem_addr(bars + s), parity = (phase >> s) & 1u;
+        bool w = mbar_try_wait(bar, parity);
+        if (!w) w = wait_long(bar, parity);
+        ok = __all_sync(0xffffffffu, w);
+        if (!ok) return;
+        phase ^= 1u << s;
+        pending &= ~(1u << s);
+    };
+    for (int i = 0; i < count;) {
+        const int src = i & 31;
         if (src == 0) {
             if (i) cur = next;
+            firsts = __ballot_sync(0xffffffffu, cur.bits & Tile::kFirst);
+            lasts = __ballot_sync(0xffffffffu, cur.bits & Tile::kLast);
+            fulls = __ballot_sync(0xffffffffu, (cur.bits & 31) == kPageSize);
             next = tile_of(i + 32 + lane);
         }
-        const int bits = __shfl_sync(0xffffffffu, cur.bits, src);
-        const bool first = (bits & Tile::kFirst) || i == 0, end = (bits & Tile::kLast) || i == count - 1;
-        const int b = __shfl_sync(0xffffffffu, cur.b, src), h = __shfl_sync(0xffffffffu, cur.h, src);
-        if (first) {
-            begins = bits & Tile::kFirst;
-            st.start(a, b, h, lane);
+        if (i == 0 || ((firsts >> src) & 1u)) {
+            begins = (firsts >> src) & 1u;
+            st.start(a, __shfl_sync(0xffffffffu, cur.b, src), __shfl_sync(0xffffffffu, cur.h, src), lane);
         }
-        if (ok && !__all_sync(0xffffffffu, mbar_wait_bounded(smem_addr(bars + stage), (phase >> stage) & 1u, kWaitLimitNs))) {
-            ok = false;   // the rest of the share is left out
-            if (lane == 0) kv4_error(a.err, KVC_DEVERR_WAIT_TIMEOUT);
-        }
+        // Two tiles at once where both are full pages of this row (and in cur).
+        const bool two = ((fulls >> src) & 3u) == 3u && !((lasts >> src) & 1u);
+        const int n = two ? 2 : 1, at = src + n - 1;
         if (ok) {
-            phase ^= 1u << stage;
-            pending &= ~(1u << stage);
-            if (bits & 31) st.page(ring + stage * B::kBytes, bits & 31, a.scale, lane);
-            __syncwarp();
-            if (i + R < count) {
-                if (lane == ((int)(i + R) & 31)) issue(src + R < 32 ? cur : next, stage);
-                pending |= 1u << stage;
+            const int s1 = stage + 1 == R ? 0 : stage + 1;
+            wait(stage);
+            if (two && ok) wait(s1);
+            if (!ok) {   // the rest of the share is left out
+                if (lane == 0) kv4_error(a.err, KVC_DEVERR_WAIT_TIMEOUT);
+            } else {
+                if (two) {
+                    const uint8_t* const tiles[2] = {ring + stage * B::kBytes, ring + s1 * B::kBytes};
+                    st.pages(tiles, kPageSize, a.scale, lane);
+                } else {
+                    const uint8_t* const tiles[1] = {ring + stage * B::kBytes};
+                    const int valid = __shfl_sync(0xffffffffu, cur.bits, src) & 31;
+                    if (valid) st.pages(tiles, valid, a.scale, lane);
+                }
+                __syncwarp();
+                if (i + R < count) {
+                    if (lane == ((src + R) & 31)) issue(src + R < 32 ? cur : next, stage);
+                    pending |= 1u << stage;
+                }
+                if (two && i + 1 + R < count) {
+                    if (lane == ((src + 1 + R) & 31)) issue(src + 1 + R < 32 ? cur : next, s1);
+                    pending |= 1u << s1;
+                }
+                stage = two ? s1 + 1 : s1;
+                if (stage == R) stage = 0;
             }
         }
-        if (end) {
+        i += n;
+        const bool ends = (lasts >> at) & 1u;
+        if (ends || i == count) {
+            const int b = __shfl_sync(0xffffffffu, cur.b, at), h = __shfl_sync(0xffffffffu, cur.h, at);
             st.finish();
-            const bool ends = bits & Tile::kLast;
             if (begins && ends) {
                 st.write_out(a, b, h, lane);
             } else {
                 // A part that is not the share's last one began before it.
-                if (i == count - 1) {
-                    for (int s = 0; s < R; ++s)   // (only after a wait that gave up)
-                        if (pending & (1u << s)) mbar_wait_bounded(smem_addr(bars + s), (phase >> s) & 1u, kWaitLimitNs);
-                    pending = 0;
-                    __syncwarp();
-                }
-                const int k = i == count - 1 ? 1 : 0;
+                const int k = i == count ? 1 : 0;
+                if (k) drain();
                 st.write_part(k ? reinterpret_cast<float*>(ring) : heads + warp * part_floats(a.G, D), a.G, lane);
                 if (lane == 0) infos[2 * warp + k] = {b, h, begins, ends};
             }
         }
     }
-    for (int s = 0; s < R; ++s)
-        if (pending & (1u << s)) mbar_wait_bounded(smem_addr(bars + s), (phase >> s) & 1u, kWaitLimitNs);
+    drain();
 
     // Rows without tokens.
     for (int r = blockIdx.x; r < a.batch; r += gridDim.x)
@@ -637,7 +690,7 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, AttnShape<D, NG
 
     // What crosses CTAs: the last one to arrive merges it.
     auto ctas_of = [&](const PartInfo& in, int* c0, int* c1) {
-        const int64_t n = pages[in.b + 1] - pages[in.b], first = (int64_t)pages[in.b] * a.H + in.h * n;
+        const uint32_t n = pages[in.b + 1] - pages[in.b], first = pages[in.b] * H + in.h * n;
         *c0 = cta_of(first);
         *c1 = cta_of(first + n - 1);
     };
