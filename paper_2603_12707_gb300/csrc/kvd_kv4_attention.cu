@@ -19,7 +19,7 @@
 //
 // Schedule.  The work is the list of all (row, KV head, page) tiles, a row's
 // heads in turn and a head's pages in order.  Every warp of a persistent grid
-// takes an equal, consecutive share of it, found from a scan over the rows'
+// takes a consecutive share of equal cost, found from a scan over the rows'
 // lengths in shared memory: no plan, no host lengths, and rows of any
 // raggedness give equal shares.  A tile is one consecutive block of the pool,
 // streamed by one bulk copy into the warp's ring of shared memory; K is the
@@ -41,8 +41,10 @@ namespace {
 
 constexpr uint64_t kWaitLimitNs = 1000000000ull;
 constexpr float kLn2 = 0.6931471805599453f;
-// Tiles that a warp takes at least: a small call uses fewer warps rather than merge more parts.
-constexpr int kMinTiles = 2;
+// What starting and ending a (row, KV head) costs a warp, in tiles: shares count it.
+constexpr uint32_t kRowCost = 3;
+// What a warp takes at least, in tiles: a small call uses fewer warps rather than merge more parts.
+constexpr uint32_t kMinShare = 2;
 
 constexpr int kCtasPerSm = 2;
 
@@ -64,13 +66,13 @@ struct AttnArgs {
     int32_t* err;
 };
 
-// The shape of a variant: warps per CTA, CTAs per SM, ring stages per warp.
+// The shape of a variant: warps per CTA, CTAs per SM, ring stages (of two tiles) per warp.
 template <int D, int NG>
 struct AttnShape {
     static constexpr int kWarps = NG == 4 ? 6 : 8;
     static constexpr int kCtas = kCtasPerSm;
-    static constexpr int kStages = D == 64 ? 8 : 4;
-    static constexpr int kRing = kStages * Kv4Block<D, NG>::kBytes;   // of one warp
+    static constexpr int kStages = D == 64 ? 4 : 2;
+    static constexpr int kRing = kStages * 2 * Kv4Block<D, NG>::kBytes;   // of one warp
 };
 
 // The rest of a wait that has not ended at once (out of line).
@@ -94,17 +96,21 @@ struct AttnSmem {   // byte offsets in dynamic shared memory
     static constexpr int kInfo = kBars + S::kWarps * S::kStages * 8;
     static constexpr int kHeads = kInfo + S::kWarps * 2 * (int)sizeof(PartInfo);   // a warp's first part: [kWarps][part_floats]
     __host__ __device__ static constexpr int pages(int G) { return kHeads + S::kWarps * part_floats(G, D) * 4; }   // [batch + 1]
-    __host__ __device__ static constexpr int last(int G, int batch) { return pages(G) + (batch + 1) * 4; }         // [batch] bytes
+    __host__ __device__ static constexpr int costs(int G, int batch) { return pages(G) + (batch + 1) * 4; }        // [batch + 1]
+    __host__ __device__ static constexpr int last(int G, int batch) { return costs(G, batch) + (batch + 1) * 4; }  // [batch] bytes
     __host__ __device__ static constexpr int bytes(int G, int batch) { return last(G, batch) + batch; }
 };
 
 // What a lane knows of one tile.
 struct Tile {
-    const uint8_t* src;
-    int32_t b, h;
-    int32_t bits;     // valid tokens (0 .. 16), kFirst / kLast page of its (row, KV head)
-    static constexpr int kFirst = 32, kLast = 64;
+    const uint8_t* src;   // null: none
+    uint32_t bits;        // valid tokens (0 .. 16), kFirst / kLast page of its (row, KV head), which follows
+    static constexpr uint32_t kFirst = 32, kLast = 64;
+    static __device__ __forceinline__ uint32_t pack(int b, int h) { return (uint32_t)h << 7 | (uint32_t)b << 17; }
+    static __device__ __forceinline__ int row(uint32_t bits) { return (int)(bits >> 17); }
+    static __device__ __forceinline__ int head(uint32_t bits) { return (int)(bits >> 7 & 1023u); }
 };
+static_assert(kKv4MaxHeads <= 1024 && kKv4MaxBatch <= 1 << 15, "Tile::pack");
 
 // The running state of a warp for one (row, KV head): lane (g = lane / 4, j =
 // lane % 4) holds columns n = 2j and 2j + 1 of everything, tokens g and g + 8 of a
@@ -116,6 +122,7 @@ struct State {
     static constexpr int MT = D / 16;     // 16-element tiles of the output
     uint32_t qf[2 * NW][2];               // q as the K product's column operand
     float qsum[NG][2];                    // sum of q over a group, in the accumulators' units
+    float qoff[4];                        // -8 times it, as the accumulators begin (kept for one group: registers)
     float qback[2];                       // undoes q's power of two
     float m[2], l[2];
     float o[MT][4], e[NG][4], z[NG][2];
@@ -170,6 +177,8 @@ struct State {
             qsum[k][0] = __shfl_sync(0xffffffffu, sums[k], 8 * j);
             qsum[k][1] = __shfl_sync(0xffffffffu, sums[k], 8 * j + 4);
         }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) qoff[c] = NG == 1 ? -8.f * qsum[0][c & 1] : 0.f;
         qback[0] = __shfl_sync(0xffffffffu, back, 8 * j);
         qback[1] = __shfl_sync(0xffffffffu, back, 8 * j + 4);
 #pragma unroll
@@ -234,28 +243,36 @@ struct State {
             load_scales(sc + B::kScales, mv[p][0]);
             load_scales(sc + B::kScales + 8 * NG * 4, mv[p][1]);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) s[p][c] = 0.f;
-#pragma unroll
             for (int k = 0; k < NG; ++k) {
-                const float c0 = -8.f * qsum[k][0], c1 = -8.f * qsum[k][1];
-                float acc[4] = {c0, c1, c0, c1};
+                float acc[4];
+                if constexpr (NG > 1) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) acc[c] = -8.f * qsum[k][c & 1];
+                }
 #pragma unroll
                 for (int i = k * (NW / NG); i < (k + 1) * (NW / NG); ++i) {
                     const uint32_t a8 = ka[i] >> 8, b8 = kb[i] >> 8;
-                    mma_f16_16816(acc, ka[i] & 0x000f000fu, kb[i] & 0x000f000fu, ka[i] & 0x00f000f0u, kb[i] & 0x00f000f0u,
-                                  qf[2 * i][0], qf[2 * i][1]);
+                    if (NG == 1 && i == 0)
+                        mma_f16_16816(acc, ka[i] & 0x000f000fu, kb[i] & 0x000f000fu, ka[i] & 0x00f000f0u, kb[i] & 0x00f000f0u,
+                                      qf[2 * i][0], qf[2 * i][1], qoff);
+                    else
+                        mma_f16_16816(acc, ka[i] & 0x000f000fu, kb[i] & 0x000f000fu, ka[i] & 0x00f000f0u, kb[i] & 0x00f000f0u,
+                                      qf[2 * i][0], qf[2 * i][1]);
                     mma_f16_16816(acc, a8 & 0x000f000fu, b8 & 0x000f000fu, a8 & 0x00f000f0u, b8 & 0x00f000f0u,
                                   qf[2 * i + 1][0], qf[2 * i + 1][1]);
                 }
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const float ss = T::lo(mk[t][k]), sz = T::hi(mk[t][k]);
-                    s[p][2 * t] += ss * acc[2 * t] + sz * qsum[k][0];
-                    s[p][2 * t + 1] += ss * acc[2 * t + 1] + sz * qsum[k][1];
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float& x = s[p][2 * t + c];
+                        x = fmaf(ss, acc[2 * t + c], k == 0 ? sz * qsum[k][c] : fmaf(sz, qsum[k][c], x));
+                    }
                 }
             }
 #pragma unroll
-            for (int c = 0; c < 4; ++c) s[p][c] = (s[p][c] * scale) * qback[c & 1];
+            for (int c = 0; c < 4; ++c) s[p][c] *= scale;   // and by qback where it meets m
             if (NP == 1 && valid < kPageSize) {   // slots past the end may hold anything
                 if (g >= valid) {
                     s[p][0] = s[p][1] = -INFINITY;
@@ -280,10 +297,13 @@ struct State {
 #pragma unroll
             for (int k = 0; k < NG; ++k) vmax = fmaxf(vmax, fmaxf(fabsf(T::lo(mv[p][0][k])), fabsf(T::lo(mv[p][1][k]))));
         }
+        pm0 *= qback[0];
+        pm1 *= qback[1];
         if (__any_sync(0xffffffffu, pm0 > m[0] + 8.f || pm1 > m[1] + 8.f || vmax > vlimit)) move_references(pm0, pm1, vmax);
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-            const float p0 = ex2(s[p][0] - m[0]), p1 = ex2(s[p][1] - m[1]), p2 = ex2(s[p][2] - m[0]), p3 = ex2(s[p][3] - m[1]);
+            const float p0 = ex2(fmaf(s[p][0], qback[0], -m[0])), p1 = ex2(fmaf(s[p][1], qback[1], -m[1]));
+            const float p2 = ex2(fmaf(s[p][2], qback[0], -m[0])), p3 = ex2(fmaf(s[p][3], qback[1], -m[1]));
             l[0] += p0 + p2;
             l[1] += p1 + p3;
             uint32_t va[NW], vb[NW];
@@ -293,8 +313,8 @@ struct State {
             for (int k = 0; k < NG; ++k) {
                 const float s0 = T::lo(mv[p][0][k]) * vs, s1 = T::lo(mv[p][1][k]) * vs;
                 const float z0 = T::hi(mv[p][0][k]), z1 = T::hi(mv[p][1][k]);
-                z[k][0] += p0 * z0 + p2 * z1;
-                z[k][1] += p1 * z0 + p3 * z1;
+                z[k][0] = fmaf(p0, z0, fmaf(p2, z1, z[k][0]));
+                z[k][1] = fmaf(p1, z0, fmaf(p3, z1, z[k][1]));
                 // (p s')^T as the column operand: the packed pairs are 8x8 tiles
                 // [token][n] in the fragment layout, their transposes are the operand.
                 const uint32_t b0 = movmatrix_trans(pack_f16(p0 * s0, p1 * s0));
@@ -448,7 +468,7 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, AttnShape<D, NG
     using M = AttnSmem<D, NG>;
     constexpr int W = S::kWarps, R = S::kStages, E = D / 32;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ uint32_t warp_pages[W];
+    __shared__ uint64_t warp_pages[W];
     __shared__ int arrived[2];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint8_t* ring = smem + warp * S::kRing;
@@ -456,6 +476,7 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, AttnShape<D, NG
     PartInfo* infos = reinterpret_cast<PartInfo*>(smem + M::kInfo);
     float* heads = reinterpret_cast<float*>(smem + M::kHeads);
     uint32_t* pages = reinterpret_cast<uint32_t*>(smem + M::pages(a.G));   // pages of the rows before each row
+    uint32_t* costs = reinterpret_cast<uint32_t*>(smem + M::costs(a.G, a.batch));   // the same with kRowCost for each that is not empty
     uint8_t* last = smem + M::last(a.G, a.batch);                          // tokens on each row's last page
     if (lane < R) mbar_init(smem_addr(bars + lane), 1);
     fence_mbar_init();
@@ -464,11 +485,11 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, AttnShape<D, NG
     griddep_launch_dependents();
 
     // Pages of the rows before each row.
-    if (tid == 0) pages[0] = 0;
-    uint64_t before = 0;
+    if (tid == 0) pages[0] = costs[0] = 0;
+    uint64_t before = 0;      // pages in the low, rows that are not empty in the high 24 bits
     for (int r0 = 0; r0 < a.batch; r0 += W * 32) {
         const int r = r0 + tid;
-        uint32_t n = 0;
+        uint64_t sum = 0;
         if (r < a.batch) {
             const int seq = a.seq_ids ? a.seq_ids[r] : r;
             int len = seq >= 0 && seq < a.max_seqs ? a.lens[seq] : -1;
@@ -476,13 +497,13 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, AttnShape<D, NG
                 if (blockIdx.x == 0) kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
                 len = 0;
             }
-            n = (uint32_t)(len + kPageSize - 1) / kPageSize;
+            const uint32_t n = (uint32_t)(len + kPageSize - 1) / kPageSize;
             last[r] = (uint8_t)(len - ((int)n - 1) * kPageSize);
+            sum = n | (uint64_t)(n != 0) << 40;
         }
-        uint32_t sum = n;
 #pragma unroll
         for (int k = 1; k < 32; k <<= 1) {
-            const uint32_t up = __shfl_up_sync(0xffffffffu, sum, k);
+            const uint64_t up = __shfl_up_sync(0xffffffffu, sum, k);
             if (lane >= k) sum += up;
         }
         if (lane == 31) warp_pages[warp] = sum;
@@ -493,145 +514,162 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, AttnShape<D, NG
             if (w < warp) mine += warp_pages[w];
             before += warp_pages[w];
         }
-        if (r < a.batch) pages[r + 1] = (uint32_t)(mine + sum);
+        mine += sum;
+        if (r < a.batch) {
+            pages[r + 1] = (uint32_t)mine;
+            costs[r + 1] = (uint32_t)mine + (uint32_t)(mine >> 40) * kRowCost;
+        }
         __syncthreads();
     }
-
-    if (before * a.H > 0x7fffffffull) {   // the same in all threads
+    const uint64_t all_pages = before & 0xffffffffffull;
+    if (all_pages * a.H > 0x7fffffffull) {   // the same in all threads
         if (blockIdx.x == 0 && tid == 0) kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
         return;
     }
 
-    // Shares: the first `extra` warps take one tile more than the others.
-    const uint32_t H = a.H, total = (uint32_t)before * H;
-    const uint32_t warps = min(gridDim.x * W, (total + kMinTiles - 1) / kMinTiles);
-    const uint32_t base = warps ? total / warps : 0, extra = warps ? total % warps : 0;
-    const uint32_t me = blockIdx.x * W + warp;
-    const uint32_t lo = me * base + min(me, extra);
-    const int count = me < warps ? (int)(base + (me < extra)) : 0;
-    auto cta_of = [&](uint32_t at) {   // the CTA whose share holds a tile
-        const uint32_t long_ones = extra * (base + 1);
+    // Shares: equal parts of the list of tiles in which every (row, KV head)
+    // is preceded by kRowCost empty places; the first `extra` warps take one place more.
+    const uint32_t H = a.H, places = costs[a.batch] * H;
+    const uint32_t warps = min(gridDim.x * W, (places + kMinShare - 1) / kMinShare);
+    const uint32_t base = warps ? places / warps : 0, extra = warps ? places % warps : 0;
+    auto cta_of = [&](int b, int h, uint32_t p) {   // the CTA whose share holds page p of a (row, KV head)
+        const uint32_t n = pages[b + 1] - pages[b];
+        const uint32_t at = costs[b] * H + h * (n + kRowCost) + kRowCost + p, long_ones = extra * (base + 1);
         return (int)((at < long_ones ? at / (base + 1) : extra + (at - long_ones) / base) / W);
     };
+    auto row_of = [&](const uint32_t* sums, uint32_t x) {   // the last row with sums[row] <= x (so not empty, where x < sums[batch])
+        int r0 = 0, r1 = a.batch;
+        while (r1 - r0 > 1) {
+            const int mid = (r0 + r1) >> 1;
+            if (sums[mid] <= x) r0 = mid;
+            else r1 = mid;
+        }
+        return r0;
+    };
+    uint32_t lo = 0;
+    {   // lane 0: tiles before this warp's share, lane 1: up to its end
+        const uint32_t w = min(blockIdx.x * W + warp + (lane & 1), warps), at = w * base + min(w, extra);
+        if (w < warps) {
+            const int r = row_of(costs, at / H);
+            const uint32_t n = pages[r + 1] - pages[r], in_row = at - costs[r] * H, h = in_row / (n + kRowCost);
+            const uint32_t off = in_row - h * (n + kRowCost);
+            lo = pages[r] * H + h * n + (off > kRowCost ? off - kRowCost : 0);
+        } else {
+            lo = pages[a.batch] * H;
+        }
+    }
+    const int count = (int)(__shfl_sync(0xffffffffu, lo, 1) - __shfl_sync(0xffffffffu, lo, 0));
+    lo = __shfl_sync(0xffffffffu, lo, 0);
     const uint64_t policy = l2_policy_evict_first();
 
     auto tile_of = [&](int i) {   // tile i of this warp's share
-        Tile t{a.pool, 0, 0, 0};
+        Tile t{nullptr, 0};
         if (i >= count) return t;
-        const uint32_t at = lo + i, page_row = at / H;
-        int r0 = 0, r1 = a.batch;     // the last row with pages[row] <= page_row that is not empty
-        while (r1 - r0 > 1) {
-            const int mid = (r0 + r1) >> 1;
-            if (pages[mid] <= page_row) r0 = mid;
-            else r1 = mid;
-        }
+        const uint32_t at = lo + i;
+        const int r0 = row_of(pages, at / H);
         const uint32_t first = pages[r0], n = pages[r0 + 1] - first, in_row = at - first * H;
-        t.b = r0;
-        t.h = (int)(in_row / n);
-        const int p = (int)(in_row - t.h * n);
+        const int h = (int)(in_row / n), p = (int)(in_row - h * n);
         const int seq = a.seq_ids ? a.seq_ids[r0] : r0;
         const int32_t page = a.block_table[(int64_t)seq * a.max_pages + p];
         int valid = p == (int)n - 1 ? last[r0] : kPageSize;
         if (page >= 0 && page < a.num_pages) {
-            t.src = a.pool + ((int64_t)page * a.H + t.h) * B::kBytes;
+            t.src = a.pool + ((int64_t)page * a.H + h) * B::kBytes;
         } else {                      // read page 0 in its place, and leave its tokens out
             kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
+            t.src = a.pool;
             valid = 0;
         }
-        t.bits = valid | (p == 0 ? Tile::kFirst : 0) | (p == (int)n - 1 ? Tile::kLast : 0);
+        t.bits = Tile::pack(r0, h) | valid | (p == 0 ? Tile::kFirst : 0u) | (p == (int)n - 1 ? Tile::kLast : 0u);
         return t;
     };
-    uint32_t pending = 0, phase = 0;
-    auto issue = [&](const Tile& t, int stage) {   // by the lane that holds the tile
-        const uint32_t bar = smem_addr(bars + stage);
-        mbar_arrive_expect_tx(bar, B::kBytes);
-        bulk_load(smem_addr(ring + stage * B::kBytes), t.src, B::kBytes, bar, policy);
+    // The ring's stages hold two tiles each and are used in turn: tiles 2k and
+    // 2k + 1 of the share lie in stage k % R.  Their copies are started by the lanes that hold the tiles.
+    const uint32_t ring_at = smem_addr(ring), bars_at = smem_addr(bars);
+    auto issue = [&](const uint8_t* from, int i, int stage) {
+        if (!from) return;
+        const uint32_t bar = bars_at + 8 * stage;
+        if (!(lane & 1)) mbar_arrive_expect_tx(bar, i + 1 < count ? 2 * B::kBytes : B::kBytes);
+        bulk_load(ring_at + (2 * stage + (lane & 1)) * B::kBytes, from, B::kBytes, bar, policy);
     };
 
-    auto drain = [&] {   // copies in flight (only after a wait that gave up)
-        for (int s = 0; pending; ++s, pending >>= 1)
-            if (pending & 1u) mbar_wait_bounded(smem_addr(bars + s), (phase >> s) & 1u, kWaitLimitNs);
-        __syncwarp();
-    };
     __syncwarp();
-    Tile cur = tile_of(lane), next = cur;
-    if (lane < R && lane < count) issue(cur, lane);
-    pending = (1u << min(count, R)) - 1u;
+    Tile next = tile_of(lane);
+    uint32_t cur = next.bits;         // of the 32 tiles in work; next: the 32 after them
+    const uint8_t* from = next.src;   // the tile that this lane starts next
+    if (lane < 2 * R) issue(from, lane, lane >> 1);
     State<D, NG, T> st;
     bool ok = true, begins = true;
-    uint32_t firsts = 0, lasts = 0, fulls = 0;   // of the 32 tiles in cur
     int stage = 0;
-    // The next stage's copy has landed.
-    auto wait = [&](int s) {
-        const uint32_t bar = smem_addr(bars + s), parity = (phase >> s) & 1u;
-        bool w = mbar_try_wait(bar, parity);
-        if (!w) w = wait_long(bar, parity);
-        ok = __all_sync(0xffffffffu, w);
-        if (!ok) return;
-        phase ^= 1u << s;
-        pending &= ~(1u << s);
+    uint32_t parity = 0;              // of the stages' phase: flips where the stages begin again
+    auto start = [&](int src, bool first) {
+        begins = first;
+        const uint32_t t = __shfl_sync(0xffffffffu, cur, src);
+        st.start(a, Tile::row(t), Tile::head(t), lane);
     };
-    for (int i = 0; i < count;) {
-        const int src = i & 31;
-        if (src == 0) {
-            if (i) cur = next;
-            firsts = __ballot_sync(0xffffffffu, cur.bits & Tile::kFirst);
-            lasts = __ballot_sync(0xffffffffu, cur.bits & Tile::kLast);
-            fulls = __ballot_sync(0xffffffffu, (cur.bits & 31) == kPageSize);
-            next = tile_of(i + 32 + lane);
+    auto end = [&](int i, int src, bool ends) {
+        const uint32_t t = __shfl_sync(0xffffffffu, cur, src);
+        const int b = Tile::row(t), h = Tile::head(t);
+        st.finish();
+        if (begins && ends) {
+            st.write_out(a, b, h, lane);
+        } else {
+            // A part that is not the share's last one began before it.
+            const int k = i == count - 1 ? 1 : 0;
+            __syncwarp();             // the ring's last tiles have been read
+            st.write_part(k ? reinterpret_cast<float*>(ring) : heads + warp * part_floats(a.G, D), a.G, lane);
+            if (lane == 0) infos[2 * warp + k] = {b, h, begins, ends};
         }
-        if (i == 0 || ((firsts >> src) & 1u)) {
-            begins = (firsts >> src) & 1u;
-            st.start(a, __shfl_sync(0xffffffffu, cur.b, src), __shfl_sync(0xffffffffu, cur.h, src), lane);
-        }
-        // Two tiles at once where both are full pages of this row (and in cur).
-        const bool two = ((fulls >> src) & 3u) == 3u && !((lasts >> src) & 1u);
-        const int n = two ? 2 : 1, at = src + n - 1;
-        if (ok) {
-            const int s1 = stage + 1 == R ? 0 : stage + 1;
-            wait(stage);
-            if (two && ok) wait(s1);
-            if (!ok) {   // the rest of the share is left out
-                if (lane == 0) kv4_error(a.err, KVC_DEVERR_WAIT_TIMEOUT);
-            } else {
-                if (two) {
-                    const uint8_t* const tiles[2] = {ring + stage * B::kBytes, ring + s1 * B::kBytes};
-                    st.pages(tiles, kPageSize, a.scale, lane);
-                } else {
-                    const uint8_t* const tiles[1] = {ring + stage * B::kBytes};
-                    const int valid = __shfl_sync(0xffffffffu, cur.bits, src) & 31;
-                    if (valid) st.pages(tiles, valid, a.scale, lane);
+    };
+    for (int i0 = 0; i0 < count; i0 += 32) {
+        if (i0) cur = next.bits;
+        const int here = min(32, count - i0);
+        // Of the 32 tiles in cur: first and last pages; where a state starts and
+        // ends; even tiles that make a pair of full pages of one row with the next one.
+        const uint32_t firsts = __ballot_sync(0xffffffffu, cur & Tile::kFirst);
+        const uint32_t lasts = __ballot_sync(0xffffffffu, cur & Tile::kLast);
+        const uint32_t fulls = __ballot_sync(0xffffffffu, (cur & 31) == kPageSize);
+        uint32_t opens = firsts | (i0 == 0 ? 1u : 0u);
+        uint32_t closes = lasts | (i0 + 32 >= count ? 1u << (here - 1) : 0u);
+        uint32_t pairs = fulls & (fulls >> 1) & ~lasts;
+        next = tile_of(i0 + 32 + lane);
+        for (int src = 0; src < here; src += 2, opens >>= 2, closes >>= 2, pairs >>= 2) {
+            if (ok) {
+                const uint32_t bar = bars_at + 8 * stage;
+                bool w = mbar_try_wait(bar, parity);
+                if (!w) w = wait_long(bar, parity);
+                ok = __all_sync(0xffffffffu, w);
+                if (!ok) {   // the rest of the share is left out; copies in flight land first
+                    if (lane == 0) kv4_error(a.err, KVC_DEVERR_WAIT_TIMEOUT);
+                    const int done = (i0 + src) / 2, all = (count + 1) / 2;
+                    for (int k = done; k < min(done + R, all); ++k) mbar_wait_bounded(bars_at + 8 * (k % R), (k / R) & 1, kWaitLimitNs);
                 }
-                __syncwarp();
-                if (i + R < count) {
-                    if (lane == ((src + R) & 31)) issue(src + R < 32 ? cur : next, stage);
-                    pending |= 1u << stage;
-                }
-                if (two && i + 1 + R < count) {
-                    if (lane == ((src + 1 + R) & 31)) issue(src + 1 + R < 32 ? cur : next, s1);
-                    pending |= 1u << s1;
-                }
-                stage = two ? s1 + 1 : s1;
-                if (stage == R) stage = 0;
             }
-        }
-        i += n;
-        const bool ends = (lasts >> at) & 1u;
-        if (ends || i == count) {
-            const int b = __shfl_sync(0xffffffffu, cur.b, at), h = __shfl_sync(0xffffffffu, cur.h, at);
-            st.finish();
-            if (begins && ends) {
-                st.write_out(a, b, h, lane);
+            const uint8_t* tile = ring + 2 * stage * B::kBytes;
+            if (pairs & 1u) {
+                if (opens & 1u) start(src, (firsts >> src) & 1u);
+                const uint8_t* const tiles[2] = {tile, tile + B::kBytes};
+                if (ok) st.pages(tiles, kPageSize, a.scale, lane);
+                if (closes & 2u) end(i0 + src + 1, src + 1, (lasts >> (src + 1)) & 1u);
             } else {
-                // A part that is not the share's last one began before it.
-                const int k = i == count ? 1 : 0;
-                if (k) drain();
-                st.write_part(k ? reinterpret_cast<float*>(ring) : heads + warp * part_floats(a.G, D), a.G, lane);
-                if (lane == 0) infos[2 * warp + k] = {b, h, begins, ends};
+#pragma unroll 1
+                for (int t = 0; t < 2 && src + t < here; ++t) {
+                    if ((opens >> t) & 1u) start(src + t, (firsts >> (src + t)) & 1u);
+                    const uint8_t* const tiles[1] = {tile + t * B::kBytes};
+                    const int valid = (int)(__shfl_sync(0xffffffffu, cur, src + t) & 31);
+                    if (ok && valid) st.pages(tiles, valid, a.scale, lane);
+                    if ((closes >> t) & 1u) end(i0 + src + t, src + t, (lasts >> (src + t)) & 1u);
+                }
+            }
+            __syncwarp();
+            const int to = (src + 2 * R) & 31;
+            if (to == 0) from = next.src;
+            if (ok && (lane >> 1) == (to >> 1)) issue(from, i0 + src + 2 * R + (lane & 1), stage);
+            if (++stage == R) {
+                stage = 0;
+                parity ^= 1u;
             }
         }
     }
-    drain();
 
     // Rows without tokens.
     for (int r = blockIdx.x; r < a.batch; r += gridDim.x)
@@ -690,9 +728,8 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, AttnShape<D, NG
 
     // What crosses CTAs: the last one to arrive merges it.
     auto ctas_of = [&](const PartInfo& in, int* c0, int* c1) {
-        const uint32_t n = pages[in.b + 1] - pages[in.b], first = pages[in.b] * H + in.h * n;
-        *c0 = cta_of(first);
-        *c1 = cta_of(first + n - 1);
+        *c0 = cta_of(in.b, in.h, 0);
+        *c1 = cta_of(in.b, in.h, pages[in.b + 1] - pages[in.b] - 1);
     };
     __syncthreads();
     if (tid < 2) {
@@ -772,7 +809,7 @@ struct LaunchAttention {
         static OncePerDevice once;
         const int smem = AttnSmem<D, NG>::bytes(a.G, a.batch);
         constexpr int most = AttnSmem<D, NG>::bytes(kMaxGroup, kKv4MaxBatch);
-        static_assert(2 * part_floats(kMaxGroup, D) * 4 <= 2 * S::kRing && part_floats(kMaxGroup, D) * 4 <= S::kRing, "");
+        static_assert(part_floats(kMaxGroup, D) * 4 <= S::kRing, "a part lies in its warp's ring");
         static_assert(most <= 227 * 1024, "shared memory of a CTA");
         cudaError_t e = once.set_attribute(attention_kernel<D, NG, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
         if (e != cudaSuccess) return e;
