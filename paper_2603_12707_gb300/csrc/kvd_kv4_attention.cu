@@ -46,8 +46,6 @@ constexpr uint32_t kRowCost = 3;
 // What a warp takes at least, in tiles: a small call uses fewer warps rather than merge more parts.
 constexpr uint32_t kMinShare = 2;
 
-constexpr int kCtasPerSm = 2;
-
 struct AttnArgs {
     const uint8_t* pool;
     int64_t num_pages;
@@ -62,18 +60,28 @@ struct AttnArgs {
     float* lse;
     float scale;         // softmax scale * log2(e) * 2^24 (the accumulators' unit)
     int32_t* counters;   // [grid]: CTAs that have left their part of the row that starts in CTA i; zero between calls
+    uint32_t* sums;      // [2][batch + 1] where shared memory does not hold them: the same from every CTA
     float* parts;        // [grid][2][G][D + 2]: a CTA's part of the row that began before it, and of the one that goes on
     int32_t* err;
 };
 
-// The shape of a variant: warps per CTA, CTAs per SM, ring stages (of two tiles) per warp.
+// The shape of a variant: warps of the one CTA per SM (with two CTAs the older
+// one's warps are served first, and half the SM idles while the other ends: 64
+// MHA rows 5 us more), ring stages (of two tiles) per warp.
 template <int D, int NG>
 struct AttnShape {
-    static constexpr int kWarps = NG == 4 ? 6 : 8;
-    static constexpr int kCtas = kCtasPerSm;
+    static constexpr int kWarps = NG == 4 ? 12 : 16;
     static constexpr int kStages = D == 64 ? 4 : 2;
     static constexpr int kRing = kStages * 2 * Kv4Block<D, NG>::kBytes;   // of one warp
 };
+
+// Everything the CTA wrote before (a barrier before this call) is visible to who adds after it.
+__device__ __forceinline__ int atomic_add_acq_rel(int32_t* p, int32_t v)
+{
+    int32_t old;
+    asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], %2;" : "=r"(old) : "l"(p), "r"(v) : "memory");
+    return old;
+}
 
 // The rest of a wait that has not ended at once (out of line).
 __device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity)
@@ -81,13 +89,16 @@ __device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity)
     return mbar_wait_bounded(bar, parity, kWaitLimitNs);
 }
 
+// Rows whose sums lie in shared memory; those of larger batches in the workspace.
+constexpr int kSmemRows = 1024;
+
 // A warp's part of a (row, KV head) that other warps hold parts of, too.
 struct PartInfo {
     int32_t b, h;       // b < 0: none
     int32_t begins, ends;
 };
 
-__host__ __device__ constexpr int part_floats(int G, int D) { return G * (D + 2); }   // o [G][D], m [G], l [G]
+__host__ __device__ constexpr int part_floats(int G, int D) { return G * D + ((2 * G + 3) & ~3); }   // o [G][D], m [G], l [G]
 
 template <int D, int NG>
 struct AttnSmem {   // byte offsets in dynamic shared memory
@@ -95,10 +106,8 @@ struct AttnSmem {   // byte offsets in dynamic shared memory
     static constexpr int kBars = S::kWarps * S::kRing;
     static constexpr int kInfo = kBars + S::kWarps * S::kStages * 8;
     static constexpr int kHeads = kInfo + S::kWarps * 2 * (int)sizeof(PartInfo);   // a warp's first part: [kWarps][part_floats]
-    __host__ __device__ static constexpr int pages(int G) { return kHeads + S::kWarps * part_floats(G, D) * 4; }   // [batch + 1]
-    __host__ __device__ static constexpr int costs(int G, int batch) { return pages(G) + (batch + 1) * 4; }        // [batch + 1]
-    __host__ __device__ static constexpr int last(int G, int batch) { return costs(G, batch) + (batch + 1) * 4; }  // [batch] bytes
-    __host__ __device__ static constexpr int bytes(int G, int batch) { return last(G, batch) + batch; }
+    __host__ __device__ static constexpr int pages(int G) { return kHeads + S::kWarps * part_floats(G, D) * 4; }   // [2][batch + 1]
+    __host__ __device__ static constexpr int bytes(int G, int batch) { return pages(G) + (batch <= kSmemRows ? 2 * (batch + 1) * 4 : 0); }
 };
 
 // What a lane knows of one tile.
@@ -440,14 +449,68 @@ struct RowSum {
 #pragma unroll
         for (int i = 0; i < E; ++i) o[i] = 0.f;
     }
-    __device__ __forceinline__ void add(const float (&x)[E], float mx, float lx)
+    // Adds row n of the lanes' parts, in the lanes' order (null: none): a
+    // lane loads its part's (m, l), then all lanes the rows, eight in flight.
+    // The loads pass L1 by: parts may come from other SMs.
+    __device__ __forceinline__ void merge(const float* mine, int G, int n, int lane)
     {
-        const float top = fmaxf(m, mx);
-        const float a = m == top ? 1.f : ex2(m - top), b = mx == top ? 1.f : ex2(mx - top);
-        m = top;
-        l = l * a + lx * b;
+        float mc = -INFINITY, lc = 0.f;
+        if (mine) {
+            mc = load_cg(mine + G * D + n);
+            lc = load_cg(mine + G * (D + 1) + n);
+        }
+        const int count = 32 - __clz(__ballot_sync(0xffffffffu, mine != nullptr));
+        float top = fmaxf(m, mc);
 #pragma unroll
-        for (int i = 0; i < E; ++i) o[i] = o[i] * a + x[i] * b;
+        for (int k = 1; k < 32; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
+        const float al = m == top ? 1.f : ex2(m - top), w = mc == top ? 1.f : ex2(mc - top);
+        float sum = w * lc;
+#pragma unroll
+        for (int k = 1; k < 32; k <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+        m = top;
+        l = l * al + sum;
+#pragma unroll
+        for (int i = 0; i < E; ++i) o[i] *= al;
+        const unsigned long long row = mine ? reinterpret_cast<unsigned long long>(mine + n * D) : 0ull;
+#pragma unroll 1
+        for (int c = 0; c < count; c += 8) {
+            float x[8][E], wc[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float* p = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, row, (c + u) & 31));
+                wc[u] = __shfl_sync(0xffffffffu, w, (c + u) & 31);
+#pragma unroll
+                for (int i = 0; i < E; ++i) x[u][i] = 0.f;
+                if (p && c + u < count) load_cg(p + lane * E, x[u]);
+                else wc[u] = 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int i = 0; i < E; ++i) o[i] = fmaf(x[u][i], wc[u], o[i]);
+        }
+    }
+    __device__ __forceinline__ void write_part(float* part, int G, int n, int lane) const
+    {
+        if constexpr (E == 4) *reinterpret_cast<float4*>(part + n * D + lane * 4) = make_float4(o[0], o[1], o[2], o[3]);
+        else *reinterpret_cast<float2*>(part + n * D + lane * 2) = make_float2(o[0], o[1]);
+        if (lane == 0) {
+            part[G * D + n] = m;
+            part[G * (D + 1) + n] = l;
+        }
+    }
+    static __device__ __forceinline__ float load_cg(const float* p)   // shared or global memory
+    {
+        float x;
+        asm volatile("ld.cg.f32 %0, [%1];" : "=f"(x) : "l"(p) : "memory");
+        return x;
+    }
+    static __device__ __forceinline__ void load_cg(const float* p, float (&x)[E])
+    {
+        if constexpr (E == 4)
+            asm volatile("ld.cg.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]) : "l"(p) : "memory");
+        else
+            asm volatile("ld.cg.v2.f32 {%0, %1}, [%2];" : "=f"(x[0]), "=f"(x[1]) : "l"(p) : "memory");
     }
     template <class T>
     __device__ __forceinline__ void write_out(const AttnArgs& a, int b, int h, int n, int lane) const
@@ -461,7 +524,7 @@ struct RowSum {
 };
 
 template <int D, int NG, class T>
-__global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, AttnShape<D, NG>::kCtas) attention_kernel(AttnArgs a)
+__global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_kernel(AttnArgs a)
 {
     using S = AttnShape<D, NG>;
     using B = Kv4Block<D, NG>;
@@ -470,14 +533,16 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, AttnShape<D, NG
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ uint64_t warp_pages[W];
     __shared__ int arrived[2];
+    __shared__ int2 spans[2];   // first and last CTA of what began before this CTA, and of what goes on after it
+    static_assert(2 * W <= 32, "a lane for each part");
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint8_t* ring = smem + warp * S::kRing;
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + M::kBars) + warp * R;
     PartInfo* infos = reinterpret_cast<PartInfo*>(smem + M::kInfo);
     float* heads = reinterpret_cast<float*>(smem + M::kHeads);
-    uint32_t* pages = reinterpret_cast<uint32_t*>(smem + M::pages(a.G));   // pages of the rows before each row
-    uint32_t* costs = reinterpret_cast<uint32_t*>(smem + M::costs(a.G, a.batch));   // the same with kRowCost for each that is not empty
-    uint8_t* last = smem + M::last(a.G, a.batch);                          // tokens on each row's last page
+    // Tiles of the rows before each row, and the same with kRowCost for each (row, KV head) that has some.
+    uint32_t* pages = a.batch <= kSmemRows ? reinterpret_cast<uint32_t*>(smem + M::pages(a.G)) : a.sums;
+    uint32_t* costs = pages + a.batch + 1;
     if (lane < R) mbar_init(smem_addr(bars + lane), 1);
     fence_mbar_init();
     if (tid < 2 * W) infos[tid].b = -1;
@@ -485,6 +550,7 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, AttnShape<D, NG
     griddep_launch_dependents();
 
     // Pages of the rows before each row.
+    const uint32_t H = a.H;
     if (tid == 0) pages[0] = costs[0] = 0;
     uint64_t before = 0;      // pages in the low, rows that are not empty in the high 24 bits
     for (int r0 = 0; r0 < a.batch; r0 += W * 32) {
@@ -498,7 +564,6 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, AttnShape<D, NG
                 len = 0;
             }
             const uint32_t n = (uint32_t)(len + kPageSize - 1) / kPageSize;
-            last[r] = (uint8_t)(len - ((int)n - 1) * kPageSize);
             sum = n | (uint64_t)(n != 0) << 40;
         }
 #pragma unroll
@@ -516,8 +581,8 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, AttnShape<D, NG
         }
         mine += sum;
         if (r < a.batch) {
-            pages[r + 1] = (uint32_t)mine;
-            costs[r + 1] = (uint32_t)mine + (uint32_t)(mine >> 40) * kRowCost;
+            pages[r + 1] = (uint32_t)mine * H;
+            costs[r + 1] = ((uint32_t)mine + (uint32_t)(mine >> 40) * kRowCost) * H;
         }
         __syncthreads();
     }
@@ -529,16 +594,12 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, AttnShape<D, NG
 
     // Shares: equal parts of the list of tiles in which every (row, KV head)
     // is preceded by kRowCost empty places; the first `extra` warps take one place more.
-    const uint32_t H = a.H, places = costs[a.batch] * H;
+    const uint32_t places = costs[a.batch];
     const uint32_t warps = min(gridDim.x * W, (places + kMinShare - 1) / kMinShare);
     const uint32_t base = warps ? places / warps : 0, extra = warps ? places % warps : 0;
-    auto cta_of = [&](int b, int h, uint32_t p) {   // the CTA whose share holds page p of a (row, KV head)
-        const uint32_t n = pages[b + 1] - pages[b];
-        const uint32_t at = costs[b] * H + h * (n + kRowCost) + kRowCost + p, long_ones = extra * (base + 1);
-        return (int)((at < long_ones ? at / (base + 1) : extra + (at - long_ones) / base) / W);
-    };
     auto row_of = [&](const uint32_t* sums, uint32_t x) {   // the last row with sums[row] <= x (so not empty, where x < sums[batch])
         int r0 = 0, r1 = a.batch;
+#pragma unroll 1
         while (r1 - r0 > 1) {
             const int mid = (r0 + r1) >> 1;
             if (sums[mid] <= x) r0 = mid;
@@ -550,12 +611,11 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, AttnShape<D, NG
     {   // lane 0: tiles before this warp's share, lane 1: up to its end
         const uint32_t w = min(blockIdx.x * W + warp + (lane & 1), warps), at = w * base + min(w, extra);
         if (w < warps) {
-            const int r = row_of(costs, at / H);
-            const uint32_t n = pages[r + 1] - pages[r], in_row = at - costs[r] * H, h = in_row / (n + kRowCost);
-            const uint32_t off = in_row - h * (n + kRowCost);
-            lo = pages[r] * H + h * n + (off > kRowCost ? off - kRowCost : 0);
+            const int r = row_of(costs, at);
+            const uint32_t n = (costs[r + 1] - costs[r]) / H, in_row = at - costs[r], h = in_row / n, off = in_row - h * n;
+            lo = pages[r] + h * (n - kRowCost) + (off > kRowCost ? off - kRowCost : 0);
         } else {
-            lo = pages[a.batch] * H;
+            lo = pages[a.batch];
         }
     }
     const int count = (int)(__shfl_sync(0xffffffffu, lo, 1) - __shfl_sync(0xffffffffu, lo, 0));
@@ -566,12 +626,12 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, AttnShape<D, NG
         Tile t{nullptr, 0};
         if (i >= count) return t;
         const uint32_t at = lo + i;
-        const int r0 = row_of(pages, at / H);
-        const uint32_t first = pages[r0], n = pages[r0 + 1] - first, in_row = at - first * H;
+        const int r0 = row_of(pages, at);
+        const uint32_t n = (pages[r0 + 1] - pages[r0]) / H, in_row = at - pages[r0];
         const int h = (int)(in_row / n), p = (int)(in_row - h * n);
         const int seq = a.seq_ids ? a.seq_ids[r0] : r0;
         const int32_t page = a.block_table[(int64_t)seq * a.max_pages + p];
-        int valid = p == (int)n - 1 ? last[r0] : kPageSize;
+        int valid = min(kPageSize, a.lens[seq] - p * kPageSize);
         if (page >= 0 && page < a.num_pages) {
             t.src = a.pool + ((int64_t)page * a.H + h) * B::kBytes;
         } else {                      // read page 0 in its place, and leave its tokens out
@@ -592,78 +652,83 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, AttnShape<D, NG
         bulk_load(ring_at + (2 * stage + (lane & 1)) * B::kBytes, from, B::kBytes, bar, policy);
     };
 
-    __syncwarp();
-    Tile next = tile_of(lane);
-    uint32_t cur = next.bits;         // of the 32 tiles in work; next: the 32 after them
-    const uint8_t* from = next.src;   // the tile that this lane starts next
-    if (lane < 2 * R) issue(from, lane, lane >> 1);
     State<D, NG, T> st;
+    Tile next{nullptr, 0};            // of the 32 tiles after those in work, whose bits are cur
+    const uint8_t* from = nullptr;    // the tile that this lane starts next
+    uint32_t cur = 0;
     bool ok = true, begins = true;
     int stage = 0;
     uint32_t parity = 0;              // of the stages' phase: flips where the stages begin again
-    auto start = [&](int src, bool first) {
-        begins = first;
-        const uint32_t t = __shfl_sync(0xffffffffu, cur, src);
-        st.start(a, Tile::row(t), Tile::head(t), lane);
-    };
-    auto end = [&](int i, int src, bool ends) {
-        const uint32_t t = __shfl_sync(0xffffffffu, cur, src);
-        const int b = Tile::row(t), h = Tile::head(t);
-        st.finish();
-        if (begins && ends) {
-            st.write_out(a, b, h, lane);
-        } else {
-            // A part that is not the share's last one began before it.
-            const int k = i == count - 1 ? 1 : 0;
-            __syncwarp();             // the ring's last tiles have been read
-            st.write_part(k ? reinterpret_cast<float*>(ring) : heads + warp * part_floats(a.G, D), a.G, lane);
-            if (lane == 0) infos[2 * warp + k] = {b, h, begins, ends};
-        }
-    };
-    for (int i0 = 0; i0 < count; i0 += 32) {
-        if (i0) cur = next.bits;
-        const int here = min(32, count - i0);
-        // Of the 32 tiles in cur: first and last pages; where a state starts and
-        // ends; even tiles that make a pair of full pages of one row with the next one.
-        const uint32_t firsts = __ballot_sync(0xffffffffu, cur & Tile::kFirst);
-        const uint32_t lasts = __ballot_sync(0xffffffffu, cur & Tile::kLast);
-        const uint32_t fulls = __ballot_sync(0xffffffffu, (cur & 31) == kPageSize);
-        uint32_t opens = firsts | (i0 == 0 ? 1u : 0u);
-        uint32_t closes = lasts | (i0 + 32 >= count ? 1u << (here - 1) : 0u);
-        uint32_t pairs = fulls & (fulls >> 1) & ~lasts;
-        next = tile_of(i0 + 32 + lane);
-        for (int src = 0; src < here; src += 2, opens >>= 2, closes >>= 2, pairs >>= 2) {
-            if (ok) {
-                const uint32_t bar = bars_at + 8 * stage;
-                bool w = mbar_try_wait(bar, parity);
-                if (!w) w = wait_long(bar, parity);
-                ok = __all_sync(0xffffffffu, w);
-                if (!ok) {   // the rest of the share is left out; copies in flight land first
-                    if (lane == 0) kv4_error(a.err, KVC_DEVERR_WAIT_TIMEOUT);
-                    const int done = (i0 + src) / 2, all = (count + 1) / 2;
-                    for (int k = done; k < min(done + R, all); ++k) mbar_wait_bounded(bars_at + 8 * (k % R), (k / R) & 1, kWaitLimitNs);
-                }
-            }
-            const uint8_t* tile = ring + 2 * stage * B::kBytes;
-            if (pairs & 1u) {
-                if (opens & 1u) start(src, (firsts >> src) & 1u);
-                const uint8_t* const tiles[2] = {tile, tile + B::kBytes};
-                if (ok) st.pages(tiles, kPageSize, a.scale, lane);
-                if (closes & 2u) end(i0 + src + 1, src + 1, (lasts >> (src + 1)) & 1u);
-            } else {
+    // Of the 32 tiles in cur: first and last pages; where a state starts and
+    // ends; tiles that are full pages of one row together with the next one.
+    uint32_t firsts = 0, lasts = 0, opens = 0, closes = 0, pairs = 0;
 #pragma unroll 1
-                for (int t = 0; t < 2 && src + t < here; ++t) {
-                    if ((opens >> t) & 1u) start(src + t, (firsts >> (src + t)) & 1u);
-                    const uint8_t* const tiles[1] = {tile + t * B::kBytes};
-                    const int valid = (int)(__shfl_sync(0xffffffffu, cur, src + t) & 31);
-                    if (ok && valid) st.pages(tiles, valid, a.scale, lane);
-                    if ((closes >> t) & 1u) end(i0 + src + t, src + t, (lasts >> (src + t)) & 1u);
-                }
+    for (int i = -32; i < count;) {
+        const int src = i & 31;
+        if (src == 0) {
+            cur = next.bits;
+            next = tile_of(i + 32 + lane);
+            if (i < 0) {              // fill the ring
+                from = next.src;
+                __syncwarp();
+                if (lane < 2 * R) issue(from, lane, lane >> 1);
+                i = 0;
+                continue;
             }
+            firsts = __ballot_sync(0xffffffffu, cur & Tile::kFirst);
+            lasts = __ballot_sync(0xffffffffu, cur & Tile::kLast);
+            const uint32_t fulls = __ballot_sync(0xffffffffu, (cur & 31) == kPageSize);
+            opens = firsts | (i == 0 ? 1u : 0u);
+            closes = lasts | (i + 32 >= count ? 1u << (count - 1 - i) : 0u);
+            pairs = fulls & (fulls >> 1) & ~lasts & 0x55555555u;
+        }
+        if ((opens >> src) & 1u) {    // before the wait: q arrives meanwhile
+            begins = (firsts >> src) & 1u;
+            const uint32_t t = __shfl_sync(0xffffffffu, cur, src);
+            st.start(a, Tile::row(t), Tile::head(t), lane);
+        }
+        if (ok && !(i & 1)) {
+            const uint32_t bar = bars_at + 8 * stage;
+            bool w = mbar_try_wait(bar, parity);
+            if (!w) w = wait_long(bar, parity);
+            ok = __all_sync(0xffffffffu, w);
+            if (!ok) {   // the rest of the share is left out; copies in flight land first
+                if (lane == 0) kv4_error(a.err, KVC_DEVERR_WAIT_TIMEOUT);
+                for (int k = i / 2; k < min(i / 2 + R, (count + 1) / 2); ++k) wait_long(bars_at + 8 * (k % R), (k / R) & 1);
+            }
+        }
+        const uint8_t* tile = ring + (2 * stage + (i & 1)) * B::kBytes;
+        int at = src;                 // the last tile of this turn
+        if ((pairs >> src) & 1u) {
+            ++at;
+            const uint8_t* const tiles[2] = {tile, tile + B::kBytes};
+            if (ok) st.pages(tiles, kPageSize, a.scale, lane);
+        } else {
+            const uint8_t* const tiles[1] = {tile};
+            const int valid = (int)(__shfl_sync(0xffffffffu, cur, src) & 31);
+            if (ok && valid) st.pages(tiles, valid, a.scale, lane);
+        }
+        i += at - src + 1;
+        if ((closes >> at) & 1u) {
+            const uint32_t t = __shfl_sync(0xffffffffu, cur, at);
+            const int b = Tile::row(t), h = Tile::head(t);
+            const bool ends = (lasts >> at) & 1u;
+            st.finish();
+            if (begins && ends) {
+                st.write_out(a, b, h, lane);
+            } else {
+                // A part that is not the share's last one began before it.
+                const int k = i == count ? 1 : 0;
+                __syncwarp();         // the ring's last tiles have been read
+                st.write_part(k ? reinterpret_cast<float*>(ring) : heads + warp * part_floats(a.G, D), a.G, lane);
+                if (lane == 0) infos[2 * warp + k] = {b, h, begins, ends};
+            }
+        }
+        if (at & 1) {                 // the stage is done
             __syncwarp();
-            const int to = (src + 2 * R) & 31;
+            const int to = (at - 1 + 2 * R) & 31;
             if (to == 0) from = next.src;
-            if (ok && (lane >> 1) == (to >> 1)) issue(from, i0 + src + 2 * R + (lane & 1), stage);
+            if (ok && (lane >> 1) == (to >> 1)) issue(from, i - 2 + 2 * R + (lane & 1), stage);
             if (++stage == R) {
                 stage = 0;
                 parity ^= 1u;
@@ -672,96 +737,117 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, AttnShape<D, NG
     }
 
     // Rows without tokens.
-    for (int r = blockIdx.x; r < a.batch; r += gridDim.x)
-        if (pages[r] == pages[r + 1]) {
-            for (int i = tid; i < a.Hq * (D / 8); i += W * 32)
-                *reinterpret_cast<uint4*>(a.out + r * a.out_stride + i * 8) = make_uint4(0u, 0u, 0u, 0u);
-            if (a.lse)
-                for (int i = tid; i < a.Hq; i += W * 32) a.lse[(int64_t)r * a.Hq + i] = -INFINITY;
-        }
+    if ((int)(before >> 40) != a.batch)
+        for (int r = blockIdx.x; r < a.batch; r += gridDim.x)
+            if (pages[r] == pages[r + 1]) {
+                for (int i = tid; i < a.Hq * (D / 8); i += W * 32)
+                    *reinterpret_cast<uint4*>(a.out + r * a.out_stride + i * 8) = make_uint4(0u, 0u, 0u, 0u);
+                if (a.lse)
+                    for (int i = tid; i < a.Hq; i += W * 32) a.lse[(int64_t)r * a.Hq + i] = -INFINITY;
+            }
     __syncthreads();
 
-    // Merge this CTA's parts: one (group of adjacent parts, query row) per warp and turn.
+    // This CTA's parts, in the order of the list, one in each lane: a group of
+    // them belongs to one (row, KV head).
     const int PF = part_floats(a.G, D);
-    auto part_of = [&](int e) {
-        return e & 1 ? reinterpret_cast<const float*>(smem + (e >> 1) * S::kRing) : heads + (e >> 1) * PF;
-    };
-    int turn = 0, open[2] = {-1, -1};   // entries of the groups that go on before and after this CTA
-    for (int e = 0; e < 2 * W;) {
-        if (infos[e].b < 0) {
-            ++e;
-            continue;
-        }
-        int f = e + 1, ends = infos[e].ends;
-        for (; f < 2 * W && !ends; ++f)
-            if (infos[f].b >= 0) ends = infos[f].ends;
-        const PartInfo& in = infos[e];
-        const int slot = in.begins ? 1 : 0;
-        const bool whole = in.begins && ends;
-        if (!whole) open[slot] = e;
-        for (int n = 0; n < a.G; ++n, ++turn) {
-            if (turn % W != warp) continue;
-            RowSum<D> sum;
-            for (int k = e; k < f; ++k) {
-                if (infos[k].b < 0) continue;
-                const float* p = part_of(k);
-                float x[E];
-#pragma unroll
-                for (int i = 0; i < E; ++i) x[i] = p[n * D + lane * E + i];
-                sum.add(x, p[a.G * D + n], p[a.G * (D + 1) + n]);
-            }
-            if (whole) {
-                sum.template write_out<T>(a, in.b, in.h, n, lane);
+    const PartInfo mine = lane < 2 * W ? infos[lane] : PartInfo{-1, 0, 0, 0};
+    const uint32_t valid = __ballot_sync(0xffffffffu, mine.b >= 0);
+    if (!valid) return;
+    const uint32_t begin = __ballot_sync(0xffffffffu, mine.b >= 0 && mine.begins);
+    const uint32_t ending = __ballot_sync(0xffffffffu, mine.b >= 0 && mine.ends);
+    const uint32_t groups = begin | (valid & (0u - valid));
+    // The parts of the first group may have begun before this CTA, those of the last one may go on after it.
+    const int first = __ffs(groups) - 1, last = 31 - __clz(groups);
+    const bool from_before = !((begin >> first) & 1u);
+    const bool goes_on = !(ending >> last) && !(last == first && from_before);
+    const bool crosses = from_before || goes_on;
+    if (tid < 2 && (tid ? goes_on : from_before)) {
+        // The CTAs that hold parts of it (while the others merge).
+        const PartInfo in = infos[tid ? last : first];
+        auto cta_of = [&](uint32_t p) {   // the CTA whose share holds page p
+            const uint32_t n = (pages[in.b + 1] - pages[in.b]) / H, place = costs[in.b] + in.h * (n + kRowCost) + kRowCost + p;
+            const uint32_t long_ones = extra * (base + 1);
+            return (int)((place < long_ones ? place / (base + 1) : extra + (place - long_ones) / base) / W);
+        };
+        spans[tid] = make_int2(cta_of(0), cta_of((pages[in.b + 1] - pages[in.b]) / H - 1));
+    }
+    // Pass 0 merges the groups in shared memory, pass 1 (k = 0, 1) the parts of all CTAs of what
+    // crosses them, by the last CTA to arrive; where those are many, several warps share a row's
+    // and pass 2 merges their sums.
+    const int jobs0 = __popc(groups) * a.G;
+#pragma unroll 1
+    for (int pass = 0, k = 0;; ) {
+        const int parts = pass ? spans[k].y - spans[k].x + 1 : 0;
+        const int split = parts > 16 ? max(1, W / a.G) : 1, each = (parts + split - 1) / split;
+        const int jobs = pass == 0 ? jobs0 : pass == 1 ? a.G * split : a.G;
+#pragma unroll 1
+        for (int job = warp; job < jobs; job += W) {
+            int n, b, h, c = 0, end = 0;
+            float* to = nullptr;      // null: this is the whole row
+            uint32_t members = 0;
+            if (pass == 0) {
+                uint32_t rest = groups;
+                for (int u = job / a.G; u > 0; --u) rest &= rest - 1u;
+                n = job % a.G;
+                const int e = __ffs(rest) - 1;
+                rest &= rest - 1u;
+                members = valid & (0xffffffffu << e) & (rest ? (rest & (0u - rest)) - 1u : 0xffffffffu);
+                const bool whole = ((begin >> e) & 1u) && (ending & members);
+                if (!whole) to = a.parts + ((int64_t)blockIdx.x * 2 + ((begin >> e) & 1u)) * PF;
+                b = __shfl_sync(0xffffffffu, mine.b, e);
+                h = __shfl_sync(0xffffffffu, mine.h, e);
+                c = e;
+                end = 32;             // (a lane for each part from e on)
             } else {
-                float* to = a.parts + ((int64_t)blockIdx.x * 2 + slot) * PF;
-#pragma unroll
-                for (int i = 0; i < E; ++i) to[n * D + lane * E + i] = sum.o[i];
-                if (lane == 0) {
-                    to[a.G * D + n] = sum.m;
-                    to[a.G * (D + 1) + n] = sum.l;
+                n = pass == 1 ? job / split : job;
+                b = infos[k ? last : first].b;
+                h = infos[k ? last : first].h;
+                c = pass == 1 ? job % split * each : 0;
+                end = pass == 1 ? min(parts, c + each) : split;
+                if (pass == 1 && split > 1) to = heads + (job % split) * PF;
+            }
+            RowSum<D> sum;
+#pragma unroll 1
+            for (; c < end; c += 32) {
+                const int i = c + lane;
+                const float* p = nullptr;
+                if (pass == 0) {
+                    if (i < 32 && ((members >> i) & 1u)) p = i & 1 ? reinterpret_cast<const float*>(smem + (i >> 1) * S::kRing) : heads + (i >> 1) * PF;
+                } else if (i < end) {
+                    p = pass == 1 ? a.parts + ((int64_t)(spans[k].x + i) * 2 + (i == 0 ? 1 : 0)) * PF : heads + i * PF;
+                }
+                sum.merge(p, a.G, n, lane);
+            }
+            if (to) sum.write_part(to, a.G, n, lane);
+            else sum.template write_out<T>(a, b, h, n, lane);
+        }
+        if (pass == 0) {
+            if (!crosses) return;
+            __syncthreads();
+            if (tid < 2) {
+                arrived[tid] = 0;
+                if (tid ? goes_on : from_before) {
+                    const int2 at = spans[tid];
+                    if (atomic_add_acq_rel(a.counters + at.x, 1) == at.y - at.x) {
+                        a.counters[at.x] = 0;
+                        arrived[tid] = 1;
+                    }
                 }
             }
+            __syncthreads();
+            pass = 1;
+            k = -1;
+        } else if (pass == 1 && split > 1) {
+            __syncthreads();
+            pass = 2;
+            continue;
+        } else if (pass == 2) {
+            __syncthreads();
+            pass = 1;
         }
-        e = f;
-    }
-    if (open[0] < 0 && open[1] < 0) return;
-
-    // What crosses CTAs: the last one to arrive merges it.
-    auto ctas_of = [&](const PartInfo& in, int* c0, int* c1) {
-        *c0 = cta_of(in.b, in.h, 0);
-        *c1 = cta_of(in.b, in.h, pages[in.b + 1] - pages[in.b] - 1);
-    };
-    __syncthreads();
-    if (tid < 2) {
-        arrived[tid] = 0;
-        if (open[tid] >= 0) {
-            int c0, c1;
-            ctas_of(infos[open[tid]], &c0, &c1);
-            __threadfence();
-            if (atomicAdd(a.counters + c0, 1) == c1 - c0) {
-                a.counters[c0] = 0;
-                arrived[tid] = 1;
-            }
-            __threadfence();
-        }
-    }
-    __syncthreads();
-    for (int k = 0; k < 2; ++k) {
-        if (!arrived[k]) continue;
-        const PartInfo& in = infos[open[k]];
-        int c0, c1;
-        ctas_of(in, &c0, &c1);
-        for (int n = warp; n < a.G; n += W) {
-            RowSum<D> sum;
-            for (int c = c0; c <= c1; ++c) {
-                const float* p = a.parts + ((int64_t)c * 2 + (c == c0 ? 1 : 0)) * PF;
-                float x[E];
-#pragma unroll
-                for (int i = 0; i < E; ++i) x[i] = __ldcg(p + n * D + lane * E + i);
-                sum.add(x, __ldcg(p + a.G * D + n), __ldcg(p + a.G * (D + 1) + n));
-            }
-            sum.template write_out<T>(a, in.b, in.h, n, lane);
-        }
+        do ++k;
+        while (k < 2 && !arrived[k]);
+        if (k == 2) return;
     }
 }
 
@@ -776,25 +862,14 @@ int device_sms()
     return n;
 }
 
-constexpr int kSmemPerSm = 228 * 1024, kSmemPerCta = 1024 + 128;   // what an SM has, what a CTA takes beside its dynamic part
-
-template <int D, int NG>
-struct AttnPlan {
-    using S = AttnShape<D, NG>;
-    static int ctas_per_sm(int G, int batch)
+// The workspace: counters, sums of large batches, parts.
+struct Workspace {
+    int64_t sums, parts, bytes;   // offsets of the latter two, and the whole
+    Workspace(int sms, int G, int D)
     {
-        const int fit = kSmemPerSm / (AttnSmem<D, NG>::bytes(G, batch) + kSmemPerCta);
-        return fit < S::kCtas ? fit : S::kCtas;
-    }
-};
-
-struct WorkspaceOf {
-    int sms, G;
-    template <int D, int NG, class T>
-    int64_t operator()() const
-    {
-        const int64_t ctas = (int64_t)sms * AttnShape<D, NG>::kCtas;
-        return 256 * ((ctas * 4 + 255) / 256) + ctas * 2 * part_floats(G, D) * 4;
+        sums = 256 * (((int64_t)sms * 4 + 255) / 256);
+        parts = sums + 256 * ((2 * (kKv4MaxBatch + 1) * 4 + 255) / 256);
+        bytes = parts + (int64_t)sms * 2 * part_floats(G, D) * 4;
     }
 };
 
@@ -808,13 +883,12 @@ struct LaunchAttention {
         using S = AttnShape<D, NG>;
         static OncePerDevice once;
         const int smem = AttnSmem<D, NG>::bytes(a.G, a.batch);
-        constexpr int most = AttnSmem<D, NG>::bytes(kMaxGroup, kKv4MaxBatch);
+        constexpr int most = AttnSmem<D, NG>::bytes(kMaxGroup, kSmemRows);
         static_assert(part_floats(kMaxGroup, D) * 4 <= S::kRing, "a part lies in its warp's ring");
-        static_assert(most <= 227 * 1024, "shared memory of a CTA");
+        static_assert(most <= 226 * 1024, "shared memory of a CTA");
         cudaError_t e = once.set_attribute(attention_kernel<D, NG, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
         if (e != cudaSuccess) return e;
-        const int grid = sms * AttnPlan<D, NG>::ctas_per_sm(a.G, a.batch);
-        return kv4_launch(attention_kernel<D, NG, T>, dim3((unsigned)grid), S::kWarps * 32, (size_t)smem, st, a);
+        return kv4_launch(attention_kernel<D, NG, T>, dim3((unsigned)sms), S::kWarps * 32, (size_t)smem, st, a);
     }
 };
 
@@ -838,7 +912,7 @@ extern "C" KVC_API int64_t kv4_workspace_bytes(const kv4_pool* pool, int32_t num
     if (int rc = check_heads(pool, num_q_heads)) return rc;
     const int sms = device_sms();
     if (!sms) return kv4_fail(KVC_ERR_CUDA, "kv4_workspace_bytes: cannot query the current device");
-    return kv4_dispatch(*pool, WorkspaceOf{sms, num_q_heads / pool->num_kv_heads});
+    return Workspace(sms, num_q_heads / pool->num_kv_heads, pool->head_dim).bytes;
 }
 
 extern "C" KVC_API int kv4_decode_attention(const kv4_pool* pool, const kv_tables* tables, int32_t batch,
@@ -864,7 +938,8 @@ extern "C" KVC_API int kv4_decode_attention(const kv4_pool* pool, const kv_table
     const int sms = device_sms();
     if (!sms) return kv4_fail(KVC_ERR_CUDA, "kv4_decode_attention: cannot query the current device");
     const int G = num_q_heads / pool->num_kv_heads;
-    if (workspace_bytes < kv4_dispatch(*pool, WorkspaceOf{sms, G}))
+    const Workspace ws(sms, G, pool->head_dim);
+    if (workspace_bytes < ws.bytes)
         return kv4_fail(KVC_ERR_INVALID, "kv4_decode_attention: the workspace is smaller than kv4_workspace_bytes()");
     const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)pool->head_dim);
     AttnArgs a{};
@@ -886,8 +961,9 @@ extern "C" KVC_API int kv4_decode_attention(const kv4_pool* pool, const kv_table
     a.lse = lse;
     a.scale = scale * 1.4426950408889634f * 0x1p24f;
     a.err = device_error;
-    const int64_t most = (int64_t)sms * kCtasPerSm * 4;
-    a.counters = static_cast<int32_t*>(workspace);
-    a.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + 256 * ((most + 255) / 256));
+    uint8_t* const work = static_cast<uint8_t*>(workspace);
+    a.counters = reinterpret_cast<int32_t*>(work);
+    a.sums = reinterpret_cast<uint32_t*>(work + ws.sums);
+    a.parts = reinterpret_cast<float*>(work + ws.parts);
     return kv4_launch_result(kv4_dispatch(*pool, LaunchAttention{a, sms, static_cast<cudaStream_t>(stream)}));
 }
