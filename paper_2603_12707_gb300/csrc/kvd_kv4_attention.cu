@@ -112,9 +112,10 @@ struct AttnSmem {   // byte offsets in dynamic shared memory
 
 // What a lane knows of one tile.
 struct Tile {
-    const uint8_t* src;   // null: none
+    const uint8_t* src;   // null: none; kAlone is added where the share ends with it
     uint32_t bits;        // valid tokens (0 .. 16), kFirst / kLast page of its (row, KV head), which follows
     static constexpr uint32_t kFirst = 32, kLast = 64;
+    static constexpr uint64_t kAlone = 1;
     static __device__ __forceinline__ uint32_t pack(int b, int h) { return (uint32_t)h << 7 | (uint32_t)b << 17; }
     static __device__ __forceinline__ int row(uint32_t bits) { return (int)(bits >> 17); }
     static __device__ __forceinline__ int head(uint32_t bits) { return (int)(bits >> 7 & 1023u); }
@@ -209,48 +210,35 @@ struct State {
         vlimit = -1.f;   // below any |s'|: the first page sets E
     }
 
-    static __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[NW])
+    template <int N>
+    static __device__ __forceinline__ void load_shared(uint32_t at, uint32_t (&w)[N])
     {
-        if constexpr (NW == 4) {
-            const uint4 u = *reinterpret_cast<const uint4*>(p);
-            w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
-        } else {
-            const uint2 u = *reinterpret_cast<const uint2*>(p);
-            w[0] = u.x, w[1] = u.y;
-        }
+        if constexpr (N == 4)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
+        else if constexpr (N == 2)
+            asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
+        else
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(at));
     }
 
-    static __device__ __forceinline__ void load_scales(const uint8_t* p, uint32_t (&w)[NG])
-    {
-        if constexpr (NG == 4) {
-            const uint4 u = *reinterpret_cast<const uint4*>(p);
-            w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
-        } else if constexpr (NG == 2) {
-            const uint2 u = *reinterpret_cast<const uint2*>(p);
-            w[0] = u.x, w[1] = u.y;
-        } else {
-            w[0] = *reinterpret_cast<const uint32_t*>(p);
-        }
-    }
-
-    // NP pages in shared memory; `valid` (1 .. 16) of a single page's tokens
-    // count, all of a pair's.  Two at a time share the checks and keep two chains of products in flight.
+    // NP pages in shared memory, from `at` on; `valid` (1 .. 16) of a single page's
+    // tokens count, all of a pair's.  Two at a time share the checks and keep two chains of products in flight.
     template <int NP>
-    __device__ __forceinline__ void pages(const uint8_t* const (&st)[NP], int valid, float scale, int lane)
+    __device__ __forceinline__ void pages(uint32_t at, int valid, float scale, int lane)
     {
         const int g = lane >> 2;
+        const uint32_t codes = at + lane * NW * 4, scales = at + 2 * B::kCodes + g * NG * 4;
         float s[NP][4];
         uint32_t mv[NP][2][NG];
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             uint32_t ka[NW], kb[NW], mk[2][NG];
-            load_words(st[p] + lane * NW * 4, ka);
-            load_words(st[p] + (32 + lane) * NW * 4, kb);
-            const uint8_t* sc = st[p] + 2 * B::kCodes + g * NG * 4;
-            load_scales(sc, mk[0]);
-            load_scales(sc + 8 * NG * 4, mk[1]);
-            load_scales(sc + B::kScales, mv[p][0]);
-            load_scales(sc + B::kScales + 8 * NG * 4, mv[p][1]);
+            load_shared(codes + p * B::kBytes, ka);
+            load_shared(codes + p * B::kBytes + 32 * NW * 4, kb);
+            load_shared(scales + p * B::kBytes, mk[0]);
+            load_shared(scales + p * B::kBytes + 8 * NG * 4, mk[1]);
+            load_shared(scales + p * B::kBytes + B::kScales, mv[p][0]);
+            load_shared(scales + p * B::kBytes + B::kScales + 8 * NG * 4, mv[p][1]);
 #pragma unroll
             for (int k = 0; k < NG; ++k) {
                 float acc[4];
@@ -316,8 +304,8 @@ struct State {
             l[0] += p0 + p2;
             l[1] += p1 + p3;
             uint32_t va[NW], vb[NW];
-            load_words(st[p] + B::kCodes + lane * NW * 4, va);
-            load_words(st[p] + B::kCodes + (32 + lane) * NW * 4, vb);
+            load_shared(codes + p * B::kBytes + B::kCodes, va);
+            load_shared(codes + p * B::kBytes + B::kCodes + 32 * NW * 4, vb);
 #pragma unroll
             for (int k = 0; k < NG; ++k) {
                 const float s0 = T::lo(mv[p][0][k]) * vs, s1 = T::lo(mv[p][1][k]) * vs;
@@ -622,9 +610,10 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
     lo = __shfl_sync(0xffffffffu, lo, 0);
     const uint64_t policy = l2_policy_evict_first();
 
+    bool ok = true;
     auto tile_of = [&](int i) {   // tile i of this warp's share
         Tile t{nullptr, 0};
-        if (i >= count) return t;
+        if (i >= count || !ok) return t;
         const uint32_t at = lo + i;
         const int r0 = row_of(pages, at);
         const uint32_t n = (pages[r0 + 1] - pages[r0]) / H, in_row = at - pages[r0];
@@ -639,80 +628,80 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
             t.src = a.pool;
             valid = 0;
         }
+        if (i == count - 1) t.src += Tile::kAlone;
         t.bits = Tile::pack(r0, h) | valid | (p == 0 ? Tile::kFirst : 0u) | (p == (int)n - 1 ? Tile::kLast : 0u);
         return t;
     };
     // The ring's stages hold two tiles each and are used in turn: tiles 2k and
     // 2k + 1 of the share lie in stage k % R.  Their copies are started by the lanes that hold the tiles.
     const uint32_t ring_at = smem_addr(ring), bars_at = smem_addr(bars);
-    auto issue = [&](const uint8_t* from, int i, int stage) {
-        if (!from) return;
-        const uint32_t bar = bars_at + 8 * stage;
-        if (!(lane & 1)) mbar_arrive_expect_tx(bar, i + 1 < count ? 2 * B::kBytes : B::kBytes);
-        bulk_load(ring_at + (2 * stage + (lane & 1)) * B::kBytes, from, B::kBytes, bar, policy);
+    auto issue = [&](const uint8_t* from, bool mine, uint32_t stage_at, uint32_t bar) {   // mine: one of two neighbours' turn
+        const uint64_t src = reinterpret_cast<uint64_t>(from);
+        bulk_load_pair(stage_at + (lane & 1) * B::kBytes, src & ~Tile::kAlone, B::kBytes, src & Tile::kAlone ? B::kBytes : 2 * B::kBytes,
+                       bar, policy, mine && src, mine && src && !(lane & 1));
     };
 
     State<D, NG, T> st;
-    Tile next{nullptr, 0};            // of the 32 tiles after those in work, whose bits are cur
+    Tile next{nullptr, 0};            // of the 32 tiles after those in work
     const uint8_t* from = nullptr;    // the tile that this lane starts next
-    uint32_t cur = 0;
-    bool ok = true, begins = true;
-    int stage = 0;
-    uint32_t parity = 0;              // of the stages' phase: flips where the stages begin again
-    // Of the 32 tiles in cur: first and last pages; where a state starts and
-    // ends; tiles that are full pages of one row together with the next one.
-    uint32_t firsts = 0, lasts = 0, opens = 0, closes = 0, pairs = 0;
+    uint32_t cur = 0;                 // of a tile in work: Tile::bits
+    constexpr uint32_t kOpen = 1, kClose = 2, kSingle = 4, kRefill = 8;
+    uint32_t what = kRefill;          // and what its turn has to do
+    int at = -32;                     // the tile that the next refill begins with
+    bool begins = true;
+    uint32_t stage_at = ring_at, bar = bars_at, parity = 0;   // of the stage in work; parity flips where the stages begin again
 #pragma unroll 1
-    for (int i = -32; i < count;) {
+    for (int i = 0; i < count;) {
         const int src = i & 31;
-        if (src == 0) {
+        uint32_t turn = __shfl_sync(0xffffffffu, what, src);
+        if (turn & kRefill) {
             cur = next.bits;
-            next = tile_of(i + 32 + lane);
-            if (i < 0) {              // fill the ring
+            next = tile_of(at + 32 + lane);
+            if (at < 0) {             // fill the ring
                 from = next.src;
                 __syncwarp();
-                if (lane < 2 * R) issue(from, lane, lane >> 1);
-                i = 0;
+                issue(from, lane < 2 * R, ring_at + (lane >> 1) * 2 * B::kBytes, bars_at + 8 * (lane >> 1));
+                at = 0;
                 continue;
             }
-            firsts = __ballot_sync(0xffffffffu, cur & Tile::kFirst);
-            lasts = __ballot_sync(0xffffffffu, cur & Tile::kLast);
+            at += 32;
+            // Pairs begin at even tiles: full pages of one row.
+            const uint32_t lasts = __ballot_sync(0xffffffffu, cur & Tile::kLast);
             const uint32_t fulls = __ballot_sync(0xffffffffu, (cur & 31) == kPageSize);
-            opens = firsts | (i == 0 ? 1u : 0u);
-            closes = lasts | (i + 32 >= count ? 1u << (count - 1 - i) : 0u);
-            pairs = fulls & (fulls >> 1) & ~lasts & 0x55555555u;
+            const uint32_t pairs = fulls & (fulls >> 1) & ~lasts & 0x55555555u;
+            const uint32_t closes = lasts | (i + 32 >= count ? 1u << (count - 1 - i) : 0u);
+            const bool pair = (pairs >> lane) & 1u;
+            what = ((cur & Tile::kFirst) || i + lane == 0 ? kOpen : 0u) | ((closes >> (lane + (pair ? 1 : 0))) & 1u ? kClose : 0u) |
+                   (pair ? 0u : kSingle) | (lane == 0 ? kRefill : 0u);
+            turn = __shfl_sync(0xffffffffu, what, 0);
         }
-        if ((opens >> src) & 1u) {    // before the wait: q arrives meanwhile
-            begins = (firsts >> src) & 1u;
+        if (turn & kOpen) {           // before the wait: q arrives meanwhile
             const uint32_t t = __shfl_sync(0xffffffffu, cur, src);
+            begins = t & Tile::kFirst;
             st.start(a, Tile::row(t), Tile::head(t), lane);
         }
-        if (ok && !(i & 1)) {
-            const uint32_t bar = bars_at + 8 * stage;
-            bool w = mbar_try_wait(bar, parity);
-            if (!w) w = wait_long(bar, parity);
-            ok = __all_sync(0xffffffffu, w);
-            if (!ok) {   // the rest of the share is left out; copies in flight land first
+        if (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity)) && ok) {
+            ok = __all_sync(0xffffffffu, wait_long(bar, parity));
+            if (!ok) {   // no more copies; those in flight land first, and the result is void
                 if (lane == 0) kv4_error(a.err, KVC_DEVERR_WAIT_TIMEOUT);
                 for (int k = i / 2; k < min(i / 2 + R, (count + 1) / 2); ++k) wait_long(bars_at + 8 * (k % R), (k / R) & 1);
+                from = next.src = nullptr;
             }
         }
-        const uint8_t* tile = ring + (2 * stage + (i & 1)) * B::kBytes;
-        int at = src;                 // the last tile of this turn
-        if ((pairs >> src) & 1u) {
-            ++at;
-            const uint8_t* const tiles[2] = {tile, tile + B::kBytes};
-            if (ok) st.pages(tiles, kPageSize, a.scale, lane);
+        const uint32_t tile = stage_at + (i & 1) * B::kBytes;
+        int last = src;               // the last tile of this turn
+        if (!(turn & kSingle)) {
+            ++last;
+            st.template pages<2>(tile, kPageSize, a.scale, lane);
         } else {
-            const uint8_t* const tiles[1] = {tile};
             const int valid = (int)(__shfl_sync(0xffffffffu, cur, src) & 31);
-            if (ok && valid) st.pages(tiles, valid, a.scale, lane);
+            if (valid) st.template pages<1>(tile, valid, a.scale, lane);
         }
-        i += at - src + 1;
-        if ((closes >> at) & 1u) {
-            const uint32_t t = __shfl_sync(0xffffffffu, cur, at);
+        i += last - src + 1;
+        if (turn & kClose) {
+            const uint32_t t = __shfl_sync(0xffffffffu, cur, last);
             const int b = Tile::row(t), h = Tile::head(t);
-            const bool ends = (lasts >> at) & 1u;
+            const bool ends = t & Tile::kLast;
             st.finish();
             if (begins && ends) {
                 st.write_out(a, b, h, lane);
@@ -724,13 +713,16 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
                 if (lane == 0) infos[2 * warp + k] = {b, h, begins, ends};
             }
         }
-        if (at & 1) {                 // the stage is done
+        if (last & 1) {               // the stage is done
             __syncwarp();
-            const int to = (at - 1 + 2 * R) & 31;
+            const int to = (last - 1 + 2 * R) & 31;
             if (to == 0) from = next.src;
-            if (ok && (lane >> 1) == (to >> 1)) issue(from, i - 2 + 2 * R + (lane & 1), stage);
-            if (++stage == R) {
-                stage = 0;
+            issue(from, (lane & ~1) == to, stage_at, bar);
+            stage_at += 2 * B::kBytes;
+            bar += 8;
+            if (bar == bars_at + 8 * R) {
+                stage_at = ring_at;
+                bar = bars_at;
                 parity ^= 1u;
             }
         }

@@ -106,13 +106,19 @@ __device__ __forceinline__ void prefetch_tensormap(const CUtensorMap* map)
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
 }
 
-// `bytes` (a multiple of 16) of consecutive global memory into shared memory;
-// both addresses 16-byte aligned.
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar, uint64_t policy)
+// A lane's copy of `bytes` (a multiple of 16) of consecutive global memory into
+// shared memory (both addresses 16-byte aligned) where `copy`, after it has announced `expect` bytes
+// on the barrier where `announce` (a barrier of one arrival; no branches).
+__device__ __forceinline__ void bulk_load_pair(uint32_t dst, uint64_t src, uint32_t bytes, uint32_t expect, uint32_t bar,
+                                               uint64_t policy, bool copy, bool announce)
 {
     asm volatile(
-        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(dst),
-        "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar), "l"(policy)
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %6, 0;\n\t"
+        "setp.ne.u32 q, %7, 0;\n\t"
+        "@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%3], %4;\n\t"
+        "@p cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %5;\n\t}" ::"r"(dst),
+        "l"(src), "r"(bytes), "r"(bar), "r"(expect), "l"(policy), "r"((uint32_t)copy), "r"((uint32_t)announce)
         : "memory");
 }
 
