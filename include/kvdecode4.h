@@ -58,9 +58,9 @@ extern "C" {
  *
  * Quantisation of a group's values x: s = rn16((max/2 - min/2) / 7.5),
  * z = rn16(min + 8 s), c = clamp(rint((x - z) / s) + 8, 0, 15), with the
- * difference, the quotient (correctly rounded) and the sum in 32 bits, rn16
- * and rint to nearest even; c = 8 where s is 0.  A group that holds an
- * infinity or a NaN stands for NaN in all its elements. */
+ * difference and the sum in 32 bits, rn16 and rint (of the exact quotient) to
+ * nearest even; c = 8 where s is 0.  A group that holds an infinity or a NaN
+ * stands for NaN in all its elements. */
 typedef struct kv4_pool {
     void *data;            /* device, kv4_pool_bytes() bytes, 128-byte aligned   */
     int64_t num_pages;     /* 1 .. 2^31 - 1                                      */

@@ -1,9 +1,12 @@
 // kv4_write and kv4_read: K and V rows of tokens into and out of the 4-bit
-// pool's blocks (layout and quantisation: kvdecode4.h).
+// pool's blocks (layout and quantisation: kvdecode4.h).  Both are copies whose
+// one side is 16-bit rows and whose other side is blocks; the bytes bound them.
 //
-// One warp per (token, KV head, K or V).  A lane holds D / 32 consecutive
-// elements, a scale group lies in group * 32 / D lanes, and the codes pass
-// through a row of shared memory into the words of the block.
+// V's codes lie in words of two neighbouring tokens, so a warp takes tokens
+// whose slots 2m and 2m + 1 follow one another as a pair (a run of tokens gives
+// pairs wherever it starts) and others alone; it goes over some KV heads of
+// them.  A lane holds 8 consecutive elements of one token's row, which are one word of K's
+// codes; V's words hold elements 8 apart, four lanes' codes each, and are made by a transposition across lanes.
 #include "kvd_kv4.h"
 #include "kvd_ptx.cuh"
 
@@ -16,6 +19,7 @@ struct RowsArgs {
     uint8_t* pool;
     int64_t num_slots;     // num_pages * 16
     int32_t H, n;
+    int32_t warp_heads;    // KV heads that a warp goes over
     const int64_t* slots;
     uint16_t* k;           // [n][H][D], row strides k_stride and v_stride
     uint16_t* v;
@@ -23,178 +27,292 @@ struct RowsArgs {
     int32_t* err;
 };
 
-template <int D, int NG>
-struct RowPlace {   // where a token's row lies in its block
-    uint8_t* codes;
-    uint32_t* scales;
-    int tok;
-    __device__ __forceinline__ RowPlace(uint8_t* pool, int64_t slot, int H, int h, bool is_v)
-    {
-        using B = Kv4Block<D, NG>;
-        tok = (int)(slot & (kPageSize - 1));
-        uint8_t* block = pool + ((slot >> 4) * H + h) * B::kBytes;
-        codes = block + (is_v ? B::kCodes : 0);
-        scales = reinterpret_cast<uint32_t*>(block + 2 * B::kCodes + (is_v ? B::kScales : 0)) + tok * NG;
-    }
+// A turn's tokens: t alone, or t and t + 1 in slots 2m and 2m + 1.
+struct Turn {
+    int64_t slot;
+    int tokens;     // 0: the token before takes it along
+    bool known;     // the slot is one of the pool's
 };
 
-// K word m of a token: [j][i]; V half-word m: [g][i].
-template <int D>
-__device__ __forceinline__ int k_element(int m, int e)
+__device__ __forceinline__ Turn turn_of(const RowsArgs& a, int64_t t, bool report)
 {
-    constexpr int NW = D / 32;
-    return 32 * (m % NW) + 8 * (m / NW) + e;
+    const int64_t s = a.slots[t];
+    const int64_t before = (s & 1) && t > 0 ? a.slots[t - 1] : -2;
+    const int64_t after = !(s & 1) && t + 1 < a.n ? a.slots[t + 1] : -2;
+    const bool known = s >= 0 && s < a.num_slots;
+    if (!known && s != -1 && report) kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
+    return {s, known && before == s - 1 ? 0 : known && after == s + 1 ? 2 : 1, known};
 }
-template <int D>
-__device__ __forceinline__ int v_element(int m, int n)
+
+// 4 x 4 bytes across the lanes of a quad: lane n gets byte n of lanes 0 .. 3.
+__device__ __forceinline__ uint32_t quad_transpose(uint32_t w, int lane)
 {
-    constexpr int NW = D / 32;
-    return 32 * (m % NW) + 8 * n + m / NW;
+    uint32_t y = __shfl_xor_sync(0xffffffffu, w, 1);
+    w = lane & 1 ? __byte_perm(w, y, 0x3715) : __byte_perm(w, y, 0x6240);
+    y = __shfl_xor_sync(0xffffffffu, w, 2);
+    return lane & 2 ? __byte_perm(w, y, 0x3276) : __byte_perm(w, y, 0x5410);
 }
-template <int D>
-__device__ __forceinline__ int v_half_offset(int tok, int m)   // bytes from the V codes' start
+
+// The low nibbles of four bytes, as 16 bits.
+__device__ __forceinline__ uint32_t low_nibbles(uint32_t w)
 {
-    constexpr int NW = D / 32;
-    const int g = m / NW, i = m % NW;
-    return ((((tok >> 3) * 8 + g) * 4 + ((tok & 7) >> 1)) * NW + i) * 4 + (tok & 1) * 2;
+    w &= 0x0f0f0f0fu;
+    w = (w | w >> 4) & 0x00ff00ffu;
+    return (w | w >> 8) & 0xffffu;
 }
+
+template <class T>
+struct Packed;
+template <>
+struct Packed<Bf16> {
+    using V = __nv_bfloat162;
+    static constexpr uint32_t kMagic = 0x43004300u;    // 128 + code in the low bits
+    static constexpr float kOffset = -136.f;           // ... to code - 8
+    static __device__ __forceinline__ V dup(float x) { return __float2bfloat162_rn(x); }
+};
+template <>
+struct Packed<Fp16> {
+    using V = __half2;
+    static constexpr uint32_t kMagic = 0x64006400u;    // 1024 + code
+    static constexpr float kOffset = -1032.f;
+    static __device__ __forceinline__ V dup(float x) { return __float2half2_rn(x); }
+};
+template <class V>
+__device__ __forceinline__ V as_pair(uint32_t w)
+{
+    return *reinterpret_cast<const V*>(&w);
+}
+template <class V>
+__device__ __forceinline__ uint32_t as_word(V v)
+{
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// s (c - 8) + z of two codes (bits 0-3 and 16-19 of `codes`): one rounding, in the cache's type.
+template <class T>
+__device__ __forceinline__ uint32_t dequantise(uint32_t codes, typename Packed<T>::V s, typename Packed<T>::V z)
+{
+    using V = typename Packed<T>::V;
+    const V c = __hadd2(as_pair<V>((codes & 0x000f000fu) | Packed<T>::kMagic), Packed<T>::dup(Packed<T>::kOffset));
+    return as_word(__hfma2(c, s, z));
+}
+
+// The codes of this lane's 8 elements (element e in bits 4e and up) and the
+// scale word of their group, which lies in GL lanes.
+//
+// The quotient.  With r = 1 / s, k = rint(d r) is the nearest code or, close to a tie,
+// its neighbour; e = d - k s is exact and k + e r is d / s but for one rounding,
+// on a tie exactly the tie.  (Where d overflows, at -8 s of the widest
+// groups that bf16 holds, that is NaN, which the clamp takes to -8 as it should.)
+template <int GL, class T>
+__device__ __forceinline__ uint32_t quantise(const uint4& row, uint32_t* scale)
+{
+    using V = typename Packed<T>::V;
+    const uint32_t w[4] = {row.x, row.y, row.z, row.w};
+    V lo = as_pair<V>(w[0]), hi = lo;
+#pragma unroll
+    for (int i = 1; i < 4; ++i) {
+        lo = __hmin2_nan(lo, as_pair<V>(w[i]));
+        hi = __hmax2_nan(hi, as_pair<V>(w[i]));
+    }
+    // (min, -max) of the group: one minimum for both.
+    const uint32_t l = as_word(lo), h = as_word(__hneg2(hi));
+    V m = __hmin2_nan(as_pair<V>(__byte_perm(l, h, 0x5410)), as_pair<V>(__byte_perm(l, h, 0x7632)));
+#pragma unroll
+    for (int k = 1; k < GL; k <<= 1) m = __hmin2_nan(m, as_pair<V>(__shfl_xor_sync(0xffffffffu, as_word(m), k)));
+    const float least = T::lo(as_word(m)), most = -T::hi(as_word(m));
+    const float half = most * 0.5f - least * 0.5f;
+    const bool broken = !(half < INFINITY);   // an infinity or a NaN in the group
+    uint32_t meta = T::pack(half / 7.5f, 0.f);
+    const float s = T::lo(meta);
+    meta |= T::pack(fmaf(8.f, s, least), 0.f) << 16;
+    const float z = T::hi(meta);
+    *scale = broken ? 0x7fff7fffu : meta;     // NaN in either type
+    // Tiny steps are scaled up, exactly, so that 1 / s is finite; a step of 0 makes every quotient 0.
+    const float up = s < 0x1p-100f ? 0x1p64f : 1.f, su = s * up;
+    const float r = s > 0.f ? 1.f / su : 0.f;
+    constexpr float kRound = 12582912.f;      // 1.5 * 2^23: adding it rounds to an integer, in the low bits
+    const uint64_t up2 = f2_pack(up, up), z2 = f2_pack(-z * up, -z * up), s2 = f2_pack(-su, -su), r2 = f2_pack(r, r);
+    const uint64_t round2 = f2_pack(kRound, kRound), one2 = f2_pack(1.f, 1.f), back2 = f2_pack(-kRound, -kRound);
+    uint32_t codes = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint64_t d = f2_fma(f2_pack(T::lo(w[i]), T::hi(w[i])), up2, z2);
+        const uint64_t k = f2_fma(f2_fma(d, r2, round2), one2, back2);
+        const uint64_t q = f2_fma(f2_fma(k, s2, d), r2, k);
+        float q0, q1;
+        f2_unpack(q, q0, q1);
+        const uint32_t c0 = __float_as_uint(fminf(fmaxf(q0, -8.f), 7.f) + (kRound + 8.f));
+        const uint32_t c1 = __float_as_uint(fminf(fmaxf(q1, -8.f), 7.f) + (kRound + 8.f));
+        codes |= (c0 & 15u) << (8 * i) | (c1 & 15u) << (8 * i + 4);
+    }
+    return broken ? 0x88888888u : codes;
+}
+
+// Codes in element order (e at bit 4e) <-> a word of K's codes (e at 16 (e % 2) + 4 (e / 2)).
+__device__ __forceinline__ uint32_t k_word(uint32_t codes)
+{
+    return low_nibbles(codes) | low_nibbles(codes >> 4) << 16;
+}
+
+// Byte offsets in a block.
+template <int D>
+__device__ __forceinline__ int v_word_offset(int tok, int g, int i)   // of the word that holds token tok
+{
+    return ((((tok >> 3) * 8 + g) * 4 + ((tok & 7) >> 1)) * (D / 32) + i) * 4;
+}
+
+// A lane's part of one step over HS heads: rows are (token of the turn, head)
+// in D / 8 lanes each, tokens 16 lanes apart.
+template <int D>
+struct Place {
+    static constexpr int HS = 128 / D;   // heads of a step
+    int second, head, m;                 // token of the turn, head of the step, 8-element part of the row
+    __device__ __forceinline__ explicit Place(int lane) : second(lane >> 4), head((lane & 15) / (D / 8)), m(lane % (D / 8)) {}
+};
 
 template <int D, int NG, class T>
 __global__ void __launch_bounds__(kRowWarps * 32) write_kernel(RowsArgs a)
 {
-    constexpr int E = D / 32;              // elements of a lane
-    constexpr int GL = 32 / NG;            // lanes of a group
-    __shared__ uint8_t row[kRowWarps][D];
+    using B = Kv4Block<D, NG>;
+    constexpr int GL = D / NG / 8, HS = Place<D>::HS, NW = D / 32;
     griddep_wait();
     griddep_launch_dependents();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t rows = (int64_t)a.n * a.H * 2;
-    for (int64_t r = (int64_t)blockIdx.x * kRowWarps + warp; r < rows; r += (int64_t)gridDim.x * kRowWarps) {
-        const bool is_v = r & 1;
-        const int h = (int)((r >> 1) % a.H);
-        const int64_t tok = (r >> 1) / a.H;
-        const int64_t slot = a.slots[tok];
-        if (slot < 0 || slot >= a.num_slots) {
-            if (slot != -1 && lane == 0) kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
-            continue;
-        }
-        const uint16_t* src = (is_v ? a.v + tok * a.v_stride : a.k + tok * a.k_stride) + (int64_t)h * D + lane * E;
-        uint32_t w[E / 2];
-        if constexpr (E == 4) {
-            const uint2 u = *reinterpret_cast<const uint2*>(src);
-            w[0] = u.x;
-            w[1] = u.y;
-        } else {
-            w[0] = *reinterpret_cast<const uint32_t*>(src);
-        }
-        float x[E];
-#pragma unroll
-        for (int i = 0; i < E / 2; ++i) {
-            x[2 * i] = T::lo(w[i]);
-            x[2 * i + 1] = T::hi(w[i]);
-        }
-        float lo = x[0], hi = x[0], sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-            lo = fminf(lo, x[i]);
-            hi = fmaxf(hi, x[i]);
-            sum += x[i] * 0.f;             // NaN where an element is not finite
-        }
-#pragma unroll
-        for (int m = 1; m < GL; m <<= 1) {
-            lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, m));
-            hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, m));
-            sum += __shfl_xor_sync(0xffffffffu, sum, m);
-        }
-        // s and z as they are held; the codes follow from those.
-        uint32_t meta = T::pack((hi * 0.5f - lo * 0.5f) / 7.5f, 0.f);
-        float s = T::lo(meta);
-        meta = (meta & 0xffffu) | (T::pack(fmaf(8.f, s, lo), 0.f) << 16);
-        float z = T::hi(meta);
-        if (sum != 0.f) meta = T::pack(__int_as_float(0x7fc00000), __int_as_float(0x7fc00000));
-        const bool flat = !(s > 0.f) || sum != 0.f;
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const float c = flat ? 8.f : fminf(fmaxf(rintf((x[i] - z) / s) + 8.f, 0.f), 15.f);
-            row[warp][lane * E + i] = (uint8_t)(int)c;
-        }
-        __syncwarp();
-        const RowPlace<D, NG> to(a.pool, slot, a.H, h, is_v);
-        if (lane % GL == 0) to.scales[lane / GL] = meta;
-        if (!is_v) {
-            if (lane < D / 8) {
-                uint32_t word = 0;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) word |= (uint32_t)row[warp][k_element<D>(lane, e)] << (16 * (e & 1) + 4 * (e >> 1));
-                reinterpret_cast<uint32_t*>(to.codes)[to.tok * (D / 8) + lane] = word;
+    const int lane = threadIdx.x & 31;
+    const Place<D> at(lane);
+    const int h0 = blockIdx.y * a.warp_heads, h1 = min(a.H, h0 + a.warp_heads);
+    const int64_t first = ((int64_t)blockIdx.x * kRowWarps + (threadIdx.x >> 5)) * 2;
+#pragma unroll 1
+    for (int64_t t = first; t < min(first + 2, (int64_t)a.n); ++t) {
+        const Turn turn = turn_of(a, t, lane == 0 && blockIdx.y == 0);
+        if (!turn.known || turn.tokens == 0) continue;
+        const bool pair = turn.tokens == 2;
+        const int tok0 = (int)(turn.slot & (kPageSize - 1)), tok = tok0 + (pair ? at.second : 0);
+        uint8_t* const page = a.pool + (turn.slot >> 4) * a.H * B::kBytes;
+        const int64_t row = t + (pair ? at.second : 0);
+        const bool mine = pair || at.second == 0;
+#pragma unroll 1
+        for (int h = h0; h < h1; h += HS) {
+            const int head = h + at.head;
+            const bool on = mine && head < h1;
+            uint4 kr = make_uint4(0u, 0u, 0u, 0u), vr = kr;
+            if (on) {
+                kr = __ldcs(reinterpret_cast<const uint4*>(a.k + row * a.k_stride + head * D) + at.m);
+                vr = __ldcs(reinterpret_cast<const uint4*>(a.v + row * a.v_stride + head * D) + at.m);
             }
-        } else if (lane < D / 4) {
-            uint32_t half = 0;
-#pragma unroll
-            for (int n = 0; n < 4; ++n) half |= (uint32_t)row[warp][v_element<D>(lane, n)] << (4 * n);
-            *reinterpret_cast<uint16_t*>(to.codes + v_half_offset<D>(to.tok, lane)) = (uint16_t)half;
+            uint8_t* const block = page + (int64_t)head * B::kBytes;
+            uint32_t ks, vs;
+            const uint32_t kw = k_word(quantise<GL, T>(kr, &ks));
+            const uint32_t vc = quad_transpose(quantise<GL, T>(vr, &vs), lane);
+            // Lane (i, n) of a token now holds byte n of the four lanes of word i: elements g = 2n and 2n + 1.
+            const int i = at.m >> 2, n = at.m & 3;
+            const uint32_t v = low_nibbles(vc) | low_nibbles(vc >> 4) << 16;
+            const uint32_t other = __shfl_xor_sync(0xffffffffu, v, 16);
+            if (on) {
+                reinterpret_cast<uint32_t*>(block)[(tok * 4 + (at.m & 3)) * NW + (at.m >> 2)] = kw;
+                if (at.m % GL == 0) {
+                    uint32_t* scales = reinterpret_cast<uint32_t*>(block + 2 * B::kCodes) + tok * NG + at.m / GL;
+                    scales[0] = ks;
+                    scales[kPageSize * NG] = vs;
+                }
+                uint8_t* const vcodes = block + B::kCodes;
+                if (pair) {   // the first token's lanes write g = 2n, the second's 2n + 1
+                    const uint32_t word = at.second ? __byte_perm(other, v, 0x7632) : __byte_perm(v, other, 0x5410);
+                    *reinterpret_cast<uint32_t*>(vcodes + v_word_offset<D>(tok0, 2 * n + at.second, i)) = word;
+                } else {
+                    uint8_t* const to = vcodes + v_word_offset<D>(tok, 2 * n, i) + (tok & 1) * 2;
+                    *reinterpret_cast<uint16_t*>(to) = (uint16_t)v;
+                    *reinterpret_cast<uint16_t*>(to + 4 * NW * 4) = (uint16_t)(v >> 16);
+                }
+            }
         }
-        __syncwarp();
     }
 }
 
 template <int D, int NG, class T>
 __global__ void __launch_bounds__(kRowWarps * 32) read_kernel(RowsArgs a)
 {
-    constexpr int E = D / 32;
-    constexpr int GL = 32 / NG;
-    __shared__ uint8_t row[kRowWarps][D];
+    using B = Kv4Block<D, NG>;
+    using V = typename Packed<T>::V;
+    constexpr int GL = D / NG / 8, HS = Place<D>::HS, NW = D / 32;
     griddep_wait();
     griddep_launch_dependents();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t rows = (int64_t)a.n * a.H * 2;
-    for (int64_t r = (int64_t)blockIdx.x * kRowWarps + warp; r < rows; r += (int64_t)gridDim.x * kRowWarps) {
-        const bool is_v = r & 1;
-        const int h = (int)((r >> 1) % a.H);
-        const int64_t tok = (r >> 1) / a.H;
-        const int64_t slot = a.slots[tok];
-        uint16_t* dst = (is_v ? a.v + tok * a.v_stride : a.k + tok * a.k_stride) + (int64_t)h * D + lane * E;
-        uint32_t w[E / 2] = {};
-        if (slot >= 0 && slot < a.num_slots) {
-            const RowPlace<D, NG> from(a.pool, slot, a.H, h, is_v);
-            if (!is_v) {
-                if (lane < D / 8) {
-                    const uint32_t word = reinterpret_cast<const uint32_t*>(from.codes)[from.tok * (D / 8) + lane];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) row[warp][k_element<D>(lane, e)] = (word >> (16 * (e & 1) + 4 * (e >> 1))) & 15;
+    const int lane = threadIdx.x & 31;
+    const Place<D> at(lane);
+    const int h0 = blockIdx.y * a.warp_heads, h1 = min(a.H, h0 + a.warp_heads);
+    const int64_t first = ((int64_t)blockIdx.x * kRowWarps + (threadIdx.x >> 5)) * 2;
+#pragma unroll 1
+    for (int64_t t = first; t < min(first + 2, (int64_t)a.n); ++t) {
+        const Turn turn = turn_of(a, t, lane == 0 && blockIdx.y == 0);
+        if (turn.tokens == 0) continue;
+        const bool pair = turn.tokens == 2;
+        if (!turn.known) {
+            for (int h = h0; h < h1; h += HS)
+                if (at.second == 0 && h + at.head < h1) {
+                    reinterpret_cast<uint4*>(a.k + t * a.k_stride + (h + at.head) * D)[at.m] = make_uint4(0u, 0u, 0u, 0u);
+                    reinterpret_cast<uint4*>(a.v + t * a.v_stride + (h + at.head) * D)[at.m] = make_uint4(0u, 0u, 0u, 0u);
                 }
-            } else if (lane < D / 4) {
-                const uint32_t half = *reinterpret_cast<const uint16_t*>(from.codes + v_half_offset<D>(from.tok, lane));
-#pragma unroll
-                for (int n = 0; n < 4; ++n) row[warp][v_element<D>(lane, n)] = (half >> (4 * n)) & 15;
-            }
-            __syncwarp();
-            const uint32_t meta = from.scales[lane / GL];
-            const float s = T::lo(meta), z = T::hi(meta);
-            float x[E];
-#pragma unroll
-            for (int i = 0; i < E; ++i) x[i] = fmaf(s, (float)row[warp][lane * E + i] - 8.f, z);
-#pragma unroll
-            for (int i = 0; i < E / 2; ++i) w[i] = T::pack(x[2 * i], x[2 * i + 1]);
-            __syncwarp();
-        } else if (slot != -1 && lane == 0) {
-            kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
+            continue;
         }
-        if constexpr (E == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
-        else *reinterpret_cast<uint32_t*>(dst) = w[0];
+        const int tok0 = (int)(turn.slot & (kPageSize - 1)), tok = tok0 + (pair ? at.second : 0);
+        const uint8_t* const page = a.pool + (turn.slot >> 4) * a.H * B::kBytes;
+#pragma unroll 1
+        for (int h = h0; h < h1; h += HS) {
+            const int head = h + at.head;
+            const bool on = (pair || at.second == 0) && head < h1;
+            // K: a word of a token's row per lane.
+            if (on) {
+                const uint8_t* block = page + (int64_t)head * B::kBytes;
+                const uint32_t w = reinterpret_cast<const uint32_t*>(block)[(tok * 4 + (at.m & 3)) * NW + (at.m >> 2)];
+                const uint32_t meta = reinterpret_cast<const uint32_t*>(block + 2 * B::kCodes)[tok * NG + at.m / GL];
+                const V s = as_pair<V>(__byte_perm(meta, meta, 0x1010)), z = as_pair<V>(__byte_perm(meta, meta, 0x3232));
+                __stcs(reinterpret_cast<uint4*>(a.k + (t + at.second) * a.k_stride + head * D) + at.m,
+                       make_uint4(dequantise<T>(w, s, z), dequantise<T>(w >> 4, s, z), dequantise<T>(w >> 8, s, z), dequantise<T>(w >> 12, s, z)));
+            }
+            // V: lane (g, j) takes elements 32 i + 8 j + g of both tokens; the 8x8
+            // tile [g][(j, token)] transposed gives lane ((j, token), c) elements 32 i + 8 j + 2c and 2c + 1 of one token.
+            const int g = lane >> 2, j = lane & 3, r = lane >> 2, c = lane & 3;
+            const bool stored = pair || (r & 1) == (tok0 & 1);
+            uint16_t* const out = a.v + (t + (pair ? r & 1 : 0)) * a.v_stride + 8 * (r >> 1) + 2 * c;
+#pragma unroll
+            for (int u = 0; u < HS; ++u) {
+                if (h + u >= h1) break;
+                const uint8_t* block = page + (int64_t)(h + u) * B::kBytes;
+                const uint32_t* scales = reinterpret_cast<const uint32_t*>(block + 2 * B::kCodes + B::kScales) + (tok0 & ~1) * NG;
+                uint32_t w[NW];
+                const uint8_t* const codes = block + B::kCodes + v_word_offset<D>(tok0, g, 0);
+                if constexpr (NW == 4) {
+                    const uint4 x = *reinterpret_cast<const uint4*>(codes);
+                    w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+                } else {
+                    const uint2 x = *reinterpret_cast<const uint2*>(codes);
+                    w[0] = x.x, w[1] = x.y;
+                }
+#pragma unroll
+                for (int i = 0; i < NW; ++i) {
+                    const uint32_t m0 = scales[i / (NW / NG)], m1 = scales[NG + i / (NW / NG)];
+                    const uint32_t x = dequantise<T>(w[i] >> (4 * j), as_pair<V>(__byte_perm(m0, m1, 0x5410)), as_pair<V>(__byte_perm(m0, m1, 0x7632)));
+                    const uint32_t y = movmatrix_trans(x);
+                    if (stored) __stcs(reinterpret_cast<uint32_t*>(out + (h + u) * D + 32 * i), y);
+                }
+            }
+        }
     }
 }
 
 template <bool kWrite>
 struct LaunchRows {
-    const RowsArgs& a;
+    RowsArgs& a;
     cudaStream_t st;
     template <int D, int NG, class T>
     cudaError_t operator()() const
     {
-        const int64_t rows = (int64_t)a.n * a.H * 2;
-        const int64_t ctas = (rows + kRowWarps - 1) / kRowWarps;
-        const dim3 grid((unsigned)(ctas < (1 << 20) ? ctas : (1 << 20)));
+        // A warp goes over as many heads as leave every SM some 32 warps of work.
+        const int64_t turns = ((int64_t)a.n + 1) / 2;
+        int heads = Place<D>::HS;
+        while (heads < 8 && heads < a.H && turns * ((a.H + 2 * heads - 1) / (2 * heads)) >= 152 * 32) heads *= 2;
+        a.warp_heads = heads;
+        const dim3 grid((unsigned)((turns + kRowWarps - 1) / kRowWarps), (unsigned)((a.H + heads - 1) / heads));
         return kv4_launch(kWrite ? write_kernel<D, NG, T> : read_kernel<D, NG, T>, grid, kRowWarps * 32, 0, st, a);
     }
 };

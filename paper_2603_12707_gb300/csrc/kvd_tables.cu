@@ -7,20 +7,29 @@
 // pages entries U_r - u_r .. U_r - 1 of the free ring, and it is granted if
 // T_r <= max_tokens and U_r <= free pages (or u_r = 0).  Rows that give tokens
 // back are the same with a third sum.
+//
+// Every CTA reads all rows and forms the sums (a few loads and a scan; rows are
+// few next to tokens) and then works out its own tokens, whose rows it
+// finds by binary search, so the map takes one launch.  What the call
+// updates (lengths, the ring's state, pages given back) is written by the last CTA that has
+// read it: a counter in the tables' state, zero between calls.
 #include "kvd_kv4.h"
 #include "kvd_ptx.cuh"
 
 namespace kvd {
 namespace {
 
-constexpr int kTablesThreads = 1024;
+constexpr int kTablesThreads = 512;
 constexpr int kRowsPerThread = kKv4MaxBatch / kTablesThreads;
+constexpr int kThreadTokens = 4;   // consecutive tokens of a thread: 16-byte stores
+constexpr int kCtaTokens = kTablesThreads * kThreadTokens;
 
 struct TablesArgs {
     int32_t* block_table;
     const int32_t* lens;
     int32_t* ring;
     const int32_t* state;
+    int32_t* arrivals;      // the state's counter
     int64_t num_pages;
     int32_t max_seqs, max_pages, batch, max_tokens;
     const int32_t* seq_ids;
@@ -31,165 +40,226 @@ struct TablesArgs {
     int32_t* lens_out;
     int32_t* state_out;
     int32_t* err;
+    int32_t wide;           // slots and positions are 16-byte aligned
 };
 
 __device__ __forceinline__ int pages_of(int n) { return (n + kPageSize - 1) / kPageSize; }
 
-// What the sums run over: tokens, pages taken, pages given back.
+// What the sums run over: tokens; pages taken in the high, given back in the low half.
 struct Sums {
-    int64_t tokens, take, back;
+    int64_t tokens;
+    uint64_t pages;
+    __device__ __forceinline__ uint32_t take() const { return (uint32_t)(pages >> 32); }
+    __device__ __forceinline__ uint32_t back() const { return (uint32_t)pages; }
 };
 
-__device__ __forceinline__ Sums operator+(const Sums& a, const Sums& b)
-{
-    return {a.tokens + b.tokens, a.take + b.take, a.back + b.back};
-}
+__device__ __forceinline__ Sums operator+(const Sums& a, const Sums& b) { return {a.tokens + b.tokens, a.pages + b.pages}; }
+__device__ __forceinline__ Sums operator-(const Sums& a, const Sums& b) { return {a.tokens - b.tokens, a.pages - b.pages}; }
 
-__device__ __forceinline__ Sums shift_up(const Sums& a, int n)
+__device__ __forceinline__ Sums scan_warp(Sums s, int lane)
 {
-    return {__shfl_up_sync(0xffffffffu, a.tokens, n), __shfl_up_sync(0xffffffffu, a.take, n),
-            __shfl_up_sync(0xffffffffu, a.back, n)};
+#pragma unroll
+    for (int n = 1; n < 32; n <<= 1) {
+        const Sums o = {__shfl_up_sync(0xffffffffu, s.tokens, n), __shfl_up_sync(0xffffffffu, s.pages, n)};
+        if (lane >= n) s = s + o;
+    }
+    return s;
 }
 
 // Exclusive sums over the block's threads, and the total.
-__device__ Sums block_scan(const Sums& mine, Sums* total, Sums* warp_sums)
+__device__ __forceinline__ Sums block_scan(const Sums& mine, Sums* total, Sums* warp_sums)
 {
+    constexpr int W = kTablesThreads / 32;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    Sums s = mine;
-    for (int n = 1; n < 32; n <<= 1) {
-        const Sums o = shift_up(s, n);
-        if (lane >= n) s = s + o;
-    }
+    const Sums s = scan_warp(mine, lane);
     if (lane == 31) warp_sums[warp] = s;
     __syncthreads();
-    if (warp == 0) {
-        Sums w = warp_sums[lane];
-        for (int n = 1; n < 32; n <<= 1) {
-            const Sums o = shift_up(w, n);
-            if (lane >= n) w = w + o;
-        }
-        warp_sums[lane] = w;
+    const Sums w = scan_warp(lane < W ? warp_sums[lane] : Sums{0, 0}, lane);
+    const int from = warp > 0 ? warp - 1 : 0;
+    Sums before = {__shfl_sync(0xffffffffu, w.tokens, from), __shfl_sync(0xffffffffu, w.pages, from)};
+    if (warp == 0) before = {0, 0};
+    *total = {__shfl_sync(0xffffffffu, w.tokens, W - 1), __shfl_sync(0xffffffffu, w.pages, W - 1)};
+    return before + s - mine;
+}
+
+// Row of entry x: the last row whose first entry is at or before it (not empty, where x is below the sum).
+__device__ __forceinline__ int find_row(const int32_t* first, int batch, int x)
+{
+    int lo = 0, hi = batch;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first[mid] <= x) lo = mid;
+        else hi = mid;
     }
-    __syncthreads();
-    *total = warp_sums[31];
-    const Sums before = warp > 0 ? warp_sums[warp - 1] : Sums{0, 0, 0};
-    return {before.tokens + s.tokens - mine.tokens, before.take + s.take - mine.take, before.back + s.back - mine.back};
+    return lo;
 }
 
 __global__ void __launch_bounds__(kTablesThreads) tables_kernel(TablesArgs a)
 {
-    __shared__ Sums warp_sums[32];
-    __shared__ int32_t row_tok[kKv4MaxBatch];    // first token of each row (at most max_tokens)
-    __shared__ int32_t row_page[kKv4MaxBatch];   // its first entry of the ring, -1: refused
-    __shared__ int32_t row_seq[kKv4MaxBatch], row_len[kKv4MaxBatch];
-    __shared__ unsigned long long taken;
+    extern __shared__ int32_t rows[];            // per row:
+    int32_t* const row_tok = rows;               // first token (at most max_tokens)
+    int32_t* const row_page = row_tok + a.batch; // its first entry of the ring, -1: refused
+    int32_t* const row_len = row_page + a.batch; // tokens before
+    int32_t* const row_seq = row_len + a.batch;
+    int32_t* const row_back = row_seq + a.batch; // first of the pages given back
+    __shared__ Sums warp_sums[kTablesThreads / 32];
+    __shared__ uint32_t taken;
+    __shared__ int is_last;
     griddep_wait();
     griddep_launch_dependents();
     const int tid = threadIdx.x;
+    const bool speaks = blockIdx.x == 0;         // one CTA reports what all find
     if (tid == 0) taken = 0;
 
     int64_t head = a.state[0], count = a.state[1];
     if (head < 0 || head >= a.num_pages || count < 0 || count > a.num_pages) {
-        if (tid == 0) kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
+        if (tid == 0 && speaks) kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
         head = count = 0;
     }
-    if (a.lens_out != a.lens)
-        for (int i = tid; i < a.max_seqs; i += kTablesThreads) a.lens_out[i] = a.lens[i];
 
     // The rows of this thread, consecutive ones.
     const int per = (a.batch + kTablesThreads - 1) / kTablesThreads;
-    int seq[kRowsPerThread], ctx[kRowsPerThread], add[kRowsPerThread], take[kRowsPerThread], back[kRowsPerThread];
-    bool fine[kRowsPerThread];
-    Sums mine{0, 0, 0};
+    const int64_t most = (int64_t)a.max_pages * kPageSize;
+    int seq[kRowsPerThread], ctx[kRowsPerThread], add[kRowsPerThread];
+    Sums of[kRowsPerThread], mine{0, 0};
 #pragma unroll
     for (int k = 0; k < kRowsPerThread; ++k) {
         const int r = tid * per + k;
-        seq[k] = ctx[k] = add[k] = take[k] = back[k] = 0;
-        fine[k] = false;
-        if (k >= per || r >= a.batch) continue;
-        seq[k] = a.seq_ids ? a.seq_ids[r] : r;
-        add[k] = a.new_lens[r];
-        const bool known = seq[k] >= 0 && seq[k] < a.max_seqs;
-        ctx[k] = known ? a.lens[seq[k]] : 0;
-        const int64_t end = (int64_t)ctx[k] + add[k], most = (int64_t)a.max_pages * kPageSize;
-        fine[k] = known && ctx[k] >= 0 && ctx[k] <= most && end >= 0 && end <= most;
-        if (fine[k]) {
-            const int d = pages_of((int)end) - pages_of(ctx[k]);
-            take[k] = max(d, 0);
-            back[k] = max(-d, 0);
-        } else {
-            kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
+        seq[k] = -1;
+        add[k] = 0;
+        if (k < per && r < a.batch) {
+            seq[k] = a.seq_ids ? a.seq_ids[r] : r;
+            add[k] = a.new_lens[r];
         }
-        mine = mine + Sums{(int64_t)max(add[k], 0), take[k], back[k]};
+    }
+#pragma unroll
+    for (int k = 0; k < kRowsPerThread; ++k) ctx[k] = seq[k] >= 0 && seq[k] < a.max_seqs ? a.lens[seq[k]] : -1;
+#pragma unroll
+    for (int k = 0; k < kRowsPerThread; ++k) {
+        const int64_t end = (int64_t)ctx[k] + add[k];
+        const bool fine = ctx[k] >= 0 && ctx[k] <= most && end >= 0 && end <= most;
+        const int d = fine ? pages_of((int)end) - pages_of(ctx[k]) : 0;
+        of[k] = {max(add[k], 0), (uint64_t)max(d, 0) << 32 | (uint32_t)max(-d, 0)};
+        if (!fine) ctx[k] = -1;
+        mine = mine + of[k];
     }
     Sums total;
     Sums at = block_scan(mine, &total, warp_sums);
-    const bool fits = count + total.back <= a.num_pages;   // else a page has been given back twice
-    if (!fits && tid == 0) kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
-    if (a.lens_out != a.lens) __syncthreads();             // the copy above, before the changes below
+    const bool fits = count + total.back() <= a.num_pages;   // else a page has been given back twice
+    if (!fits && tid == 0 && speaks) kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
 
+    int32_t errors = 0;
 #pragma unroll
     for (int k = 0; k < kRowsPerThread; ++k) {
         const int r = tid * per + k;
         if (k >= per || r >= a.batch) continue;
-        const int grow = max(add[k], 0);
-        const bool room = at.tokens + grow <= a.max_tokens || grow == 0;
-        const bool paid = take[k] == 0 || at.take + take[k] <= count;
-        const bool ok = fine[k] && room && paid && (fits || add[k] >= 0);
-        if (fine[k] && !room) kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
-        if (fine[k] && room && !paid) kv4_error(a.err, KVC_DEVERR_OOM);
+        const bool room = at.tokens + of[k].tokens <= a.max_tokens || of[k].tokens == 0;
+        const bool paid = of[k].take() == 0 || (int64_t)at.take() + of[k].take() <= count;
+        const bool ok = ctx[k] >= 0 && room && paid && (fits || add[k] >= 0);
+        if (ctx[k] < 0 || !room) errors |= KVC_DEVERR_SEQ_RANGE;
+        else if (!paid) errors |= KVC_DEVERR_OOM;
         row_tok[r] = (int32_t)min(at.tokens, (int64_t)a.max_tokens);
-        row_page[r] = ok ? (int32_t)at.take : -1;
-        row_seq[r] = seq[k];
+        row_page[r] = ok ? (int32_t)at.take() : -1;
         row_len[r] = ctx[k];
-        if (a.cu) a.cu[r] = (int32_t)min(at.tokens, (int64_t)INT32_MAX);
-        if (ok) {
-            a.lens_out[seq[k]] = ctx[k] + add[k];
-            if (take[k]) atomicMax(&taken, (unsigned long long)(at.take + take[k]));
-            for (int i = 0; i < back[k]; ++i) {
-                const int32_t page = a.block_table[(int64_t)seq[k] * a.max_pages + pages_of(ctx[k] + add[k]) + i];
-                a.ring[(head + count + at.back + i) % a.num_pages] = page;
-            }
-        }
-        at = at + Sums{(int64_t)grow, take[k], back[k]};
+        row_seq[r] = seq[k];
+        row_back[r] = (int32_t)at.back();
+        if (ok && of[k].take()) atomicMax(&taken, at.take() + of[k].take());
+        at = at + of[k];
     }
+    if (errors && speaks) kv4_error(a.err, errors);
     __syncthreads();
-    if (tid == 0) {
-        if (a.cu) a.cu[a.batch] = (int32_t)min(total.tokens, (int64_t)INT32_MAX);
-        a.state_out[0] = (int32_t)((head + (int64_t)taken) % a.num_pages);
-        a.state_out[1] = (int32_t)(count - (int64_t)taken + (fits ? total.back : 0));
-    }
+    // Every thread of this CTA has read the state and the lengths.
+    if (tid == 0) is_last = gridDim.x == 1 || atomicAdd(a.arrivals, 1) == (int)gridDim.x - 1;
 
-    // Tokens: the last row that starts at or before token t and is not empty holds it.
-    const int64_t live = min(total.tokens, (int64_t)a.max_tokens);
-    for (int64_t t = tid; t < a.max_tokens; t += kTablesThreads) {
-        int64_t slot = -1;
-        int pos = -1;
-        if (t < live) {
-            int lo = 0, hi = a.batch;   // first row that starts past t
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (row_tok[mid] <= t) lo = mid + 1;
-                else hi = mid;
+    // Tokens.
+    const int live = (int)min(total.tokens, (int64_t)a.max_tokens);
+    for (int64_t t0 = ((int64_t)blockIdx.x * kTablesThreads + tid) * kThreadTokens; t0 < a.max_tokens;
+         t0 += (int64_t)gridDim.x * kCtaTokens) {
+        int64_t slot[kThreadTokens];
+        int pos[kThreadTokens];
+        int r = -1, stop = 0, col_now = -1;      // the row in work, its end, the page in hand
+        int32_t page = -1;
+#pragma unroll
+        for (int k = 0; k < kThreadTokens; ++k) {
+            const int t = (int)t0 + k;
+            slot[k] = -1;
+            pos[k] = -1;
+            if (t >= live) continue;
+            if (t >= stop) {
+                r = r < 0 ? find_row(row_tok, a.batch, t) : r + 1;
+                while (r + 1 < a.batch && row_tok[r + 1] <= t) ++r;
+                stop = r + 1 < a.batch ? row_tok[r + 1] : live;
+                col_now = -1;
             }
-            const int r = lo - 1;
-            if (row_page[r] >= 0) {
-                pos = row_len[r] + (int)(t - row_tok[r]);
-                const int col = pos / kPageSize, fresh = col - pages_of(row_len[r]);
+            if (row_page[r] < 0) continue;
+            pos[k] = row_len[r] + (t - row_tok[r]);
+            const int col = pos[k] / kPageSize, fresh = col - pages_of(row_len[r]);
+            if (col != col_now) {
                 int32_t* entry = a.block_table + (int64_t)row_seq[r] * a.max_pages + col;
-                int32_t page;
                 if (fresh >= 0) {
-                    page = a.ring[(head + row_page[r] + fresh) % a.num_pages];
-                    if (pos % kPageSize == 0) *entry = page;   // the token that opens the page
+                    int64_t from = head + row_page[r] + fresh;
+                    if (from >= a.num_pages) from -= a.num_pages;
+                    page = a.ring[from];
+                    if (pos[k] % kPageSize == 0) *entry = page;   // the token that opens the page
                 } else {
                     page = *entry;
                 }
-                if (page >= 0 && page < a.num_pages) slot = (int64_t)page * kPageSize + pos % kPageSize;
-                else kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
+                col_now = col;
+                if (page < 0 || page >= a.num_pages) {
+                    kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
+                    page = -1;
+                }
             }
+            if (page >= 0) slot[k] = (int64_t)page * kPageSize + pos[k] % kPageSize;
         }
-        a.slots[t] = slot;
-        if (a.positions) a.positions[t] = pos;
+        if (a.wide && t0 + kThreadTokens <= a.max_tokens) {
+            longlong2* to = reinterpret_cast<longlong2*>(a.slots + t0);
+            to[0] = make_longlong2(slot[0], slot[1]);
+            to[1] = make_longlong2(slot[2], slot[3]);
+            if (a.positions) *reinterpret_cast<int4*>(a.positions + t0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < kThreadTokens; ++k)
+                if (t0 + k < a.max_tokens) {
+                    a.slots[t0 + k] = slot[k];
+                    if (a.positions) a.positions[t0 + k] = pos[k];
+                }
+        }
+    }
+    __syncthreads();
+    if (!is_last) return;
+
+    // What the call updates, by the CTA that came last to reading it.
+    if (a.lens_out != a.lens) {
+        for (int i = tid; i < a.max_seqs; i += kTablesThreads) a.lens_out[i] = a.lens[i];
+        __syncthreads();
+    }
+    at = at - mine;
+#pragma unroll
+    for (int k = 0; k < kRowsPerThread; ++k) {
+        const int r = tid * per + k;
+        if (k >= per || r >= a.batch) continue;
+        if (a.cu) a.cu[r] = (int32_t)min(at.tokens, (int64_t)INT32_MAX);
+        if (row_page[r] >= 0) a.lens_out[seq[k]] = ctx[k] + add[k];
+        at = at + of[k];
+    }
+    // The k-th page given back: from its row's first page that is not needed any more.
+    const int back = fits ? (int)total.back() : 0;
+    for (int k = tid; k < back; k += kTablesThreads) {
+        const int r = find_row(row_back, a.batch, k);
+        const int kept = pages_of(row_len[r] + a.new_lens[r]);
+        const int32_t page = a.block_table[(int64_t)row_seq[r] * a.max_pages + kept + (k - row_back[r])];
+        int64_t to = head + count + k;
+        if (to >= a.num_pages) to -= a.num_pages;
+        a.ring[to] = page;
+    }
+    if (tid == 0) {
+        if (a.cu) a.cu[a.batch] = (int32_t)min(total.tokens, (int64_t)INT32_MAX);
+        int64_t next = head + taken;
+        if (next >= a.num_pages) next -= a.num_pages;
+        a.state_out[0] = (int32_t)next;
+        a.state_out[1] = (int32_t)(count - taken + back);
+        *a.arrivals = 0;
     }
 }
 
@@ -218,6 +288,7 @@ extern "C" KVC_API int kv_tables_step(const kv_tables* tables, int32_t batch, co
     a.lens = tables->lens;
     a.ring = tables->free_ring;
     a.state = tables->free_state;
+    a.arrivals = tables->free_state + 2;
     a.num_pages = tables->num_pages;
     a.max_seqs = tables->max_seqs;
     a.max_pages = tables->max_pages;
@@ -231,6 +302,14 @@ extern "C" KVC_API int kv_tables_step(const kv_tables* tables, int32_t batch, co
     a.lens_out = lens_out ? lens_out : tables->lens;
     a.state_out = free_state_out ? free_state_out : tables->free_state;
     a.err = device_error;
-    return kv4_launch_result(
-        kv4_launch(tables_kernel, dim3(1), kTablesThreads, 0, static_cast<cudaStream_t>(stream), a));
+    a.wide = kv4_aligned(slots, 16) && kv4_aligned(positions, 16);
+    static OncePerDevice once;
+    constexpr int kRowBytes = 5 * (int)sizeof(int32_t);
+    if (cudaError_t e = once.set_attribute(tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowBytes * kKv4MaxBatch);
+        e != cudaSuccess)
+        return kv4_launch_result(e);
+    // A CTA for every kCtaTokens tokens, up to one per SM (every one reads all rows).
+    const int64_t ctas = ((int64_t)max_tokens + kCtaTokens - 1) / kCtaTokens;
+    return kv4_launch_result(kv4_launch(tables_kernel, dim3((unsigned)(ctas < 1 ? 1 : ctas < 152 ? ctas : 152)), kTablesThreads,
+                                        (size_t)kRowBytes * batch, static_cast<cudaStream_t>(stream), a));
 }
