@@ -47,13 +47,11 @@ __device__ __forceinline__ Turn turn_of(const RowsArgs& a, int64_t t, bool repor
 // 4 x 4 bytes across the lanes of a quad: lane n gets byte n of lanes 0 .. 3.
 __device__ __forceinline__ uint32_t quad_transpose(uint32_t w, int lane)
 {
-    uint32_t y = __shfl_xor_sync(0xffffffffu, w, 1);
-    w = lane & 1 ? __byte_perm(w, y, 0x3715) : __byte_perm(w, y, 0x6240);
-    y = __shfl_xor_sync(0xffffffffu, w, 2);
-    return lane & 2 ? __byte_perm(w, y, 0x3276) : __byte_perm(w, y, 0x5410);
+    w = __byte_perm(w, __shfl_xor_sync(0xffffffffu, w, 1), lane & 1 ? 0x3715 : 0x6240);
+    return __byte_perm(w, __shfl_xor_sync(0xffffffffu, w, 2), lane & 2 ? 0x3276 : 0x5410);
 }
 
-// The low nibbles of four bytes, as 16 bits.
+// The low nibbles of four bytes, as 16 bits (nibble n of lane n's byte).
 __device__ __forceinline__ uint32_t low_nibbles(uint32_t w)
 {
     w &= 0x0f0f0f0fu;
@@ -68,6 +66,7 @@ struct Packed<Bf16> {
     using V = __nv_bfloat162;
     static constexpr uint32_t kMagic = 0x43004300u;    // 128 + code in the low bits
     static constexpr float kOffset = -136.f;           // ... to code - 8
+    static constexpr bool kTiny = true;                // holds numbers whose reciprocal fp32 does not
     static __device__ __forceinline__ V dup(float x) { return __float2bfloat162_rn(x); }
 };
 template <>
@@ -75,6 +74,7 @@ struct Packed<Fp16> {
     using V = __half2;
     static constexpr uint32_t kMagic = 0x64006400u;    // 1024 + code
     static constexpr float kOffset = -1032.f;
+    static constexpr bool kTiny = false;
     static __device__ __forceinline__ V dup(float x) { return __float2half2_rn(x); }
 };
 template <class V>
@@ -97,13 +97,15 @@ __device__ __forceinline__ uint32_t dequantise(uint32_t codes, typename Packed<T
     return as_word(__hfma2(c, s, z));
 }
 
-// The codes of this lane's 8 elements (element e in bits 4e and up) and the
-// scale word of their group, which lies in GL lanes.
+// The codes of this lane's 8 elements, as K's words hold them (element e in
+// bits 16 (e % 2) + 4 (e / 2) and up), and the scale word of their group, which lies in GL lanes.
 //
 // The quotient.  With r = 1 / s, k = rint(d r) is the nearest code or, close to a tie,
 // its neighbour; e = d - k s is exact and k + e r is d / s but for one rounding,
-// on a tie exactly the tie.  (Where d overflows, at -8 s of the widest
-// groups that bf16 holds, that is NaN, which the clamp takes to -8 as it should.)
+// on a tie exactly the tie.  It is at most some 50 (z is off by half a unit of its
+// type, and s at least a thirtieth of one where it is not 0), so 16 bits hold it until
+// the clamp.  (Where d overflows, at -8 s of the widest groups that bf16 holds,
+// it is NaN, whose bits the clamp takes to 0 as it should.)
 template <int GL, class T>
 __device__ __forceinline__ uint32_t quantise(const uint4& row, uint32_t* scale)
 {
@@ -123,36 +125,31 @@ __device__ __forceinline__ uint32_t quantise(const uint4& row, uint32_t* scale)
     const float least = T::lo(as_word(m)), most = -T::hi(as_word(m));
     const float half = most * 0.5f - least * 0.5f;
     const bool broken = !(half < INFINITY);   // an infinity or a NaN in the group
-    uint32_t meta = T::pack(half / 7.5f, 0.f);
+    // half / 7.5, corrected once like the quotients below.
+    const float h0 = half * (1.f / 7.5f);
+    uint32_t meta = T::pack(fmaf(fmaf(-7.5f, h0, half), 1.f / 7.5f, h0), 0.f);
     const float s = T::lo(meta);
-    meta |= T::pack(fmaf(8.f, s, least), 0.f) << 16;
+    meta = __byte_perm(meta, T::pack(fmaf(8.f, s, least), 0.f), 0x5410);
     const float z = T::hi(meta);
     *scale = broken ? 0x7fff7fffu : meta;     // NaN in either type
-    // Tiny steps are scaled up, exactly, so that 1 / s is finite; a step of 0 makes every quotient 0.
-    const float up = s < 0x1p-100f ? 0x1p64f : 1.f, su = s * up;
+    // bf16's tiny steps are scaled up, exactly, so that 1 / s is finite; a step of 0 makes every quotient 0.
+    const float up = Packed<T>::kTiny && s < 0x1p-100f ? 0x1p64f : 1.f, su = s * up;
     const float r = s > 0.f ? 1.f / su : 0.f;
     constexpr float kRound = 12582912.f;      // 1.5 * 2^23: adding it rounds to an integer, in the low bits
     const uint64_t up2 = f2_pack(up, up), z2 = f2_pack(-z * up, -z * up), s2 = f2_pack(-su, -su), r2 = f2_pack(r, r);
-    const uint64_t round2 = f2_pack(kRound, kRound), one2 = f2_pack(1.f, 1.f), back2 = f2_pack(-kRound, -kRound);
+    const uint64_t round2 = f2_pack(kRound, kRound), back2 = f2_pack(-kRound, -kRound), code2 = f2_pack(kRound + 8.f, kRound + 8.f);
     uint32_t codes = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint64_t d = f2_fma(f2_pack(T::lo(w[i]), T::hi(w[i])), up2, z2);
-        const uint64_t k = f2_fma(f2_fma(d, r2, round2), one2, back2);
-        const uint64_t q = f2_fma(f2_fma(k, s2, d), r2, k);
+    for (int i = 3; i >= 0; --i) {
+        const uint64_t x = f2_pack(T::lo(w[i]), T::hi(w[i]));
+        const uint64_t d = Packed<T>::kTiny ? f2_fma(x, up2, z2) : f2_add(x, z2);
+        const uint64_t k = f2_add(f2_fma(d, r2, round2), back2);
         float q0, q1;
-        f2_unpack(q, q0, q1);
-        const uint32_t c0 = __float_as_uint(fminf(fmaxf(q0, -8.f), 7.f) + (kRound + 8.f));
-        const uint32_t c1 = __float_as_uint(fminf(fmaxf(q1, -8.f), 7.f) + (kRound + 8.f));
-        codes |= (c0 & 15u) << (8 * i) | (c1 & 15u) << (8 * i + 4);
+        f2_unpack(f2_add(f2_fma(f2_fma(k, s2, d), r2, k), code2), q0, q1);
+        const uint32_t c = __vimin_s16x2_relu(__byte_perm(__float_as_uint(q0), __float_as_uint(q1), 0x5410), 0x000f000fu);
+        codes = codes * 16u + c;
     }
     return broken ? 0x88888888u : codes;
-}
-
-// Codes in element order (e at bit 4e) <-> a word of K's codes (e at 16 (e % 2) + 4 (e / 2)).
-__device__ __forceinline__ uint32_t k_word(uint32_t codes)
-{
-    return low_nibbles(codes) | low_nibbles(codes >> 4) << 16;
 }
 
 // Byte offsets in a block.
@@ -160,6 +157,20 @@ template <int D>
 __device__ __forceinline__ int v_word_offset(int tok, int g, int i)   // of the word that holds token tok
 {
     return ((((tok >> 3) * 8 + g) * 4 + ((tok & 7) >> 1)) * (D / 32) + i) * 4;
+}
+
+template <int N>
+__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[N])
+{
+    if constexpr (N == 4) {
+        const uint4 x = __ldg(reinterpret_cast<const uint4*>(p));
+        w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+    } else if constexpr (N == 2) {
+        const uint2 x = __ldg(reinterpret_cast<const uint2*>(p));
+        w[0] = x.x, w[1] = x.y;
+    } else {
+        w[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
+    }
 }
 
 // A lane's part of one step over HS heads: rows are (token of the turn, head)
@@ -202,10 +213,11 @@ __global__ void __launch_bounds__(kRowWarps * 32) write_kernel(RowsArgs a)
             }
             uint8_t* const block = page + (int64_t)head * B::kBytes;
             uint32_t ks, vs;
-            const uint32_t kw = k_word(quantise<GL, T>(kr, &ks));
+            const uint32_t kw = quantise<GL, T>(kr, &ks);
             const uint32_t vc = quad_transpose(quantise<GL, T>(vr, &vs), lane);
-            // Lane (i, n) of a token now holds byte n of the four lanes of word i: elements g = 2n and 2n + 1.
-            const int i = at.m >> 2, n = at.m & 3;
+            // Lane (i, n) of a token now holds byte n of the four lanes of word
+            // i: their elements g and, in the high nibbles, g + 2.
+            const int i = at.m >> 2, g = (at.m & 1) * 4 + (at.m >> 1 & 1);
             const uint32_t v = low_nibbles(vc) | low_nibbles(vc >> 4) << 16;
             const uint32_t other = __shfl_xor_sync(0xffffffffu, v, 16);
             if (on) {
@@ -216,13 +228,13 @@ __global__ void __launch_bounds__(kRowWarps * 32) write_kernel(RowsArgs a)
                     scales[kPageSize * NG] = vs;
                 }
                 uint8_t* const vcodes = block + B::kCodes;
-                if (pair) {   // the first token's lanes write g = 2n, the second's 2n + 1
+                if (pair) {   // the first token's lanes write g, the second's g + 2
                     const uint32_t word = at.second ? __byte_perm(other, v, 0x7632) : __byte_perm(v, other, 0x5410);
-                    *reinterpret_cast<uint32_t*>(vcodes + v_word_offset<D>(tok0, 2 * n + at.second, i)) = word;
+                    *reinterpret_cast<uint32_t*>(vcodes + v_word_offset<D>(tok0, g + 2 * at.second, i)) = word;
                 } else {
-                    uint8_t* const to = vcodes + v_word_offset<D>(tok, 2 * n, i) + (tok & 1) * 2;
+                    uint8_t* const to = vcodes + v_word_offset<D>(tok, g, i) + (tok & 1) * 2;
                     *reinterpret_cast<uint16_t*>(to) = (uint16_t)v;
-                    *reinterpret_cast<uint16_t*>(to + 4 * NW * 4) = (uint16_t)(v >> 16);
+                    *reinterpret_cast<uint16_t*>(to + 2 * 4 * NW * 4) = (uint16_t)(v >> 16);
                 }
             }
         }
@@ -255,45 +267,55 @@ __global__ void __launch_bounds__(kRowWarps * 32) read_kernel(RowsArgs a)
             continue;
         }
         const int tok0 = (int)(turn.slot & (kPageSize - 1)), tok = tok0 + (pair ? at.second : 0);
+        const bool mine = pair || at.second == 0;
         const uint8_t* const page = a.pool + (turn.slot >> 4) * a.H * B::kBytes;
-#pragma unroll 1
-        for (int h = h0; h < h1; h += HS) {
-            const int head = h + at.head;
-            const bool on = (pair || at.second == 0) && head < h1;
-            // K: a word of a token's row per lane.
-            if (on) {
-                const uint8_t* block = page + (int64_t)head * B::kBytes;
-                const uint32_t w = reinterpret_cast<const uint32_t*>(block)[(tok * 4 + (at.m & 3)) * NW + (at.m >> 2)];
-                const uint32_t meta = reinterpret_cast<const uint32_t*>(block + 2 * B::kCodes)[tok * NG + at.m / GL];
-                const V s = as_pair<V>(__byte_perm(meta, meta, 0x1010)), z = as_pair<V>(__byte_perm(meta, meta, 0x3232));
-                __stcs(reinterpret_cast<uint4*>(a.k + (t + at.second) * a.k_stride + head * D) + at.m,
-                       make_uint4(dequantise<T>(w, s, z), dequantise<T>(w >> 4, s, z), dequantise<T>(w >> 8, s, z), dequantise<T>(w >> 12, s, z)));
+        // K: a word of a token's row per lane.  V: lane (g, j) takes elements
+        // 32 i + 8 j + g of both tokens; the 8x8 tile [g][(j, token)] transposed
+        // gives lane ((j, token), c) elements 32 i + 8 j + 2c and 2c + 1 of one token.
+        const int g = lane >> 2, j = lane & 3;
+        const bool stored = pair || (g & 1) == (tok0 & 1);
+        uint16_t* const k_out = a.k + (t + at.second) * a.k_stride + at.m * 8;
+        uint16_t* const v_out = a.v + (t + (pair ? g & 1 : 0)) * a.v_stride + 8 * (g >> 1) + 2 * j;
+        struct Step {   // what a lane needs of one step
+            uint32_t k, ks, v[HS][NW], vs[HS][2][NG];
+        };
+        auto load = [&](int h) {
+            Step x = {};
+            if (mine && h + at.head < h1) {
+                const uint8_t* block = page + (int64_t)(h + at.head) * B::kBytes;
+                x.k = __ldg(reinterpret_cast<const uint32_t*>(block) + (tok * 4 + (at.m & 3)) * NW + (at.m >> 2));
+                x.ks = __ldg(reinterpret_cast<const uint32_t*>(block + 2 * B::kCodes) + tok * NG + at.m / GL);
             }
-            // V: lane (g, j) takes elements 32 i + 8 j + g of both tokens; the 8x8
-            // tile [g][(j, token)] transposed gives lane ((j, token), c) elements 32 i + 8 j + 2c and 2c + 1 of one token.
-            const int g = lane >> 2, j = lane & 3, r = lane >> 2, c = lane & 3;
-            const bool stored = pair || (r & 1) == (tok0 & 1);
-            uint16_t* const out = a.v + (t + (pair ? r & 1 : 0)) * a.v_stride + 8 * (r >> 1) + 2 * c;
 #pragma unroll
             for (int u = 0; u < HS; ++u) {
                 if (h + u >= h1) break;
                 const uint8_t* block = page + (int64_t)(h + u) * B::kBytes;
-                const uint32_t* scales = reinterpret_cast<const uint32_t*>(block + 2 * B::kCodes + B::kScales) + (tok0 & ~1) * NG;
-                uint32_t w[NW];
-                const uint8_t* const codes = block + B::kCodes + v_word_offset<D>(tok0, g, 0);
-                if constexpr (NW == 4) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(codes);
-                    w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
-                } else {
-                    const uint2 x = *reinterpret_cast<const uint2*>(codes);
-                    w[0] = x.x, w[1] = x.y;
-                }
+                load_words(block + B::kCodes + v_word_offset<D>(tok0, g, 0), x.v[u]);
+                const uint8_t* scales = block + 2 * B::kCodes + B::kScales + (tok0 & ~1) * NG * 4;
+                load_words(scales, x.vs[u][0]);
+                load_words(scales + NG * 4, x.vs[u][1]);
+            }
+            return x;
+        };
+        Step next = load(h0);
+#pragma unroll 1
+        for (int h = h0; h < h1; h += HS) {
+            const Step x = next;
+            if (h + HS < h1) next = load(h + HS);
+            if (mine && h + at.head < h1) {
+                const V s = as_pair<V>(__byte_perm(x.ks, x.ks, 0x1010)), z = as_pair<V>(__byte_perm(x.ks, x.ks, 0x3232));
+                __stcs(reinterpret_cast<uint4*>(k_out + (h + at.head) * D),
+                       make_uint4(dequantise<T>(x.k, s, z), dequantise<T>(x.k >> 4, s, z), dequantise<T>(x.k >> 8, s, z), dequantise<T>(x.k >> 12, s, z)));
+            }
+#pragma unroll
+            for (int u = 0; u < HS; ++u) {
+                if (h + u >= h1) break;
 #pragma unroll
                 for (int i = 0; i < NW; ++i) {
-                    const uint32_t m0 = scales[i / (NW / NG)], m1 = scales[NG + i / (NW / NG)];
-                    const uint32_t x = dequantise<T>(w[i] >> (4 * j), as_pair<V>(__byte_perm(m0, m1, 0x5410)), as_pair<V>(__byte_perm(m0, m1, 0x7632)));
-                    const uint32_t y = movmatrix_trans(x);
-                    if (stored) __stcs(reinterpret_cast<uint32_t*>(out + (h + u) * D + 32 * i), y);
+                    const uint32_t m0 = x.vs[u][0][i / (NW / NG)], m1 = x.vs[u][1][i / (NW / NG)];
+                    const uint32_t y = movmatrix_trans(dequantise<T>(x.v[u][i] >> (4 * j), as_pair<V>(__byte_perm(m0, m1, 0x5410)),
+                                                                     as_pair<V>(__byte_perm(m0, m1, 0x7632))));
+                    if (stored) __stcs(reinterpret_cast<uint32_t*>(v_out + (h + u) * D + 32 * i), y);
                 }
             }
         }

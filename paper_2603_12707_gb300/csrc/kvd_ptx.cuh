@@ -327,6 +327,14 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
     return r;
 }
 
+// d = a + b on both lanes, round to nearest.
+__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
 // Two bf16 in one 32-bit word -> the f32 pair (exact).
 __device__ __forceinline__ uint64_t bf16x2_to_f2(uint32_t u)
 {

@@ -61,42 +61,44 @@ def _load():
     return _fns
 
 
-def _need(ok: bool, msg: str):
-    if not ok:
-        raise ValueError(msg)
-
-
+# (Calls of a few microseconds: what is said of a refused argument is put together only when it is refused.)
 def _vector(x, name, dtype, n):
     """Address of a dense CUDA vector with at least n entries (None: null)."""
     if x is None:
         return None
-    _need(x.dtype is dtype and x.is_cuda and x.is_contiguous() and x.numel() >= n,
-          f"{name} must be a contiguous CUDA tensor of {dtype} with at least {n} entries")
+    if x.dtype is not dtype or not x.is_cuda or not x.is_contiguous() or x.numel() < n:
+        raise ValueError(f"{name} must be a contiguous CUDA tensor of {dtype} with at least {n} entries")
     return x.data_ptr()
 
 
-def _rows(x, name, dtype, n, heads, dim):
-    """Address and row stride of a CUDA tensor [n][heads][dim] whose heads are dense."""
-    _need(x.dtype is dtype and x.is_cuda, f"{name} must be a CUDA tensor of {dtype}")
-    _need(x.shape == (n, heads, dim), f"{name} must have shape {(n, heads, dim)}, not {tuple(x.shape)}")
-    s = x.stride()
-    _need(s[2] == 1 and (heads == 1 or s[1] == dim), f"the heads of {name} must be dense")
-    return x.data_ptr(), s[0] if n > 1 else heads * dim
+def _rows(x, name, dtype, shape):
+    """Address and row stride of a CUDA tensor of the given shape [n][heads][dim] whose heads are dense."""
+    if x.dtype is not dtype or not x.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor of {dtype}")
+    if x.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(x.shape)}")
+    row, head, one = x.stride()
+    n, heads, dim = shape
+    if one != 1 or (head != dim and heads != 1):
+        raise ValueError(f"the heads of {name} must be dense")
+    return x.data_ptr(), row if n > 1 else heads * dim
 
 
 class Pool:
     """One layer's 4-bit pool: ``data`` uint8 [num_pages][num_kv_heads][block bytes] (see ``block_bytes``)."""
 
     def __init__(self, data: torch.Tensor, head_dim: int, group: int, dtype: torch.dtype = torch.bfloat16):
-        _need(dtype in _DTYPES, "dtype must be torch.bfloat16 or torch.float16")
-        _need(data.dtype is torch.uint8 and data.is_cuda and data.is_contiguous() and data.dim() == 3,
-              "data must be a contiguous CUDA tensor of uint8 with three dimensions")
+        if dtype not in _DTYPES:
+            raise ValueError("dtype must be torch.bfloat16 or torch.float16")
+        if data.dtype is not torch.uint8 or not data.is_cuda or not data.is_contiguous() or data.dim() != 3:
+            raise ValueError("data must be a contiguous CUDA tensor of uint8 with three dimensions")
         self.data, self.head_dim, self.group, self.dtype = data, head_dim, group, dtype
         self.num_kv_heads = data.shape[1]
         self.c = kv4_pool(data.data_ptr(), data.shape[0], data.shape[1], head_dim, group, _DTYPES[dtype])
         self.ref = ctypes.addressof(self.c)
         n = kv4_pool_bytes(self)
-        _need(n == data.numel(), f"data must have {n} bytes for its pages and heads, not {data.numel()}")
+        if n != data.numel():
+            raise ValueError(f"data must have {n} bytes for its pages and heads, not {data.numel()}")
 
     @staticmethod
     def block_bytes(head_dim: int, group: int) -> int:
@@ -117,7 +119,8 @@ class Tables:
 
     def __init__(self, block_table: torch.Tensor, lens: torch.Tensor, free_ring: torch.Tensor | None = None,
                  free_state: torch.Tensor | None = None):
-        _need(block_table.dim() == 2, "block_table must have two dimensions")
+        if block_table.dim() != 2:
+            raise ValueError("block_table must have two dimensions")
         self.max_seqs, self.max_pages = block_table.shape
         self.block_table, self.lens, self.free_ring, self.free_state = block_table, lens, free_ring, free_state
         self.c = kv_tables(_vector(block_table, "block_table", torch.int32, 0),
@@ -153,25 +156,28 @@ def kv_tables_step(tables: Tables, seq_ids, new_lens, slots, positions=None, cu_
                    free_state_out=None, device_error=None, stream=None):
     """One step of the batch of requests ``seq_ids`` (None: request i is row i)
     that ``new_lens`` changes; ``slots`` (int64) has room for the new tokens."""
-    n, i32 = new_lens.numel(), torch.int32
-    _need(seq_ids is None or seq_ids.numel() == n, "seq_ids and new_lens must have the same number of entries")
-    room = slots.numel()
-    rc = _load()["kv_tables_step"](
+    n, room, i32 = new_lens.numel(), slots.numel(), torch.int32
+    if seq_ids is not None and seq_ids.numel() != n:
+        raise ValueError("seq_ids and new_lens must have the same number of entries")
+    rc = (_fns or _load())["kv_tables_step"](
         tables.ref, n, _vector(seq_ids, "seq_ids", i32, n), _vector(new_lens, "new_lens", i32, n), room,
         _vector(slots, "slots", torch.int64, 0), _vector(positions, "positions", i32, room),
         _vector(cu_seqlens, "cu_seqlens", i32, n + 1), _vector(lens_out, "lens_out", i32, tables.max_seqs),
         _vector(free_state_out, "free_state_out", i32, 4), _vector(device_error, "device_error", i32, 1),
         kd._stream(stream))
-    kd._check(rc, "kv_tables_step")
+    if rc:
+        kd._check(rc, "kv_tables_step")
 
 
 def _kv4_rows(fn, pool: Pool, slots, k, v, device_error, stream):
     n = slots.numel()
-    k, k_stride = _rows(k, "k", pool.dtype, n, pool.num_kv_heads, pool.head_dim)
-    v, v_stride = _rows(v, "v", pool.dtype, n, pool.num_kv_heads, pool.head_dim)
-    rc = _load()[fn](pool.ref, n, _vector(slots, "slots", torch.int64, 0), k, k_stride, v, v_stride,
-                     _vector(device_error, "device_error", torch.int32, 1), kd._stream(stream))
-    kd._check(rc, fn)
+    shape = (n, pool.num_kv_heads, pool.head_dim)
+    k, k_stride = _rows(k, "k", pool.dtype, shape)
+    v, v_stride = _rows(v, "v", pool.dtype, shape)
+    rc = (_fns or _load())[fn](pool.ref, n, _vector(slots, "slots", torch.int64, 0), k, k_stride, v, v_stride,
+                               _vector(device_error, "device_error", torch.int32, 1), kd._stream(stream))
+    if rc:
+        kd._check(rc, fn)
 
 
 def kv4_write(pool: Pool, slots, k, v, device_error=None, stream=None):
@@ -187,14 +193,18 @@ def kv4_read(pool: Pool, slots, k_out, v_out, device_error=None, stream=None):
 def kv4_decode_attention(pool: Pool, tables: Tables, q, out, workspace, seq_ids=None, lse=None,
                          softmax_scale: float = 0.0, device_error=None, stream=None):
     """Decode attention of q [batch][num_q_heads][head_dim] over each row's request."""
-    _need(q.dim() == 3, "q must have three dimensions")
-    batch, heads = q.shape[0], q.shape[1]
-    _need(seq_ids is None or seq_ids.numel() == batch, "seq_ids must have an entry for each row of q")
-    q, q_stride = _rows(q, "q", pool.dtype, batch, heads, pool.head_dim)
-    out, out_stride = _rows(out, "out", pool.dtype, batch, heads, pool.head_dim)
-    rc = _load()["kv4_decode_attention"](
+    shape = q.shape
+    if len(shape) != 3 or shape[2] != pool.head_dim:
+        raise ValueError(f"q must have shape [batch][num_q_heads][{pool.head_dim}]")
+    batch, heads = shape[0], shape[1]
+    if seq_ids is not None and seq_ids.numel() != batch:
+        raise ValueError("seq_ids must have an entry for each row of q")
+    q, q_stride = _rows(q, "q", pool.dtype, shape)
+    out, out_stride = _rows(out, "out", pool.dtype, shape)
+    rc = (_fns or _load())["kv4_decode_attention"](
         pool.ref, tables.ref, batch, _vector(seq_ids, "seq_ids", torch.int32, batch), heads, q, q_stride, out,
         out_stride, _vector(lse, "lse", torch.float32, batch * heads), softmax_scale,
         _vector(workspace, "workspace", torch.uint8, 1), workspace.numel(),
         _vector(device_error, "device_error", torch.int32, 1), kd._stream(stream))
-    kd._check(rc, "kv4_decode_attention")
+    if rc:
+        kd._check(rc, "kv4_decode_attention")
