@@ -36,12 +36,10 @@ struct Turn {
 
 __device__ __forceinline__ Turn turn_of(const RowsArgs& a, int64_t t, bool report)
 {
-    const int64_t s = a.slots[t];
-    const int64_t before = (s & 1) && t > 0 ? a.slots[t - 1] : -2;
-    const int64_t after = !(s & 1) && t + 1 < a.n ? a.slots[t + 1] : -2;
-    const bool known = s >= 0 && s < a.num_slots;
+    const int64_t s = a.slots[t], before = t > 0 ? a.slots[t - 1] : -2, after = t + 1 < a.n ? a.slots[t + 1] : -2;
+    const bool known = s >= 0 && s < a.num_slots, odd = s & 1;
     if (!known && s != -1 && report) kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
-    return {s, known && before == s - 1 ? 0 : known && after == s + 1 ? 2 : 1, known};
+    return {s, known && odd && before == s - 1 ? 0 : known && !odd && after == s + 1 ? 2 : 1, known};
 }
 
 // 4 x 4 bytes across the lanes of a quad: lane n gets byte n of lanes 0 .. 3.
@@ -202,14 +200,21 @@ __global__ void __launch_bounds__(kRowWarps * 32) write_kernel(RowsArgs a)
         uint8_t* const page = a.pool + (turn.slot >> 4) * a.H * B::kBytes;
         const int64_t row = t + (pair ? at.second : 0);
         const bool mine = pair || at.second == 0;
+        const uint16_t* const k_row = a.k + row * a.k_stride + at.m * 8;
+        const uint16_t* const v_row = a.v + row * a.v_stride + at.m * 8;
+        uint4 k_next = make_uint4(0u, 0u, 0u, 0u), v_next = k_next;
+        if (mine && h0 + at.head < h1) {
+            k_next = __ldcs(reinterpret_cast<const uint4*>(k_row + (h0 + at.head) * D));
+            v_next = __ldcs(reinterpret_cast<const uint4*>(v_row + (h0 + at.head) * D));
+        }
 #pragma unroll 1
         for (int h = h0; h < h1; h += HS) {
             const int head = h + at.head;
             const bool on = mine && head < h1;
-            uint4 kr = make_uint4(0u, 0u, 0u, 0u), vr = kr;
-            if (on) {
-                kr = __ldcs(reinterpret_cast<const uint4*>(a.k + row * a.k_stride + head * D) + at.m);
-                vr = __ldcs(reinterpret_cast<const uint4*>(a.v + row * a.v_stride + head * D) + at.m);
+            const uint4 kr = k_next, vr = v_next;
+            if (mine && head + HS < h1) {   // the next head's rows come while these are worked
+                k_next = __ldcs(reinterpret_cast<const uint4*>(k_row + (head + HS) * D));
+                v_next = __ldcs(reinterpret_cast<const uint4*>(v_row + (head + HS) * D));
             }
             uint8_t* const block = page + (int64_t)head * B::kBytes;
             uint32_t ks, vs;
@@ -297,11 +302,7 @@ __global__ void __launch_bounds__(kRowWarps * 32) read_kernel(RowsArgs a)
             }
             return x;
         };
-        Step next = load(h0);
-#pragma unroll 1
-        for (int h = h0; h < h1; h += HS) {
-            const Step x = next;
-            if (h + HS < h1) next = load(h + HS);
+        auto store = [&](const Step& x, int h) {
             if (mine && h + at.head < h1) {
                 const V s = as_pair<V>(__byte_perm(x.ks, x.ks, 0x1010)), z = as_pair<V>(__byte_perm(x.ks, x.ks, 0x3232));
                 __stcs(reinterpret_cast<uint4*>(k_out + (h + at.head) * D),
@@ -318,6 +319,16 @@ __global__ void __launch_bounds__(kRowWarps * 32) read_kernel(RowsArgs a)
                     if (stored) __stcs(reinterpret_cast<uint32_t*>(v_out + (h + u) * D + 32 * i), y);
                 }
             }
+        };
+        // Two steps' loads are under way while two are worked.
+        Step next0 = load(h0), next1 = load(h0 + HS);
+#pragma unroll 1
+        for (int h = h0; h < h1; h += 2 * HS) {
+            const Step x0 = next0, x1 = next1;
+            next0 = load(h + 2 * HS);
+            next1 = load(h + 3 * HS);
+            store(x0, h);
+            store(x1, h + HS);
         }
     }
 }
