@@ -45,11 +45,15 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr uint32_t kRowCost = 3;
 // What a warp takes at least, in tiles: a small call uses fewer warps rather than merge more parts.
 constexpr uint32_t kMinShare = 2;
+// Warps of a CTA that work at least, where there is enough for them: one per scheduler.
+constexpr uint32_t kMinWarps = 4;
 
 struct AttnArgs {
     const uint8_t* pool;
     int64_t num_pages;
     int32_t H, Hq, G;
+    uint32_t H_inv;      // 2^32 / H, rounded down (2^32 - 1 for 1)
+    uint32_t G_inv;      // 2^16 / G, rounded up
     const int32_t* block_table;
     const int32_t* lens;
     int32_t max_seqs, max_pages, batch;
@@ -135,7 +139,7 @@ struct State {
     float qoff[4];                        // -8 times it, as the accumulators begin (kept for one group: registers)
     float qback[2];                       // undoes q's power of two
     float m[2], l[2];
-    float o[MT][4], e[NG][4], z[NG][2];
+    float o[MT][4], e[NG][4], z[NG][2];   // e: -8 sum p s' of a group (apart: a NaN stays in its group)
     float vs, vlimit;                     // 2^-E, and the scale above which E moves
 
     __device__ __forceinline__ void start(const AttnArgs& a, int b, int h, int lane)
@@ -242,16 +246,13 @@ struct State {
 #pragma unroll
             for (int k = 0; k < NG; ++k) {
                 float acc[4];
-                if constexpr (NG > 1) {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) acc[c] = -8.f * qsum[k][c & 1];
-                }
+                const float from[4] = {NG == 1 ? qoff[0] : 0.f, NG == 1 ? qoff[1] : 0.f, NG == 1 ? qoff[2] : 0.f, NG == 1 ? qoff[3] : 0.f};
 #pragma unroll
                 for (int i = k * (NW / NG); i < (k + 1) * (NW / NG); ++i) {
                     const uint32_t a8 = ka[i] >> 8, b8 = kb[i] >> 8;
-                    if (NG == 1 && i == 0)
+                    if (i == k * (NW / NG))
                         mma_f16_16816(acc, ka[i] & 0x000f000fu, kb[i] & 0x000f000fu, ka[i] & 0x00f000f0u, kb[i] & 0x00f000f0u,
-                                      qf[2 * i][0], qf[2 * i][1], qoff);
+                                      qf[2 * i][0], qf[2 * i][1], from);
                     else
                         mma_f16_16816(acc, ka[i] & 0x000f000fu, kb[i] & 0x000f000fu, ka[i] & 0x00f000f0u, kb[i] & 0x00f000f0u,
                                       qf[2 * i][0], qf[2 * i][1]);
@@ -260,7 +261,7 @@ struct State {
                 }
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    const float ss = T::lo(mk[t][k]), sz = T::hi(mk[t][k]);
+                    const float ss = T::lo(mk[t][k]), sz = NG == 1 ? T::hi(mk[t][k]) : fmaf(-8.f, ss, T::hi(mk[t][k]));
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         float& x = s[p][2 * t + c];
@@ -303,19 +304,20 @@ struct State {
             const float p2 = ex2(fmaf(s[p][2], qback[0], -m[0])), p3 = ex2(fmaf(s[p][3], qback[1], -m[1]));
             l[0] += p0 + p2;
             l[1] += p1 + p3;
+            const float v0 = p0 * vs, v1 = p1 * vs, v2 = p2 * vs, v3 = p3 * vs;   // (used with four groups: fewer products)
             uint32_t va[NW], vb[NW];
             load_shared(codes + p * B::kBytes + B::kCodes, va);
             load_shared(codes + p * B::kBytes + B::kCodes + 32 * NW * 4, vb);
 #pragma unroll
             for (int k = 0; k < NG; ++k) {
-                const float s0 = T::lo(mv[p][0][k]) * vs, s1 = T::lo(mv[p][1][k]) * vs;
+                const float s0 = T::lo(mv[p][0][k]), s1 = T::lo(mv[p][1][k]);
                 const float z0 = T::hi(mv[p][0][k]), z1 = T::hi(mv[p][1][k]);
                 z[k][0] = fmaf(p0, z0, fmaf(p2, z1, z[k][0]));
                 z[k][1] = fmaf(p1, z0, fmaf(p3, z1, z[k][1]));
                 // (p s')^T as the column operand: the packed pairs are 8x8 tiles
                 // [token][n] in the fragment layout, their transposes are the operand.
-                const uint32_t b0 = movmatrix_trans(pack_f16(p0 * s0, p1 * s0));
-                const uint32_t b1 = movmatrix_trans(pack_f16(p2 * s1, p3 * s1));
+                const uint32_t b0 = movmatrix_trans(NG == 4 ? pack_f16(v0 * s0, v1 * s0) : pack_f16(p0 * (s0 * vs), p1 * (s0 * vs)));
+                const uint32_t b1 = movmatrix_trans(NG == 4 ? pack_f16(v2 * s1, v3 * s1) : pack_f16(p2 * (s1 * vs), p3 * (s1 * vs)));
                 mma_f16_16816(e[k], 0xc800c800u, 0xc800c800u, 0xc800c800u, 0xc800c800u, b0, b1);   // -8 everywhere
 #pragma unroll
                 for (int i = k * (NW / NG); i < (k + 1) * (NW / NG); ++i) {
@@ -437,46 +439,51 @@ struct RowSum {
 #pragma unroll
         for (int i = 0; i < E; ++i) o[i] = 0.f;
     }
-    // Adds row n of the lanes' parts, in the lanes' order (null: none): a
-    // lane loads its part's (m, l), then all lanes the rows, eight in flight.
+    // Adds row n of the first `count` lanes' parts, in the lanes' order: `at` is a
+    // part's offset in floats from `base`, -1 for none (not the first lane's).  A lane loads its part's (m, l), all
+    // lanes the rows, eight in flight, the first ones before the weights are known.
     // The loads pass L1 by: parts may come from other SMs.
-    __device__ __forceinline__ void merge(const float* mine, int G, int n, int lane)
+    __device__ __forceinline__ void merge(const float* base, int at, int count, int G, int n, int lane)
     {
-        float mc = -INFINITY, lc = 0.f;
-        if (mine) {
-            mc = load_cg(mine + G * D + n);
-            lc = load_cg(mine + G * (D + 1) + n);
+        const bool mine = lane < count && at >= 0;
+        const int other = __shfl_sync(0xffffffffu, at, 0), from = mine ? at : other;   // something to load where there is nothing to add
+        float mc = load_cg(base + from + G * D + n), lc = load_cg(base + from + G * (D + 1) + n);
+        if (!mine) {
+            mc = -INFINITY;
+            lc = 0.f;
         }
-        const int count = 32 - __clz(__ballot_sync(0xffffffffu, mine != nullptr));
-        float top = fmaxf(m, mc);
-#pragma unroll
-        for (int k = 1; k < 32; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, k));
-        const float al = m == top ? 1.f : ex2(m - top), w = mc == top ? 1.f : ex2(mc - top);
-        float sum = w * lc;
-#pragma unroll
-        for (int k = 1; k < 32; k <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
-        m = top;
-        l = l * al + sum;
-#pragma unroll
-        for (int i = 0; i < E; ++i) o[i] *= al;
-        const unsigned long long row = mine ? reinterpret_cast<unsigned long long>(mine + n * D) : 0ull;
+        const uint32_t some = __ballot_sync(0xffffffffu, mine);
+        float w = 0.f;
 #pragma unroll 1
         for (int c = 0; c < count; c += 8) {
-            float x[8][E], wc[8];
+            float x[8][E];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const float* p = reinterpret_cast<const float*>(__shfl_sync(0xffffffffu, row, (c + u) & 31));
-                wc[u] = __shfl_sync(0xffffffffu, w, (c + u) & 31);
+            for (int u = 0; u < 8; ++u) load_cg(base + __shfl_sync(0xffffffffu, from, (c + u) & 31) + n * D + lane * E, x[u]);
+            if (c == 0) {
+                const float top = fmaxf(m, warp_max(mc)), al = m == top ? 1.f : ex2(m - top);
+                w = mc == top && mine ? 1.f : ex2(mc - top);
+                if (!mine) w = 0.f;
+                lc *= w;
+                m = top;
+                l *= al;
 #pragma unroll
-                for (int i = 0; i < E; ++i) x[u][i] = 0.f;
-                if (p && c + u < count) load_cg(p + lane * E, x[u]);
-                else wc[u] = 0.f;
+                for (int i = 0; i < E; ++i) o[i] *= al;
             }
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
+            for (int u = 0; u < 8; ++u) {
+                const bool on = c + u < 32 && ((some >> (c + u)) & 1u);
+                const float wu = __shfl_sync(0xffffffffu, w, (c + u) & 31), lu = __shfl_sync(0xffffffffu, lc, (c + u) & 31);
+                l += on ? lu : 0.f;
 #pragma unroll
-                for (int i = 0; i < E; ++i) o[i] = fmaf(x[u][i], wc[u], o[i]);
+                for (int i = 0; i < E; ++i) o[i] = fmaf(on ? x[u][i] : 0.f, wu, o[i]);
+            }
         }
+    }
+    static __device__ __forceinline__ float warp_max(float x)   // (a NaN only where all are)
+    {
+        float y;
+        asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+        return y;
     }
     __device__ __forceinline__ void write_part(float* part, int G, int n, int lane) const
     {
@@ -519,7 +526,7 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
     using M = AttnSmem<D, NG>;
     constexpr int W = S::kWarps, R = S::kStages, E = D / 32;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ uint64_t warp_pages[W];
+    __shared__ uint2 warp_pages[W];
     __shared__ int arrived[2];
     __shared__ int2 spans[2];   // first and last CTA of what began before this CTA, and of what goes on after it
     static_assert(2 * W <= 32, "a lane for each part");
@@ -539,42 +546,52 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
 
     // Pages of the rows before each row.
     const uint32_t H = a.H;
+    const int max_len = min(a.max_pages, (1 << 27) - 1) * kPageSize;
     if (tid == 0) pages[0] = costs[0] = 0;
-    uint64_t before = 0;      // pages in the low, rows that are not empty in the high 24 bits
+    uint64_t all_pages = 0;
+    uint32_t held = 0;        // rows that are not empty
     for (int r0 = 0; r0 < a.batch; r0 += W * 32) {
         const int r = r0 + tid;
-        uint64_t sum = 0;
+        uint32_t n = 0;
         if (r < a.batch) {
             const int seq = a.seq_ids ? a.seq_ids[r] : r;
             int len = seq >= 0 && seq < a.max_seqs ? a.lens[seq] : -1;
-            if (len < 0 || len > a.max_pages * kPageSize) {
+            if (len < 0 || len > max_len) {
                 if (blockIdx.x == 0) kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
                 len = 0;
             }
-            const uint32_t n = (uint32_t)(len + kPageSize - 1) / kPageSize;
-            sum = n | (uint64_t)(n != 0) << 40;
+            n = (uint32_t)(len + kPageSize - 1) / kPageSize;
         }
+        const uint32_t some = __ballot_sync(0xffffffffu, n != 0);
+        uint32_t sum = n;     // (32 rows of up to 2^27 pages: a sum of 2^32 is found below)
 #pragma unroll
         for (int k = 1; k < 32; k <<= 1) {
-            const uint64_t up = __shfl_up_sync(0xffffffffu, sum, k);
+            const uint32_t up = __shfl_up_sync(0xffffffffu, sum, k);
             if (lane >= k) sum += up;
         }
-        if (lane == 31) warp_pages[warp] = sum;
+        if (lane == 31) warp_pages[warp] = make_uint2(sum, (uint32_t)__popc(some));
         __syncthreads();
-        uint64_t mine = before;
+        uint64_t mine = all_pages;
+        uint32_t rows = held;
 #pragma unroll
         for (int w = 0; w < W; ++w) {
-            if (w < warp) mine += warp_pages[w];
-            before += warp_pages[w];
+            const uint2 x = warp_pages[w];
+            if (w < warp) {
+                mine += x.x;
+                rows += x.y;
+            }
+            all_pages += x.x;
+            held += x.y;
         }
-        mine += sum;
         if (r < a.batch) {
-            pages[r + 1] = (uint32_t)mine * H;
-            costs[r + 1] = ((uint32_t)mine + (uint32_t)(mine >> 40) * kRowCost) * H;
+            const uint32_t up_to = (uint32_t)mine + sum;
+            rows += __popc(some & (2u << lane) - 1u);
+            pages[r + 1] = up_to * H;
+            costs[r + 1] = (up_to + rows * kRowCost) * H;
         }
-        __syncthreads();
+        if (r0 + W * 32 < a.batch) __syncthreads();
     }
-    const uint64_t all_pages = before & 0xffffffffffull;
+    __syncthreads();
     if (all_pages * a.H > 0x7fffffffull) {   // the same in all threads
         if (blockIdx.x == 0 && tid == 0) kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
         return;
@@ -583,10 +600,16 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
     // Shares: equal parts of the list of tiles in which every (row, KV head)
     // is preceded by kRowCost empty places; the first `extra` warps take one place more.
     const uint32_t places = costs[a.batch];
-    const uint32_t warps = min(gridDim.x * W, (places + kMinShare - 1) / kMinShare);
+    const uint32_t wanted = (places + kMinShare - 1) / kMinShare;
+    const uint32_t cta_warps = min((uint32_t)W, max(kMinWarps, (wanted + gridDim.x - 1) / gridDim.x));   // that work, of each CTA
+    const uint32_t warps = min(gridDim.x * cta_warps, wanted);
     const uint32_t base = warps ? places / warps : 0, extra = warps ? places % warps : 0;
-    auto row_of = [&](const uint32_t* sums, uint32_t x) {   // the last row with sums[row] <= x (so not empty, where x < sums[batch])
-        int r0 = 0, r1 = a.batch;
+    // The last row from r0 on with sums[row] <= x (so not empty, where x < sums[batch]); sums[r0] <= x.
+    auto row_of = [&](const uint32_t* sums, int r0, uint32_t x) {
+        int step = 1;
+#pragma unroll 1
+        for (; r0 + step < a.batch && sums[r0 + step] <= x; step *= 2) r0 += step;
+        int r1 = min(r0 + step, a.batch);
 #pragma unroll 1
         while (r1 - r0 > 1) {
             const int mid = (r0 + r1) >> 1;
@@ -595,12 +618,23 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
         }
         return r0;
     };
+    auto over_H = [&](uint32_t x) {      // x / H for a multiple of H
+        uint32_t q = __umulhi(x, a.H_inv);
+        return q + (x - q * H >= H);
+    };
+    auto head_of = [&](uint32_t x, uint32_t n) {   // x / n, below 1024
+        int q = (int)__fdividef((float)x, (float)n);
+        q -= q * (int64_t)n > x;
+        return (uint32_t)(q + (x - q * n >= n));
+    };
     uint32_t lo = 0;
+    int row0 = 0;             // the row that this lane's next tile is at or behind
     {   // lane 0: tiles before this warp's share, lane 1: up to its end
-        const uint32_t w = min(blockIdx.x * W + warp + (lane & 1), warps), at = w * base + min(w, extra);
+        const uint32_t w = min(blockIdx.x * cta_warps + min((uint32_t)warp + (lane & 1), cta_warps), warps), at = w * base + min(w, extra);
         if (w < warps) {
-            const int r = row_of(costs, at);
-            const uint32_t n = (costs[r + 1] - costs[r]) / H, in_row = at - costs[r], h = in_row / n, off = in_row - h * n;
+            const int r = row_of(costs, 0, at);
+            const uint32_t n = over_H(costs[r + 1] - costs[r]), in_row = at - costs[r], h = head_of(in_row, n), off = in_row - h * n;
+            row0 = r;
             lo = pages[r] + h * (n - kRowCost) + (off > kRowCost ? off - kRowCost : 0);
         } else {
             lo = pages[a.batch];
@@ -608,6 +642,7 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
     }
     const int count = (int)(__shfl_sync(0xffffffffu, lo, 1) - __shfl_sync(0xffffffffu, lo, 0));
     lo = __shfl_sync(0xffffffffu, lo, 0);
+    row0 = __shfl_sync(0xffffffffu, row0, 0);
     const uint64_t policy = l2_policy_evict_first();
 
     bool ok = true;
@@ -615,9 +650,9 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
         Tile t{nullptr, 0};
         if (i >= count || !ok) return t;
         const uint32_t at = lo + i;
-        const int r0 = row_of(pages, at);
-        const uint32_t n = (pages[r0 + 1] - pages[r0]) / H, in_row = at - pages[r0];
-        const int h = (int)(in_row / n), p = (int)(in_row - h * n);
+        const int r0 = row0 = row_of(pages, row0, at);
+        const uint32_t n = over_H(pages[r0 + 1] - pages[r0]), in_row = at - pages[r0];
+        const int h = (int)head_of(in_row, n), p = (int)(in_row - h * n);
         const int seq = a.seq_ids ? a.seq_ids[r0] : r0;
         const int32_t page = a.block_table[(int64_t)seq * a.max_pages + p];
         int valid = min(kPageSize, a.lens[seq] - p * kPageSize);
@@ -729,7 +764,7 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
     }
 
     // Rows without tokens.
-    if ((int)(before >> 40) != a.batch)
+    if ((int)held != a.batch)
         for (int r = blockIdx.x; r < a.batch; r += gridDim.x)
             if (pages[r] == pages[r + 1]) {
                 for (int i = tid; i < a.Hq * (D / 8); i += W * 32)
@@ -753,15 +788,15 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
     const bool from_before = !((begin >> first) & 1u);
     const bool goes_on = !(ending >> last) && !(last == first && from_before);
     const bool crosses = from_before || goes_on;
-    if (tid < 2 && (tid ? goes_on : from_before)) {
+    if (warp == W - 1 && lane < 2 && (lane ? goes_on : from_before)) {
         // The CTAs that hold parts of it (while the others merge).
-        const PartInfo in = infos[tid ? last : first];
+        const PartInfo in = infos[lane ? last : first];
         auto cta_of = [&](uint32_t p) {   // the CTA whose share holds page p
-            const uint32_t n = (pages[in.b + 1] - pages[in.b]) / H, place = costs[in.b] + in.h * (n + kRowCost) + kRowCost + p;
+            const uint32_t n = over_H(pages[in.b + 1] - pages[in.b]), place = costs[in.b] + in.h * (n + kRowCost) + kRowCost + p;
             const uint32_t long_ones = extra * (base + 1);
-            return (int)((place < long_ones ? place / (base + 1) : extra + (place - long_ones) / base) / W);
+            return (int)((place < long_ones ? place / (base + 1) : extra + (place - long_ones) / base) / cta_warps);
         };
-        spans[tid] = make_int2(cta_of(0), cta_of((pages[in.b + 1] - pages[in.b]) / H - 1));
+        spans[lane] = make_int2(cta_of(0), cta_of(over_H(pages[in.b + 1] - pages[in.b]) - 1));
     }
     // Pass 0 merges the groups in shared memory, pass 1 (k = 0, 1) the parts of all CTAs of what
     // crosses them, by the last CTA to arrive; where those are many, several warps share a row's
@@ -770,7 +805,7 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
 #pragma unroll 1
     for (int pass = 0, k = 0;; ) {
         const int parts = pass ? spans[k].y - spans[k].x + 1 : 0;
-        const int split = parts > 16 ? max(1, W / a.G) : 1, each = (parts + split - 1) / split;
+        const int split = parts > 16 ? max(1, W / a.G) : 1, each = split > 1 ? (parts + split - 1) / split : parts;
         const int jobs = pass == 0 ? jobs0 : pass == 1 ? a.G * split : a.G;
 #pragma unroll 1
         for (int job = warp; job < jobs; job += W) {
@@ -779,8 +814,9 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
             uint32_t members = 0;
             if (pass == 0) {
                 uint32_t rest = groups;
-                for (int u = job / a.G; u > 0; --u) rest &= rest - 1u;
-                n = job % a.G;
+                const int group = (int)(job * a.G_inv >> 16);   // job / G
+                n = job - group * a.G;
+                for (int u = group; u > 0; --u) rest &= rest - 1u;
                 const int e = __ffs(rest) - 1;
                 rest &= rest - 1u;
                 members = valid & (0xffffffffu << e) & (rest ? (rest & (0u - rest)) - 1u : 0xffffffffu);
@@ -789,26 +825,24 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
                 b = __shfl_sync(0xffffffffu, mine.b, e);
                 h = __shfl_sync(0xffffffffu, mine.h, e);
                 c = e;
-                end = 32;             // (a lane for each part from e on)
+                end = 32 - __clz(members);
             } else {
-                n = pass == 1 ? job / split : job;
+                n = split > 1 && pass == 1 ? job / split : job;
                 b = infos[k ? last : first].b;
                 h = infos[k ? last : first].h;
-                c = pass == 1 ? job % split * each : 0;
+                const int share = split > 1 && pass == 1 ? job - n * split : 0;
+                c = share * each;
                 end = pass == 1 ? min(parts, c + each) : split;
-                if (pass == 1 && split > 1) to = heads + (job % split) * PF;
+                if (pass == 1 && split > 1) to = heads + share * PF;
             }
             RowSum<D> sum;
 #pragma unroll 1
             for (; c < end; c += 32) {
                 const int i = c + lane;
-                const float* p = nullptr;
-                if (pass == 0) {
-                    if (i < 32 && ((members >> i) & 1u)) p = i & 1 ? reinterpret_cast<const float*>(smem + (i >> 1) * S::kRing) : heads + (i >> 1) * PF;
-                } else if (i < end) {
-                    p = pass == 1 ? a.parts + ((int64_t)(spans[k].x + i) * 2 + (i == 0 ? 1 : 0)) * PF : heads + i * PF;
-                }
-                sum.merge(p, a.G, n, lane);
+                int off;
+                if (pass == 0) off = !((members >> (i & 31)) & 1u) || i > 31 ? -1 : i & 1 ? (i >> 1) * (S::kRing / 4) : M::kHeads / 4 + (i >> 1) * PF;
+                else off = pass == 1 ? ((spans[k].x + i) * 2 + (i == 0 ? 1 : 0)) * PF : M::kHeads / 4 + i * PF;
+                sum.merge(pass == 1 ? a.parts : reinterpret_cast<const float*>(smem), off, min(32, end - c), a.G, n, lane);
             }
             if (to) sum.write_part(to, a.G, n, lane);
             else sum.template write_out<T>(a, b, h, n, lane);
@@ -938,6 +972,8 @@ extern "C" KVC_API int kv4_decode_attention(const kv4_pool* pool, const kv_table
     a.pool = static_cast<const uint8_t*>(pool->data);
     a.num_pages = pool->num_pages;
     a.H = pool->num_kv_heads;
+    a.H_inv = a.H == 1 ? 0xffffffffu : (uint32_t)(((uint64_t)1 << 32) / a.H);
+    a.G_inv = (uint32_t)((65536 + G - 1) / G);
     a.Hq = num_q_heads;
     a.G = G;
     a.block_table = tables->block_table;
