@@ -54,6 +54,7 @@ struct AttnArgs {
     int32_t H, Hq, G;
     uint32_t H_inv;      // 2^32 / H, rounded down (2^32 - 1 for 1)
     uint32_t G_inv;      // 2^16 / G, rounded up
+    int32_t split;       // logarithm of the warps that may share a row's parts
     const int32_t* block_table;
     const int32_t* lens;
     int32_t max_seqs, max_pages, batch;
@@ -86,6 +87,24 @@ __device__ __forceinline__ int atomic_add_acq_rel(int32_t* p, int32_t v)
     asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], %2;" : "=r"(old) : "l"(p), "r"(v) : "memory");
     return old;
 }
+
+// A value that the compiler knows nothing of.
+__device__ __forceinline__ void opaque(int& x) { asm volatile("" : "+r"(x)); }
+
+__device__ __forceinline__ float rcp(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float lg2(float x)
+{
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// 1 / x of a power of two (2^-126 .. 2^126).
+__device__ __forceinline__ float inverse_power(float x) { return __uint_as_float(0x7f000000u - __float_as_uint(x)); }
 
 // The rest of a wait that has not ended at once (out of line).
 __device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity)
@@ -145,43 +164,41 @@ struct State {
     __device__ __forceinline__ void start(const AttnArgs& a, int b, int h, int lane)
     {
         const int n = lane >> 2, j = lane & 3;
-        uint4 w[NW];
+        uint32_t w[NW][4] = {};
+        if (n < a.G) {
+            const uint16_t* q = a.q + b * a.q_stride + (int64_t)(h * a.G + n) * D + 8 * j;
 #pragma unroll
-        for (int i = 0; i < NW; ++i) {
-            w[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (n < a.G)
-                w[i] = *reinterpret_cast<const uint4*>(a.q + b * a.q_stride + (int64_t)(h * a.G + n) * D + 32 * i + 8 * j);
-        }
-        float x[NW][8], top = 0.f;
-#pragma unroll
-        for (int i = 0; i < NW; ++i) {
-            const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                x[i][2 * k] = T::lo(u[k]);
-                x[i][2 * k + 1] = T::hi(u[k]);
-                top = fmaxf(top, fmaxf(fabsf(x[i][2 * k]), fabsf(x[i][2 * k + 1])));
+            for (int i = 0; i < NW; ++i) {
+                const uint4 u = *reinterpret_cast<const uint4*>(q + 32 * i);
+                w[i][0] = u.x, w[i][1] = u.y, w[i][2] = u.z, w[i][3] = u.w;
             }
         }
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        // 2^up takes the row's largest |q| into [2^14, 2^15); a row of zeros, or one that is not finite, stays as it is.
+        // The row's largest |q| in the type's own bits, which are in its order.
+        uint32_t big = 0;
+#pragma unroll
+        for (int i = 0; i < NW; ++i)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) big = __vmaxu2(big, w[i][k] & 0x7fff7fffu);
+        big = max(big >> 16, big & 0xffffu);
+        big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
+        big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
+        // 2^up takes it into [2^14, 2^15); a row of zeros, or one that is not finite, stays as it is.
+        const float top = T::lo(big);
         const int ex = (int)(__float_as_uint(top) >> 23);
         const int up = top == 0.f || ex == 255 ? 0 : max(-126, min(126, 14 + 127 - ex));
         const float mul = __uint_as_float((uint32_t)(127 + up) << 23), back = __uint_as_float((uint32_t)(127 - up) << 23);
         float sums[NG];
 #pragma unroll
-        for (int k = 0; k < NG; ++k) sums[k] = 0.f;
-#pragma unroll
         for (int i = 0; i < NW; ++i) {
+            float sum = 0.f;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 // pair k of a word: elements 2k and 2k + 1, at bits 4k; odd k meets c * 2^-20
-                const float f = k & 1 ? mul * 0.0625f : mul;
-                const uint32_t p = pack_f16(x[i][2 * k] * f, x[i][2 * k + 1] * f);
-                qf[2 * i + (k >> 1)][k & 1] = p;
-                sums[i / (NW / NG)] += (Fp16::lo(p) + Fp16::hi(p)) * (k & 1 ? 16.f : 1.f);
+                const float x0 = T::lo(w[i][k]) * mul, x1 = T::hi(w[i][k]) * mul;
+                sum += x0 + x1;
+                qf[2 * i + (k >> 1)][k & 1] = k & 1 ? pack_f16(x0 * 0.0625f, x1 * 0.0625f) : pack_f16(x0, x1);
             }
+            sums[i / (NW / NG)] = i % (NW / NG) ? sums[i / (NW / NG)] + sum : sum;
         }
 #pragma unroll
         for (int k = 0; k < NG; ++k) {
@@ -225,11 +242,13 @@ struct State {
             asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(at));
     }
 
-    // NP pages in shared memory, from `at` on; `valid` (1 .. 16) of a single page's
-    // tokens count, all of a pair's.  Two at a time share the checks and keep two chains of products in flight.
-    template <int NP>
+    // The two pages of a stage, at `at` in shared memory; `valid`: how many of
+    // their tokens count (0 .. 16 each, the second page's from bit 8 on; not both none).  Two at a time
+    // share the checks and keep two chains of products in flight.
+    static constexpr int kBoth = kPageSize | kPageSize << 8;
     __device__ __forceinline__ void pages(uint32_t at, int valid, float scale, int lane)
     {
+        constexpr int NP = 2;
         const int g = lane >> 2;
         const uint32_t codes = at + lane * NW * 4, scales = at + 2 * B::kCodes + g * NG * 4;
         float s[NP][4];
@@ -271,18 +290,17 @@ struct State {
             }
 #pragma unroll
             for (int c = 0; c < 4; ++c) s[p][c] *= scale;   // and by qback where it meets m
-            if (NP == 1 && valid < kPageSize) {   // slots past the end may hold anything
-                if (g >= valid) {
-                    s[p][0] = s[p][1] = -INFINITY;
+        }
+        if (valid != kBoth) {   // slots past the end may hold anything
 #pragma unroll
-                    for (int k = 0; k < NG; ++k) mv[p][0][k] = 0u;
-                }
-                if (g + 8 >= valid) {
-                    s[p][2] = s[p][3] = -INFINITY;
+            for (int p = 0; p < NP; ++p)
 #pragma unroll
-                    for (int k = 0; k < NG; ++k) mv[p][1][k] = 0u;
-                }
-            }
+                for (int t = 0; t < 2; ++t)
+                    if (g + 8 * t >= (valid >> (8 * p) & 31)) {
+                        s[p][2 * t] = s[p][2 * t + 1] = -INFINITY;
+#pragma unroll
+                        for (int k = 0; k < NG; ++k) mv[p][t][k] = 0u;
+                    }
         }
         // The references m and E move only when a score passes m by more than
         // 8 (log2 units) or a scale its limit: weights stay below 2^8, weights times scales
@@ -346,9 +364,9 @@ struct State {
         if (vmax > vlimit) {   // the same in all lanes
             const int ex = max(-100, (int)(__float_as_uint(vmax) >> 23) - 127);
             const float next = __uint_as_float((uint32_t)(127 + 6 - ex) << 23);   // takes vmax into [2^6, 2^7)
-            r = next / vs;
+            r = next * inverse_power(vs);
             vs = next;
-            vlimit = 128.f / next;
+            vlimit = 128.f * inverse_power(next);
         }
         l[0] *= al0;
         l[1] *= al1;
@@ -380,7 +398,7 @@ struct State {
                 for (int k = 0; k < NG; ++k) z[k][c] += __shfl_xor_sync(0xffffffffu, z[k][c], mask);
             }
         }
-        const float back = 1.f / vs;
+        const float back = inverse_power(vs);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -397,7 +415,7 @@ struct State {
         for (int c = 0; c < 2; ++c) {
             const int n = 2 * (lane & 3) + c;
             if (n >= a.G) continue;
-            const float inv = l[c] == 0.f ? 0.f : 1.f / l[c];
+            const float inv = l[c] == 0.f ? 0.f : rcp(l[c]);
             uint16_t* out = a.out + b * a.out_stride + (int64_t)(h * a.G + n) * D + g;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
@@ -405,7 +423,7 @@ struct State {
                 out[16 * mt] = (uint16_t)w;
                 out[16 * mt + 8] = (uint16_t)(w >> 16);
             }
-            if (a.lse && g == 0) a.lse[(int64_t)b * a.Hq + h * a.G + n] = (m[c] + log2f(l[c])) * kLn2;
+            if (a.lse && g == 0) a.lse[(int64_t)b * a.Hq + h * a.G + n] = (m[c] + lg2(l[c])) * kLn2;
         }
     }
 
@@ -441,7 +459,7 @@ struct RowSum {
     }
     // Adds row n of the first `count` lanes' parts, in the lanes' order: `at` is a
     // part's offset in floats from `base`, -1 for none (not the first lane's).  A lane loads its part's (m, l), all
-    // lanes the rows, eight in flight, the first ones before the weights are known.
+    // lanes the rows, four in flight, the first ones before the weights are known.
     // The loads pass L1 by: parts may come from other SMs.
     __device__ __forceinline__ void merge(const float* base, int at, int count, int G, int n, int lane)
     {
@@ -455,10 +473,10 @@ struct RowSum {
         const uint32_t some = __ballot_sync(0xffffffffu, mine);
         float w = 0.f;
 #pragma unroll 1
-        for (int c = 0; c < count; c += 8) {
-            float x[8][E];
+        for (int c = 0; c < count; c += 4) {
+            float x[4][E];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) load_cg(base + __shfl_sync(0xffffffffu, from, (c + u) & 31) + n * D + lane * E, x[u]);
+            for (int u = 0; u < 4; ++u) load_cg(base + __shfl_sync(0xffffffffu, from, (c + u) & 31) + n * D + lane * E, x[u]);
             if (c == 0) {
                 const float top = fmaxf(m, warp_max(mc)), al = m == top ? 1.f : ex2(m - top);
                 w = mc == top && mine ? 1.f : ex2(mc - top);
@@ -470,7 +488,7 @@ struct RowSum {
                 for (int i = 0; i < E; ++i) o[i] *= al;
             }
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
+            for (int u = 0; u < 4; ++u) {
                 const bool on = c + u < 32 && ((some >> (c + u)) & 1u);
                 const float wu = __shfl_sync(0xffffffffu, w, (c + u) & 31), lu = __shfl_sync(0xffffffffu, lc, (c + u) & 31);
                 l += on ? lu : 0.f;
@@ -510,11 +528,11 @@ struct RowSum {
     template <class T>
     __device__ __forceinline__ void write_out(const AttnArgs& a, int b, int h, int n, int lane) const
     {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float inv = l == 0.f ? 0.f : rcp(l);
         uint16_t* out = a.out + b * a.out_stride + (int64_t)(h * a.G + n) * D + lane * E;
 #pragma unroll
         for (int i = 0; i < E; i += 2) *reinterpret_cast<uint32_t*>(out + i) = T::pack(o[i] * inv, o[i + 1] * inv);
-        if (a.lse && lane == 0) a.lse[(int64_t)b * a.Hq + h * a.G + n] = (m + log2f(l)) * kLn2;
+        if (a.lse && lane == 0) a.lse[(int64_t)b * a.Hq + h * a.G + n] = (m + lg2(l)) * kLn2;
     }
 };
 
@@ -528,7 +546,7 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ uint2 warp_pages[W];
     __shared__ int arrived[2];
-    __shared__ int2 spans[2];   // first and last CTA of what began before this CTA, and of what goes on after it
+    __shared__ int spans[4];   // first and last CTA of what began before this CTA, and of what goes on after it
     static_assert(2 * W <= 32, "a lane for each part");
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint8_t* ring = smem + warp * S::kRing;
@@ -546,15 +564,18 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
 
     // Pages of the rows before each row.
     const uint32_t H = a.H;
+    int has_ids = a.seq_ids != nullptr;
+    opaque(has_ids);
     const int max_len = min(a.max_pages, (1 << 27) - 1) * kPageSize;
     if (tid == 0) pages[0] = costs[0] = 0;
     uint64_t all_pages = 0;
     uint32_t held = 0;        // rows that are not empty
+#pragma unroll 1
     for (int r0 = 0; r0 < a.batch; r0 += W * 32) {
         const int r = r0 + tid;
         uint32_t n = 0;
         if (r < a.batch) {
-            const int seq = a.seq_ids ? a.seq_ids[r] : r;
+            const int seq = has_ids ? a.seq_ids[r] : r;
             int len = seq >= 0 && seq < a.max_seqs ? a.lens[seq] : -1;
             if (len < 0 || len > max_len) {
                 if (blockIdx.x == 0) kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
@@ -563,7 +584,7 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
             n = (uint32_t)(len + kPageSize - 1) / kPageSize;
         }
         const uint32_t some = __ballot_sync(0xffffffffu, n != 0);
-        uint32_t sum = n;     // (32 rows of up to 2^27 pages: a sum of 2^32 is found below)
+        uint32_t sum = n;     // (below 2^32: rows have less than 2^27 pages)
 #pragma unroll
         for (int k = 1; k < 32; k <<= 1) {
             const uint32_t up = __shfl_up_sync(0xffffffffu, sum, k);
@@ -571,20 +592,14 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
         }
         if (lane == 31) warp_pages[warp] = make_uint2(sum, (uint32_t)__popc(some));
         __syncthreads();
-        uint64_t mine = all_pages;
-        uint32_t rows = held;
-#pragma unroll
-        for (int w = 0; w < W; ++w) {
-            const uint2 x = warp_pages[w];
-            if (w < warp) {
-                mine += x.x;
-                rows += x.y;
-            }
-            all_pages += x.x;
-            held += x.y;
-        }
+        // The same over the warps (a lane for each); the total in 64 bits.
+        const uint2 of = lane < W ? warp_pages[lane] : make_uint2(0u, 0u);
+        const uint32_t mine = (uint32_t)all_pages + __reduce_add_sync(0xffffffffu, lane < warp ? of.x : 0u);
+        uint32_t rows = held + __reduce_add_sync(0xffffffffu, lane < warp ? of.y : 0u);
+        all_pages += __reduce_add_sync(0xffffffffu, of.x & 0xffffu) + ((uint64_t)__reduce_add_sync(0xffffffffu, of.x >> 16) << 16);
+        held += __reduce_add_sync(0xffffffffu, of.y);
         if (r < a.batch) {
-            const uint32_t up_to = (uint32_t)mine + sum;
+            const uint32_t up_to = mine + sum;
             rows += __popc(some & (2u << lane) - 1u);
             pages[r + 1] = up_to * H;
             costs[r + 1] = (up_to + rows * kRowCost) * H;
@@ -653,7 +668,7 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
         const int r0 = row0 = row_of(pages, row0, at);
         const uint32_t n = over_H(pages[r0 + 1] - pages[r0]), in_row = at - pages[r0];
         const int h = (int)head_of(in_row, n), p = (int)(in_row - h * n);
-        const int seq = a.seq_ids ? a.seq_ids[r0] : r0;
+        const int seq = has_ids ? a.seq_ids[r0] : r0;
         const int32_t page = a.block_table[(int64_t)seq * a.max_pages + p];
         int valid = min(kPageSize, a.lens[seq] - p * kPageSize);
         if (page >= 0 && page < a.num_pages) {
@@ -680,7 +695,7 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
     Tile next{nullptr, 0};            // of the 32 tiles after those in work
     const uint8_t* from = nullptr;    // the tile that this lane starts next
     uint32_t cur = 0;                 // of a tile in work: Tile::bits
-    constexpr uint32_t kOpen = 1, kClose = 2, kSingle = 4, kRefill = 8;
+    constexpr uint32_t kOpen = 1, kClose = 2, kSingle = 4, kRefill = 8, kFull = 16;
     uint32_t what = kRefill;          // and what its turn has to do
     int at = -32;                     // the tile that the next refill begins with
     bool begins = true;
@@ -700,14 +715,14 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
                 continue;
             }
             at += 32;
-            // Pairs begin at even tiles: full pages of one row.
+            // A stage's two tiles are worked together where they are pages of one row.
             const uint32_t lasts = __ballot_sync(0xffffffffu, cur & Tile::kLast);
             const uint32_t fulls = __ballot_sync(0xffffffffu, (cur & 31) == kPageSize);
-            const uint32_t pairs = fulls & (fulls >> 1) & ~lasts & 0x55555555u;
-            const uint32_t closes = lasts | (i + 32 >= count ? 1u << (count - 1 - i) : 0u);
-            const bool pair = (pairs >> lane) & 1u;
+            const uint32_t here = i + 32 < count ? 0xffffffffu : (2u << (count - 1 - i)) - 1u;   // tiles that there are
+            const uint32_t closes = lasts | (i + 32 < count ? 0u : (here >> 1) + 1u);
+            const bool pair = (here >> 1 & ~lasts & 0x55555555u) >> lane & 1u;
             what = ((cur & Tile::kFirst) || i + lane == 0 ? kOpen : 0u) | ((closes >> (lane + (pair ? 1 : 0))) & 1u ? kClose : 0u) |
-                   (pair ? 0u : kSingle) | (lane == 0 ? kRefill : 0u);
+                   (pair ? 0u : kSingle) | (lane == 0 ? kRefill : 0u) | (pair && (fulls >> lane & 3u) == 3u ? kFull : 0u);
             turn = __shfl_sync(0xffffffffu, what, 0);
         }
         if (turn & kOpen) {           // before the wait: q arrives meanwhile
@@ -719,19 +734,19 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
             ok = __all_sync(0xffffffffu, wait_long(bar, parity));
             if (!ok) {   // no more copies; those in flight land first, and the result is void
                 if (lane == 0) kv4_error(a.err, KVC_DEVERR_WAIT_TIMEOUT);
+                #pragma unroll 1
                 for (int k = i / 2; k < min(i / 2 + R, (count + 1) / 2); ++k) wait_long(bars_at + 8 * (k % R), (k / R) & 1);
                 from = next.src = nullptr;
             }
         }
-        const uint32_t tile = stage_at + (i & 1) * B::kBytes;
-        int last = src;               // the last tile of this turn
-        if (!(turn & kSingle)) {
-            ++last;
-            st.template pages<2>(tile, kPageSize, a.scale, lane);
-        } else {
-            const int valid = (int)(__shfl_sync(0xffffffffu, cur, src) & 31);
-            if (valid) st.template pages<1>(tile, valid, a.scale, lane);
+        const int last = turn & kSingle ? src : src + 1;   // the last tile of this turn
+        int valid = State<D, NG, T>::kBoth;
+        if (!(turn & kFull)) {
+            const int v0 = (int)(__shfl_sync(0xffffffffu, cur, src) & 31), v1 = (int)(__shfl_sync(0xffffffffu, cur, last) & 31);
+            valid = !(turn & kSingle) ? v0 | v1 << 8 : i & 1 ? v0 << 8 : v0;
         }
+        opaque(valid);                // (one copy of the work, not one for each kind of turn: code is fetched once a launch)
+        if (valid) st.pages(stage_at, valid, a.scale, lane);
         i += last - src + 1;
         if (turn & kClose) {
             const uint32_t t = __shfl_sync(0xffffffffu, cur, last);
@@ -765,11 +780,14 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
 
     // Rows without tokens.
     if ((int)held != a.batch)
+#pragma unroll 1
         for (int r = blockIdx.x; r < a.batch; r += gridDim.x)
             if (pages[r] == pages[r + 1]) {
+#pragma unroll 1
                 for (int i = tid; i < a.Hq * (D / 8); i += W * 32)
                     *reinterpret_cast<uint4*>(a.out + r * a.out_stride + i * 8) = make_uint4(0u, 0u, 0u, 0u);
                 if (a.lse)
+#pragma unroll 1
                     for (int i = tid; i < a.Hq; i += W * 32) a.lse[(int64_t)r * a.Hq + i] = -INFINITY;
             }
     __syncthreads();
@@ -788,15 +806,14 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
     const bool from_before = !((begin >> first) & 1u);
     const bool goes_on = !(ending >> last) && !(last == first && from_before);
     const bool crosses = from_before || goes_on;
-    if (warp == W - 1 && lane < 2 && (lane ? goes_on : from_before)) {
-        // The CTAs that hold parts of it (while the others merge).
-        const PartInfo in = infos[lane ? last : first];
-        auto cta_of = [&](uint32_t p) {   // the CTA whose share holds page p
-            const uint32_t n = over_H(pages[in.b + 1] - pages[in.b]), place = costs[in.b] + in.h * (n + kRowCost) + kRowCost + p;
-            const uint32_t long_ones = extra * (base + 1);
-            return (int)((place < long_ones ? place / (base + 1) : extra + (place - long_ones) / base) / cta_warps);
-        };
-        spans[lane] = make_int2(cta_of(0), cta_of(over_H(pages[in.b + 1] - pages[in.b]) - 1));
+    if (warp == W - 1 && lane < 4 && (lane >> 1 ? goes_on : from_before)) {
+        // The CTAs that hold the first and the last page of it (while the others merge).
+        const PartInfo in = infos[lane >> 1 ? last : first];
+        const uint32_t n = over_H(pages[in.b + 1] - pages[in.b]), p = lane & 1 ? n - 1 : 0;
+        const uint32_t place = costs[in.b] + in.h * (n + kRowCost) + kRowCost + p, long_ones = extra * (base + 1);
+        const bool in_long = place < long_ones;
+        const uint32_t w = (in_long ? place : place - long_ones) / (in_long ? base + 1 : base) + (in_long ? 0 : extra);
+        spans[lane] = (int)(w / cta_warps);
     }
     // Pass 0 merges the groups in shared memory, pass 1 (k = 0, 1) the parts of all CTAs of what
     // crosses them, by the last CTA to arrive; where those are many, several warps share a row's
@@ -804,9 +821,10 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
     const int jobs0 = __popc(groups) * a.G;
 #pragma unroll 1
     for (int pass = 0, k = 0;; ) {
-        const int parts = pass ? spans[k].y - spans[k].x + 1 : 0;
-        const int split = parts > 16 ? max(1, W / a.G) : 1, each = split > 1 ? (parts + split - 1) / split : parts;
-        const int jobs = pass == 0 ? jobs0 : pass == 1 ? a.G * split : a.G;
+        opaque(pass);
+        const int parts = pass ? spans[2 * k + 1] - spans[2 * k] + 1 : 0;
+        const int split = parts > 16 ? a.split : 0, each = (parts + (1 << split) - 1) >> split;   // (logarithm)
+        const int jobs = pass == 0 ? jobs0 : pass == 1 ? a.G << split : a.G;
 #pragma unroll 1
         for (int job = warp; job < jobs; job += W) {
             int n, b, h, c = 0, end = 0;
@@ -827,13 +845,13 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
                 c = e;
                 end = 32 - __clz(members);
             } else {
-                n = split > 1 && pass == 1 ? job / split : job;
+                n = pass == 1 ? job >> split : job;
                 b = infos[k ? last : first].b;
                 h = infos[k ? last : first].h;
-                const int share = split > 1 && pass == 1 ? job - n * split : 0;
-                c = share * each;
-                end = pass == 1 ? min(parts, c + each) : split;
-                if (pass == 1 && split > 1) to = heads + share * PF;
+                const int share = job - (n << split);
+                c = pass == 1 ? share * each : 0;
+                end = pass == 1 ? min(parts, c + each) : 1 << split;
+                if (pass == 1 && split) to = heads + share * PF;
             }
             RowSum<D> sum;
 #pragma unroll 1
@@ -841,7 +859,7 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
                 const int i = c + lane;
                 int off;
                 if (pass == 0) off = !((members >> (i & 31)) & 1u) || i > 31 ? -1 : i & 1 ? (i >> 1) * (S::kRing / 4) : M::kHeads / 4 + (i >> 1) * PF;
-                else off = pass == 1 ? ((spans[k].x + i) * 2 + (i == 0 ? 1 : 0)) * PF : M::kHeads / 4 + i * PF;
+                else off = pass == 1 ? ((spans[2 * k] + i) * 2 + (i == 0 ? 1 : 0)) * PF : M::kHeads / 4 + i * PF;
                 sum.merge(pass == 1 ? a.parts : reinterpret_cast<const float*>(smem), off, min(32, end - c), a.G, n, lane);
             }
             if (to) sum.write_part(to, a.G, n, lane);
@@ -853,9 +871,9 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
             if (tid < 2) {
                 arrived[tid] = 0;
                 if (tid ? goes_on : from_before) {
-                    const int2 at = spans[tid];
-                    if (atomic_add_acq_rel(a.counters + at.x, 1) == at.y - at.x) {
-                        a.counters[at.x] = 0;
+                    const int c0 = spans[2 * tid], c1 = spans[2 * tid + 1];
+                    if (atomic_add_acq_rel(a.counters + c0, 1) == c1 - c0) {
+                        a.counters[c0] = 0;
                         arrived[tid] = 1;
                     }
                 }
@@ -863,7 +881,7 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
             __syncthreads();
             pass = 1;
             k = -1;
-        } else if (pass == 1 && split > 1) {
+        } else if (pass == 1 && split) {
             __syncthreads();
             pass = 2;
             continue;
@@ -912,6 +930,8 @@ struct LaunchAttention {
         constexpr int most = AttnSmem<D, NG>::bytes(kMaxGroup, kSmemRows);
         static_assert(part_floats(kMaxGroup, D) * 4 <= S::kRing, "a part lies in its warp's ring");
         static_assert(most <= 226 * 1024, "shared memory of a CTA");
+        a.split = 0;
+        while (a.G << (a.split + 1) <= S::kWarps) ++a.split;
         cudaError_t e = once.set_attribute(attention_kernel<D, NG, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
         if (e != cudaSuccess) return e;
         return kv4_launch(attention_kernel<D, NG, T>, dim3((unsigned)sms), S::kWarps * 32, (size_t)smem, st, a);
