@@ -32,6 +32,7 @@
 // arrive (a counter per first CTA, which it sets back to zero) merges the parts in
 // the order of the list.
 #include <cmath>
+#include <type_traits>
 
 #include "kvd_kv4.h"
 #include "kvd_ptx.cuh"
@@ -135,10 +136,9 @@ struct AttnSmem {   // byte offsets in dynamic shared memory
 
 // What a lane knows of one tile.
 struct Tile {
-    const uint8_t* src;   // null: none; kAlone is added where the share ends with it
+    const uint8_t* src;   // null: none
     uint32_t bits;        // valid tokens (0 .. 16), kFirst / kLast page of its (row, KV head), which follows
     static constexpr uint32_t kFirst = 32, kLast = 64;
-    static constexpr uint64_t kAlone = 1;
     static __device__ __forceinline__ uint32_t pack(int b, int h) { return (uint32_t)h << 7 | (uint32_t)b << 17; }
     static __device__ __forceinline__ int row(uint32_t bits) { return (int)(bits >> 17); }
     static __device__ __forceinline__ int head(uint32_t bits) { return (int)(bits >> 7 & 1023u); }
@@ -153,9 +153,11 @@ struct State {
     using B = Kv4Block<D, NG>;
     static constexpr int NW = D / 32;     // code words of a lane per 8 tokens
     static constexpr int MT = D / 16;     // 16-element tiles of the output
+    // The K accumulators hold 2^-24 q c; sums of q are taken in a unit that the cache's type holds (8 times 2^22 at most).
+    static constexpr bool kHalf = std::is_same_v<T, Fp16>;
+    static constexpr float kSumUnit = kHalf ? 0x1p-10f : 0x1p-24f;
     uint32_t qf[2 * NW][2];               // q as the K product's column operand
-    float qsum[NG][2];                    // sum of q over a group, in the accumulators' units
-    float qoff[4];                        // -8 times it, as the accumulators begin (kept for one group: registers)
+    uint32_t qz[3];                       // (-8, 1) * sum of q over group j, in terms of the cache's type
     float qback[2];                       // undoes q's power of two
     float m[2], l[2];
     float o[MT][4], e[NG][4], z[NG][2];   // e: -8 sum p s' of a group (apart: a NaN stays in its group)
@@ -200,16 +202,20 @@ struct State {
             }
             sums[i / (NW / NG)] = i % (NW / NG) ? sums[i / (NW / NG)] + sum : sum;
         }
+        // Lane j takes its group's sum, in two (fp16) or three (bf16) terms: 22 or 24 bits.
+        float rest = 0.f;
 #pragma unroll
         for (int k = 0; k < NG; ++k) {
             sums[k] += __shfl_xor_sync(0xffffffffu, sums[k], 1);
             sums[k] += __shfl_xor_sync(0xffffffffu, sums[k], 2);
-            sums[k] *= 0x1p-24f;
-            qsum[k][0] = __shfl_sync(0xffffffffu, sums[k], 8 * j);
-            qsum[k][1] = __shfl_sync(0xffffffffu, sums[k], 8 * j + 4);
+            if (j == k) rest = sums[k] * kSumUnit;
         }
 #pragma unroll
-        for (int c = 0; c < 4; ++c) qoff[c] = NG == 1 ? -8.f * qsum[0][c & 1] : 0.f;
+        for (int k = 0; k < 3; ++k) {
+            const float term = T::lo(T::pack(rest, 0.f));
+            qz[k] = T::pack(-8.f * term, term);
+            rest -= term;
+        }
         qback[0] = __shfl_sync(0xffffffffu, back, 8 * j);
         qback[1] = __shfl_sync(0xffffffffu, back, 8 * j + 4);
 #pragma unroll
@@ -242,6 +248,13 @@ struct State {
             asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(at));
     }
 
+    static __device__ __forceinline__ uint32_t load_shared(uint32_t at)
+    {
+        uint32_t w[1];
+        load_shared(at, w);
+        return w[0];
+    }
+
     // The two pages of a stage, at `at` in shared memory; `valid`: how many of
     // their tokens count (0 .. 16 each, the second page's from bit 8 on; not both none).  Two at a time
     // share the checks and keep two chains of products in flight.
@@ -251,6 +264,7 @@ struct State {
         constexpr int NP = 2;
         const int g = lane >> 2;
         const uint32_t codes = at + lane * NW * 4, scales = at + 2 * B::kCodes + g * NG * 4;
+        const uint32_t own = scales + (lane & (NG - 1)) * 4;   // group j's word (of lanes that have none: another one's, against zeros)
         float s[NP][4];
         uint32_t mv[NP][2][NG];
 #pragma unroll
@@ -262,16 +276,32 @@ struct State {
             load_shared(scales + p * B::kBytes + 8 * NG * 4, mk[1]);
             load_shared(scales + p * B::kBytes + B::kScales, mv[p][0]);
             load_shared(scales + p * B::kBytes + B::kScales + 8 * NG * 4, mv[p][1]);
+            // sum_groups (z - 8 s) sum q: the scale words (s, z) as they lie against (-8, 1) sum q.
+            const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+            float base[4];
+            uint32_t w0, w1;
+            if constexpr (NG == 1) {
+                w0 = mk[0][0], w1 = mk[1][0];
+            } else {
+                w0 = load_shared(own + p * B::kBytes), w1 = load_shared(own + p * B::kBytes + 8 * NG * 4);
+            }
+            if constexpr (kHalf) {
+                mma_f16_16816(base, w0, w1, w0, w1, qz[0], qz[1], zero);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) base[c] *= 0x1p-24f / kSumUnit;
+            } else {
+                mma_bf16_16816(base, w0, w1, w0, w1, qz[0], qz[1], zero);
+                mma_bf16_16816(base, w0, w1, w0, w1, qz[2], 0u);
+            }
 #pragma unroll
             for (int k = 0; k < NG; ++k) {
                 float acc[4];
-                const float from[4] = {NG == 1 ? qoff[0] : 0.f, NG == 1 ? qoff[1] : 0.f, NG == 1 ? qoff[2] : 0.f, NG == 1 ? qoff[3] : 0.f};
 #pragma unroll
                 for (int i = k * (NW / NG); i < (k + 1) * (NW / NG); ++i) {
                     const uint32_t a8 = ka[i] >> 8, b8 = kb[i] >> 8;
                     if (i == k * (NW / NG))
                         mma_f16_16816(acc, ka[i] & 0x000f000fu, kb[i] & 0x000f000fu, ka[i] & 0x00f000f0u, kb[i] & 0x00f000f0u,
-                                      qf[2 * i][0], qf[2 * i][1], from);
+                                      qf[2 * i][0], qf[2 * i][1], zero);
                     else
                         mma_f16_16816(acc, ka[i] & 0x000f000fu, kb[i] & 0x000f000fu, ka[i] & 0x00f000f0u, kb[i] & 0x00f000f0u,
                                       qf[2 * i][0], qf[2 * i][1]);
@@ -279,15 +309,10 @@ struct State {
                                   qf[2 * i + 1][0], qf[2 * i + 1][1]);
                 }
 #pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const float ss = T::lo(mk[t][k]), sz = NG == 1 ? T::hi(mk[t][k]) : fmaf(-8.f, ss, T::hi(mk[t][k]));
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        float& x = s[p][2 * t + c];
-                        x = fmaf(ss, acc[2 * t + c], k == 0 ? sz * qsum[k][c] : fmaf(sz, qsum[k][c], x));
-                    }
-                }
+                for (int c = 0; c < 4; ++c) base[c] = fmaf(T::lo(mk[c >> 1][k]), acc[c], base[c]);
             }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) s[p][c] = base[c];
 #pragma unroll
             for (int c = 0; c < 4; ++c) s[p][c] *= scale;   // and by qback where it meets m
         }
@@ -678,104 +703,106 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
             t.src = a.pool;
             valid = 0;
         }
-        if (i == count - 1) t.src += Tile::kAlone;
         t.bits = Tile::pack(r0, h) | valid | (p == 0 ? Tile::kFirst : 0u) | (p == (int)n - 1 ? Tile::kLast : 0u);
         return t;
     };
     // The ring's stages hold two tiles each and are used in turn: tiles 2k and
     // 2k + 1 of the share lie in stage k % R.  Their copies are started by the lanes that hold the tiles.
     const uint32_t ring_at = smem_addr(ring), bars_at = smem_addr(bars);
-    auto issue = [&](const uint8_t* from, bool mine, uint32_t stage_at, uint32_t bar) {   // mine: one of two neighbours' turn
-        const uint64_t src = reinterpret_cast<uint64_t>(from);
-        bulk_load_pair(stage_at + (lane & 1) * B::kBytes, src & ~Tile::kAlone, B::kBytes, src & Tile::kAlone ? B::kBytes : 2 * B::kBytes,
-                       bar, policy, mine && src, mine && src && !(lane & 1));
-    };
+    const uint32_t ring_lane = ring_at + (lane & 1) * B::kBytes;
 
     State<D, NG, T> st;
     Tile next{nullptr, 0};            // of the 32 tiles after those in work
-    const uint8_t* from = nullptr;    // the tile that this lane starts next
+    const uint8_t* from = nullptr;    // the tile that this lane starts next, in stage turn `when` of 16 (-1: none),
+    int when = -1;
+    uint32_t expect = 0;              // and the bytes that it announces: of both tiles of a stage
+    auto take_next = [&](int i) {     // the copies of `next`, whose first tile is i
+        from = next.src;
+        when = from ? lane >> 1 : -1;
+        expect = !from || lane & 1 ? 0u : i + lane + 1 < count ? 2 * B::kBytes : B::kBytes;
+    };
     uint32_t cur = 0;                 // of a tile in work: Tile::bits
-    constexpr uint32_t kOpen = 1, kClose = 2, kSingle = 4, kRefill = 8, kFull = 16;
+    constexpr uint32_t kOpen = 1, kClose = 2, kSingle = 4, kRefill = 8, kFull = 16, kHold = 32;
     uint32_t what = kRefill;          // and what its turn has to do
     int at = -32;                     // the tile that the next refill begins with
     bool begins = true;
-    uint32_t stage_at = ring_at, bar = bars_at, parity = 0;   // of the stage in work; parity flips where the stages begin again
+    uint32_t stage = 0;               // stages done, from the share's first on
 #pragma unroll 1
     for (int i = 0; i < count;) {
         const int src = i & 31;
         uint32_t turn = __shfl_sync(0xffffffffu, what, src);
-        if (turn & kRefill) {
-            cur = next.bits;
-            next = tile_of(at + 32 + lane);
-            if (at < 0) {             // fill the ring
-                from = next.src;
-                __syncwarp();
-                issue(from, lane < 2 * R, ring_at + (lane >> 1) * 2 * B::kBytes, bars_at + 8 * (lane >> 1));
-                at = 0;
-                continue;
+        int valid = State<D, NG, T>::kBoth;
+        if (turn != kFull) {          // not just two full pages
+            if (turn & kRefill) {
+                cur = next.bits;
+                next = tile_of(at + 32 + lane);
+                if (at < 0) {         // fill the ring
+                    take_next(0);
+                    __syncwarp();
+                    bulk_load_turn(ring_lane + (lane >> 1) * 2 * B::kBytes, from, B::kBytes, expect, bars_at + 8 * (lane >> 1), policy, when,
+                                   lane < 2 * R ? lane >> 1 : -2);
+                    at = 0;
+                    continue;
+                }
+                at += 32;
+                // A stage's two tiles are worked together where they are pages of one row.
+                const uint32_t lasts = __ballot_sync(0xffffffffu, cur & Tile::kLast);
+                const uint32_t fulls = __ballot_sync(0xffffffffu, (cur & 31) == kPageSize);
+                const uint32_t here = i + 32 < count ? 0xffffffffu : (2u << (count - 1 - i)) - 1u;   // tiles that there are
+                const uint32_t closes = lasts | (i + 32 < count ? 0u : (here >> 1) + 1u);
+                const bool pair = (here >> 1 & ~lasts & 0x55555555u) >> lane & 1u;
+                what = ((cur & Tile::kFirst) || i + lane == 0 ? kOpen : 0u) | ((closes >> (lane + (pair ? 1 : 0))) & 1u ? kClose : 0u) |
+                       (pair ? 0u : kSingle) | (lane == 0 ? kRefill : 0u) | (pair && (fulls >> lane & 3u) == 3u ? kFull : 0u) |
+                       (pair || lane & 1 ? 0u : kHold);
+                turn = __shfl_sync(0xffffffffu, what, 0);
             }
-            at += 32;
-            // A stage's two tiles are worked together where they are pages of one row.
-            const uint32_t lasts = __ballot_sync(0xffffffffu, cur & Tile::kLast);
-            const uint32_t fulls = __ballot_sync(0xffffffffu, (cur & 31) == kPageSize);
-            const uint32_t here = i + 32 < count ? 0xffffffffu : (2u << (count - 1 - i)) - 1u;   // tiles that there are
-            const uint32_t closes = lasts | (i + 32 < count ? 0u : (here >> 1) + 1u);
-            const bool pair = (here >> 1 & ~lasts & 0x55555555u) >> lane & 1u;
-            what = ((cur & Tile::kFirst) || i + lane == 0 ? kOpen : 0u) | ((closes >> (lane + (pair ? 1 : 0))) & 1u ? kClose : 0u) |
-                   (pair ? 0u : kSingle) | (lane == 0 ? kRefill : 0u) | (pair && (fulls >> lane & 3u) == 3u ? kFull : 0u);
-            turn = __shfl_sync(0xffffffffu, what, 0);
+            if (turn & kOpen) {       // before the wait: q arrives meanwhile
+                const uint32_t t = __shfl_sync(0xffffffffu, cur, src);
+                begins = t & Tile::kFirst;
+                st.start(a, Tile::row(t), Tile::head(t), lane);
+            }
+            if (!(turn & kFull)) {
+                const int v0 = (int)(__shfl_sync(0xffffffffu, cur, src) & 31), v1 = (int)(__shfl_sync(0xffffffffu, cur, (src + 1) & 31) & 31);
+                valid = !(turn & kSingle) ? v0 | v1 << 8 : i & 1 ? v0 << 8 : v0;
+            }
         }
-        if (turn & kOpen) {           // before the wait: q arrives meanwhile
-            const uint32_t t = __shfl_sync(0xffffffffu, cur, src);
-            begins = t & Tile::kFirst;
-            st.start(a, Tile::row(t), Tile::head(t), lane);
-        }
+        const uint32_t place = stage % R, bar = bars_at + 8 * place, parity = stage / R & 1u;
         if (!__all_sync(0xffffffffu, mbar_try_wait(bar, parity)) && ok) {
             ok = __all_sync(0xffffffffu, wait_long(bar, parity));
             if (!ok) {   // no more copies; those in flight land first, and the result is void
                 if (lane == 0) kv4_error(a.err, KVC_DEVERR_WAIT_TIMEOUT);
-                #pragma unroll 1
+#pragma unroll 1
                 for (int k = i / 2; k < min(i / 2 + R, (count + 1) / 2); ++k) wait_long(bars_at + 8 * (k % R), (k / R) & 1);
-                from = next.src = nullptr;
+                when = -1;
+                next.src = nullptr;
             }
-        }
-        const int last = turn & kSingle ? src : src + 1;   // the last tile of this turn
-        int valid = State<D, NG, T>::kBoth;
-        if (!(turn & kFull)) {
-            const int v0 = (int)(__shfl_sync(0xffffffffu, cur, src) & 31), v1 = (int)(__shfl_sync(0xffffffffu, cur, last) & 31);
-            valid = !(turn & kSingle) ? v0 | v1 << 8 : i & 1 ? v0 << 8 : v0;
         }
         opaque(valid);                // (one copy of the work, not one for each kind of turn: code is fetched once a launch)
-        if (valid) st.pages(stage_at, valid, a.scale, lane);
-        i += last - src + 1;
-        if (turn & kClose) {
-            const uint32_t t = __shfl_sync(0xffffffffu, cur, last);
-            const int b = Tile::row(t), h = Tile::head(t);
-            const bool ends = t & Tile::kLast;
-            st.finish();
-            if (begins && ends) {
-                st.write_out(a, b, h, lane);
-            } else {
-                // A part that is not the share's last one began before it.
-                const int k = i == count ? 1 : 0;
-                __syncwarp();         // the ring's last tiles have been read
-                st.write_part(k ? reinterpret_cast<float*>(ring) : heads + warp * part_floats(a.G, D), a.G, lane);
-                if (lane == 0) infos[2 * warp + k] = {b, h, begins, ends};
+        if (valid) st.pages(ring_at + place * 2 * B::kBytes, valid, a.scale, lane);
+        i += turn & kSingle ? 1 : 2;
+        if (turn & (kClose | kHold)) {
+            if (turn & kClose) {
+                const uint32_t t = __shfl_sync(0xffffffffu, cur, (i - 1) & 31);
+                const int b = Tile::row(t), h = Tile::head(t);
+                const bool ends = t & Tile::kLast;
+                st.finish();
+                if (begins && ends) {
+                    st.write_out(a, b, h, lane);
+                } else {
+                    // A part that is not the share's last one began before it.
+                    const int k = i == count ? 1 : 0;
+                    __syncwarp();     // the ring's last tiles have been read
+                    st.write_part(k ? reinterpret_cast<float*>(ring) : heads + warp * part_floats(a.G, D), a.G, lane);
+                    if (lane == 0) infos[2 * warp + k] = {b, h, begins, ends};
+                }
             }
+            if (turn & kHold) continue;   // the stage's other tile is to come
         }
-        if (last & 1) {               // the stage is done
-            __syncwarp();
-            const int to = (last - 1 + 2 * R) & 31;
-            if (to == 0) from = next.src;
-            issue(from, (lane & ~1) == to, stage_at, bar);
-            stage_at += 2 * B::kBytes;
-            bar += 8;
-            if (bar == bars_at + 8 * R) {
-                stage_at = ring_at;
-                bar = bars_at;
-                parity ^= 1u;
-            }
-        }
+        __syncwarp();
+        const int issue = (stage + R) & 15;
+        if (issue == 0) take_next((stage + R) * 2);
+        bulk_load_turn(ring_lane + place * 2 * B::kBytes, from, B::kBytes, expect, bar, policy, when, issue);
+        ++stage;
     }
 
     // Rows without tokens.

@@ -107,18 +107,18 @@ __device__ __forceinline__ void prefetch_tensormap(const CUtensorMap* map)
 }
 
 // A lane's copy of `bytes` (a multiple of 16) of consecutive global memory into
-// shared memory (both addresses 16-byte aligned) where `copy`, after it has announced `expect` bytes
-// on the barrier where `announce` (a barrier of one arrival; no branches).
-__device__ __forceinline__ void bulk_load_pair(uint32_t dst, uint64_t src, uint32_t bytes, uint32_t expect, uint32_t bar,
-                                               uint64_t policy, bool copy, bool announce)
+// shared memory (both addresses 16-byte aligned) where `when` == `turn`, after it has announced
+// `expect` bytes on the barrier, if any (a barrier of one arrival; no branches).
+__device__ __forceinline__ void bulk_load_turn(uint32_t dst, const void* src, uint32_t bytes, uint32_t expect, uint32_t bar,
+                                               uint64_t policy, int when, int turn)
 {
     asm volatile(
         "{\n\t.reg .pred p, q;\n\t"
-        "setp.ne.u32 p, %6, 0;\n\t"
-        "setp.ne.u32 q, %7, 0;\n\t"
+        "setp.eq.s32 p, %6, %7;\n\t"
+        "setp.ne.and.u32 q, %4, 0, p;\n\t"
         "@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%3], %4;\n\t"
         "@p cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %5;\n\t}" ::"r"(dst),
-        "l"(src), "r"(bytes), "r"(bar), "r"(expect), "l"(policy), "r"((uint32_t)copy), "r"((uint32_t)announce)
+        "l"(src), "r"(bytes), "r"(bar), "r"(expect), "l"(policy), "r"(when), "r"(turn)
         : "memory");
 }
 
@@ -272,6 +272,17 @@ __device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32
 {
     asm volatile(
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+        "{%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
+}
+
+// The same for bf16 operands.
+__device__ __forceinline__ void mma_bf16_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                              uint32_t b0, uint32_t b1, const float (&c)[4])
+{
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
         "{%8,%9}, {%10,%11,%12,%13};"
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
