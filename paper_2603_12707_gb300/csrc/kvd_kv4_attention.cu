@@ -73,12 +73,13 @@ struct AttnArgs {
 
 // The shape of a variant: warps of the one CTA per SM (with two CTAs the older
 // one's warps are served first, and half the SM idles while the other ends: 64
-// MHA rows 5 us more), ring stages (of two tiles) per warp.
+// MHA rows 5 us more), tiles of a ring stage, which a warp works together.
 template <int D, int NG>
 struct AttnShape {
     static constexpr int kWarps = NG == 4 ? 12 : 16;
-    static constexpr int kStages = D == 64 ? 4 : 2;
-    static constexpr int kRing = kStages * 2 * Kv4Block<D, NG>::kBytes;   // of one warp
+    static constexpr int kStages = 2;
+    static constexpr int kTiles = D == 64 ? 4 : 2;
+    static constexpr int kStage = kTiles * Kv4Block<D, NG>::kBytes;
 };
 
 // Everything the CTA wrote before (a barrier before this call) is visible to who adds after it.
@@ -127,8 +128,9 @@ __host__ __device__ constexpr int part_floats(int G, int D) { return G * D + ((2
 template <int D, int NG>
 struct AttnSmem {   // byte offsets in dynamic shared memory
     using S = AttnShape<D, NG>;
-    static constexpr int kBars = S::kWarps * S::kRing;
-    static constexpr int kInfo = kBars + S::kWarps * S::kStages * 8;
+    static constexpr int R = S::kStages, kRing = R * S::kStage;
+    static constexpr int kBars = S::kWarps * kRing;
+    static constexpr int kInfo = kBars + S::kWarps * R * 8;
     static constexpr int kHeads = kInfo + S::kWarps * 2 * (int)sizeof(PartInfo);   // a warp's first part: [kWarps][part_floats]
     __host__ __device__ static constexpr int pages(int G) { return kHeads + S::kWarps * part_floats(G, D) * 4; }   // [2][batch + 1]
     __host__ __device__ static constexpr int bytes(int G, int batch) { return pages(G) + (batch <= kSmemRows ? 2 * (batch + 1) * 4 : 0); }
@@ -255,13 +257,13 @@ struct State {
         return w[0];
     }
 
-    // The two pages of a stage, at `at` in shared memory; `valid`: how many of
-    // their tokens count (0 .. 16 each, the second page's from bit 8 on; not both none).  Two at a time
-    // share the checks and keep two chains of products in flight.
-    static constexpr int kBoth = kPageSize | kPageSize << 8;
+    // The pages of a stage, at `at` in shared memory; `valid`: how many of their
+    // tokens count (0 .. 16, a byte for each page; not all none).  Together they
+    // share the checks and keep several chains of products in flight.
+    static constexpr int NP = AttnShape<D, NG>::kTiles;
+    static constexpr int kAll = NP == 4 ? 0x10101010 : 0x1010;
     __device__ __forceinline__ void pages(uint32_t at, int valid, float scale, int lane)
     {
-        constexpr int NP = 2;
         const int g = lane >> 2;
         const uint32_t codes = at + lane * NW * 4, scales = at + 2 * B::kCodes + g * NG * 4;
         const uint32_t own = scales + (lane & (NG - 1)) * 4;   // group j's word (of lanes that have none: another one's, against zeros)
@@ -316,7 +318,7 @@ struct State {
 #pragma unroll
             for (int c = 0; c < 4; ++c) s[p][c] *= scale;   // and by qback where it meets m
         }
-        if (valid != kBoth) {   // slots past the end may hold anything
+        if (valid != kAll) {   // slots past the end may hold anything
 #pragma unroll
             for (int p = 0; p < NP; ++p)
 #pragma unroll
@@ -567,14 +569,14 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
     using S = AttnShape<D, NG>;
     using B = Kv4Block<D, NG>;
     using M = AttnSmem<D, NG>;
-    constexpr int W = S::kWarps, R = S::kStages, E = D / 32;
+    constexpr int W = S::kWarps, N = S::kTiles, R = S::kStages;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ uint2 warp_pages[W];
     __shared__ int arrived[2];
     __shared__ int spans[4];   // first and last CTA of what began before this CTA, and of what goes on after it
     static_assert(2 * W <= 32, "a lane for each part");
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    uint8_t* ring = smem + warp * S::kRing;
+    uint8_t* ring = smem + warp * M::kRing;
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + M::kBars) + warp * R;
     PartInfo* infos = reinterpret_cast<PartInfo*>(smem + M::kInfo);
     float* heads = reinterpret_cast<float*>(smem + M::kHeads);
@@ -706,24 +708,24 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
         t.bits = Tile::pack(r0, h) | valid | (p == 0 ? Tile::kFirst : 0u) | (p == (int)n - 1 ? Tile::kLast : 0u);
         return t;
     };
-    // The ring's stages hold two tiles each and are used in turn: tiles 2k and
-    // 2k + 1 of the share lie in stage k % R.  Their copies are started by the lanes that hold the tiles.
+    // The ring's stages hold N tiles each and are used in turn: tiles N k .. of
+    // the share lie in stage k % R.  Their copies are started by the lanes that hold the tiles.
     const uint32_t ring_at = smem_addr(ring), bars_at = smem_addr(bars);
-    const uint32_t ring_lane = ring_at + (lane & 1) * B::kBytes;
+    const uint32_t ring_lane = ring_at + (lane % N) * B::kBytes;
 
     State<D, NG, T> st;
     Tile next{nullptr, 0};            // of the 32 tiles after those in work
-    const uint8_t* from = nullptr;    // the tile that this lane starts next, in stage turn `when` of 16 (-1: none),
+    const uint8_t* from = nullptr;    // the tile that this lane starts next, in turn `when` of the 32 / N (-1: none),
     int when = -1;
-    uint32_t expect = 0;              // and the bytes that it announces: of both tiles of a stage
+    uint32_t expect = 0;              // and the bytes that it announces: of its stage's tiles
     auto take_next = [&](int i) {     // the copies of `next`, whose first tile is i
         from = next.src;
-        when = from ? lane >> 1 : -1;
-        expect = !from || lane & 1 ? 0u : i + lane + 1 < count ? 2 * B::kBytes : B::kBytes;
+        when = from ? lane / N : -1;
+        expect = from && lane % N == 0 ? min(N, count - i - lane) * B::kBytes : 0u;
     };
     uint32_t cur = 0;                 // of a tile in work: Tile::bits
-    constexpr uint32_t kOpen = 1, kClose = 2, kSingle = 4, kRefill = 8, kFull = 16, kHold = 32;
-    uint32_t what = kRefill;          // and what its turn has to do
+    constexpr uint32_t kOpen = 1, kClose = 2, kRefill = 4, kFull = 8, kHold = 16;   // and from bit 8 on, if not kFull: tiles
+    uint32_t what = kRefill;          // and what the turn that begins with it has to do
     int at = -32;                     // the tile that the next refill begins with
     bool begins = true;
     uint32_t stage = 0;               // stages done, from the share's first on
@@ -731,29 +733,29 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
     for (int i = 0; i < count;) {
         const int src = i & 31;
         uint32_t turn = __shfl_sync(0xffffffffu, what, src);
-        int valid = State<D, NG, T>::kBoth;
-        if (turn != kFull) {          // not just two full pages
+        int valid = State<D, NG, T>::kAll, tiles = N;
+        if (turn != kFull) {          // not just a stage of full pages
             if (turn & kRefill) {
                 cur = next.bits;
                 next = tile_of(at + 32 + lane);
                 if (at < 0) {         // fill the ring
                     take_next(0);
                     __syncwarp();
-                    bulk_load_turn(ring_lane + (lane >> 1) * 2 * B::kBytes, from, B::kBytes, expect, bars_at + 8 * (lane >> 1), policy, when,
-                                   lane < 2 * R ? lane >> 1 : -2);
+                    bulk_load_turn(ring_lane + lane / N * S::kStage, from, B::kBytes, expect, bars_at + 8 * (lane / N), policy, when,
+                                   lane < N * R ? lane / N : -2);
                     at = 0;
                     continue;
                 }
                 at += 32;
-                // A stage's two tiles are worked together where they are pages of one row.
+                // A turn takes a stage's tiles as far as they are pages of one row.
                 const uint32_t lasts = __ballot_sync(0xffffffffu, cur & Tile::kLast);
                 const uint32_t fulls = __ballot_sync(0xffffffffu, (cur & 31) == kPageSize);
-                const uint32_t here = i + 32 < count ? 0xffffffffu : (2u << (count - 1 - i)) - 1u;   // tiles that there are
-                const uint32_t closes = lasts | (i + 32 < count ? 0u : (here >> 1) + 1u);
-                const bool pair = (here >> 1 & ~lasts & 0x55555555u) >> lane & 1u;
-                what = ((cur & Tile::kFirst) || i + lane == 0 ? kOpen : 0u) | ((closes >> (lane + (pair ? 1 : 0))) & 1u ? kClose : 0u) |
-                       (pair ? 0u : kSingle) | (lane == 0 ? kRefill : 0u) | (pair && (fulls >> lane & 3u) == 3u ? kFull : 0u) |
-                       (pair || lane & 1 ? 0u : kHold);
+                const uint32_t closes = lasts | (i + 32 < count ? 0u : 1u << (count - 1 - i));
+                constexpr uint32_t kEnds = N == 4 ? 0x88888888u : 0xaaaaaaaau;   // a stage's last tile
+                const int run = __ffs((closes | kEnds) >> lane);
+                const bool full = run == N && (~fulls >> lane & ((1u << N) - 1u)) == 0;
+                what = ((cur & Tile::kFirst) || i + lane == 0 ? kOpen : 0u) | (closes >> (lane + run - 1) & 1u ? kClose : 0u) |
+                       (lane == 0 ? kRefill : 0u) | (kEnds >> (lane + run - 1) & 1u ? 0u : kHold) | (full ? kFull : (uint32_t)run << 8);
                 turn = __shfl_sync(0xffffffffu, what, 0);
             }
             if (turn & kOpen) {       // before the wait: q arrives meanwhile
@@ -762,8 +764,13 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
                 st.start(a, Tile::row(t), Tile::head(t), lane);
             }
             if (!(turn & kFull)) {
-                const int v0 = (int)(__shfl_sync(0xffffffffu, cur, src) & 31), v1 = (int)(__shfl_sync(0xffffffffu, cur, (src + 1) & 31) & 31);
-                valid = !(turn & kSingle) ? v0 | v1 << 8 : i & 1 ? v0 << 8 : v0;
+                tiles = (int)(turn >> 8);
+                valid = 0;
+#pragma unroll
+                for (int p = 0; p < N; ++p) {
+                    const int t = (src & ~(N - 1)) + p, v = (int)(__shfl_sync(0xffffffffu, cur, t) & 31);
+                    if (t >= src && t < src + tiles) valid |= v << (8 * p);
+                }
             }
         }
         const uint32_t place = stage % R, bar = bars_at + 8 * place, parity = stage / R & 1u;
@@ -772,14 +779,14 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
             if (!ok) {   // no more copies; those in flight land first, and the result is void
                 if (lane == 0) kv4_error(a.err, KVC_DEVERR_WAIT_TIMEOUT);
 #pragma unroll 1
-                for (int k = i / 2; k < min(i / 2 + R, (count + 1) / 2); ++k) wait_long(bars_at + 8 * (k % R), (k / R) & 1);
+                for (int k = i / N; k < min(i / N + R, (count + N - 1) / N); ++k) wait_long(bars_at + 8 * (k % R), (k / R) & 1);
                 when = -1;
                 next.src = nullptr;
             }
         }
         opaque(valid);                // (one copy of the work, not one for each kind of turn: code is fetched once a launch)
-        if (valid) st.pages(ring_at + place * 2 * B::kBytes, valid, a.scale, lane);
-        i += turn & kSingle ? 1 : 2;
+        if (valid) st.pages(ring_at + place * S::kStage, valid, a.scale, lane);
+        i += tiles;
         if (turn & (kClose | kHold)) {
             if (turn & kClose) {
                 const uint32_t t = __shfl_sync(0xffffffffu, cur, (i - 1) & 31);
@@ -796,12 +803,12 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
                     if (lane == 0) infos[2 * warp + k] = {b, h, begins, ends};
                 }
             }
-            if (turn & kHold) continue;   // the stage's other tile is to come
+            if (turn & kHold) continue;   // more of the stage is to come
         }
         __syncwarp();
-        const int issue = (stage + R) & 15;
-        if (issue == 0) take_next((stage + R) * 2);
-        bulk_load_turn(ring_lane + place * 2 * B::kBytes, from, B::kBytes, expect, bar, policy, when, issue);
+        const int issue = (stage + R) & (32 / N - 1);
+        if (issue == 0) take_next((stage + R) * N);
+        bulk_load_turn(ring_lane + place * S::kStage, from, B::kBytes, expect, bar, policy, when, issue);
         ++stage;
     }
 
@@ -885,7 +892,7 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
             for (; c < end; c += 32) {
                 const int i = c + lane;
                 int off;
-                if (pass == 0) off = !((members >> (i & 31)) & 1u) || i > 31 ? -1 : i & 1 ? (i >> 1) * (S::kRing / 4) : M::kHeads / 4 + (i >> 1) * PF;
+                if (pass == 0) off = !((members >> (i & 31)) & 1u) || i > 31 ? -1 : i & 1 ? (i >> 1) * (M::kRing / 4) : M::kHeads / 4 + (i >> 1) * PF;
                 else off = pass == 1 ? ((spans[2 * k] + i) * 2 + (i == 0 ? 1 : 0)) * PF : M::kHeads / 4 + i * PF;
                 sum.merge(pass == 1 ? a.parts : reinterpret_cast<const float*>(smem), off, min(32, end - c), a.G, n, lane);
             }
@@ -952,16 +959,16 @@ struct LaunchAttention {
     cudaError_t operator()() const
     {
         using S = AttnShape<D, NG>;
+        using M = AttnSmem<D, NG>;
+        constexpr int kMost = M::bytes(kMaxGroup, kSmemRows);
+        static_assert(part_floats(kMaxGroup, D) * 4 <= M::kRing, "a part lies in its warp's ring");
+        static_assert(kMost <= 226 * 1024, "shared memory of a CTA, beside its static part");
         static OncePerDevice once;
-        const int smem = AttnSmem<D, NG>::bytes(a.G, a.batch);
-        constexpr int most = AttnSmem<D, NG>::bytes(kMaxGroup, kSmemRows);
-        static_assert(part_floats(kMaxGroup, D) * 4 <= S::kRing, "a part lies in its warp's ring");
-        static_assert(most <= 226 * 1024, "shared memory of a CTA");
+        if (cudaError_t e = once.set_attribute(attention_kernel<D, NG, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost); e != cudaSuccess)
+            return e;
         a.split = 0;
         while (a.G << (a.split + 1) <= S::kWarps) ++a.split;
-        cudaError_t e = once.set_attribute(attention_kernel<D, NG, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
-        if (e != cudaSuccess) return e;
-        return kv4_launch(attention_kernel<D, NG, T>, dim3((unsigned)sms), S::kWarps * 32, (size_t)smem, st, a);
+        return kv4_launch(attention_kernel<D, NG, T>, dim3((unsigned)sms), S::kWarps * 32, (size_t)M::bytes(a.G, a.batch), st, a);
     }
 };
 
