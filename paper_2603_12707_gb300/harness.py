@@ -1,4 +1,5 @@
-"""Drive a decode session of a workload through the C ABI.
+"""Drive a decode session of a workload through the C ABI: over the bf16 cache
+(``DecodeSession``) or over the 4-bit one (``Kv4Session``).
 
 Sets up a cache for a ``WorkloadConfig`` (pool sized for the prefix plus
 ``extra_tokens`` decode steps, page order and reservation order from the
@@ -11,6 +12,7 @@ from __future__ import annotations
 
 import numpy as np
 
+from . import kv4
 from . import kvdecode as kd
 from . import workloads as wl
 
@@ -86,3 +88,70 @@ class DecodeSession:
 
     def __exit__(self, *exc):
         self.close()
+
+
+class Kv4Session:
+    """The same session over a 4-bit cache: every step's block tables and slot
+    map are built on the device from the requests' lengths, new K and V are
+    quantised into their slots, and decode attention reads the 4-bit pages.
+    Nothing synchronises but ``check``."""
+
+    def __init__(self, cfg: wl.WorkloadConfig, extra_tokens: int = 8, group: int = 64, device="cuda", stream=None,
+                 lens=None, slack_pages: int = 8):
+        import torch
+        self.cfg = cfg
+        self.stream = stream
+        self.lens0 = np.array(wl.context_lengths(cfg) if lens is None else lens, dtype=np.int64)
+        self.lens = np.zeros_like(self.lens0)      # held so far: fill_prefix admits the requests
+        P = kv4.PAGE_SIZE
+        max_pages = int((int(self.lens0.max()) + extra_tokens + P - 1) // P)
+        num_pages = int(sum((int(n) + extra_tokens + P - 1) // P for n in self.lens0)) + slack_pages
+        self.pools = [kv4.Pool.empty(num_pages, cfg.num_kv_heads, cfg.head_dim, group, device=device)
+                      for _ in range(cfg.phys_layers)]
+        self.tables = kv4.Tables.empty(num_pages, cfg.batch, max(1, max_pages), device=device)
+        order = wl.page_order(cfg, num_pages)
+        if order is not None:
+            self.tables.free_ring.copy_(torch.from_numpy(order))
+        i32 = dict(dtype=torch.int32, device=device)
+        self.error = torch.zeros(1, **i32)
+        self.ones = torch.ones(cfg.batch, **i32)
+        self.step_slots = torch.empty(cfg.batch, dtype=torch.int64, device=device)
+        self.workspace = kv4.kv4_workspace(self.pools[0], cfg.num_q_heads)
+        self._torch, self._i32 = torch, i32
+
+    def grow(self, new_lens):
+        """Requests grow by new_lens tokens (host sequence), or give -n back; returns the new tokens' slots."""
+        new = self._torch.tensor([int(n) for n in new_lens], **self._i32)
+        slots = self._torch.empty(int(sum(max(0, int(n)) for n in new_lens)), dtype=self._torch.int64, device=new.device)
+        kv4.kv_tables_step(self.tables, None, new, slots, device_error=self.error, stream=self.stream)
+        self.lens += np.array(new_lens, dtype=np.int64)
+        return slots
+
+    def fill_prefix(self, layers=None):
+        """Admit every request and write its cached prefix into the given layer pools."""
+        cfg = self.cfg
+        slots = self.grow(self.lens0)
+        for l in range(cfg.phys_layers) if layers is None else layers:
+            k, v, _ = wl.packed_prefix(cfg, [l], self.lens0, slots.device)
+            kv4.kv4_write(self.pools[l], slots, k[0], v[0], device_error=self.error, stream=self.stream)
+
+    def begin_step(self):
+        kv4.kv_tables_step(self.tables, None, self.ones, self.step_slots, device_error=self.error, stream=self.stream)
+        self.lens += 1
+
+    def phys(self, layer: int) -> int:
+        return layer % self.cfg.phys_layers
+
+    def append(self, layer: int, k_new, v_new):
+        kv4.kv4_write(self.pools[self.phys(layer)], self.step_slots, k_new, v_new, device_error=self.error,
+                      stream=self.stream)
+
+    def attend(self, layer: int, q, out, scale: float = 0.0, lse=None):
+        kv4.kv4_decode_attention(self.pools[self.phys(layer)], self.tables, q, out, self.workspace, lse=lse,
+                                 softmax_scale=scale, device_error=self.error, stream=self.stream)
+
+    def check(self):
+        """Wait for the device and raise if a call has found something wrong."""
+        bits = int(self.error.item())
+        if bits:
+            raise RuntimeError(f"device error bits {bits:#x}")
