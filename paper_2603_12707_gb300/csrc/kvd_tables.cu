@@ -13,16 +13,16 @@
 // finds by binary search, so the map takes one launch.  What the call
 // updates (lengths, the ring's state, pages given back) is written by the last CTA that has
 // read it: a counter in the tables' state, zero between calls.
+//
+// A small call is latency, and much of that the fetching of its instructions
+// (every launch fetches them anew): loops stay rolled.  TODO figures
 #include "kvd_kv4.h"
 #include "kvd_ptx.cuh"
 
 namespace kvd {
 namespace {
 
-constexpr int kTablesThreads = 512;
-constexpr int kRowsPerThread = kKv4MaxBatch / kTablesThreads;
-constexpr int kThreadTokens = 4;   // consecutive tokens of a thread: 16-byte stores
-constexpr int kCtaTokens = kTablesThreads * kThreadTokens;
+constexpr int kMaxThreads = 1024;
 
 struct TablesArgs {
     int32_t* block_table;
@@ -32,6 +32,7 @@ struct TablesArgs {
     int32_t* arrivals;      // the state's counter
     int64_t num_pages;
     int32_t max_seqs, max_pages, batch, max_tokens;
+    int32_t cta_tokens;     // tokens of a CTA
     const int32_t* seq_ids;
     const int32_t* new_lens;
     int64_t* slots;
@@ -40,7 +41,6 @@ struct TablesArgs {
     int32_t* lens_out;
     int32_t* state_out;
     int32_t* err;
-    int32_t wide;           // slots and positions are 16-byte aligned
 };
 
 __device__ __forceinline__ int pages_of(int n) { return (n + kPageSize - 1) / kPageSize; }
@@ -56,36 +56,42 @@ struct Sums {
 __device__ __forceinline__ Sums operator+(const Sums& a, const Sums& b) { return {a.tokens + b.tokens, a.pages + b.pages}; }
 __device__ __forceinline__ Sums operator-(const Sums& a, const Sums& b) { return {a.tokens - b.tokens, a.pages - b.pages}; }
 
-__device__ __forceinline__ Sums scan_warp(Sums s, int lane)
+// Exclusive sums over the block's threads on top of `before`, which moves on by their total.
+__device__ __forceinline__ Sums block_scan(const Sums& mine, Sums* before, Sums* warp_sums)
 {
-#pragma unroll
-    for (int n = 1; n < 32; n <<= 1) {
-        const Sums o = {__shfl_up_sync(0xffffffffu, s.tokens, n), __shfl_up_sync(0xffffffffu, s.pages, n)};
-        if (lane >= n) s = s + o;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    Sums s = mine, ahead = {0, 0}, total = {0, 0};
+#pragma unroll 1
+    for (int level = 0; level < 2; ++level) {   // over the lanes, over the warps
+#pragma unroll 1
+        for (int n = 1; n < 32; n <<= 1) {
+            const Sums o = {__shfl_up_sync(0xffffffffu, s.tokens, n), __shfl_up_sync(0xffffffffu, s.pages, n)};
+            if (lane >= n) s = s + o;
+        }
+        if (level == 0) {
+            ahead = s - mine;
+            if (lane == 31) warp_sums[warp] = s;
+            __syncthreads();
+            s = lane < warps ? warp_sums[lane] : Sums{0, 0};
+        }
     }
-    return s;
+    const int from = max(warp - 1, 0);
+    const Sums w = {__shfl_sync(0xffffffffu, s.tokens, from), __shfl_sync(0xffffffffu, s.pages, from)};
+    total = {__shfl_sync(0xffffffffu, s.tokens, 31), __shfl_sync(0xffffffffu, s.pages, 31)};
+    const Sums start = *before;
+    *before = start + total;
+    return start + ahead + (warp ? w : Sums{0, 0});
 }
 
-// Exclusive sums over the block's threads, and the total.
-__device__ __forceinline__ Sums block_scan(const Sums& mine, Sums* total, Sums* warp_sums)
+// Row of entry x: the last row from `lo` on whose first entry is at or before
+// it (not empty, where x is below the sum); first[lo] <= x.
+__device__ __forceinline__ int find_row(const int32_t* first, int lo, int batch, int x)
 {
-    constexpr int W = kTablesThreads / 32;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const Sums s = scan_warp(mine, lane);
-    if (lane == 31) warp_sums[warp] = s;
-    __syncthreads();
-    const Sums w = scan_warp(lane < W ? warp_sums[lane] : Sums{0, 0}, lane);
-    const int from = warp > 0 ? warp - 1 : 0;
-    Sums before = {__shfl_sync(0xffffffffu, w.tokens, from), __shfl_sync(0xffffffffu, w.pages, from)};
-    if (warp == 0) before = {0, 0};
-    *total = {__shfl_sync(0xffffffffu, w.tokens, W - 1), __shfl_sync(0xffffffffu, w.pages, W - 1)};
-    return before + s - mine;
-}
-
-// Row of entry x: the last row whose first entry is at or before it (not empty, where x is below the sum).
-__device__ __forceinline__ int find_row(const int32_t* first, int batch, int x)
-{
-    int lo = 0, hi = batch;
+    int step = 1;
+#pragma unroll 1
+    for (; lo + step < batch && first[lo + step] <= x; step *= 2) lo += step;
+    int hi = min(lo + step, batch);
+#pragma unroll 1
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (first[mid] <= x) lo = mid;
@@ -94,7 +100,7 @@ __device__ __forceinline__ int find_row(const int32_t* first, int batch, int x)
     return lo;
 }
 
-__global__ void __launch_bounds__(kTablesThreads) tables_kernel(TablesArgs a)
+__global__ void __launch_bounds__(kMaxThreads) tables_kernel(TablesArgs a)
 {
     extern __shared__ int32_t rows[];            // per row:
     int32_t* const row_tok = rows;               // first token (at most max_tokens)
@@ -102,151 +108,107 @@ __global__ void __launch_bounds__(kTablesThreads) tables_kernel(TablesArgs a)
     int32_t* const row_len = row_page + a.batch; // tokens before
     int32_t* const row_seq = row_len + a.batch;
     int32_t* const row_back = row_seq + a.batch; // first of the pages given back
-    __shared__ Sums warp_sums[kTablesThreads / 32];
+    __shared__ Sums warp_sums[kMaxThreads / 32];
     __shared__ uint32_t taken;
     __shared__ int is_last;
-    griddep_wait();
-    griddep_launch_dependents();
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, threads = blockDim.x;
     const bool speaks = blockIdx.x == 0;         // one CTA reports what all find
     if (tid == 0) taken = 0;
+    griddep_wait();
+    griddep_launch_dependents();
 
     int64_t head = a.state[0], count = a.state[1];
+    // Rows, a block's threads at a time; the next ones are loaded meanwhile.
+    const int64_t most = (int64_t)a.max_pages * kPageSize;
+    Sums total{0, 0};
+    int32_t errors = 0;
+    auto row_seq_of = [&](int r) { return r >= a.batch ? -1 : a.seq_ids ? a.seq_ids[r] : r; };
+    auto row_len_of = [&](int seq) { return seq >= 0 && seq < a.max_seqs ? a.lens[seq] : -1; };
+    int seq = row_seq_of(tid), add = tid < a.batch ? a.new_lens[tid] : 0, ctx = row_len_of(seq);
     if (head < 0 || head >= a.num_pages || count < 0 || count > a.num_pages) {
-        if (tid == 0 && speaks) kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
+        errors = KVC_DEVERR_PAGE_RANGE;
         head = count = 0;
     }
-
-    // The rows of this thread, consecutive ones.
-    const int per = (a.batch + kTablesThreads - 1) / kTablesThreads;
-    const int64_t most = (int64_t)a.max_pages * kPageSize;
-    int seq[kRowsPerThread], ctx[kRowsPerThread], add[kRowsPerThread];
-    Sums of[kRowsPerThread], mine{0, 0};
-#pragma unroll
-    for (int k = 0; k < kRowsPerThread; ++k) {
-        const int r = tid * per + k;
-        seq[k] = -1;
-        add[k] = 0;
-        if (k < per && r < a.batch) {
-            seq[k] = a.seq_ids ? a.seq_ids[r] : r;
-            add[k] = a.new_lens[r];
+#pragma unroll 1
+    for (int r0 = 0; r0 < a.batch; r0 += threads) {
+        const int r = r0 + tid, next = r + threads;
+        const int next_seq = row_seq_of(next), next_add = next < a.batch ? a.new_lens[next] : 0;
+        const int64_t end = (int64_t)ctx + add;
+        const bool fine = ctx >= 0 && ctx <= most && end >= 0 && end <= most;
+        const int d = fine ? pages_of((int)end) - pages_of(ctx) : 0;
+        const Sums mine = {max(add, 0), (uint64_t)max(d, 0) << 32 | (uint32_t)max(-d, 0)};
+        const Sums at = block_scan(mine, &total, warp_sums);
+        if (r < a.batch) {
+            const bool room = at.tokens + mine.tokens <= a.max_tokens || mine.tokens == 0;
+            const bool paid = mine.take() == 0 || (int64_t)at.take() + mine.take() <= count;
+            const bool ok = fine && room && paid;
+            if (!fine || !room) errors |= KVC_DEVERR_SEQ_RANGE;
+            else if (!paid) errors |= KVC_DEVERR_OOM;
+            row_tok[r] = (int32_t)min(at.tokens, (int64_t)a.max_tokens);
+            row_page[r] = ok ? (int32_t)at.take() : -1;
+            row_len[r] = ctx;
+            row_seq[r] = seq;
+            row_back[r] = (int32_t)at.back();
+            if (ok && mine.take()) atomicMax(&taken, at.take() + mine.take());
+            if (speaks && a.cu) a.cu[r] = (int32_t)min(at.tokens, (int64_t)INT32_MAX);
         }
+        seq = next_seq;
+        add = next_add;
+        ctx = row_len_of(seq);
+        __syncthreads();
     }
-#pragma unroll
-    for (int k = 0; k < kRowsPerThread; ++k) ctx[k] = seq[k] >= 0 && seq[k] < a.max_seqs ? a.lens[seq[k]] : -1;
-#pragma unroll
-    for (int k = 0; k < kRowsPerThread; ++k) {
-        const int64_t end = (int64_t)ctx[k] + add[k];
-        const bool fine = ctx[k] >= 0 && ctx[k] <= most && end >= 0 && end <= most;
-        const int d = fine ? pages_of((int)end) - pages_of(ctx[k]) : 0;
-        of[k] = {max(add[k], 0), (uint64_t)max(d, 0) << 32 | (uint32_t)max(-d, 0)};
-        if (!fine) ctx[k] = -1;
-        mine = mine + of[k];
-    }
-    Sums total;
-    Sums at = block_scan(mine, &total, warp_sums);
     const bool fits = count + total.back() <= a.num_pages;   // else a page has been given back twice
-    if (!fits && tid == 0 && speaks) kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
-
-    int32_t errors = 0;
-#pragma unroll
-    for (int k = 0; k < kRowsPerThread; ++k) {
-        const int r = tid * per + k;
-        if (k >= per || r >= a.batch) continue;
-        const bool room = at.tokens + of[k].tokens <= a.max_tokens || of[k].tokens == 0;
-        const bool paid = of[k].take() == 0 || (int64_t)at.take() + of[k].take() <= count;
-        const bool ok = ctx[k] >= 0 && room && paid && (fits || add[k] >= 0);
-        if (ctx[k] < 0 || !room) errors |= KVC_DEVERR_SEQ_RANGE;
-        else if (!paid) errors |= KVC_DEVERR_OOM;
-        row_tok[r] = (int32_t)min(at.tokens, (int64_t)a.max_tokens);
-        row_page[r] = ok ? (int32_t)at.take() : -1;
-        row_len[r] = ctx[k];
-        row_seq[r] = seq[k];
-        row_back[r] = (int32_t)at.back();
-        if (ok && of[k].take()) atomicMax(&taken, at.take() + of[k].take());
-        at = at + of[k];
-    }
+    if (!fits) errors |= KVC_DEVERR_PAGE_RANGE;
     if (errors && speaks) kv4_error(a.err, errors);
-    __syncthreads();
     // Every thread of this CTA has read the state and the lengths.
     if (tid == 0) is_last = gridDim.x == 1 || atomicAdd(a.arrivals, 1) == (int)gridDim.x - 1;
 
-    // Tokens.
+    // This CTA's tokens.
     const int live = (int)min(total.tokens, (int64_t)a.max_tokens);
-    for (int64_t t0 = ((int64_t)blockIdx.x * kTablesThreads + tid) * kThreadTokens; t0 < a.max_tokens;
-         t0 += (int64_t)gridDim.x * kCtaTokens) {
-        int64_t slot[kThreadTokens];
-        int pos[kThreadTokens];
-        int r = -1, stop = 0, col_now = -1;      // the row in work, its end, the page in hand
-        int32_t page = -1;
-#pragma unroll
-        for (int k = 0; k < kThreadTokens; ++k) {
-            const int t = (int)t0 + k;
-            slot[k] = -1;
-            pos[k] = -1;
-            if (t >= live) continue;
-            if (t >= stop) {
-                r = r < 0 ? find_row(row_tok, a.batch, t) : r + 1;
-                while (r + 1 < a.batch && row_tok[r + 1] <= t) ++r;
-                stop = r + 1 < a.batch ? row_tok[r + 1] : live;
-                col_now = -1;
+    const int64_t first = (int64_t)blockIdx.x * a.cta_tokens, stop = min(first + a.cta_tokens, (int64_t)a.max_tokens);
+    int r = 0;
+#pragma unroll 1
+    for (int64_t t = first + tid; t < stop; t += threads) {
+        int64_t slot = -1;
+        int pos = -1;
+        if (t < live) {
+            r = find_row(row_tok, r, a.batch, (int)t);
+            if (row_page[r] >= 0) {
+                const int len = row_len[r];
+                pos = len + ((int)t - row_tok[r]);
+                const int col = pos / kPageSize, fresh = col - pages_of(len);
+                int32_t* const entry = a.block_table + (int64_t)row_seq[r] * a.max_pages + col;
+                int64_t from = head + row_page[r] + fresh;
+                if (from >= a.num_pages) from -= a.num_pages;
+                const int32_t page = fresh >= 0 ? a.ring[from] : *entry;
+                if (fresh >= 0 && pos % kPageSize == 0) *entry = page;   // the token that opens the page
+                if (page >= 0 && page < a.num_pages) slot = (int64_t)page * kPageSize + pos % kPageSize;
+                else kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
             }
-            if (row_page[r] < 0) continue;
-            pos[k] = row_len[r] + (t - row_tok[r]);
-            const int col = pos[k] / kPageSize, fresh = col - pages_of(row_len[r]);
-            if (col != col_now) {
-                int32_t* entry = a.block_table + (int64_t)row_seq[r] * a.max_pages + col;
-                if (fresh >= 0) {
-                    int64_t from = head + row_page[r] + fresh;
-                    if (from >= a.num_pages) from -= a.num_pages;
-                    page = a.ring[from];
-                    if (pos[k] % kPageSize == 0) *entry = page;   // the token that opens the page
-                } else {
-                    page = *entry;
-                }
-                col_now = col;
-                if (page < 0 || page >= a.num_pages) {
-                    kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
-                    page = -1;
-                }
-            }
-            if (page >= 0) slot[k] = (int64_t)page * kPageSize + pos[k] % kPageSize;
         }
-        if (a.wide && t0 + kThreadTokens <= a.max_tokens) {
-            longlong2* to = reinterpret_cast<longlong2*>(a.slots + t0);
-            to[0] = make_longlong2(slot[0], slot[1]);
-            to[1] = make_longlong2(slot[2], slot[3]);
-            if (a.positions) *reinterpret_cast<int4*>(a.positions + t0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
-        } else {
-#pragma unroll
-            for (int k = 0; k < kThreadTokens; ++k)
-                if (t0 + k < a.max_tokens) {
-                    a.slots[t0 + k] = slot[k];
-                    if (a.positions) a.positions[t0 + k] = pos[k];
-                }
-        }
+        a.slots[t] = slot;
+        if (a.positions) a.positions[t] = pos;
     }
     __syncthreads();
     if (!is_last) return;
 
     // What the call updates, by the CTA that came last to reading it.
     if (a.lens_out != a.lens) {
-        for (int i = tid; i < a.max_seqs; i += kTablesThreads) a.lens_out[i] = a.lens[i];
+#pragma unroll 1
+        for (int i = tid; i < a.max_seqs; i += threads) a.lens_out[i] = a.lens[i];
         __syncthreads();
     }
-    at = at - mine;
-#pragma unroll
-    for (int k = 0; k < kRowsPerThread; ++k) {
-        const int r = tid * per + k;
-        if (k >= per || r >= a.batch) continue;
-        if (a.cu) a.cu[r] = (int32_t)min(at.tokens, (int64_t)INT32_MAX);
-        if (row_page[r] >= 0) a.lens_out[seq[k]] = ctx[k] + add[k];
-        at = at + of[k];
+#pragma unroll 1
+    for (int i = tid; i < a.batch; i += threads) {
+        const int n = a.new_lens[i];
+        if (row_page[i] >= 0 && (fits || n >= 0)) a.lens_out[row_seq[i]] = row_len[i] + n;
     }
     // The k-th page given back: from its row's first page that is not needed any more.
     const int back = fits ? (int)total.back() : 0;
-    for (int k = tid; k < back; k += kTablesThreads) {
-        const int r = find_row(row_back, a.batch, k);
+    r = 0;
+#pragma unroll 1
+    for (int k = tid; k < back; k += threads) {
+        r = find_row(row_back, r, a.batch, k);
         const int kept = pages_of(row_len[r] + a.new_lens[r]);
         const int32_t page = a.block_table[(int64_t)row_seq[r] * a.max_pages + kept + (k - row_back[r])];
         int64_t to = head + count + k;
@@ -302,14 +264,17 @@ extern "C" KVC_API int kv_tables_step(const kv_tables* tables, int32_t batch, co
     a.lens_out = lens_out ? lens_out : tables->lens;
     a.state_out = free_state_out ? free_state_out : tables->free_state;
     a.err = device_error;
-    a.wide = kv4_aligned(slots, 16) && kv4_aligned(positions, 16);
     static OncePerDevice once;
     constexpr int kRowBytes = 5 * (int)sizeof(int32_t);
     if (cudaError_t e = once.set_attribute(tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowBytes * kKv4MaxBatch);
         e != cudaSuccess)
         return kv4_launch_result(e);
-    // A CTA for every kCtaTokens tokens, up to one per SM (every one reads all rows).
-    const int64_t ctas = ((int64_t)max_tokens + kCtaTokens - 1) / kCtaTokens;
-    return kv4_launch_result(kv4_launch(tables_kernel, dim3((unsigned)(ctas < 1 ? 1 : ctas < 152 ? ctas : 152)), kTablesThreads,
-                                        (size_t)kRowBytes * batch, static_cast<cudaStream_t>(stream), a));
+    // Few rows: small blocks, whose scans and barriers are shorter.  A CTA for
+    // every two tokens of each thread, up to one per SM (every one reads all rows).
+    const int threads = batch <= 256 ? 256 : kMaxThreads;
+    int64_t ctas = ((int64_t)max_tokens + 2 * threads - 1) / (2 * threads);
+    ctas = ctas < 1 ? 1 : ctas < 152 ? ctas : 152;
+    a.cta_tokens = (int32_t)(((int64_t)max_tokens + ctas - 1) / ctas);
+    return kv4_launch_result(kv4_launch(tables_kernel, dim3((unsigned)ctas), threads, (size_t)kRowBytes * batch,
+                                        static_cast<cudaStream_t>(stream), a));
 }

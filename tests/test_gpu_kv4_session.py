@@ -76,7 +76,7 @@ def test_drafts_are_taken_back_and_requests_closed(kvlib):
 def test_a_full_pool_is_reported(kvlib):
     from paper_2603_12707_gb300.harness import Kv4Session
     cfg = wl.custom("kv4_full", 1, 8, 8, 64, 2, lens=[16, 16], seed=3)
-    sess = Kv4Session(cfg, extra_tokens=16, group=64, slack_pages=0)
+    sess = Kv4Session(cfg, extra_tokens=32, group=64, slack_pages=0)
     sess.fill_prefix()
     sess.grow([16, 16])
     sess.check()
