@@ -135,9 +135,8 @@ KVC_API int kv4_read(const kv4_pool *pool, int32_t n, const int64_t *slots, void
                      void *v_out, int64_t v_stride, int32_t *device_error, void *stream);
 
 /* Bytes of kv4_decode_attention's workspace on the current device, or a
- * negative KVC_ERR_*: the same for every batch and length.  A workspace is zero-filled
- * before its first use (each call leaves its counters at zero) and serves
- * calls that are ordered on one stream. */
+ * negative KVC_ERR_*: the same for every batch and length.  What it holds
+ * between calls does not matter; it serves calls that are ordered on one stream. */
 KVC_API int64_t kv4_workspace_bytes(const kv4_pool *pool, int32_t num_q_heads);
 
 /* Decode attention of `batch` rows (<= 4096) over all lens[i] tokens of each

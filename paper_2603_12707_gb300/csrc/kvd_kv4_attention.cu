@@ -28,9 +28,7 @@
 //
 // A (row, KV head) that lies in one warp's share is written by that warp.
 // Others leave (o, m, l) per warp in shared memory, where the CTA merges what
-// it holds; what crosses CTAs goes through the workspace and the last CTA to
-// arrive (a counter per first CTA, which it sets back to zero) merges the parts in
-// the order of the list.
+// it holds; what crosses CTAs goes through the workspace to a second launch.
 #include <cmath>
 #include <type_traits>
 
@@ -49,13 +47,19 @@ constexpr uint32_t kMinShare = 2;
 // Warps of a CTA that work at least, where there is enough for them: one per scheduler.
 constexpr uint32_t kMinWarps = 4;
 
+// A (row, KV head) that begins in a CTA and goes on in others (b < 0: there is none).
+struct PartSpan {
+    int32_t b, h, last;   // the last CTA that holds a part of it
+    int32_t unused;
+};
+
 struct AttnArgs {
     const uint8_t* pool;
     int64_t num_pages;
     int32_t H, Hq, G;
     uint32_t H_inv;      // 2^32 / H, rounded down (2^32 - 1 for 1)
     uint32_t G_inv;      // 2^16 / G, rounded up
-    int32_t split;       // logarithm of the warps that may share a row's parts
+    int32_t merge_shift; // logarithm of the warps that share a row in the merge
     const int32_t* block_table;
     const int32_t* lens;
     int32_t max_seqs, max_pages, batch;
@@ -65,7 +69,7 @@ struct AttnArgs {
     int64_t q_stride, out_stride;
     float* lse;
     float scale;         // softmax scale * log2(e) * 2^24 (the accumulators' unit)
-    int32_t* counters;   // [grid]: CTAs that have left their part of the row that starts in CTA i; zero between calls
+    PartSpan* spans;     // [grid]: what goes on after a CTA
     uint32_t* sums;      // [2][batch + 1] where shared memory does not hold them: the same from every CTA
     float* parts;        // [grid][2][G][D + 2]: a CTA's part of the row that began before it, and of the one that goes on
     int32_t* err;
@@ -81,14 +85,6 @@ struct AttnShape {
     static constexpr int kTiles = D == 64 ? 4 : 2;
     static constexpr int kStage = kTiles * Kv4Block<D, NG>::kBytes;
 };
-
-// Everything the CTA wrote before (a barrier before this call) is visible to who adds after it.
-__device__ __forceinline__ int atomic_add_acq_rel(int32_t* p, int32_t v)
-{
-    int32_t old;
-    asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], %2;" : "=r"(old) : "l"(p), "r"(v) : "memory");
-    return old;
-}
 
 // A value that the compiler knows nothing of.
 __device__ __forceinline__ void opaque(int& x) { asm volatile("" : "+r"(x)); }
@@ -474,7 +470,7 @@ struct State {
     }
 };
 
-// One query row of a part: o elements lane * E .. of this lane, m and l.
+// One query row of merged parts: o elements lane * E .. of this lane, m and l.
 template <int D>
 struct RowSum {
     static constexpr int E = D / 32;
@@ -485,14 +481,15 @@ struct RowSum {
         for (int i = 0; i < E; ++i) o[i] = 0.f;
     }
     // Adds row n of the first `count` lanes' parts, in the lanes' order: `at` is a
-    // part's offset in floats from `base`, -1 for none (not the first lane's).  A lane loads its part's (m, l), all
-    // lanes the rows, four in flight, the first ones before the weights are known.
-    // The loads pass L1 by: parts may come from other SMs.
+    // part's offset in floats from `base` (shared memory, or global memory, whose L1 is
+    // passed by), -1 for none (not the first lane's).  A lane loads its part's (m, l),
+    // all lanes the rows, U in flight, the first ones before the weights are known.
+    template <int U, bool kGlobal>
     __device__ __forceinline__ void merge(const float* base, int at, int count, int G, int n, int lane)
     {
         const bool mine = lane < count && at >= 0;
         const int other = __shfl_sync(0xffffffffu, at, 0), from = mine ? at : other;   // something to load where there is nothing to add
-        float mc = load_cg(base + from + G * D + n), lc = load_cg(base + from + G * (D + 1) + n);
+        float mc = load<kGlobal>(base + from + G * D + n), lc = load<kGlobal>(base + from + G * (D + 1) + n);
         if (!mine) {
             mc = -INFINITY;
             lc = 0.f;
@@ -500,14 +497,13 @@ struct RowSum {
         const uint32_t some = __ballot_sync(0xffffffffu, mine);
         float w = 0.f;
 #pragma unroll 1
-        for (int c = 0; c < count; c += 4) {
-            float x[4][E];
+        for (int c = 0; c < count; c += U) {
+            float x[U][E];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) load_cg(base + __shfl_sync(0xffffffffu, from, (c + u) & 31) + n * D + lane * E, x[u]);
+            for (int u = 0; u < U; ++u) load<kGlobal>(base + __shfl_sync(0xffffffffu, from, (c + u) & 31) + n * D + lane * E, x[u]);
             if (c == 0) {
                 const float top = fmaxf(m, warp_max(mc)), al = m == top ? 1.f : ex2(m - top);
-                w = mc == top && mine ? 1.f : ex2(mc - top);
-                if (!mine) w = 0.f;
+                w = !mine ? 0.f : mc == top ? 1.f : ex2(mc - top);
                 lc *= w;
                 m = top;
                 l *= al;
@@ -515,7 +511,7 @@ struct RowSum {
                 for (int i = 0; i < E; ++i) o[i] *= al;
             }
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
+            for (int u = 0; u < U; ++u) {
                 const bool on = c + u < 32 && ((some >> (c + u)) & 1u);
                 const float wu = __shfl_sync(0xffffffffu, w, (c + u) & 31), lu = __shfl_sync(0xffffffffu, lc, (c + u) & 31);
                 l += on ? lu : 0.f;
@@ -539,18 +535,22 @@ struct RowSum {
             part[G * (D + 1) + n] = l;
         }
     }
-    static __device__ __forceinline__ float load_cg(const float* p)   // shared or global memory
+    template <bool kGlobal>
+    static __device__ __forceinline__ float load(const float* p)
     {
-        float x;
-        asm volatile("ld.cg.f32 %0, [%1];" : "=f"(x) : "l"(p) : "memory");
-        return x;
+        if constexpr (kGlobal) return __ldcg(p);
+        return *p;
     }
-    static __device__ __forceinline__ void load_cg(const float* p, float (&x)[E])
+    template <bool kGlobal>
+    static __device__ __forceinline__ void load(const float* p, float (&x)[E])
     {
-        if constexpr (E == 4)
-            asm volatile("ld.cg.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]) : "l"(p) : "memory");
-        else
-            asm volatile("ld.cg.v2.f32 {%0, %1}, [%2];" : "=f"(x[0]), "=f"(x[1]) : "l"(p) : "memory");
+        if constexpr (E == 4) {
+            const float4 v = kGlobal ? __ldcg(reinterpret_cast<const float4*>(p)) : *reinterpret_cast<const float4*>(p);
+            x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+        } else {
+            const float2 v = kGlobal ? __ldcg(reinterpret_cast<const float2*>(p)) : *reinterpret_cast<const float2*>(p);
+            x[0] = v.x, x[1] = v.y;
+        }
     }
     template <class T>
     __device__ __forceinline__ void write_out(const AttnArgs& a, int b, int h, int n, int lane) const
@@ -563,8 +563,89 @@ struct RowSum {
     }
 };
 
+// x / H for a multiple x of H.
+__device__ __forceinline__ uint32_t multiple_over(uint32_t x, uint32_t H, uint32_t H_inv)
+{
+    const uint32_t q = __umulhi(x, H_inv);
+    return q + (x - q * H >= H);
+}
+
+// The warps' shares: the first `extra` of them have base + 1 places, the others base; the warps of a CTA that have one.
+struct Shares {
+    uint32_t base, extra, cta_warps;
+};
+
+// What is left when the CTA's warps have worked their shares: rows without
+// tokens, the merges of what lies in this CTA, the span of what goes on after it.  (Out of line: the
+// registers that this takes are not the main loop's.)
 template <int D, int NG, class T>
-__global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_kernel(AttnArgs a)
+__device__ __noinline__ void finish_cta(const AttnArgs& a, uint8_t* smem, const Shares sh, bool all_held)
+{
+    using S = AttnShape<D, NG>;
+    using M = AttnSmem<D, NG>;
+    constexpr int W = S::kWarps;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t H = a.H;
+    const PartInfo* infos = reinterpret_cast<const PartInfo*>(smem + M::kInfo);
+    const uint32_t* pages = a.batch <= kSmemRows ? reinterpret_cast<const uint32_t*>(smem + M::pages(a.G)) : a.sums;
+    const uint32_t* costs = pages + a.batch + 1;
+    // Rows without tokens.
+    if (!all_held)
+#pragma unroll 1
+        for (int r = blockIdx.x; r < a.batch; r += gridDim.x)
+            if (pages[r] == pages[r + 1]) {
+#pragma unroll 1
+                for (int i = tid; i < a.Hq * (D / 8); i += W * 32)
+                    *reinterpret_cast<uint4*>(a.out + r * a.out_stride + i * 8) = make_uint4(0u, 0u, 0u, 0u);
+                if (a.lse)
+#pragma unroll 1
+                    for (int i = tid; i < a.Hq; i += W * 32) a.lse[(int64_t)r * a.Hq + i] = -INFINITY;
+            }
+    __syncthreads();
+
+    // This CTA's parts, in the order of the list, one in each lane: a group of
+    // them belongs to one (row, KV head).
+    const int PF = part_floats(a.G, D);
+    const PartInfo mine = lane < 2 * W ? infos[lane] : PartInfo{-1, 0, 0, 0};
+    const uint32_t valid = __ballot_sync(0xffffffffu, mine.b >= 0);
+    const uint32_t begin = __ballot_sync(0xffffffffu, mine.b >= 0 && mine.begins);
+    const uint32_t ending = __ballot_sync(0xffffffffu, mine.b >= 0 && mine.ends);
+    const uint32_t groups = begin | (valid & (0u - valid));
+    if (warp == W - 1 && lane == 0) {
+        PartSpan span{-1, 0, 0, 0};
+        const int last = 31 - __clz(groups);   // (the last group begins here, or it is the only one)
+        if (begin && !(ending >> last) && ((begin >> last) & 1u)) {
+            // It goes on: the CTA whose share holds its last page.
+            const PartInfo in = infos[last];
+            const uint32_t n = multiple_over(pages[in.b + 1] - pages[in.b], H, a.H_inv);
+            const uint32_t place = costs[in.b] + (in.h + 1) * (n + kRowCost) - 1, long_ones = sh.extra * (sh.base + 1);
+            const bool in_long = place < long_ones;
+            const uint32_t w = (in_long ? place : place - long_ones) / (in_long ? sh.base + 1 : sh.base) + (in_long ? 0 : sh.extra);
+            span = {in.b, in.h, (int)(w / sh.cta_warps), 0};
+        }
+        a.spans[blockIdx.x] = span;
+    }
+    const int jobs = __popc(groups) * a.G;
+#pragma unroll 1
+    for (int job = warp; job < jobs; job += W) {
+        uint32_t rest = groups;
+        const int group = (int)(job * a.G_inv >> 16), n = job - group * a.G;   // job / G
+#pragma unroll 1
+        for (int u = group; u > 0; --u) rest &= rest - 1u;
+        const int e = __ffs(rest) - 1, i = e + lane;
+        rest &= rest - 1u;
+        const uint32_t members = valid & (0xffffffffu << e) & (rest ? (rest & (0u - rest)) - 1u : 0xffffffffu);
+        const PartInfo row = infos[e];
+        RowSum<D> sum;
+        const int off = i > 31 || !((members >> i) & 1u) ? -1 : i & 1 ? (i >> 1) * (M::kRing / 4) : M::kHeads / 4 + (i >> 1) * PF;
+        sum.template merge<4, false>(reinterpret_cast<const float*>(smem), off, 32 - __clz(members) - e, a.G, n, lane);
+        if (row.begins && (ending & members)) sum.template write_out<T>(a, row.b, row.h, n, lane);
+        else sum.write_part(a.parts + ((int64_t)blockIdx.x * 2 + row.begins) * PF, a.G, n, lane);
+    }
+}
+
+template <int D, int NG, class T>
+__global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_kernel(const __grid_constant__ AttnArgs a)
 {
     using S = AttnShape<D, NG>;
     using B = Kv4Block<D, NG>;
@@ -572,8 +653,6 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
     constexpr int W = S::kWarps, N = S::kTiles, R = S::kStages;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ uint2 warp_pages[W];
-    __shared__ int arrived[2];
-    __shared__ int spans[4];   // first and last CTA of what began before this CTA, and of what goes on after it
     static_assert(2 * W <= 32, "a lane for each part");
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint8_t* ring = smem + warp * M::kRing;
@@ -635,6 +714,7 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
     }
     __syncthreads();
     if (all_pages * a.H > 0x7fffffffull) {   // the same in all threads
+        if (tid == 0) a.spans[blockIdx.x] = {-1, 0, 0, 0};
         if (blockIdx.x == 0 && tid == 0) kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
         return;
     }
@@ -660,10 +740,7 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
         }
         return r0;
     };
-    auto over_H = [&](uint32_t x) {      // x / H for a multiple of H
-        uint32_t q = __umulhi(x, a.H_inv);
-        return q + (x - q * H >= H);
-    };
+    auto over_H = [&](uint32_t x) { return multiple_over(x, H, a.H_inv); };
     auto head_of = [&](uint32_t x, uint32_t n) {   // x / n, below 1024
         int q = (int)__fdividef((float)x, (float)n);
         q -= q * (int64_t)n > x;
@@ -812,121 +889,43 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
         ++stage;
     }
 
-    // Rows without tokens.
-    if ((int)held != a.batch)
-#pragma unroll 1
-        for (int r = blockIdx.x; r < a.batch; r += gridDim.x)
-            if (pages[r] == pages[r + 1]) {
-#pragma unroll 1
-                for (int i = tid; i < a.Hq * (D / 8); i += W * 32)
-                    *reinterpret_cast<uint4*>(a.out + r * a.out_stride + i * 8) = make_uint4(0u, 0u, 0u, 0u);
-                if (a.lse)
-#pragma unroll 1
-                    for (int i = tid; i < a.Hq; i += W * 32) a.lse[(int64_t)r * a.Hq + i] = -INFINITY;
-            }
-    __syncthreads();
+    finish_cta<D, NG, T>(a, smem, Shares{base, extra, cta_warps}, (int)held == a.batch);
+}
 
-    // This CTA's parts, in the order of the list, one in each lane: a group of
-    // them belongs to one (row, KV head).
-    const int PF = part_floats(a.G, D);
-    const PartInfo mine = lane < 2 * W ? infos[lane] : PartInfo{-1, 0, 0, 0};
-    const uint32_t valid = __ballot_sync(0xffffffffu, mine.b >= 0);
-    if (!valid) return;
-    const uint32_t begin = __ballot_sync(0xffffffffu, mine.b >= 0 && mine.begins);
-    const uint32_t ending = __ballot_sync(0xffffffffu, mine.b >= 0 && mine.ends);
-    const uint32_t groups = begin | (valid & (0u - valid));
-    // The parts of the first group may have begun before this CTA, those of the last one may go on after it.
-    const int first = __ffs(groups) - 1, last = 31 - __clz(groups);
-    const bool from_before = !((begin >> first) & 1u);
-    const bool goes_on = !(ending >> last) && !(last == first && from_before);
-    const bool crosses = from_before || goes_on;
-    if (warp == W - 1 && lane < 4 && (lane >> 1 ? goes_on : from_before)) {
-        // The CTAs that hold the first and the last page of it (while the others merge).
-        const PartInfo in = infos[lane >> 1 ? last : first];
-        const uint32_t n = over_H(pages[in.b + 1] - pages[in.b]), p = lane & 1 ? n - 1 : 0;
-        const uint32_t place = costs[in.b] + in.h * (n + kRowCost) + kRowCost + p, long_ones = extra * (base + 1);
-        const bool in_long = place < long_ones;
-        const uint32_t w = (in_long ? place : place - long_ones) / (in_long ? base + 1 : base) + (in_long ? 0 : extra);
-        spans[lane] = (int)(w / cta_warps);
-    }
-    // Pass 0 merges the groups in shared memory, pass 1 (k = 0, 1) the parts of all CTAs of what
-    // crosses them, by the last CTA to arrive; where those are many, several warps share a row's
-    // and pass 2 merges their sums.
-    const int jobs0 = __popc(groups) * a.G;
+// What crosses CTAs: CTA c merges the parts of the (row, KV head) that goes on
+// after CTA c of the launch before this one, several warps a row of it where there are many.
+constexpr int kMergeWarps = 32, kMergeFew = 8;
+template <int D, class T>
+__global__ void __launch_bounds__(kMergeWarps * 32) merge_kernel(const __grid_constant__ AttnArgs a)
+{
+    __shared__ float sums[kMergeWarps * part_floats(1, D)];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    griddep_wait();
+    griddep_launch_dependents();
+    const PartSpan span = a.spans[blockIdx.x];
+    if (span.b < 0) return;
+    const int parts = span.last - (int)blockIdx.x + 1, PF = part_floats(a.G, D);
+    const int shift = parts > kMergeFew ? a.merge_shift : 0;   // 2^shift warps a row
+    const int n = warp >> shift, share = warp - (n << shift), each = (parts + (1 << shift) - 1) >> shift;
+    RowSum<D> sum;
+    if (n < a.G) {
 #pragma unroll 1
-    for (int pass = 0, k = 0;; ) {
-        opaque(pass);
-        const int parts = pass ? spans[2 * k + 1] - spans[2 * k] + 1 : 0;
-        const int split = parts > 16 ? a.split : 0, each = (parts + (1 << split) - 1) >> split;   // (logarithm)
-        const int jobs = pass == 0 ? jobs0 : pass == 1 ? a.G << split : a.G;
-#pragma unroll 1
-        for (int job = warp; job < jobs; job += W) {
-            int n, b, h, c = 0, end = 0;
-            float* to = nullptr;      // null: this is the whole row
-            uint32_t members = 0;
-            if (pass == 0) {
-                uint32_t rest = groups;
-                const int group = (int)(job * a.G_inv >> 16);   // job / G
-                n = job - group * a.G;
-                for (int u = group; u > 0; --u) rest &= rest - 1u;
-                const int e = __ffs(rest) - 1;
-                rest &= rest - 1u;
-                members = valid & (0xffffffffu << e) & (rest ? (rest & (0u - rest)) - 1u : 0xffffffffu);
-                const bool whole = ((begin >> e) & 1u) && (ending & members);
-                if (!whole) to = a.parts + ((int64_t)blockIdx.x * 2 + ((begin >> e) & 1u)) * PF;
-                b = __shfl_sync(0xffffffffu, mine.b, e);
-                h = __shfl_sync(0xffffffffu, mine.h, e);
-                c = e;
-                end = 32 - __clz(members);
-            } else {
-                n = pass == 1 ? job >> split : job;
-                b = infos[k ? last : first].b;
-                h = infos[k ? last : first].h;
-                const int share = job - (n << split);
-                c = pass == 1 ? share * each : 0;
-                end = pass == 1 ? min(parts, c + each) : 1 << split;
-                if (pass == 1 && split) to = heads + share * PF;
-            }
-            RowSum<D> sum;
-#pragma unroll 1
-            for (; c < end; c += 32) {
-                const int i = c + lane;
-                int off;
-                if (pass == 0) off = !((members >> (i & 31)) & 1u) || i > 31 ? -1 : i & 1 ? (i >> 1) * (M::kRing / 4) : M::kHeads / 4 + (i >> 1) * PF;
-                else off = pass == 1 ? ((spans[2 * k] + i) * 2 + (i == 0 ? 1 : 0)) * PF : M::kHeads / 4 + i * PF;
-                sum.merge(pass == 1 ? a.parts : reinterpret_cast<const float*>(smem), off, min(32, end - c), a.G, n, lane);
-            }
-            if (to) sum.write_part(to, a.G, n, lane);
-            else sum.template write_out<T>(a, b, h, n, lane);
+        for (int c = share * each, end = min(parts, c + each); c < end; c += 32) {
+            const int i = c + lane;
+            sum.template merge<8, true>(a.parts, ((blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * PF, min(32, end - c), a.G, n, lane);
         }
-        if (pass == 0) {
-            if (!crosses) return;
-            __syncthreads();
-            if (tid < 2) {
-                arrived[tid] = 0;
-                if (tid ? goes_on : from_before) {
-                    const int c0 = spans[2 * tid], c1 = spans[2 * tid + 1];
-                    if (atomic_add_acq_rel(a.counters + c0, 1) == c1 - c0) {
-                        a.counters[c0] = 0;
-                        arrived[tid] = 1;
-                    }
-                }
-            }
-            __syncthreads();
-            pass = 1;
-            k = -1;
-        } else if (pass == 1 && split) {
-            __syncthreads();
-            pass = 2;
-            continue;
-        } else if (pass == 2) {
-            __syncthreads();
-            pass = 1;
+        if (!shift) {
+            sum.template write_out<T>(a, span.b, span.h, n, lane);
+            return;
         }
-        do ++k;
-        while (k < 2 && !arrived[k]);
-        if (k == 2) return;
+        sum.write_part(sums + warp * part_floats(1, D), 1, 0, lane);
     }
+    if (!shift) return;
+    __syncthreads();
+    if (share || n >= a.G) return;
+    RowSum<D> all;
+    all.template merge<4, false>(sums, (warp + lane) * part_floats(1, D), 1 << shift, 1, 0, lane);
+    all.template write_out<T>(a, span.b, span.h, n, lane);
 }
 
 int device_sms()
@@ -940,12 +939,12 @@ int device_sms()
     return n;
 }
 
-// The workspace: counters, sums of large batches, parts.
+// The workspace: spans, sums of large batches, parts.
 struct Workspace {
     int64_t sums, parts, bytes;   // offsets of the latter two, and the whole
     Workspace(int sms, int G, int D)
     {
-        sums = 256 * (((int64_t)sms * 4 + 255) / 256);
+        sums = 256 * ((sms * (int64_t)sizeof(PartSpan) + 255) / 256);
         parts = sums + 256 * ((2 * (kKv4MaxBatch + 1) * 4 + 255) / 256);
         bytes = parts + (int64_t)sms * 2 * part_floats(G, D) * 4;
     }
@@ -966,9 +965,11 @@ struct LaunchAttention {
         static OncePerDevice once;
         if (cudaError_t e = once.set_attribute(attention_kernel<D, NG, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost); e != cudaSuccess)
             return e;
-        a.split = 0;
-        while (a.G << (a.split + 1) <= S::kWarps) ++a.split;
-        return kv4_launch(attention_kernel<D, NG, T>, dim3((unsigned)sms), S::kWarps * 32, (size_t)M::bytes(a.G, a.batch), st, a);
+        a.merge_shift = 0;
+        while (a.G << (a.merge_shift + 1) <= kMergeWarps) ++a.merge_shift;
+        cudaError_t e = kv4_launch(attention_kernel<D, NG, T>, dim3((unsigned)sms), S::kWarps * 32, (size_t)M::bytes(a.G, a.batch), st, a);
+        if (e == cudaSuccess) e = kv4_launch(merge_kernel<D, T>, dim3((unsigned)sms), kMergeWarps * 32, 0, st, a);
+        return e;
     }
 };
 
@@ -1044,7 +1045,7 @@ extern "C" KVC_API int kv4_decode_attention(const kv4_pool* pool, const kv_table
     a.scale = scale * 1.4426950408889634f * 0x1p24f;
     a.err = device_error;
     uint8_t* const work = static_cast<uint8_t*>(workspace);
-    a.counters = reinterpret_cast<int32_t*>(work);
+    a.spans = reinterpret_cast<PartSpan*>(work);
     a.sums = reinterpret_cast<uint32_t*>(work + ws.sums);
     a.parts = reinterpret_cast<float*>(work + ws.parts);
     return kv4_launch_result(kv4_dispatch(*pool, LaunchAttention{a, sms, static_cast<cudaStream_t>(stream)}));

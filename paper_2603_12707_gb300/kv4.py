@@ -146,10 +146,10 @@ def kv4_pool_bytes(pool: Pool) -> int:
 
 
 def kv4_workspace(pool: Pool, num_q_heads: int) -> torch.Tensor:
-    """A workspace of kv4_workspace_bytes(), zero-filled as its first use wants it."""
+    """A workspace of kv4_workspace_bytes()."""
     n = _load()["kv4_workspace_bytes"](pool.ref, num_q_heads)
     kd._check(min(n, 0), "kv4_workspace_bytes")
-    return torch.zeros(n, dtype=torch.uint8, device=pool.data.device)
+    return torch.empty(n, dtype=torch.uint8, device=pool.data.device)
 
 
 def kv_tables_step(tables: Tables, seq_ids, new_lens, slots, positions=None, cu_seqlens=None, lens_out=None,
