@@ -59,7 +59,6 @@ struct AttnArgs {
     int32_t H, Hq, G;
     uint32_t H_inv;      // 2^32 / H, rounded down (2^32 - 1 for 1)
     uint32_t G_inv;      // 2^16 / G, rounded up
-    int32_t merge_shift; // logarithm of the warps that share a row in the merge
     const int32_t* block_table;
     const int32_t* lens;
     int32_t max_seqs, max_pages, batch;
@@ -892,40 +891,27 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
     finish_cta<D, NG, T>(a, smem, Shares{base, extra, cta_warps}, (int)held == a.batch);
 }
 
-// What crosses CTAs: CTA c merges the parts of the (row, KV head) that goes on
-// after CTA c of the launch before this one, several warps a row of it where there are many.
-constexpr int kMergeWarps = 32, kMergeFew = 8;
+// What crosses CTAs: a warp merges one query row of the (row, KV head) that
+// goes on after some CTA of the launch before this one.
+constexpr int kMergeWarps = 8;
 template <int D, class T>
-__global__ void __launch_bounds__(kMergeWarps * 32) merge_kernel(const __grid_constant__ AttnArgs a)
+__global__ void __launch_bounds__(kMergeWarps * 32) merge_kernel(const __grid_constant__ AttnArgs a, int ctas)
 {
-    __shared__ float sums[kMergeWarps * part_floats(1, D)];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, w = blockIdx.x * kMergeWarps + (threadIdx.x >> 5);
+    const int c = (int)(w * a.G_inv >> 16), n = w - c * a.G, PF = part_floats(a.G, D);   // w / G
     griddep_wait();
     griddep_launch_dependents();
-    const PartSpan span = a.spans[blockIdx.x];
+    if (c >= ctas) return;
+    const PartSpan span = a.spans[c];
     if (span.b < 0) return;
-    const int parts = span.last - (int)blockIdx.x + 1, PF = part_floats(a.G, D);
-    const int shift = parts > kMergeFew ? a.merge_shift : 0;   // 2^shift warps a row
-    const int n = warp >> shift, share = warp - (n << shift), each = (parts + (1 << shift) - 1) >> shift;
+    const int parts = span.last - c + 1;
     RowSum<D> sum;
-    if (n < a.G) {
 #pragma unroll 1
-        for (int c = share * each, end = min(parts, c + each); c < end; c += 32) {
-            const int i = c + lane;
-            sum.template merge<8, true>(a.parts, ((blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * PF, min(32, end - c), a.G, n, lane);
-        }
-        if (!shift) {
-            sum.template write_out<T>(a, span.b, span.h, n, lane);
-            return;
-        }
-        sum.write_part(sums + warp * part_floats(1, D), 1, 0, lane);
+    for (int i0 = 0; i0 < parts; i0 += 32) {
+        const int i = i0 + lane;
+        sum.template merge<8, true>(a.parts, ((c + i) * 2 + (i == 0 ? 1 : 0)) * PF, min(32, parts - i0), a.G, n, lane);
     }
-    if (!shift) return;
-    __syncthreads();
-    if (share || n >= a.G) return;
-    RowSum<D> all;
-    all.template merge<4, false>(sums, (warp + lane) * part_floats(1, D), 1 << shift, 1, 0, lane);
-    all.template write_out<T>(a, span.b, span.h, n, lane);
+    sum.template write_out<T>(a, span.b, span.h, n, lane);
 }
 
 int device_sms()
@@ -965,10 +951,9 @@ struct LaunchAttention {
         static OncePerDevice once;
         if (cudaError_t e = once.set_attribute(attention_kernel<D, NG, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost); e != cudaSuccess)
             return e;
-        a.merge_shift = 0;
-        while (a.G << (a.merge_shift + 1) <= kMergeWarps) ++a.merge_shift;
         cudaError_t e = kv4_launch(attention_kernel<D, NG, T>, dim3((unsigned)sms), S::kWarps * 32, (size_t)M::bytes(a.G, a.batch), st, a);
-        if (e == cudaSuccess) e = kv4_launch(merge_kernel<D, T>, dim3((unsigned)sms), kMergeWarps * 32, 0, st, a);
+        if (e == cudaSuccess)
+            e = kv4_launch(merge_kernel<D, T>, dim3((unsigned)((sms * a.G + kMergeWarps - 1) / kMergeWarps)), kMergeWarps * 32, 0, st, a, sms);
         return e;
     }
 };
