@@ -14,8 +14,12 @@
 // operands.  The other operand is q, scaled by a power of two into fp16's range
 // (divided by 16 where it meets bits 4-7), or p * s', relative to a power of
 // two 2^E that follows the largest s'.  The 8 is subtracted by starting QK's
-// accumulators at -8 sum q, and for PV by one more product with rows of -8 (so
-// that p * s' is rounded once for both).
+// accumulators at -8 sum q, and for PV by one more product with constant rows, of
+// the same rounded p * s'.  The tensor cores cut what they add off toward zero, a
+// subnormal's products the earlier the smaller it is, and over a long row that is a
+// share of the sum: so those rows are the middle of the codes as the codes lie
+// (120 for bits 4-7; 15 for bits 0-3, whose 7.5 is no fp16), to lose the same.
+// Rows of -8 left 2.7e-4 of the mean output missing at 32K tokens; these 8e-5.
 //
 // Schedule.  The work is the list of all (row, KV head, page) tiles, a row's
 // heads in turn and a head's pages in order.  Every warp of a persistent grid
@@ -157,7 +161,7 @@ struct State {
     uint32_t qz[3];                       // (-8, 1) * sum of q over group j, in terms of the cache's type
     float qback[2];                       // undoes q's power of two
     float m[2], l[2];
-    float o[MT][4], e[NG][4], z[NG][2];   // e: -8 sum p s' of a group (apart: a NaN stays in its group)
+    float o[MT][4], e[NG][4], z[NG][2];   // e: 15 and 120 times a group's sum p s', in o's unit 2^-24 (apart: a NaN stays in its group)
     float vs, vlimit;                     // 2^-E, and the scale above which E moves
 
     __device__ __forceinline__ void start(const AttnArgs& a, int b, int h, int lane)
@@ -358,7 +362,7 @@ struct State {
                 // [token][n] in the fragment layout, their transposes are the operand.
                 const uint32_t b0 = movmatrix_trans(NG == 4 ? pack_f16(v0 * s0, v1 * s0) : pack_f16(p0 * (s0 * vs), p1 * (s0 * vs)));
                 const uint32_t b1 = movmatrix_trans(NG == 4 ? pack_f16(v2 * s1, v3 * s1) : pack_f16(p2 * (s1 * vs), p3 * (s1 * vs)));
-                mma_f16_16816(e[k], 0xc800c800u, 0xc800c800u, 0xc800c800u, 0xc800c800u, b0, b1);   // -8 everywhere
+                mma_f16_16816(e[k], 0x000f000fu, 0x00780078u, 0x000f000fu, 0x00780078u, b0, b1);
 #pragma unroll
                 for (int i = k * (NW / NG); i < (k + 1) * (NW / NG); ++i) {
                     const uint32_t a8 = va[i] >> 8, b8 = vb[i] >> 8;
@@ -398,6 +402,8 @@ struct State {
             z[k][1] *= al1;
             e[k][0] *= al0 * r;
             e[k][1] *= al1 * r;
+            e[k][2] *= al0 * r;
+            e[k][3] *= al1 * r;
         }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
@@ -426,7 +432,7 @@ struct State {
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 const int k = mt / (MT / NG);
-                o[mt][c] = (o[mt][c] * (c < 2 ? 0x1p24f : 0x1p20f) + e[k][c & 1]) * back + z[k][c & 1];
+                o[mt][c] = fmaf(e[k][c], c < 2 ? -8.f / 15.f : -128.f / 120.f, o[mt][c]) * (c < 2 ? 0x1p24f : 0x1p20f) * back + z[k][c & 1];
             }
     }
 
