@@ -1,12 +1,18 @@
 // kv4_write and kv4_read: K and V rows of tokens into and out of the 4-bit
 // pool's blocks (layout and quantisation: kvdecode4.h).  Both are copies whose
-// one side is 16-bit rows and whose other side is blocks; the bytes bound them.
+// one side is 16-bit rows and whose other side is blocks.
 //
 // V's codes lie in words of two neighbouring tokens, so a warp takes tokens
 // whose slots 2m and 2m + 1 follow one another as a pair (a run of tokens gives
 // pairs wherever it starts) and others alone; it goes over some KV heads of
 // them.  A lane holds 8 consecutive elements of one token's row, which are one word of K's
 // codes; V's words hold elements 8 apart, four lanes' codes each, and are made by a transposition across lanes.
+//
+// Measured on 57344 tokens of 32 heads of 128, groups of 64, bf16 (1.20 GB each
+// way, 177 us at the speed of a copy): kv4_write 255 us, 4.7 TB/s, bound by the
+// instructions (278 for a pair's head; the schedulers issue 4 of 5 cycles);
+// kv4_read 196 us, 6.1 TB/s, bound by memory.  32 warps an SM (64
+// registers) do better than 24 in both.  A call for 64 tokens takes 2.8 and 2.1 us of the device.
 #include "kvd_kv4.h"
 #include "kvd_ptx.cuh"
 
@@ -181,7 +187,7 @@ struct Place {
 };
 
 template <int D, int NG, class T>
-__global__ void __launch_bounds__(kRowWarps * 32) write_kernel(RowsArgs a)
+__global__ void __launch_bounds__(kRowWarps * 32, 4) write_kernel(RowsArgs a)
 {
     using B = Kv4Block<D, NG>;
     constexpr int GL = D / NG / 8, HS = Place<D>::HS, NW = D / 32;
@@ -247,7 +253,7 @@ __global__ void __launch_bounds__(kRowWarps * 32) write_kernel(RowsArgs a)
 }
 
 template <int D, int NG, class T>
-__global__ void __launch_bounds__(kRowWarps * 32) read_kernel(RowsArgs a)
+__global__ void __launch_bounds__(kRowWarps * 32, D == 128 && NG <= 2 ? 4 : 3) read_kernel(RowsArgs a)
 {
     using B = Kv4Block<D, NG>;
     using V = typename Packed<T>::V;
@@ -340,10 +346,13 @@ struct LaunchRows {
     template <int D, int NG, class T>
     cudaError_t operator()() const
     {
-        // A warp goes over as many heads as leave every SM some 32 warps of work.
+        // A warp goes over as many heads as leave every SM some 32 warps of work: a
+        // warp's start is two trips to memory, slots and rows, that nothing hides (32
+        // heads of 57344 tokens: 276 us at 8 heads a warp, 255 at 32; reading, 231 and 196).
+        // Several pairs of tokens a warp, as one run or 16 tokens apart, are slower (268 and 208 at best).
         const int64_t turns = ((int64_t)a.n + 1) / 2;
         int heads = Place<D>::HS;
-        while (heads < 8 && heads < a.H && turns * ((a.H + 2 * heads - 1) / (2 * heads)) >= 152 * 32) heads *= 2;
+        while (heads < a.H && turns * ((a.H + 2 * heads - 1) / (2 * heads)) >= 152 * 32) heads *= 2;
         a.warp_heads = heads;
         const dim3 grid((unsigned)((turns + kRowWarps - 1) / kRowWarps), (unsigned)((a.H + heads - 1) / heads));
         return kv4_launch(kWrite ? write_kernel<D, NG, T> : read_kernel<D, NG, T>, grid, kRowWarps * 32, 0, st, a);
