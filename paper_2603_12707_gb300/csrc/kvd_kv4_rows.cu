@@ -9,10 +9,10 @@
 // codes; V's words hold elements 8 apart, four lanes' codes each, and are made by a transposition across lanes.
 //
 // Measured on 57344 tokens of 32 heads of 128, groups of 64, bf16 (1.20 GB each
-// way, 177 us at the speed of a copy): kv4_write 255 us, 4.7 TB/s, bound by the
-// instructions (278 for a pair's head; the schedulers issue 4 of 5 cycles);
+// way, 177 us at the speed of a copy): kv4_write 240 us, 5.0 TB/s, bound by the
+// instructions (245 for a pair's head; the schedulers issue 77 % of cycles, ALU and FMA pipes are 64 % busy);
 // kv4_read 196 us, 6.1 TB/s, bound by memory.  32 warps an SM (64
-// registers) do better than 24 in both.  A call for 64 tokens takes 2.8 and 2.1 us of the device.
+// registers) do better than 24 in both.  A call for 64 tokens takes 2.6 and 2.1 us of the device.
 #include "kvd_kv4.h"
 #include "kvd_ptx.cuh"
 
@@ -101,17 +101,9 @@ __device__ __forceinline__ uint32_t dequantise(uint32_t codes, typename Packed<T
     return as_word(__hfma2(c, s, z));
 }
 
-// The codes of this lane's 8 elements, as K's words hold them (element e in
-// bits 16 (e % 2) + 4 (e / 2) and up), and the scale word of their group, which lies in GL lanes.
-//
-// The quotient.  With r = 1 / s, k = rint(d r) is the nearest code or, close to a tie,
-// its neighbour; e = d - k s is exact and k + e r is d / s but for one rounding,
-// on a tie exactly the tie.  It is at most some 50 (z is off by half a unit of its
-// type, and s at least a thirtieth of one where it is not 0), so 16 bits hold it until
-// the clamp.  (Where d overflows, at -8 s of the widest groups that bf16 holds,
-// it is NaN, whose bits the clamp takes to 0 as it should.)
-template <int GL, class T>
-__device__ __forceinline__ uint32_t quantise(const uint4& row, uint32_t* scale)
+// (min, -max) of this lane's 8 elements, in the cache's type: one minimum serves both.
+template <class T>
+__device__ __forceinline__ uint32_t range_of(const uint4& row)
 {
     using V = typename Packed<T>::V;
     const uint32_t w[4] = {row.x, row.y, row.z, row.w};
@@ -121,24 +113,48 @@ __device__ __forceinline__ uint32_t quantise(const uint4& row, uint32_t* scale)
         lo = __hmin2_nan(lo, as_pair<V>(w[i]));
         hi = __hmax2_nan(hi, as_pair<V>(w[i]));
     }
-    // (min, -max) of the group: one minimum for both.
     const uint32_t l = as_word(lo), h = as_word(__hneg2(hi));
-    V m = __hmin2_nan(as_pair<V>(__byte_perm(l, h, 0x5410)), as_pair<V>(__byte_perm(l, h, 0x7632)));
-#pragma unroll
-    for (int k = 1; k < GL; k <<= 1) m = __hmin2_nan(m, as_pair<V>(__shfl_xor_sync(0xffffffffu, as_word(m), k)));
-    const float least = T::lo(as_word(m)), most = -T::hi(as_word(m));
+    return as_word(__hmin2_nan(as_pair<V>(__byte_perm(l, h, 0x5410)), as_pair<V>(__byte_perm(l, h, 0x7632))));
+}
+
+constexpr uint32_t kBroken = 0x7fff7fffu;     // the scale word of a group with an infinity or a NaN: NaN in either type
+
+// bf16's tiny steps are scaled up, exactly, so that 1 / s is finite.
+template <class T>
+__device__ __forceinline__ float scale_up(float s)
+{
+    return Packed<T>::kTiny && s < 0x1p-100f ? 0x1p64f : 1.f;
+}
+
+// The scale word (s, z) of a group's (min, -max), and 1 / s (scaled down by scale_up; 0 for a
+// step of 0, which makes every quotient 0).
+template <class T>
+__device__ __forceinline__ uint32_t scale_of(uint32_t range, float* r)
+{
+    const float least = T::lo(range), most = -T::hi(range);
     const float half = most * 0.5f - least * 0.5f;
-    const bool broken = !(half < INFINITY);   // an infinity or a NaN in the group
     // half / 7.5, corrected once like the quotients below.
     const float h0 = half * (1.f / 7.5f);
-    uint32_t meta = T::pack(fmaf(fmaf(-7.5f, h0, half), 1.f / 7.5f, h0), 0.f);
-    const float s = T::lo(meta);
-    meta = __byte_perm(meta, T::pack(fmaf(8.f, s, least), 0.f), 0x5410);
-    const float z = T::hi(meta);
-    *scale = broken ? 0x7fff7fffu : meta;     // NaN in either type
-    // bf16's tiny steps are scaled up, exactly, so that 1 / s is finite; a step of 0 makes every quotient 0.
-    const float up = Packed<T>::kTiny && s < 0x1p-100f ? 0x1p64f : 1.f, su = s * up;
-    const float r = s > 0.f ? 1.f / su : 0.f;
+    const uint32_t step = T::pack(fmaf(fmaf(-7.5f, h0, half), 1.f / 7.5f, h0), 0.f);
+    const float s = T::lo(step);
+    *r = s > 0.f ? 1.f / (s * scale_up<T>(s)) : 0.f;
+    return half < INFINITY ? __byte_perm(step, T::pack(fmaf(8.f, s, least), 0.f), 0x5410) : kBroken;
+}
+
+// The codes of this lane's 8 elements, as K's words hold them (element e in
+// bits 16 (e % 2) + 4 (e / 2) and up).
+//
+// The quotient.  With r = 1 / s, k = rint(d r) is the nearest code or, close to a tie,
+// its neighbour; e = d - k s is exact and k + e r is d / s but for one rounding,
+// on a tie exactly the tie.  It is at most some 50 (z is off by half a unit of its
+// type, and s at least a thirtieth of one where it is not 0), so 16 bits hold it until
+// the clamp.  (Where d overflows, at -8 s of the widest groups that bf16 holds,
+// it is NaN, whose bits the clamp takes to 0 as it should.)
+template <class T>
+__device__ __forceinline__ uint32_t quantise(const uint4& row, uint32_t scale, float r)
+{
+    const uint32_t w[4] = {row.x, row.y, row.z, row.w};
+    const float s = T::lo(scale), z = T::hi(scale), up = scale_up<T>(s), su = s * up;
     constexpr float kRound = 12582912.f;      // 1.5 * 2^23: adding it rounds to an integer, in the low bits
     const uint64_t up2 = f2_pack(up, up), z2 = f2_pack(-z * up, -z * up), s2 = f2_pack(-su, -su), r2 = f2_pack(r, r);
     const uint64_t round2 = f2_pack(kRound, kRound), back2 = f2_pack(-kRound, -kRound), code2 = f2_pack(kRound + 8.f, kRound + 8.f);
@@ -153,7 +169,7 @@ __device__ __forceinline__ uint32_t quantise(const uint4& row, uint32_t* scale)
         const uint32_t c = __vimin_s16x2_relu(__byte_perm(__float_as_uint(q0), __float_as_uint(q1), 0x5410), 0x000f000fu);
         codes = codes * 16u + c;
     }
-    return broken ? 0x88888888u : codes;
+    return scale == kBroken ? 0x88888888u : codes;
 }
 
 // Byte offsets in a block.
@@ -223,9 +239,19 @@ __global__ void __launch_bounds__(kRowWarps * 32, 4) write_kernel(RowsArgs a)
                 v_next = __ldcs(reinterpret_cast<const uint4*>(v_row + (head + HS) * D));
             }
             uint8_t* const block = page + (int64_t)head * B::kBytes;
-            uint32_t ks, vs;
-            const uint32_t kw = quantise<GL, T>(kr, &ks);
-            const uint32_t vc = quad_transpose(quantise<GL, T>(vr, &vs), lane);
+            // Groups lie in GL lanes, whose even ones work out K's scale and whose odd ones V's (both in every lane: 255 us for 240).
+            using V = typename Packed<T>::V;
+            const bool odd = lane & 1;
+            const uint32_t k_range = range_of<T>(kr), v_range = range_of<T>(vr);
+            V range = __hmin2_nan(as_pair<V>(odd ? v_range : k_range), as_pair<V>(__shfl_xor_sync(0xffffffffu, odd ? k_range : v_range, 1)));
+#pragma unroll
+            for (int k = 2; k < GL; k <<= 1) range = __hmin2_nan(range, as_pair<V>(__shfl_xor_sync(0xffffffffu, as_word(range), k)));
+            float r;
+            const uint32_t scale = scale_of<T>(as_word(range), &r), scale_x = __shfl_xor_sync(0xffffffffu, scale, 1);
+            const float r_x = __shfl_xor_sync(0xffffffffu, r, 1);
+            const uint32_t ks = odd ? scale_x : scale, vs = odd ? scale : scale_x;
+            const uint32_t kw = quantise<T>(kr, ks, odd ? r_x : r);
+            const uint32_t vc = quad_transpose(quantise<T>(vr, vs, odd ? r : r_x), lane);
             // Lane (i, n) of a token now holds byte n of the four lanes of word
             // i: their elements g and, in the high nibbles, g + 2.
             const int i = at.m >> 2, g = (at.m & 1) * 4 + (at.m >> 1 & 1);
