@@ -9,17 +9,21 @@
 //
 // so scales and middles multiply scores and weights, 16 per page, and the codes
 // go into the tensor cores as they are: a 4-bit code under a mask is an fp16
-// subnormal, c * 2^-24 in bits 0-3 and c * 2^-20 in bits 4-7, whose product with
-// another fp16 is exact.  Eight codes take five instructions to become four
-// operands.  The other operand is q, scaled by a power of two into fp16's range
-// (divided by 16 where it meets bits 4-7), or p * s', relative to a power of
-// two 2^E that follows the largest s'.  The 8 is subtracted by starting QK's
-// accumulators at -8 sum q, and for PV by one more product with constant rows, of
-// the same rounded p * s'.  The tensor cores cut what they add off toward zero, a
-// subnormal's products the earlier the smaller it is, and over a long row that is a
-// share of the sum: so those rows are the middle of the codes as the codes lie
-// (120 for bits 4-7; 15 for bits 0-3, whose 7.5 is no fp16), to lose the same.
+// subnormal, or nearly one, c * 2^-24 in bits 0-3 and c * 2^-20 in bits 4-7 (up to
+// bit 10 a word's value is its bits), whose product with another fp16 is exact.  Eight of
+// V's codes take five instructions to become four operands, of K's six.  The other
+// operand is q, scaled by a power of two into fp16's range (and by what its codes' place
+// asks), or p * s', relative to a power of two 2^E that follows the largest s'.
+//
+// The tensor cores cut what they add off toward zero, and the products of a
+// subnormal the earlier the smaller it is.  So K's codes are moved up by three bits
+// (relative error of one token's score, rms: 2.4e-7 with an fp16 q, 2.1e-6 where they lie; 64
+// MHA rows 56.0 -> 56.9 us).  For V it is a share of the sum that shows where a long row's outputs are
+// small, and the codes' 8 is subtracted by one more product of the same rounded
+// p * s' with constant rows that lose as much: the middle of the codes as the codes lie
+// (120 for bits 4-7; 15 for bits 0-3, whose 7.5 is no fp16).
 // Rows of -8 left 2.7e-4 of the mean output missing at 32K tokens; these 8e-5.
+// QK's accumulators start at -8 sum q.
 //
 // Schedule.  The work is the list of all (row, KV head, page) tiles, a row's
 // heads in turn and a head's pages in order.  Every warp of a persistent grid
@@ -43,9 +47,9 @@
 // 3.0e-4 off in fp16, of which 2.1e-4 are the output's own rounding, and 1.7e-3 in bf16, all of it that.
 //
 // Measured (device, calls in a graph; 6.8 TB/s is a copy's rate).  64 rows of 640 - 1344
-// tokens, 32 KV heads, d 128: 56.0 us, 288 MB, 5.2 TB/s; 8 rows of 32K tokens,
+// tokens, 32 KV heads, d 128: 57.0 us, 288 MB, 5.1 TB/s; 8 rows of 32K tokens,
 // 28 query on 4 KV heads, groups of 32: 39.5 us, 168 MB, 4.2 TB/s; one row of 2337: 9.6 us.
-// A further byte costs 1 / 6.7 TB/s (groups of 128), 6.4 (64), 6.0 (32), 5.6 (d 64): close
+// A further byte costs 1 / 6.5 TB/s (groups of 128), 6.3 (64), 5.9 (32), 5.6 (d 64): close
 // to memory, beside which a tile's 267 to 357 instructions keep the ALU 58 % and
 // the tensor cores 34 % busy.  What is left is fixed, some 12 us a call: the
 // scan and the search 2.5, first tiles 1, the end of the shares and the CTA's merge 3, the
@@ -90,7 +94,7 @@ struct AttnArgs {
     uint16_t* out;
     int64_t q_stride, out_stride;
     float* lse;
-    float scale;         // softmax scale * log2(e) * 2^24 (the accumulators' unit)
+    float scale;         // softmax scale * log2(e) * 2^21 (the accumulators' unit)
     PartSpan* spans;     // [grid]: what goes on after a CTA
     uint32_t* sums;      // [2][batch + 1] where shared memory does not hold them: the same from every CTA
     float* parts;        // [grid][2][G][D + 2]: a CTA's part of the row that began before it, and of the one that goes on
@@ -176,9 +180,9 @@ struct State {
     using B = Kv4Block<D, NG>;
     static constexpr int NW = D / 32;     // code words of a lane per 8 tokens
     static constexpr int MT = D / 16;     // 16-element tiles of the output
-    // The K accumulators hold 2^-24 q c; sums of q are taken in a unit that the cache's type holds (8 times 2^22 at most).
+    // The K accumulators hold 2^-21 q c; sums of q are taken in a unit that the cache's type holds (8 times 2^22 at most).
     static constexpr bool kHalf = std::is_same_v<T, Fp16>;
-    static constexpr float kSumUnit = kHalf ? 0x1p-10f : 0x1p-24f;
+    static constexpr float kSumUnit = kHalf ? 0x1p-10f : 0x1p-21f;
     uint32_t qf[2 * NW][2];               // q as the K product's column operand
     uint32_t qz[3];                       // (-8, 1) * sum of q over group j, in terms of the cache's type
     float qback[2];                       // undoes q's power of two
@@ -218,10 +222,10 @@ struct State {
             float sum = 0.f;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                // pair k of a word: elements 2k and 2k + 1, at bits 4k; odd k meets c * 2^-20
+                // pair k of a word: elements 2k and 2k + 1, at bits 4k; as q meets c * 2^-21, 2^-20, 2^-21, 2^-17
                 const float x0 = T::lo(w[i][k]) * mul, x1 = T::hi(w[i][k]) * mul;
                 sum += x0 + x1;
-                qf[2 * i + (k >> 1)][k & 1] = k & 1 ? pack_f16(x0 * 0.0625f, x1 * 0.0625f) : pack_f16(x0, x1);
+                qf[2 * i + (k >> 1)][k & 1] = k & 1 ? pack_f16(x0 * (k == 1 ? 0.5f : 0.0625f), x1 * (k == 1 ? 0.5f : 0.0625f)) : pack_f16(x0, x1);
             }
             sums[i / (NW / NG)] = i % (NW / NG) ? sums[i / (NW / NG)] + sum : sum;
         }
@@ -286,6 +290,8 @@ struct State {
     __device__ __forceinline__ void pages(uint32_t at, int valid, float scale, int lane)
     {
         const int g = lane >> 2;
+        int eight = 8;         // a multiplication: the shifts' pipe is the busiest
+        opaque(eight);
         const uint32_t codes = at + lane * NW * 4, scales = at + 2 * B::kCodes + g * NG * 4;
         const uint32_t own = scales + (lane & (NG - 1)) * 4;   // group j's word (of lanes that have none: another one's, against zeros)
         float s[NP][4];
@@ -311,7 +317,7 @@ struct State {
             if constexpr (kHalf) {
                 mma_f16_16816(base, w0, w1, w0, w1, qz[0], qz[1], zero);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) base[c] *= 0x1p-24f / kSumUnit;
+                for (int c = 0; c < 4; ++c) base[c] *= 0x1p-21f / kSumUnit;
             } else {
                 mma_bf16_16816(base, w0, w1, w0, w1, qz[0], qz[1], zero);
                 mma_bf16_16816(base, w0, w1, w0, w1, qz[2], 0u);
@@ -321,14 +327,14 @@ struct State {
                 float acc[4];
 #pragma unroll
                 for (int i = k * (NW / NG); i < (k + 1) * (NW / NG); ++i) {
-                    const uint32_t a8 = ka[i] >> 8, b8 = kb[i] >> 8;
+                    const uint32_t a0 = ka[i] * eight, b0 = kb[i] * eight, a5 = ka[i] >> 5, b5 = kb[i] >> 5;
                     if (i == k * (NW / NG))
-                        mma_f16_16816(acc, ka[i] & 0x000f000fu, kb[i] & 0x000f000fu, ka[i] & 0x00f000f0u, kb[i] & 0x00f000f0u,
+                        mma_f16_16816(acc, a0 & 0x00780078u, b0 & 0x00780078u, ka[i] & 0x00f000f0u, kb[i] & 0x00f000f0u,
                                       qf[2 * i][0], qf[2 * i][1], zero);
                     else
-                        mma_f16_16816(acc, ka[i] & 0x000f000fu, kb[i] & 0x000f000fu, ka[i] & 0x00f000f0u, kb[i] & 0x00f000f0u,
+                        mma_f16_16816(acc, a0 & 0x00780078u, b0 & 0x00780078u, ka[i] & 0x00f000f0u, kb[i] & 0x00f000f0u,
                                       qf[2 * i][0], qf[2 * i][1]);
-                    mma_f16_16816(acc, a8 & 0x000f000fu, b8 & 0x000f000fu, a8 & 0x00f000f0u, b8 & 0x00f000f0u,
+                    mma_f16_16816(acc, a5 & 0x00780078u, b5 & 0x00780078u, a5 & 0x07800780u, b5 & 0x07800780u,
                                   qf[2 * i + 1][0], qf[2 * i + 1][1]);
                 }
 #pragma unroll
@@ -1055,7 +1061,7 @@ extern "C" KVC_API int kv4_decode_attention(const kv4_pool* pool, const kv_table
     a.q_stride = q_stride;
     a.out_stride = out_stride;
     a.lse = lse;
-    a.scale = scale * 1.4426950408889634f * 0x1p24f;
+    a.scale = scale * 1.4426950408889634f * 0x1p21f;
     a.err = device_error;
     uint8_t* const work = static_cast<uint8_t*>(workspace);
     a.spans = reinterpret_cast<PartSpan*>(work);
