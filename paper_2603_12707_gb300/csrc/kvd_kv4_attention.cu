@@ -18,7 +18,7 @@
 // The tensor cores cut what they add off toward zero, and the products of a
 // subnormal the earlier the smaller it is.  So K's codes are moved up by three bits
 // (relative error of one token's score, rms: 2.4e-7 with an fp16 q, 2.1e-6 where they lie; 64
-// MHA rows 56.0 -> 56.9 us).  For V it is a share of the sum that shows where a long row's outputs are
+// MHA rows 56.0 -> 57.0 us).  For V it is a share of the sum that shows where a long row's outputs are
 // small, and the codes' 8 is subtracted by one more product of the same rounded
 // p * s' with constant rows that lose as much: the middle of the codes as the codes lie
 // (120 for bits 4-7; 15 for bits 0-3, whose 7.5 is no fp16).
@@ -44,14 +44,14 @@
 // as fp16's own values, more than bf16's (and a bf16 q
 // loses only what is below 2^-35 of its row's largest).  sum q is 2 (fp16) or 3 (bf16) terms.  All
 // sums, m, l and parts are fp32.  Against 64 bits, outputs over 32K tokens are
-// 3.0e-4 off in fp16, of which 2.1e-4 are the output's own rounding, and 1.7e-3 in bf16, all of it that.
+// 2.9e-4 off in fp16, of which 2.1e-4 are the output's own rounding, and 1.7e-3 in bf16, all of it that.
 //
 // Measured (device, calls in a graph; 6.8 TB/s is a copy's rate).  64 rows of 640 - 1344
 // tokens, 32 KV heads, d 128: 57.0 us, 288 MB, 5.1 TB/s; 8 rows of 32K tokens,
-// 28 query on 4 KV heads, groups of 32: 39.5 us, 168 MB, 4.2 TB/s; one row of 2337: 9.6 us.
-// A further byte costs 1 / 6.5 TB/s (groups of 128), 6.3 (64), 5.9 (32), 5.6 (d 64): close
-// to memory, beside which a tile's 267 to 357 instructions keep the ALU 58 % and
-// the tensor cores 34 % busy.  What is left is fixed, some 12 us a call: the
+// 28 query on 4 KV heads, groups of 32: 39.7 us, 168 MB, 4.2 TB/s; one row of 2337: 9.6 us.
+// A further byte costs 1 / 6.4 TB/s (groups of 128), 6.2 (64), 5.9 (32), 5.5 (d 64): close
+// to memory, beside which a tile's 275 to 365 instructions keep the ALU 57 % and
+// the tensor cores 33 % busy.  What is left is fixed, some 12 us a call: the
 // scan and the search 2.5, first tiles 1, the end of the shares and the CTA's merge 3, the
 // second launch 2 to 3, and that a launch fetches its instructions anew (loops stay
 // rolled and every large part has one call site: 74 KB -> 53 KB of code took one short row from 15.8 to 10.6 us).

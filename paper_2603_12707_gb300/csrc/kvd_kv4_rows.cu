@@ -374,8 +374,8 @@ struct LaunchRows {
     {
         // A warp goes over as many heads as leave every SM some 32 warps of work: a
         // warp's start is two trips to memory, slots and rows, that nothing hides (32
-        // heads of 57344 tokens: 276 us at 8 heads a warp, 255 at 32; reading, 231 and 196).
-        // Several pairs of tokens a warp, as one run or 16 tokens apart, are slower (268 and 208 at best).
+        // heads of 57344 tokens: 252 us at 8 heads a warp, 240 at 32; reading, 208 and 196).
+        // Several pairs of tokens a warp, as one run or 16 tokens apart, are 5 to 15 % slower.
         const int64_t turns = ((int64_t)a.n + 1) / 2;
         int heads = Place<D>::HS;
         while (heads < a.H && turns * ((a.H + 2 * heads - 1) / (2 * heads)) >= 152 * 32) heads *= 2;

@@ -105,6 +105,31 @@ def test_attention_of_small_and_large_values(kv4, dtype, q_scale, kv_scale):
     run_attention(kv4, [3, 70, 515], 4, 4, 64, 32, dtype, seed=9, q_scale=q_scale, kv_scale=kv_scale)
 
 
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("d,group", SHAPES)
+def test_scores_of_single_tokens(kv4, d, group, dtype):
+    """A row of one token: its log-sum-exp is the score itself, with nothing to average.
+
+    A score is d / 16 accumulations and a few operations on the groups' sums, of a size of
+    at most a = scale * sum_d |q_d| (8 s + |z|); each rounds to 2^-24 or cuts off at 2^-23 of
+    that.  Half of d / 16 + 4 steps at 2^-23 leave 2^-20 a at d = 128, and less at 64; errors of
+    different signs take it to half of that."""
+    b, hq, hkv = 64, 8, 2
+    table, pages = make_tables([1] * b, 11)
+    blocks = random_pool(pages, hkv, d, group, dtype, 12)
+    q = torch.randn((b, hq, d), generator=torch.Generator().manual_seed(13)).to(dtype)
+    pool = kv4.Pool(torch.from_numpy(blocks).cuda(), d, group, dtype)
+    tabs = kv4.Tables(torch.from_numpy(table).cuda(), torch.ones(b, dtype=torch.int32, device="cuda"))
+    out, lse = torch.empty((b, hq, d), dtype=dtype, device="cuda"), torch.empty((b, hq), device="cuda")
+    kv4.kv4_decode_attention(pool, tabs, q.cuda(), out, kv4.kv4_workspace(pool, hq), lse=lse)
+    k, _, (s, z), _ = values(blocks[table[:, 0]], d, group, dtype)                  # [b, hkv, 16, d]
+    k, size = (np.repeat(x[:, :, 0], hq // hkv, 1) for x in (k, 8 * s + np.abs(z)))
+    x = (q.double().numpy() * k).sum(-1) * d ** -0.5
+    a = (np.abs(q.double().numpy()) * size).sum(-1) * d ** -0.5
+    err = np.abs(lse.double().cpu().numpy() - x)
+    assert (err <= 2.0 ** -21 * a).all(), float((err / a).max() * 2 ** 21)
+
+
 def test_attention_of_bf16_values_that_fp16_cannot_hold(kv4):
     run_attention(kv4, [40, 300], 8, 2, 128, 32, BF, seed=2, q_scale=1e-30, kv_scale=1e25)
     run_attention(kv4, [40, 300], 8, 2, 128, 32, BF, seed=2, q_scale=1e20, kv_scale=1e-22)
