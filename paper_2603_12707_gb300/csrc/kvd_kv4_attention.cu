@@ -23,7 +23,7 @@
 // p * s' with constant rows that lose as much: the middle of the codes as the codes lie
 // (120 for bits 4-7; 15 for bits 0-3, whose 7.5 is no fp16).
 // Rows of -8 left 2.7e-4 of the mean output missing at 32K tokens; these 8e-5.
-// QK's accumulators start at -8 sum q.
+// For K the 8 is in sum_groups (z - 8 s) sum q, a product of the scale words as they lie.
 //
 // Schedule.  The work is the list of all (row, KV head, page) tiles, a row's
 // heads in turn and a head's pages in order.  Every warp of a persistent grid
