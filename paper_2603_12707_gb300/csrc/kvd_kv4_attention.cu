@@ -23,6 +23,10 @@
 // p * s' with constant rows that lose as much: the middle of the codes as the codes lie
 // (120 for bits 4-7; 15 for bits 0-3, whose 7.5 is no fp16).
 // Rows of -8 left 2.7e-4 of the mean output missing at 32K tokens; these 8e-5.
+// What is lost all the same is of one sign and grows with the running sum, so after every 32 tiles
+// of a row its sums go from the tensor cores' accumulators to fp32 ones, which are rounded to nearest, and
+// begin anew: fp16 outputs of flat weights are 3.1e-4 off where a warp works 57, 256, 1024 or 2048
+// pages of a row (2.1e-4 of it is their own rounding); in one sum 3.1e-4, 9.9e-4, 1.2e-2 and 2.8e-2.
 // For K the 8 is in sum_groups (z - 8 s) sum q, a product of the scale words as they lie.
 //
 // Schedule.  The work is the list of all (row, KV head, page) tiles, a row's
@@ -172,6 +176,22 @@ struct Tile {
 };
 static_assert(kKv4MaxHeads <= 1024 && kKv4MaxBatch <= 1 << 15, "Tile::pack");
 
+// Sums of o over what lies behind of a (row, KV head), put away every 32 tiles (State::close): in units of
+// one, relative to the m of that time.  They lie in the thread's local memory, behind an address
+// that the compiler cannot turn into registers: those are full (64 MHA rows 57.9 -> 59.7 us, 8 of 32K tokens
+// 40.4 -> 41.6).
+template <int D>
+struct Closed {
+    float4 o[D / 16];
+    float m[2];
+    __device__ __forceinline__ Closed& hidden()
+    {
+        Closed* p = this;
+        asm volatile("" : "+l"(p) : : "memory");
+        return *p;
+    }
+};
+
 // The running state of a warp for one (row, KV head): lane (g = lane / 4, j =
 // lane % 4) holds columns n = 2j and 2j + 1 of everything, tokens g and g + 8 of a
 // page's scores, elements 16 mt + g and 16 mt + g + 8 of the output.
@@ -189,6 +209,8 @@ struct State {
     float m[2], l[2];
     float o[MT][4], e[NG][4], z[NG][2];   // e: 15 and 120 times a group's sum p s', in o's unit 2^-24 (apart: a NaN stays in its group)
     float vs, vlimit;                     // 2^-E, and the scale above which E moves
+
+    bool closed;                          // whether close() has put something away
 
     __device__ __forceinline__ void start(const AttnArgs& a, int b, int h, int lane)
     {
@@ -262,6 +284,7 @@ struct State {
         }
         vs = 0x1p100f;
         vlimit = -1.f;   // below any |s'|: the first page sets E
+        closed = false;
     }
 
     template <int N>
@@ -442,7 +465,49 @@ struct State {
         }
     }
 
-    // The sums over all lanes' tokens; o is then the unnormalised output.
+    // o becomes what it stands for, relative to m, with what close() has put away.
+    __device__ __forceinline__ void settle(Closed<D>& sums)
+    {
+        const float back = inverse_power(vs);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                o[mt][c] = fmaf(e[mt / (MT / NG)][c], c < 2 ? -8.f / 15.f : -128.f / 120.f, o[mt][c]) * (c < 2 ? 0x1p24f : 0x1p20f) * back;
+        if (closed) {
+            const Closed<D>& put = sums.hidden();
+            const float f0 = put.m[0] == m[0] ? 1.f : ex2(put.m[0] - m[0]), f1 = put.m[1] == m[1] ? 1.f : ex2(put.m[1] - m[1]);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+                const float4 x = put.o[mt];
+                o[mt][0] = fmaf(x.x, f0, o[mt][0]);
+                o[mt][1] = fmaf(x.y, f1, o[mt][1]);
+                o[mt][2] = fmaf(x.z, f0, o[mt][2]);
+                o[mt][3] = fmaf(x.w, f1, o[mt][3]);
+            }
+        }
+    }
+
+    // Puts what settle() has made of o away; o and e begin anew (z and l are fp32 sums as it is).
+    __device__ __forceinline__ void close(Closed<D>& sums)
+    {
+        Closed<D>& put = sums.hidden();
+        put.m[0] = m[0];
+        put.m[1] = m[1];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+            put.o[mt] = make_float4(o[mt][0], o[mt][1], o[mt][2], o[mt][3]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) o[mt][c] = 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < NG; ++k)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) e[k][c] = 0.f;
+        closed = true;
+    }
+
+    // The sums over all lanes' tokens; o (settled) is then the unnormalised output.
     __device__ __forceinline__ void finish()
     {
 #pragma unroll
@@ -454,14 +519,10 @@ struct State {
                 for (int k = 0; k < NG; ++k) z[k][c] += __shfl_xor_sync(0xffffffffu, z[k][c], mask);
             }
         }
-        const float back = inverse_power(vs);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const int k = mt / (MT / NG);
-                o[mt][c] = fmaf(e[k][c], c < 2 ? -8.f / 15.f : -128.f / 120.f, o[mt][c]) * (c < 2 ? 0x1p24f : 0x1p20f) * back + z[k][c & 1];
-            }
+            for (int c = 0; c < 4; ++c) o[mt][c] += z[mt / (MT / NG)][c & 1];
     }
 
     __device__ __forceinline__ void write_out(const AttnArgs& a, int b, int h, int lane) const
@@ -824,6 +885,7 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
     const uint32_t ring_lane = ring_at + (lane % N) * B::kBytes;
 
     State<D, NG, T> st;
+    Closed<D> closed_sums;
     Tile next{nullptr, 0};            // of the 32 tiles after those in work
     const uint8_t* from = nullptr;    // the tile that this lane starts next, in turn `when` of the 32 / N (-1: none),
     int when = -1;
@@ -897,7 +959,9 @@ __global__ void __launch_bounds__(AttnShape<D, NG>::kWarps * 32, 1) attention_ke
         opaque(valid);                // (one copy of the work, not one for each kind of turn: code is fetched once a launch)
         if (valid) st.pages(ring_at + place * S::kStage, valid, a.scale, lane);
         i += tiles;
-        if (turn & (kClose | kHold)) {
+        if ((turn & (kClose | kHold)) || (i & 31) == 0) {
+            if ((turn & kClose) || (i & 31) == 0) st.settle(closed_sums);   // (one copy of it)
+            if (!(turn & (kClose | kHold))) st.close(closed_sums);
             if (turn & kClose) {
                 const uint32_t t = __shfl_sync(0xffffffffu, cur, (i - 1) & 31);
                 const int b = Tile::row(t), h = Tile::head(t);
