@@ -150,10 +150,12 @@ KVC_API int64_t kv4_workspace_bytes(const kv4_pool *pool, int32_t num_q_heads);
  * zeros and lse = -infinity; so does one whose id is out of range or whose length is
  * negative or above max_pages * 16, with KVC_DEVERR_SEQ_RANGE.  The tokens of a
  * page id outside the pool are left out, with KVC_DEVERR_PAGE_RANGE.  Rows that
- * together pass 2^31 pages times KV heads set KVC_DEVERR_SEQ_RANGE and nothing is written.  Scores,
- * softmax statistics and sums are held in 32 bits; a q that is not finite
- * gives NaN.  The result of a call does not depend on timing: partial results
- * are merged in the order of their tokens. */
+ * together pass 2^31 pages times KV heads set KVC_DEVERR_SEQ_RANGE and nothing
+ * is written.  Scores, softmax statistics and sums are held in 32 bits.  What meets
+ * V's codes, a token's weight times its scale, is rounded to 11 bits, below 2^-20 of the
+ * largest of its sum (a query head's over the elements of a scale group) to
+ * multiples of 2^-30 of that.  A q that is not finite gives NaN.  The result of a call does
+ * not depend on timing: partial results are merged in the order of their tokens. */
 KVC_API int kv4_decode_attention(const kv4_pool *pool, const kv_tables *tables, int32_t batch, const int32_t *seq_ids,
                                  int32_t num_q_heads, const void *q, int64_t q_stride, void *out, int64_t out_stride,
                                  float *lse, float softmax_scale, void *workspace, int64_t workspace_bytes,

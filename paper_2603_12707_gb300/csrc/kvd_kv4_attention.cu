@@ -13,7 +13,10 @@
 // bit 10 a word's value is its bits), whose product with another fp16 is exact.  Eight of
 // V's codes take five instructions to become four operands, of K's six.  The other
 // operand is q, scaled by a power of two into fp16's range (and by what its codes' place
-// asks), or p * s', relative to a power of two 2^E that follows the largest s'.
+// asks), or p * s', relative to a power of two 2^E that follows the largest of them: one for each
+// query head and scale group, so that neither another group's scales, nor another head's tokens, nor wide
+// tokens of no weight take bits away (one E of the largest s' alone: a token of 2^40 times the others'
+// scale and e^-90 of their weight moved outputs by 0.35).
 //
 // The tensor cores cut what they add off toward zero, and the products of a
 // subnormal the earlier the smaller it is.  So K's codes are moved up by three bits
@@ -45,8 +48,8 @@
 // of 32K tokens 22.8 us against 17, 64 rows of 32 KV heads 57.0 against 55.3).
 //
 // Roundings to fewer than 32 bits.  q and p * s' are fp16 operands, 11 bits: as many
-// as fp16's own values, more than bf16's (and a bf16 q
-// loses only what is below 2^-35 of its row's largest).  sum q is 2 (fp16) or 3 (bf16) terms.  All
+// as fp16's own values, more than bf16's (a bf16 q
+// loses only what is below 2^-35 of its row's largest, p * s' below 2^-31 of the largest in its sum).  sum q is 2 (fp16) or 3 (bf16) terms.  All
 // sums, m, l and parts are fp32.  Against 64 bits, outputs over 32K tokens are
 // 2.9e-4 off in fp16, of which 2.1e-4 are the output's own rounding, and 1.7e-3 in bf16, all of it that.
 //
@@ -207,8 +210,8 @@ struct State {
     uint32_t qz[3];                       // (-8, 1) * sum of q over group j, in terms of the cache's type
     float qback[2];                       // undoes q's power of two
     float m[2], l[2];
-    float o[MT][4], e[NG][4], z[NG][2];   // e: 15 and 120 times a group's sum p s', in o's unit 2^-24 (apart: a NaN stays in its group)
-    float vs, vlimit;                     // 2^-E, and the scale above which E moves
+    float o[MT][4], e[NG][4], z[NG][2];   // e: 15 and 120 times a group's sum p s', in o's unit 2^(E - 24) (apart: a NaN stays in its group)
+    float vs[NG][2];                      // 2^-E of each sum: of a group's elements in a column
 
     bool closed;                          // whether close() has put something away
 
@@ -279,11 +282,10 @@ struct State {
 #pragma unroll
         for (int k = 0; k < NG; ++k) {
             z[k][0] = z[k][1] = 0.f;
+            vs[k][0] = vs[k][1] = 0x1p126f;
 #pragma unroll
             for (int c = 0; c < 4; ++c) e[k][c] = 0.f;
         }
-        vs = 0x1p100f;
-        vlimit = -1.f;   // below any |s'|: the first page sets E
         closed = false;
     }
 
@@ -379,27 +381,31 @@ struct State {
                         for (int k = 0; k < NG; ++k) mv[p][t][k] = 0u;
                     }
         }
-        // The references m and E move only when a score passes m by more than
-        // 8 (log2 units) or a scale its limit: weights stay below 2^8, weights times scales
-        // below 2^15, and most pages skip the reductions and the rescale.
-        float vmax = 0.f, pm0 = -INFINITY, pm1 = -INFINITY;
+        // The references m and E move only when a score passes m by more than 4 (log2 units), or a
+        // scale 2^(E + 11), or a weight times scale 2^(E + 15): most pages skip the reductions and the rescale.
+        float pm[2] = {-INFINITY, -INFINITY}, smax[NG];
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-            pm0 = fmaxf(pm0, fmaxf(s[p][0], s[p][2]));
-            pm1 = fmaxf(pm1, fmaxf(s[p][1], s[p][3]));
+            pm[0] = fmaxf(pm[0], fmaxf(s[p][0], s[p][2]));
+            pm[1] = fmaxf(pm[1], fmaxf(s[p][1], s[p][3]));
 #pragma unroll
-            for (int k = 0; k < NG; ++k) vmax = fmaxf(vmax, fmaxf(fabsf(T::lo(mv[p][0][k])), fabsf(T::lo(mv[p][1][k]))));
+            for (int k = 0; k < NG; ++k) {
+                const float x = fmaxf(fabsf(T::lo(mv[p][0][k])), fabsf(T::lo(mv[p][1][k])));
+                smax[k] = p ? fmaxf(smax[k], x) : x;
+            }
         }
-        pm0 *= qback[0];
-        pm1 *= qback[1];
-        if (__any_sync(0xffffffffu, pm0 > m[0] + 8.f || pm1 > m[1] + 8.f || vmax > vlimit)) move_references(pm0, pm1, vmax);
+        pm[0] *= qback[0];
+        pm[1] *= qback[1];
+        bool moves = pm[0] > m[0] + 4.f || pm[1] > m[1] + 4.f;
+#pragma unroll
+        for (int k = 0; k < NG; ++k) moves |= smax[k] * fmaxf(vs[k][0], vs[k][1]) > 2048.f;
+        if (__any_sync(0xffffffffu, moves)) check_references(pm, smax, s, mv);
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
             const float p0 = ex2(fmaf(s[p][0], qback[0], -m[0])), p1 = ex2(fmaf(s[p][1], qback[1], -m[1]));
             const float p2 = ex2(fmaf(s[p][2], qback[0], -m[0])), p3 = ex2(fmaf(s[p][3], qback[1], -m[1]));
             l[0] += p0 + p2;
             l[1] += p1 + p3;
-            const float v0 = p0 * vs, v1 = p1 * vs, v2 = p2 * vs, v3 = p3 * vs;   // (used with four groups: fewer products)
             uint32_t va[NW], vb[NW];
             load_shared(codes + p * B::kBytes + B::kCodes, va);
             load_shared(codes + p * B::kBytes + B::kCodes + 32 * NW * 4, vb);
@@ -411,8 +417,9 @@ struct State {
                 z[k][1] = fmaf(p1, z0, fmaf(p3, z1, z[k][1]));
                 // (p s')^T as the column operand: the packed pairs are 8x8 tiles
                 // [token][n] in the fragment layout, their transposes are the operand.
-                const uint32_t b0 = movmatrix_trans(NG == 4 ? pack_f16(v0 * s0, v1 * s0) : pack_f16(p0 * (s0 * vs), p1 * (s0 * vs)));
-                const uint32_t b1 = movmatrix_trans(NG == 4 ? pack_f16(v2 * s1, v3 * s1) : pack_f16(p2 * (s1 * vs), p3 * (s1 * vs)));
+                // (In this order: s' 2^-E may pass fp32 where p is 0.)
+                const uint32_t b0 = movmatrix_trans(pack_f16(p0 * s0 * vs[k][0], p1 * s0 * vs[k][1]));
+                const uint32_t b1 = movmatrix_trans(pack_f16(p2 * s1 * vs[k][0], p3 * s1 * vs[k][1]));
                 mma_f16_16816(e[k], 0x000f000fu, 0x00780078u, 0x000f000fu, 0x00780078u, b0, b1);
 #pragma unroll
                 for (int i = k * (NW / NG); i < (k + 1) * (NW / NG); ++i) {
@@ -424,56 +431,79 @@ struct State {
         }
     }
 
-    // m and E follow the lanes' largest scores and scale.
-    __device__ __forceinline__ void move_references(float pm0, float pm1, float vmax)
+    // What a lane's largest weight and scale make bounds its products: wide scales of small weights may stay.
+    __device__ __forceinline__ void check_references(const float (&pm)[2], const float (&smax)[NG], const float (&s)[NP][4], const uint32_t (&mv)[NP][2][NG])
     {
+        const float w0 = ex2(pm[0] - m[0]), w1 = ex2(pm[1] - m[1]);   // (NaN where no token of a row counts so far)
+        bool moves = w0 > 16.f || w1 > 16.f;
 #pragma unroll
-        for (int mask = 4; mask < 32; mask <<= 1) {
-            pm0 = fmaxf(pm0, __shfl_xor_sync(0xffffffffu, pm0, mask));
-            pm1 = fmaxf(pm1, __shfl_xor_sync(0xffffffffu, pm1, mask));
-            vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, mask));
+        for (int k = 0; k < NG; ++k) moves |= fmaxf(w0 * vs[k][0], w1 * vs[k][1]) * smax[k] > 32768.f;
+        if (__any_sync(0xffffffffu, moves)) move_references(pm, s, mv);
+    }
+
+    // m follows the lanes' largest scores, E the largest weight times scale.  As m rises, what is in a
+    // sum weighs less: E falls with it (rounded up, so that the sum is not made smaller), and then rises to where
+    // the tokens at hand are in [2^6, 2^7) if they are above.
+    __device__ __forceinline__ void move_references(const float (&pm)[2], const float (&s)[NP][4], const uint32_t (&mv)[NP][2][NG])
+    {
+        float al[2], fall[2];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            float to = pm[c];
+#pragma unroll
+            for (int mask = 4; mask < 32; mask <<= 1) to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, mask));
+            to = fmaxf(to, m[c]);
+            const float by = to == m[c] ? 0.f : m[c] - to;   // (at -infinity, too)
+            al[c] = ex2(by);
+            fall[c] = __uint_as_float((uint32_t)(127 + (int)fminf(ceilf(-by), 100.f)) << 23);
+            m[c] = to;
+            l[c] *= al[c];
         }
-        const float n0 = fmaxf(m[0], pm0), n1 = fmaxf(m[1], pm1);
-        const float al0 = n0 == m[0] ? 1.f : ex2(m[0] - n0), al1 = n1 == m[1] ? 1.f : ex2(m[1] - n1);
-        m[0] = n0;
-        m[1] = n1;
-        float r = 1.f;
-        if (vmax > vlimit) {   // the same in all lanes
-            const int ex = max(-100, (int)(__float_as_uint(vmax) >> 23) - 127);
-            const float next = __uint_as_float((uint32_t)(127 + 6 - ex) << 23);   // takes vmax into [2^6, 2^7)
-            r = next * inverse_power(vs);
-            vs = next;
-            vlimit = 128.f * inverse_power(next);
-        }
-        l[0] *= al0;
-        l[1] *= al1;
+        float top[NG][2];
+#pragma unroll
+        for (int k = 0; k < NG; ++k) top[k][0] = top[k][1] = 0x1p-120f;   // E >= -126
+#pragma unroll
+        for (int p = 0; p < NP; ++p)
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const float w = ex2(fmaf(s[p][2 * t + c], qback[c], -m[c]));
+#pragma unroll
+                    for (int k = 0; k < NG; ++k) top[k][c] = fmaxf(top[k][c], fabsf(w * T::lo(mv[p][t][k])));
+                }
 #pragma unroll
         for (int k = 0; k < NG; ++k) {
-            z[k][0] *= al0;
-            z[k][1] *= al1;
-            e[k][0] *= al0 * r;
-            e[k][1] *= al1 * r;
-            e[k][2] *= al0 * r;
-            e[k][3] *= al1 * r;
-        }
+            uint32_t most = __byte_perm(__float_as_uint(top[k][0]), __float_as_uint(top[k][1]), 0x7632);   // (exponents are enough)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-            o[mt][0] *= al0 * r;
-            o[mt][1] *= al1 * r;
-            o[mt][2] *= al0 * r;
-            o[mt][3] *= al1 * r;
+            for (int mask = 4; mask < 32; mask <<= 1) most = __vmaxu2(most, __shfl_xor_sync(0xffffffffu, most, mask));
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const float next = __uint_as_float(0x82000000u - ((c ? most : most << 16) & 0x7f800000u));   // 2^6 over the power of two in most
+                const float to = fminf(vs[k][c] * fall[c], next), r = to * inverse_power(vs[k][c]) * al[c];
+                vs[k][c] = to;
+                z[k][c] *= al[c];
+                e[k][c] *= r;
+                e[k][c + 2] *= r;
+#pragma unroll
+                for (int mt = k * (MT / NG); mt < (k + 1) * (MT / NG); ++mt) {
+                    o[mt][c] *= r;
+                    o[mt][c + 2] *= r;
+                }
+            }
         }
     }
 
     // o becomes what it stands for, relative to m, with what close() has put away.
     __device__ __forceinline__ void settle(Closed<D>& sums)
     {
-        const float back = inverse_power(vs);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int mt = 0; mt < MT; ++mt) {
+            const int k = mt / (MT / NG);
 #pragma unroll
             for (int c = 0; c < 4; ++c)
-                o[mt][c] = fmaf(e[mt / (MT / NG)][c], c < 2 ? -8.f / 15.f : -128.f / 120.f, o[mt][c]) * (c < 2 ? 0x1p24f : 0x1p20f) * back;
+                o[mt][c] = fmaf(e[k][c], c < 2 ? -8.f / 15.f : -128.f / 120.f, o[mt][c]) * (c < 2 ? 0x1p24f : 0x1p20f) * inverse_power(vs[k][c & 1]);
+        }
         if (closed) {
             const Closed<D>& put = sums.hidden();
             const float f0 = put.m[0] == m[0] ? 1.f : ex2(put.m[0] - m[0]), f1 = put.m[1] == m[1] ? 1.f : ex2(put.m[1] - m[1]);
