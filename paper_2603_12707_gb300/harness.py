@@ -94,36 +94,49 @@ class Kv4Session:
     """The same session over a 4-bit cache: every step's block tables and slot
     map are built on the device from the requests' lengths, new K and V are
     quantised into their slots, and decode attention reads the 4-bit pages.
-    Nothing synchronises but ``check``."""
+
+    Everything that the session makes and does is ordered on its stream (None: the
+    default one), whatever stream is current in torch: tensors passed to ``append``
+    and ``attend`` must be ready there, and what comes back is.  ``begin_step``, ``append`` and
+    ``attend`` only enqueue; ``grow`` and ``fill_prefix`` copy host lengths to the device and
+    ``check`` reads from it, which wait for the stream."""
 
     def __init__(self, cfg: wl.WorkloadConfig, extra_tokens: int = 8, group: int = 64, device="cuda", stream=None,
                  lens=None, slack_pages: int = 8):
         import torch
         self.cfg = cfg
         self.stream = stream
+        self._torch, self._i32 = torch, dict(dtype=torch.int32, device=device)
         self.lens0 = np.array(wl.context_lengths(cfg) if lens is None else lens, dtype=np.int64)
         self.lens = np.zeros_like(self.lens0)      # held so far: fill_prefix admits the requests
         P = kv4.PAGE_SIZE
         max_pages = int((int(self.lens0.max()) + extra_tokens + P - 1) // P)
         num_pages = int(sum((int(n) + extra_tokens + P - 1) // P for n in self.lens0)) + slack_pages
-        self.pools = [kv4.Pool.empty(num_pages, cfg.num_kv_heads, cfg.head_dim, group, device=device)
-                      for _ in range(cfg.phys_layers)]
-        self.tables = kv4.Tables.empty(num_pages, cfg.batch, max(1, max_pages), device=device)
-        order = wl.page_order(cfg, num_pages)
-        if order is not None:
-            self.tables.free_ring.copy_(torch.from_numpy(order))
-        i32 = dict(dtype=torch.int32, device=device)
-        self.error = torch.zeros(1, **i32)
-        self.ones = torch.ones(cfg.batch, **i32)
-        self.step_slots = torch.empty(cfg.batch, dtype=torch.int64, device=device)
-        self.workspace = kv4.kv4_workspace(self.pools[0], cfg.num_q_heads)
-        self._torch, self._i32 = torch, i32
+        with self._on_stream():
+            self.pools = [kv4.Pool.empty(num_pages, cfg.num_kv_heads, cfg.head_dim, group, device=device)
+                          for _ in range(cfg.phys_layers)]
+            self.tables = kv4.Tables.empty(num_pages, cfg.batch, max(1, max_pages), device=device)
+            order = wl.page_order(cfg, num_pages)
+            if order is not None:
+                self.tables.free_ring.copy_(torch.from_numpy(order))
+            self.error = torch.zeros(1, **self._i32)
+            self.ones = torch.ones(cfg.batch, **self._i32)
+            self.step_slots = torch.empty(cfg.batch, dtype=torch.int64, device=device)
+            self.workspace = kv4.kv4_workspace(self.pools[0], cfg.num_q_heads)
+
+    def _on_stream(self):
+        """torch's work and memory on the session's stream: a block that is freed is handed out again behind what reads it."""
+        cuda, s = self._torch.cuda, self.stream
+        if not isinstance(s, cuda.Stream):
+            s = cuda.ExternalStream(int(s)) if s else cuda.default_stream()
+        return cuda.stream(s)
 
     def grow(self, new_lens):
         """Requests grow by new_lens tokens (host sequence), or give -n back; returns the new tokens' slots."""
-        new = self._torch.tensor([int(n) for n in new_lens], **self._i32)
-        slots = self._torch.empty(int(sum(max(0, int(n)) for n in new_lens)), dtype=self._torch.int64, device=new.device)
-        kv4.kv_tables_step(self.tables, None, new, slots, device_error=self.error, stream=self.stream)
+        with self._on_stream():
+            new = self._torch.tensor([int(n) for n in new_lens], **self._i32)
+            slots = self._torch.empty(int(sum(max(0, int(n)) for n in new_lens)), dtype=self._torch.int64, device=new.device)
+            kv4.kv_tables_step(self.tables, None, new, slots, device_error=self.error, stream=self.stream)
         self.lens += np.array(new_lens, dtype=np.int64)
         return slots
 
@@ -131,9 +144,11 @@ class Kv4Session:
         """Admit every request and write its cached prefix into the given layer pools."""
         cfg = self.cfg
         slots = self.grow(self.lens0)
-        for l in range(cfg.phys_layers) if layers is None else layers:
-            k, v, _ = wl.packed_prefix(cfg, [l], self.lens0, slots.device)
-            kv4.kv4_write(self.pools[l], slots, k[0], v[0], device_error=self.error, stream=self.stream)
+        with self._on_stream():
+            for l in range(cfg.phys_layers) if layers is None else layers:
+                k, v, _ = wl.packed_prefix(cfg, [l], self.lens0, slots.device)
+                kv4.kv4_write(self.pools[l], slots, k[0], v[0], device_error=self.error, stream=self.stream)
+                del k, v
 
     def begin_step(self):
         kv4.kv_tables_step(self.tables, None, self.ones, self.step_slots, device_error=self.error, stream=self.stream)
@@ -151,7 +166,8 @@ class Kv4Session:
                                  softmax_scale=scale, device_error=self.error, stream=self.stream)
 
     def check(self):
-        """Wait for the device and raise if a call has found something wrong."""
-        bits = int(self.error.item())
+        """Wait for the session's stream and raise if a call has found something wrong."""
+        with self._on_stream():
+            bits = int(self.error.item())
         if bits:
             raise RuntimeError(f"device error bits {bits:#x}")
