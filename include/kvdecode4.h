@@ -113,7 +113,8 @@ KVC_API int64_t kv4_pool_bytes(const kv4_pool *pool);
  * (KVC_DEVERR_SEQ_RANGE), where its new tokens pass max_tokens (the same), or
  * where the free pages do not cover what it and the rows before it need
  * (KVC_DEVERR_OOM; rows that need no page still grow).  A page id outside the
- * pool sets KVC_DEVERR_PAGE_RANGE, and its tokens get slot -1.  Should the
+ * pool sets KVC_DEVERR_PAGE_RANGE; its tokens get slot -1, and where it is given back it is
+ * left out: it does not become a free page.  Should the
  * pages given back not fit the ring (a page given back twice), all rows that
  * give back are refused with KVC_DEVERR_PAGE_RANGE. */
 KVC_API int kv_tables_step(const kv_tables *tables, int32_t batch, const int32_t *seq_ids, const int32_t *new_lens,

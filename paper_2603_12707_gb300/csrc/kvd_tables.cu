@@ -207,16 +207,43 @@ __global__ void __launch_bounds__(kMaxThreads) tables_kernel(TablesArgs a)
         if (row_page[i] >= 0 && (fits || n >= 0)) a.lens_out[row_seq[i]] = row_len[i] + n;
     }
     // The k-th page given back: from its row's first page that is not needed any more.
-    const int back = fits ? (int)total.back() : 0;
-    r = 0;
+    // Ids outside the pool are left out: where there are any, one warp does it again, and those behind move up.
+    const int total_back = fits ? (int)total.back() : 0;
+    int back = total_back, workers = threads;
+    bool bad = false;
 #pragma unroll 1
-    for (int k = tid; k < back; k += threads) {
-        r = find_row(row_back, r, a.batch, k);
-        const int kept = pages_of(row_len[r] + a.new_lens[r]);
-        const int32_t page = a.block_table[(int64_t)row_seq[r] * a.max_pages + kept + (k - row_back[r])];
-        int64_t to = head + count + k;
-        if (to >= a.num_pages) to -= a.num_pages;
-        a.ring[to] = page;
+    for (int pass = 0; pass < 2; ++pass) {
+        int given = 0;
+        r = 0;
+#pragma unroll 1
+        for (int k0 = 0; k0 < total_back; k0 += workers) {
+            const int k = k0 + tid;
+            int32_t page = -1;
+            if (k < total_back) {
+                r = find_row(row_back, r, a.batch, k);
+                const int kept = pages_of(row_len[r] + a.new_lens[r]);
+                page = a.block_table[(int64_t)row_seq[r] * a.max_pages + kept + (k - row_back[r])];
+            }
+            const bool fine = page >= 0 && page < a.num_pages;
+            bad |= !fine && k < total_back;
+            int at = k;
+            if (pass == 1) {
+                const uint32_t some = __ballot_sync(0xffffffffu, fine);
+                at = given + __popc(some & ((1u << tid) - 1u));
+                given += __popc(some);
+            }
+            int64_t to = head + count + at;
+            if (to >= a.num_pages) to -= a.num_pages;
+            if (fine) a.ring[to] = page;
+        }
+        if (pass == 1) {
+            back = given;
+            break;
+        }
+        if (!__syncthreads_or(bad)) break;
+        if (tid == 0) kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
+        if (tid >= 32) return;
+        workers = 32;
     }
     if (tid == 0) {
         if (a.cu) a.cu[a.batch] = (int32_t)min(total.tokens, (int64_t)INT32_MAX);
