@@ -119,11 +119,12 @@ __device__ __forceinline__ uint32_t range_of(const uint4& row)
 
 constexpr uint32_t kBroken = 0x7fff7fffu;     // the scale word of a group with an infinity or a NaN: NaN in either type
 
-// bf16's tiny steps are scaled up, exactly, so that 1 / s is finite.
+// bf16's tiny steps are scaled up, exactly, so that 1 / s is finite (elements are tiny then, too; a step of
+// 0 may have large ones, which would overflow).
 template <class T>
 __device__ __forceinline__ float scale_up(float s)
 {
-    return Packed<T>::kTiny && s < 0x1p-100f ? 0x1p64f : 1.f;
+    return Packed<T>::kTiny && s < 0x1p-100f && s > 0.f ? 0x1p64f : 1.f;
 }
 
 // The scale word (s, z) of a group's (min, -max), and 1 / s (scaled down by scale_up; 0 for a
