@@ -59,8 +59,10 @@ extern "C" {
  * Quantisation of a group's values x: s = rn16((max/2 - min/2) / 7.5),
  * z = rn16(min + 8 s), c = clamp(rint((x - z) / s) + 8, 0, 15), with the
  * difference and the sum in 32 bits, rn16 and rint (of the exact quotient) to
- * nearest even; c = 8 where s is 0.  A group that holds an infinity or a NaN
- * stands for NaN in all its elements. */
+ * nearest even; c = 8 where s is 0.  Where z + 7 s or z - 8 s would round to an
+ * infinity (a group that holds numbers at the end of the type's range), s is the next
+ * smaller number and z = min + 8 s is rounded toward zero: what is finite stays finite.
+ * A group that holds an infinity or a NaN stands for NaN in all its elements. */
 typedef struct kv4_pool {
     void *data;            /* device, kv4_pool_bytes() bytes, 128-byte aligned   */
     int64_t num_pages;     /* 1 .. 2^31 - 1                                      */
@@ -155,7 +157,9 @@ KVC_API int64_t kv4_workspace_bytes(const kv4_pool *pool, int32_t num_q_heads);
  * is written.  Scores, softmax statistics and sums are held in 32 bits.  What meets
  * V's codes, a token's weight times its scale, is rounded to 11 bits, below 2^-20 of the
  * largest of its sum (a query head's over the elements of a scale group) to
- * multiples of 2^-30 of that.  A q that is not finite gives NaN.  The result of a call does
+ * multiples of 2^-30 of that.  Outputs that would round to an infinity are the type's
+ * largest number; sums of weights up to 16 times V have to be numbers of 32 bits (bf16: V
+ * below 2^100 always is).  A q that is not finite gives NaN.  The result of a call does
  * not depend on timing: partial results are merged in the order of their tokens. */
 KVC_API int kv4_decode_attention(const kv4_pool *pool, const kv_tables *tables, int32_t batch, const int32_t *seq_ids,
                                  int32_t num_q_heads, const void *q, int64_t q_stride, void *out, int64_t out_stride,

@@ -75,11 +75,27 @@ struct Bf16 {
     static __device__ __forceinline__ float lo(uint32_t w) { return __uint_as_float(w << 16); }
     static __device__ __forceinline__ float hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
     static __device__ __forceinline__ uint32_t pack(float a, float b) { return pack_bf16(a, b); }
+    static __device__ __forceinline__ uint32_t pack_finite(float a, float b)   // (what rounds to an infinity: the largest number)
+    {
+        uint32_t r;
+        asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+        return r;
+    }
+    static __device__ __forceinline__ uint32_t toward_zero(float a) { return __float_as_uint(a) >> 16; }
+    static constexpr float kOver = 0x1.ffp127f, kNear = 0x1.f0p127f;   // the least that rounds to infinity; groups below kNear hold nothing that does
 };
 struct Fp16 {
     static __device__ __forceinline__ float lo(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w & 0xffffu))); }
     static __device__ __forceinline__ float hi(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w >> 16))); }
     static __device__ __forceinline__ uint32_t pack(float a, float b) { return pack_f16(a, b); }
+    static __device__ __forceinline__ uint32_t pack_finite(float a, float b)
+    {
+        uint32_t r;
+        asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+        return r;
+    }
+    static __device__ __forceinline__ uint32_t toward_zero(float a) { return __half_as_ushort(__float2half_rz(a)); }
+    static constexpr float kOver = 65520.f, kNear = 65300.f;
 };
 
 __device__ __forceinline__ void kv4_error(int32_t* err, int32_t bit)

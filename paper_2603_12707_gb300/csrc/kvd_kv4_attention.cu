@@ -566,7 +566,7 @@ struct State {
             uint16_t* out = a.out + b * a.out_stride + (int64_t)(h * a.G + n) * D + g;
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
-                const uint32_t w = T::pack(o[mt][c] * inv, o[mt][c + 2] * inv);
+                const uint32_t w = T::pack_finite(o[mt][c] * inv, o[mt][c + 2] * inv);
                 out[16 * mt] = (uint16_t)w;
                 out[16 * mt + 8] = (uint16_t)(w >> 16);
             }
@@ -682,7 +682,7 @@ struct RowSum {
         const float inv = l == 0.f ? 0.f : rcp(l);
         uint16_t* out = a.out + b * a.out_stride + (int64_t)(h * a.G + n) * D + lane * E;
 #pragma unroll
-        for (int i = 0; i < E; i += 2) *reinterpret_cast<uint32_t*>(out + i) = T::pack(o[i] * inv, o[i + 1] * inv);
+        for (int i = 0; i < E; i += 2) *reinterpret_cast<uint32_t*>(out + i) = T::pack_finite(o[i] * inv, o[i + 1] * inv);
         if (a.lse && lane == 0) a.lse[(int64_t)b * a.Hq + h * a.G + n] = (m + lg2(l)) * kLn2;
     }
 };

@@ -129,6 +129,11 @@ __device__ __forceinline__ float scale_up(float s)
 
 // The scale word (s, z) of a group's (min, -max), and 1 / s (scaled down by scale_up; 0 for a
 // step of 0, which makes every quotient 0).
+//
+// Where z + 7 s or z - 8 s would round to an infinity, s is the next smaller number and z is rounded toward
+// zero.  Then 15 s is at least 7.5 units of s below max - min, so the top is below max where z > 0; where z < 0 the top would
+// need 7 s past the type's range, which 15 s has.  The bottom is at least min where z < 0; where z > 0 it is
+// less than a unit of z below, and s is above an eighth of the range there, z below a fifteenth.
 template <class T>
 __device__ __forceinline__ uint32_t scale_of(uint32_t range, float* r)
 {
@@ -136,10 +141,15 @@ __device__ __forceinline__ uint32_t scale_of(uint32_t range, float* r)
     const float half = most * 0.5f - least * 0.5f;
     // half / 7.5, corrected once like the quotients below.
     const float h0 = half * (1.f / 7.5f);
-    const uint32_t step = T::pack(fmaf(fmaf(-7.5f, h0, half), 1.f / 7.5f, h0), 0.f);
-    const float s = T::lo(step);
+    uint32_t step = T::pack(fmaf(fmaf(-7.5f, h0, half), 1.f / 7.5f, h0), 0.f);
+    float s = T::lo(step);
+    uint32_t middle = T::pack(fmaf(8.f, s, least), 0.f);
+    if (fmaxf(most, -least) > T::kNear && (fmaf(7.f, s, T::lo(middle)) >= T::kOver || fmaf(-8.f, s, T::lo(middle)) <= -T::kOver)) {
+        s = T::lo(--step);
+        middle = T::toward_zero(fmaf(8.f, s, least));
+    }
     *r = s > 0.f ? 1.f / (s * scale_up<T>(s)) : 0.f;
-    return half < INFINITY ? __byte_perm(step, T::pack(fmaf(8.f, s, least), 0.f), 0x5410) : kBroken;
+    return half < INFINITY ? __byte_perm(step, middle, 0x5410) : kBroken;
 }
 
 // The codes of this lane's 8 elements, as K's words hold them (element e in
