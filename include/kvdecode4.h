@@ -149,7 +149,7 @@ KVC_API int64_t kv4_workspace_bytes(const kv4_pool *pool, int32_t num_q_heads);
  *   lse       device [batch][num_q_heads] float, out, or NULL: the natural
  *             logarithm of each softmax's denominator, sum_t exp(scale q.k_t)
  *   workspace device, workspace_bytes >= kv4_workspace_bytes(), 256-byte aligned
- * softmax_scale <= 0 selects 1 / sqrt(head_dim).  A request of length 0 gives
+ * softmax_scale (below 2^100) <= 0 selects 1 / sqrt(head_dim).  A request of length 0 gives
  * zeros and lse = -infinity; so does one whose id is out of range or whose length is
  * negative or above max_pages * 16, with KVC_DEVERR_SEQ_RANGE.  The tokens of a
  * page id outside the pool are left out, with KVC_DEVERR_PAGE_RANGE.  Rows that
@@ -159,7 +159,7 @@ KVC_API int64_t kv4_workspace_bytes(const kv4_pool *pool, int32_t num_q_heads);
  * largest of its sum (a query head's over the elements of a scale group) to
  * multiples of 2^-30 of that.  Outputs that would round to an infinity are the type's
  * largest number; sums of weights up to 16 times V have to be numbers of 32 bits (bf16: V
- * below 2^100 always is).  A q that is not finite gives NaN.  The result of a call does
+ * below 2^90 always is).  A q that is not finite gives NaN.  The result of a call does
  * not depend on timing: partial results are merged in the order of their tokens. */
 KVC_API int kv4_decode_attention(const kv4_pool *pool, const kv_tables *tables, int32_t batch, const int32_t *seq_ids,
                                  int32_t num_q_heads, const void *q, int64_t q_stride, void *out, int64_t out_stride,

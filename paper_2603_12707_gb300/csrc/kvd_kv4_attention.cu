@@ -1125,8 +1125,8 @@ extern "C" KVC_API int kv4_decode_attention(const kv4_pool* pool, const kv_table
         return kv4_fail(KVC_ERR_INVALID, "kv4_decode_attention: rows must be 16-byte aligned, strides multiples of 8 elements");
     if (batch > 1 && (q_stride < 0 || out_stride < (int64_t)num_q_heads * pool->head_dim))
         return kv4_fail(KVC_ERR_INVALID, "kv4_decode_attention: q_stride must be >= 0, out rows must not overlap");
-    if (!(softmax_scale <= 0.f) && !std::isfinite(softmax_scale))
-        return kv4_fail(KVC_ERR_INVALID, "kv4_decode_attention: softmax_scale must be finite");
+    if (!(softmax_scale < 0x1p100f))   // (with the scores' unit it has to be a number of 32 bits)
+        return kv4_fail(KVC_ERR_INVALID, "kv4_decode_attention: softmax_scale must be below 2^100");
     if (!kv4_aligned(workspace, 256) || workspace_bytes < 256)
         return kv4_fail(KVC_ERR_INVALID, "kv4_decode_attention: workspace must be 256-byte aligned and of kv4_workspace_bytes()");
     const int sms = device_sms();

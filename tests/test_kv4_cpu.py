@@ -112,3 +112,17 @@ def test_table_steps_that_are_refused(kv4):
     assert call(batch=0) == INVALID and call(batch=5) == INVALID and call(batch=4097, ids=16) == INVALID
     for kw in (dict(free_ring=None), dict(free_state=None), dict(num_pages=0), dict(num_pages=2 ** 31)):
         assert call(t=tables(kv4, **kw)) == INVALID
+
+
+def test_softmax_scales_that_overflow_are_refused(kv4):
+    """Scores are held in a unit of 2^-21: a scale that is no number there made every output NaN."""
+    ref = ctypes.addressof
+    p, t = pool(kv4), tables(kv4)
+
+    def call(scale):
+        return kv4._load()["kv4_decode_attention"](ref(p), ref(t), 2, None, 8, 16, 1024, 16, 1024, None, scale, 256, 0, None, None)
+
+    for scale in (2.0 ** 100, 1e33, 3e38, float("inf"), float("nan")):
+        assert call(scale) == INVALID and "softmax_scale" in kv4.kd.load().kv_last_error().decode()
+    for scale in (2.0 ** 99, 0.0, -1.0, float("-inf")):    # refused for its workspace, after the scale
+        assert call(scale) == INVALID and "workspace" in kv4.kd.load().kv_last_error().decode()
