@@ -87,3 +87,56 @@ def test_a_full_pool_is_reported(kvlib):
     sess.begin_step()
     with pytest.raises(RuntimeError, match="0x8"):
         sess.check()
+
+
+def held_rows(blocks, pages, n, side, d, group):
+    """Values and steps of a request's n tokens, and the sizes of their middles, float64 [n, H, D]."""
+    c, s, z = (x[np.arange(n) // P if pages is None else pages[np.arange(n) // P], :, np.arange(n) % P]
+               for x in unpack(blocks, d, group, torch.bfloat16)[side])
+    return s * (c - 8) + z, s, np.abs(z)
+
+
+@pytest.mark.parametrize("cfg,group", [
+    (wl.custom("kv4_near_gqa", 1, 28, 4, 128, 4, lens=[17, 300, 64, 1], seed=31), 32),
+    (wl.custom("kv4_near_mha", 1, 8, 8, 128, 3, lens=[5, 1000, 16], seed=32), 128),
+    (wl.custom("kv4_near_d64", 1, 14, 2, 64, 3, lens=[900, 33, 2], seed=33), 64),
+])
+def test_what_is_held_and_attended_is_near_what_was_written(kvlib, cfg, group):
+    """Against the original K and V, not their codes.  A value is off by at most half a step and the roundings of s
+    and z to the type: u = 2^-8 of each, 7.5 and 1 times.  Over tokens those errors are spread evenly: a score is off by a
+    standard deviation of scale sqrt(sum_d q_d^2 s^2 / 12 + sum_groups (sum_d q_d)^2 (u z)^2 / 3), an output by
+    sqrt(sum_t w^2 (s'^2 / 12 + (u z')^2 / 3 + score^2 (v - o)^2)); six of them, the change of weights to first order and a
+    quarter more for the rest, and what the arithmetic and the output's type add (2^-8 of the output and 1 % of a step)."""
+    from paper_2603_12707_gb300.harness import Kv4Session
+    sess = Kv4Session(cfg, extra_tokens=4, group=group)
+    sess.fill_prefix()
+    sess.begin_step()
+    q, kn, vn = wl.step_inputs(cfg, 0, 0, "cuda")
+    out = torch.empty_like(q)
+    sess.append(0, kn, vn)
+    sess.attend(0, q, out)
+    sess.check()
+    blocks, table = held(sess, 0)
+    d, hq, hkv = cfg.head_dim, cfg.num_q_heads, cfg.num_kv_heads
+    qd, got, scale, u = q.double().cpu().numpy(), out.double().cpu().numpy(), d ** -0.5, 2.0 ** -8
+    for b in range(cfg.batch):
+        n = int(sess.lens[b])
+        rows = []
+        for side, (kind, new) in enumerate((("k", kn), ("v", vn))):
+            x = torch.cat([wl.kv_block(cfg, 0, b, n - 1, kind, "cuda"), new[b:b + 1]]).double().cpu().numpy()
+            y, s, z = held_rows(blocks, table[b], n, side, d, group)
+            assert (np.abs(x - y) <= s * (0.5 + 7.5 * u) + z * u + 1e-30).all()
+            rows.append((x, s, z))
+        (k, sk, zk), (v, sv, zv) = rows
+        for h in range(hq):
+            g = h // (hq // hkv)
+            x = k[:, g] @ qd[b, h] * scale
+            w = np.exp(x - x.max())
+            w /= w.sum()
+            o = w @ v[:, g]
+            sums = qd[b, h].reshape(-1, group).sum(-1)
+            score = scale * np.sqrt((qd[b, h] ** 2 * sk[:, g] ** 2).sum(-1) / 12 + (sums ** 2 * (u * zk[:, g, ::group]) ** 2).sum(-1) / 3)
+            dev = np.sqrt((w ** 2) @ (sv[:, g] ** 2 / 12 + (u * zv[:, g]) ** 2 / 3 + score[:, None] ** 2 * (v[:, g] - o) ** 2))
+            lim = 6 * 1.25 * dev + u * np.abs(o) + 0.01 * sv[:, g].max()
+            err = np.abs(got[b, h] - o)
+            assert (err <= lim).all(), (b, h, float((err - lim).max()))
