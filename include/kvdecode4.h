@@ -77,7 +77,9 @@ typedef struct kv4_pool {
  * hold anything.  The free pages are free_ring[(free_state[0] + k) %
  * num_pages], k < free_state[1], the next one to be handed out first;
  * free_state[2] and [3] belong to the library and start at zero.  A request's
- * pages are its own. */
+ * pages are its own.  They serve the pools of this header: decode_attention_noalloc takes its
+ * lengths from the host.  Tokens given back are drafts that the caller has rejected; what
+ * verifies them lies with the caller, the attention here takes one token a request. */
 typedef struct kv_tables {
     int32_t *block_table;  /* device, [max_seqs][max_pages]                      */
     int32_t *lens;         /* device, [max_seqs]                                 */

@@ -54,11 +54,11 @@
 // 2.9e-4 off in fp16, of which 2.1e-4 are the output's own rounding, and 1.7e-3 in bf16, all of it that.
 //
 // Measured (device, calls in a graph; 6.8 TB/s is a copy's rate).  64 rows of 640 - 1344
-// tokens, 32 KV heads, d 128: 57.0 us, 288 MB, 5.1 TB/s; 8 rows of 32K tokens,
-// 28 query on 4 KV heads, groups of 32: 39.7 us, 168 MB, 4.2 TB/s; one row of 2337: 9.6 us.
-// A further byte costs 1 / 6.4 TB/s (groups of 128), 6.2 (64), 5.9 (32), 5.5 (d 64): close
-// to memory, beside which a tile's 275 to 365 instructions keep the ALU 57 % and
-// the tensor cores 33 % busy.  What is left is fixed, some 12 us a call: the
+// tokens, 32 KV heads, d 128: 60.3 us, 288 MB, 4.8 TB/s; 8 rows of 32K tokens,
+// 28 query on 4 KV heads, groups of 32: 42.7 us, 168 MB, 3.9 TB/s; one row of 2337: 9.8 us.
+// A further byte costs 1 / 6.1 TB/s (groups of 128), 5.5 (64), 5.5 (32), 5.3 (d 64): close
+// to memory, beside which a tile's 290 to 406 instructions keep the ALU 56 % and
+// the tensor cores 31 % busy.  What is left is fixed, some 13 us a call: the
 // scan and the search 2.5, first tiles 1, the end of the shares and the CTA's merge 3, the
 // second launch 2 to 3, and that a launch fetches its instructions anew (loops stay
 // rolled and every large part has one call site: 74 KB -> 53 KB of code took one short row from 15.8 to 10.6 us).
@@ -74,7 +74,7 @@ namespace {
 constexpr uint64_t kWaitLimitNs = 1000000000ull;
 constexpr float kLn2 = 0.6931471805599453f;
 // What starting and ending a (row, KV head) costs a warp, in tiles: shares count it
-// (64 rows of 0 - 8192 tokens, log-uniform: 57 us, 102 where shares are tiles alone).
+// (64 rows of 0 - 8192 tokens, log-uniform: 55 us, 115 where shares are tiles alone).
 constexpr uint32_t kRowCost = 3;
 // What a warp takes at least, in tiles: a small call uses fewer warps rather than merge more parts.
 constexpr uint32_t kMinShare = 2;

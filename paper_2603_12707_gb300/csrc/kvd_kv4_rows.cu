@@ -9,9 +9,9 @@
 // codes; V's words hold elements 8 apart, four lanes' codes each, and are made by a transposition across lanes.
 //
 // Measured on 57344 tokens of 32 heads of 128, groups of 64, bf16 (1.20 GB each
-// way, 177 us at the speed of a copy): kv4_write 240 us, 5.0 TB/s, bound by the
-// instructions (245 for a pair's head; the schedulers issue 77 % of cycles, ALU and FMA pipes are 64 % busy);
-// kv4_read 196 us, 6.1 TB/s, bound by memory.  32 warps an SM (64
+// way, 177 us at the speed of a copy): kv4_write 247 us, 4.9 TB/s, bound by the
+// instructions (254 for a pair's head; the schedulers issue 77 % of cycles, the ALU pipe is 66 % busy);
+// kv4_read 197 us, 6.1 TB/s, bound by memory.  32 warps an SM (64
 // registers) do better than 24 in both.  A call for 64 tokens takes 2.6 and 2.1 us of the device.
 #include "kvd_kv4.h"
 #include "kvd_ptx.cuh"

@@ -16,9 +16,9 @@
 //
 // A small call is latency, and much of that the fetching of its instructions
 // (every launch fetches them anew): loops stay rolled.  On the device, 32 rows
-// that decode take 3.6 us, 157 mixed rows 5.3, 1500 prompts of 450K
-// tokens 10.0 (5.7 MB; the scan over the rows, then 0.6 TB/s of stores whose rows
-// each thread looks up for four tokens at a time).
+// that decode take 3.6 us, 157 mixed rows 5.1, 1500 prompts of 450K
+// tokens 10.0 (5.7 MB; the scan over the rows, then for every token a search of its row,
+// which starts at the thread's last one, a load of its page id, and two stores).
 #include "kvd_kv4.h"
 #include "kvd_ptx.cuh"
 
