@@ -99,7 +99,7 @@ def run(kv4, blocks, table, lens, kept, q, hkv, group, dtype, rows=4096, scale=0
             continue
         le = np.abs(lse[at] - r_lse[which[at]])
         assert (le <= lse_lim[which[at]]).all(), (i, n, float((le - lse_lim[which[at]]).max()))
-        for j in range(q.shape[0]):
+        for j in np.unique(which[at]):
             off = e[which[at] == j].mean((0, 2))
             assert (np.abs(off) <= mean[j]).all(), (i, n, j, off, mean[j])
         errors.append(e)
