@@ -17,7 +17,7 @@ INCLUDE = os.path.join(ROOT, "include")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libkvdecode.so")
 SOURCES = ["kvd_host.cpp", "kvd_rules.cpp", "kvd_cache.cu", "kvd_decode.cu", "kvd_merge.cu", "kvd_cluster.cu", "kvd_noalloc.cu",
-           "kvd_tables.cu", "kvd_kv4_rows.cu", "kvd_kv4_attention.cu"]
+           "kvd_tables.cu", "kvd_kv4_rows.cu", "kvd_kv4_attention.cu", "kvd_rope.cu", "kvd_kv16_plan.cu", "kvd_kv16_attention.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -30,7 +30,7 @@ def nvcc() -> str:
 
 def _inputs():
     files = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
-    files += [os.path.join(INCLUDE, f) for f in ("kvdecode.h", "kvdecode4.h")]
+    files += [os.path.join(INCLUDE, f) for f in ("kvdecode.h", "kvdecode4.h", "kvdecode16.h")]
     files.append(os.path.abspath(__file__))
     return files
 
