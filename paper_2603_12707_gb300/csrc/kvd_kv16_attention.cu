@@ -30,10 +30,12 @@
 namespace kvd {
 namespace {
 
-constexpr uint64_t kLimitNs = 1000000000ull;
-constexpr int kThreads = 32 * kAttnWarps;
-constexpr int kTilePages = 8;                      // of a tile of a large run: 128 tokens
-constexpr int kLoadWarp = 8, kMmaWarp = 9;         // after two streams of four softmax warps
+constexpr uint64_t kLimitNs = 1000000000ull;       // of waits for copies before leaving
+constexpr long long kLimitCycles = 2000000000ll;   // of all others: a second
+constexpr int kSoftmaxWarps = 16;                  // two streams of two halves of four
+constexpr int kThreads = 32 * (kSoftmaxWarps + 4);
+constexpr int kRegisters = 96;                     // of a thread at launch
+constexpr int kLoadWarp = kSoftmaxWarps, kMmaWarp = kSoftmaxWarps + 1;
 
 template <int D>
 struct Geo {
@@ -46,7 +48,6 @@ struct Geo {
     static constexpr int kStages = D == 128 ? 2 : 4;              // of a record warp's ring: K and V of a page each
     static constexpr int kWarpRing = kStages * 2 * kPageBytes;
     static constexpr int kData = kRing + kSlots * kTileBytes > kAttnWarps * kWarpRing ? kRing + kSlots * kTileBytes : kAttnWarps * kWarpRing;
-    static constexpr int kSmem = kData + 1024;
 };
 
 template <class T>
@@ -73,14 +74,28 @@ struct AttnArgs {
     int32_t* err;
 };
 
+constexpr int kSegments = 8;         // told ahead: a tile at least each, so the ring ends it at five
+
 struct Control {                     // in shared memory
-    uint64_t full[16], empty[16];    // ring slots of large runs
+    uint64_t full[10], empty[10];    // ring slots of large runs
+    uint64_t told[kSegments];
     uint64_t scores[2], weights[2], output[2], queries, drained;   // by stream
-    uint64_t stage[kAttnWarps][4];   // rings of record warps
-    int32_t pages_known[8];          // by tile: bits of its pages that are there (a tile's scores are worked before the 5th after it is loaded)
+    uint64_t pair[2][4];             // of a stream's two warps with the same rows
+    int32_t pair_again[2][2][4];     // [stream][half][rows]: its weights want a higher reference
+    float pair_value[2][2][4][32];   // a row's largest score, or its sum of weights
+    int32_t pages_known[8];          // by tile: bits of its pages that are there (a tile's are read before the eighth after it is loaded)
     uint32_t tmem;
     int32_t gave_up;                 // a wait ran out: everybody leaves
+    uint64_t last;                   // what was issued before leaving so
+    union {
+        Segment segment[kSegments];
+        uint64_t stage[kAttnWarps][4];   // rings of record warps
+    };
 };
+
+template <int D>
+constexpr int kSharedBytes = Geo<D>::kData + (int)sizeof(Control);
+static_assert(kSharedBytes<128> <= 232448 && kSharedBytes<64> <= 232448, "shared memory of a CTA");
 
 __device__ __forceinline__ bool plan_fits(const PlanHeader& h, const AttnArgs& a)
 {
@@ -93,29 +108,14 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, Contro
 {
     const uint32_t addr = smem_addr(bar);
     if (__all_sync(0xffffffffu, mbar_try_wait(addr, parity))) return true;
-    const uint64_t t0 = global_timer_ns();
+    const long long t0 = clock64();
     while (true) {
         const bool ok = mbar_try_wait(addr, parity);
-        const bool late = global_timer_ns() - t0 > kLimitNs || *reinterpret_cast<volatile int32_t*>(&c.gave_up);
+        const bool late = clock64() - t0 > kLimitCycles || *reinterpret_cast<volatile int32_t*>(&c.gave_up);
         if (__all_sync(0xffffffffu, ok)) return true;
         if (__any_sync(0xffffffffu, late)) {
             *reinterpret_cast<volatile int32_t*>(&c.gave_up) = 1;
             if ((threadIdx.x & 31) == 0) kv4_error(err, KVC_DEVERR_WAIT_TIMEOUT);
-            return false;
-        }
-    }
-}
-
-__device__ __forceinline__ bool thread_wait(uint64_t* bar, uint32_t parity, Control& c, int32_t* err)
-{
-    const uint32_t addr = smem_addr(bar);
-    if (mbar_try_wait(addr, parity)) return true;
-    const uint64_t t0 = global_timer_ns();
-    while (true) {
-        if (mbar_try_wait(addr, parity)) return true;
-        if (global_timer_ns() - t0 > kLimitNs || *reinterpret_cast<volatile int32_t*>(&c.gave_up)) {
-            *reinterpret_cast<volatile int32_t*>(&c.gave_up) = 1;
-            kv4_error(err, KVC_DEVERR_WAIT_TIMEOUT);
             return false;
         }
     }
@@ -127,307 +127,367 @@ __device__ __forceinline__ void arrive(uint64_t* bar)
 }
 
 // ------------------------------------------------------------ large runs, tcgen05
-// A worker's segments: pages [page, stop) of a job.
-struct Segment {
-    int run, job, page, stop;
-    Run r;
-    int head, row0, rows;        // KV head, first batch row, batch rows
-    bool wide;                   // each stream has rows of its own
-    int rows0;                   // batch rows of stream 0 (wide), else of both
-    __device__ __forceinline__ int tiles() const { return (stop - page + kTilePages - 1) / kTilePages; }
+// Both streams work on every tile (wide), or they take turns.  Tiles of K run ahead of those of V by one for each tile that is
+// in work, so the ring's order within a segment is K 0 .. A - 1, then V n, K n + A, as far as there are any: where a tile lies in it.
+struct Order {
+    int ahead, tiles;
+    __device__ __forceinline__ Order(int n, bool wide) : ahead(min(wide ? 1 : 2, n)), tiles(n) {}
+    __device__ __forceinline__ int k(int j) const { return j < ahead ? j : 2 * j - ahead + 1; }
+    __device__ __forceinline__ int v(int n) const { return min(ahead + 2 * n, tiles + n); }
 };
 
-struct Segments {
-    const AttnArgs& a;
-    int run, job, page;
-    int64_t end;                 // of this worker's share, in cost units
-    __device__ __forceinline__ Segments(const AttnArgs& args, const PlanHeader& h, int worker) : a(args)
-    {
-        const CtaStart s = a.view.cta_starts[worker];
-        run = s.run;
-        job = s.job;
-        page = s.page;
-        end = share_start(worker + 1, h.cost, h.prefix_ctas);
-    }
-    __device__ __forceinline__ bool next(Segment& s)
-    {
-        while (run < a.batch) {
-            s.r = a.view.runs[run];
-            const int jobs = s.r.chunks * a.hkv;
-            if (s.r.pages == 0 || job >= jobs) {
-                run += s.r.pages == 0 ? 1 : s.r.rows;
-                job = page = 0;
-                continue;
-            }
-            const int w = page_cost(s.r.rows, s.r.chunks, a.G);
-            const int64_t first = s.r.cost + (int64_t)job * s.r.pages * w, left = end - first;
-            const int64_t stop = left <= 0 ? 0 : (left + w - 1) / w;
-            s.run = run;
-            s.job = job;
-            s.page = page;
-            s.stop = (int)(stop < s.r.pages ? stop : s.r.pages);
-            if (s.stop <= page) return false;
-            s.head = job / s.r.chunks;
-            const int each = chunk_rows(s.r.rows, s.r.chunks), chunk = job - s.head * s.r.chunks;
-            s.row0 = run + chunk * each;
-            s.rows = min(each, s.r.rows - chunk * each);
-            s.wide = chunk_wide(s.rows, a.G);
-            s.rows0 = s.wide ? (s.rows + 1) / 2 : s.rows;
-            ++job;
-            page = 0;
-            return true;
-        }
-        return false;
-    }
-};
-
-// Pages of a tile, and of those the ones that a stream works on.
-__device__ __forceinline__ int tile_pages(const Segment& s, int tile) { return min(kTilePages, s.stop - s.page - tile * kTilePages); }
-__device__ __forceinline__ int stream_first(const Segment& s, int np, int stream) { return s.wide || stream == 0 ? 0 : (np + 1) / 2; }
-__device__ __forceinline__ int stream_pages(const Segment& s, int np, int stream) { return s.wide ? np : stream == 0 ? (np + 1) / 2 : np / 2; }
-
+// The loading warp: goes through the worker's share segment by segment, tells the others of each and loads its tiles.
 template <int D>
-__device__ __forceinline__ void load_tiles(const AttnArgs& a, const PlanHeader& h, Control& c, uint8_t* smem, const CUtensorMap* mk,
-                                           const CUtensorMap* mv, int lane)
+__device__ __forceinline__ void load_tiles(const AttnArgs& a, const CtaStart& start, Control& c, uint8_t* smem, const CUtensorMap* mk,
+                                           const CUtensorMap* mv)
 {
     using G = Geo<D>;
-    Segments segs(a, h, blockIdx.x);
-    Segment s;
-    uint32_t n = 0, tile_no = 0;                          // tiles of K and V so far; of both
+    const int lane = threadIdx.x & 31, p = lane % kTilePages, block = lane / kTilePages;
     const uint64_t policy = l2_policy_evict_first();
-    const int p = lane % kTilePages, block = lane / kTilePages;
-    bool fine = true;
-    while (fine && segs.next(s)) {
-        const int32_t* row = a.table + (int64_t)s.r.req * a.max_pages;
-        const int tiles = s.tiles();
-        int id = p < tile_pages(s, 0) ? row[s.page + p] : -1;
-#pragma unroll 1
-        for (int t = 0; t < tiles && fine; ++t, ++tile_no) {
-            const int np = tile_pages(s, t);
-            const int next = t + 1 < tiles && p < tile_pages(s, t + 1) ? row[s.page + (t + 1) * kTilePages + p] : -1;
-            const bool known = p < np && id >= 0 && id < a.num_pages;
-            const uint32_t mask = __ballot_sync(0xffffffffu, known) & 0xffu;
-            if (mask != (1u << np) - 1u && lane == 0) kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
-#pragma unroll 1
-            for (int side = 0; side < 2; ++side, ++n) {   // K, V
-                const int slot = n % G::kSlots;
-                if (!(fine = warp_wait(&c.empty[slot], (n / G::kSlots & 1) ^ 1, c, a.err))) break;
-                const uint32_t bar = smem_addr(&c.full[slot]);
-                if (lane == 0) {
-                    if (side == 0) c.pages_known[tile_no % 8] = (int32_t)mask;
-                    mbar_arrive_expect_tx(bar, __popc(mask) * (uint32_t)G::kPageBytes);
-                }
-                __syncwarp();
-                if (known && block < G::kBlocks)
-                    tma_load_3d(smem_addr(smem + G::kRing + slot * G::kTileBytes + block * G::kBlockBytes + p * 2048), side ? mv : mk, 0,
-                                (id * a.hkv + s.head) * kPageSize, block, bar, policy);
-            }
-            id = next;
+    uint32_t n = 0, tile_no = 0, told = 0;                // tiles of K and V so far; of both; segments
+    auto tell = [&](const Segment& s) {
+        if (lane == 0) {
+            c.segment[told % kSegments] = s;
+            arrive(&c.told[told % kSegments]);
         }
+        ++told;
+        __syncwarp();
+    };
+    Run r = start.r;
+    Segment s = start.s;
+    int run = start.run, job = start.job;
+    bool fine = true;
+    while (fine) {
+        if (s.pages == 0) {                               // the next segment
+            if (r.pages == 0 || job >= r.chunks * a.hkv) {
+                run += r.pages == 0 ? 1 : r.rows;
+                if (run >= a.batch) break;
+                r = a.view.runs[run];
+                job = 0;
+                continue;
+            }
+            s = make_segment(r, run, job, 0, start.end, a.hkv, a.G, blockIdx.x);
+            if (s.pages == 0) break;
+            ++job;
+        }
+        tell(s);
+
+        const int32_t* row = a.table + (int64_t)r.req * a.max_pages + s.first;
+        const int tiles = s.tiles();
+        const Order order(tiles, s.wide);
+        // Page ids of the next tile of K, and those of the tiles of which V is still to come (one or two).
+        auto ids_of = [&](int t) { return t < tiles && p < s.tile_pages(t) ? row[t * kTilePages + p] : -1; };
+        int next = ids_of(0), even = -1, odd = -1, kt = 0, vt = 0;
+#pragma unroll 1
+        for (int i = 0; i < 2 * tiles; ++i, ++n) {
+            const bool of_k = kt < tiles && i == order.k(kt);
+            const int t = of_k ? kt++ : vt++;
+            int id = t & 1 ? odd : even;
+            if (of_k) {
+                id = next;
+                next = ids_of(kt);
+                even = t & 1 ? even : id;
+                odd = t & 1 ? id : odd;
+            }
+            const int np = s.tile_pages(t), slot = n % G::kSlots;
+            const bool known = p < np && id >= 0 && id < a.num_pages;
+            const uint32_t mask = __ballot_sync(0xffffffffu, known) & 0xffu, bar = smem_addr(&c.full[slot]);
+            if (!(fine = warp_wait(&c.empty[slot], (n / G::kSlots & 1) ^ 1, c, a.err))) break;
+            if (lane == 0) {
+                if (of_k) c.pages_known[(tile_no + t) % 8] = (int32_t)mask;
+                if (mask != (1u << np) - 1u) kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
+                mbar_arrive_expect_tx(bar, __popc(mask) * (uint32_t)G::kPageBytes);
+            }
+            __syncwarp();
+            if (known && block < G::kBlocks)
+                tma_load_3d(smem_addr(smem + G::kRing + slot * G::kTileBytes + block * G::kBlockBytes + p * 2048), of_k ? mk : mv, 0,
+                            (id * a.hkv + s.head) * kPageSize, block, bar, policy);
+        }
+        tile_no += tiles;
+        s.pages = 0;
     }
+    if (fine) tell(s);
     // Where others gave up: what is under way arrives before the CTA leaves.
     if (*reinterpret_cast<volatile int32_t*>(&c.gave_up))
         for (uint32_t i = n > G::kSlots ? n - G::kSlots : 0; i < n; ++i)
             mbar_wait_bounded(smem_addr(&c.full[i % G::kSlots]), i / G::kSlots & 1, kLimitNs);
 }
 
+// The issuing warp.  (All of it goes along, so that addresses and descriptors stay in uniform registers; one lane issues.)
 template <int D, class T>
-__device__ __forceinline__ void issue_products(const AttnArgs& a, const PlanHeader& h, Control& c, uint8_t* smem)
+__device__ __forceinline__ void issue_products(const AttnArgs& a, Control& c, uint8_t* smem)
 {
     using G = Geo<D>;
     constexpr bool kBf16 = std::is_same_v<T, Bf16>;
-    Segments segs(a, h, blockIdx.x);
-    Segment s;
     const uint32_t base = smem_addr(smem), tm = c.tmem;
-    uint32_t n = 0, segment = 0, ready[2] = {0, 0};
-    // K tiles of a stream against its queries.
-    auto scores = [&](int stream, uint32_t slot, int np) {
-        const int pages = stream_pages(s, np, stream);
-        if (pages == 0) return;
-        const uint32_t q = base + (s.wide ? stream * G::kTileBytes : 0);
-        const uint32_t k = base + G::kRing + slot * G::kTileBytes + stream_first(s, np, stream) * 2048;
-        const uint32_t idesc = mma_desc(kBf16, false, kTileRows, pages * kPageSize);
+    const bool one = elect_one();
+    uint32_t n0 = 0, ready[2] = {0, 0};
+    bool wide = false;
+    // K of a tile against a stream's queries.
+    auto scores = [&](int stream, uint32_t slot, int pages) {
+        const uint64_t q = smem_desc(base + (wide ? stream * G::kTileBytes : 0), 16, 1024);
+        const uint64_t k = smem_desc(base + G::kRing + slot * G::kTileBytes, 16, 1024);
+        const uint32_t idesc = mma_desc(kBf16, false, kTileRows, pages * kPageSize), d = tm + stream * 128;
+        if (one) {
 #pragma unroll
-        for (int ks = 0; ks < D / 16; ++ks) {
-            const uint32_t off = (ks / 4) * G::kBlockBytes + (ks % 4) * 32;
-            mma_ss(tm + stream * 128, smem_desc(q + off, 16, 1024), smem_desc(k + off, 16, 1024), idesc, ks > 0);
-        }
-    };
-    // A stream's weights against V.
-    auto outputs = [&](int stream, uint32_t slot, int np, bool add) {
-        const int pages = stream_pages(s, np, stream);
-        const uint32_t v = base + G::kRing + slot * G::kTileBytes + stream_first(s, np, stream) * 2048;
-        const uint32_t idesc = mma_desc(kBf16, true, kTileRows, D);
-#pragma unroll 1
-        for (int kk = 0; kk < pages; ++kk)
-            mma_ts(tm + 256 + stream * 128, tm + stream * 128 + kk * 8, smem_desc(v + kk * 2048, G::kBlockBytes, 1024), idesc, add || kk > 0);
-    };
-    while (segs.next(s)) {
-        const int tiles = s.tiles();
-        if (!thread_wait(&c.queries, segment & 1, c, a.err)) return;
-        uint32_t slot = n % G::kSlots;
-        if (!thread_wait(&c.full[slot], n / G::kSlots & 1, c, a.err)) return;
-        tmem_fence_after();
-        for (int st = 0; st < 2; ++st) {
-            scores(st, slot, tile_pages(s, 0));
-            mma_commit(smem_addr(&c.scores[st]));
-            arrive(&c.scores[st]);       // (what the loading warp has said of the tile comes along)
-        }
-        mma_commit(smem_addr(&c.empty[slot]));
-        ++n;
-#pragma unroll 1
-        for (int t = 0; t < tiles; ++t) {
-            const uint32_t vslot = n % G::kSlots, vpar = n / G::kSlots & 1;
-            ++n;
-            const uint32_t kslot = n % G::kSlots, kpar = n / G::kSlots & 1;
-            const bool more = t + 1 < tiles;
-            const int np = tile_pages(s, t), np2 = more ? tile_pages(s, t + 1) : 0;
-            if (!thread_wait(&c.full[vslot], vpar, c, a.err)) return;
-#pragma unroll 1
-            for (int st = 0; st < 2; ++st) {
-                if (!thread_wait(&c.weights[st], ready[st]++ & 1, c, a.err)) return;
-                tmem_fence_after();
-                outputs(st, vslot, np, t > 0);
-                if (st == 1) mma_commit(smem_addr(&c.empty[vslot]));
-                if (more) {
-                    if (st == 0 && !thread_wait(&c.full[kslot], kpar, c, a.err)) return;
-                    scores(st, kslot, np2);
-                    mma_commit(smem_addr(&c.scores[st]));
-                    arrive(&c.scores[st]);
-                    if (st == 1) mma_commit(smem_addr(&c.empty[kslot]));
-                } else {
-                    mma_commit(smem_addr(&c.output[st]));
-                }
+            for (int ks = 0; ks < D / 16; ++ks) {
+                const uint32_t off = ((ks / 4) * G::kBlockBytes + (ks % 4) * 32) >> 4;
+                mma_ss(d, q + off, k + off, idesc, ks > 0);
             }
-            if (more) ++n;
+            mma_commit(smem_addr(&c.scores[stream]));
+            arrive(&c.scores[stream]);       // (what the loading warp has said of the tile comes along)
         }
-        ++segment;
-    }
-}
-
-// Bits of a tile's 128 tokens, from a stream's first page on, that take part.
-__device__ __forceinline__ uint32_t token_bits(int word, int first_page, int pages, uint32_t known, int valid)
-{
-    // valid: tokens of the tile before the prefix's end
-    uint32_t m = 0;
+        __syncwarp();
+    };
+    // A stream's weights against V; a half's weights lie where its scores were.
+    auto outputs = [&](int stream, uint32_t slot, int pages, bool add) {
+        const int half = (pages + 1) / 2;
+        const uint64_t v = smem_desc(base + G::kRing + slot * G::kTileBytes, G::kBlockBytes, 1024);
+        const uint32_t idesc = mma_desc(kBf16, true, kTileRows, D), d = tm + 256 + stream * 128, w = tm + stream * 128;
+        if (one) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int pg = 2 * word + i;
-        if (pg < pages && (known >> (first_page + pg) & 1u)) {
-            const int n = min(max(valid - (first_page + pg) * kPageSize, 0), kPageSize);
-            m |= ((1u << n) - 1u) << (16 * i);
+            for (int kk = 0; kk < kTilePages; ++kk)
+                if (kk < pages) mma_ts(d, w + kk * 8 + (kk < half ? 0 : half * 8), v + kk * (2048 >> 4), idesc, add || kk > 0);
         }
+        __syncwarp();
+    };
+    auto commit = [&](uint64_t* bar) {
+        if (one) mma_commit(smem_addr(bar));
+        __syncwarp();
+    };
+    auto slot_of = [&](int at) { return (n0 + at) % G::kSlots; };
+    auto arrived = [&](int at) { return warp_wait(&c.full[slot_of(at)], (n0 + at) / G::kSlots & 1, c, a.err); };
+#pragma unroll 1
+    for (uint32_t segment = 0;; ++segment) {
+        if (!warp_wait(&c.told[segment % kSegments], segment / kSegments & 1, c, a.err)) return;
+        const Segment s = c.segment[segment % kSegments];
+        if (s.pages == 0) return;
+        wide = s.wide;
+        const int tiles = s.tiles(), step = wide ? 1 : 2;
+        const Order order(tiles, wide);
+        if (!warp_wait(&c.queries, segment & 1, c, a.err)) return;
+        // The streams' first tiles, then turns: a tile's weights against its V, the stream's next tile of K against its queries.
+        const int turns = wide ? 2 * tiles : tiles;
+#pragma unroll 1
+        for (int i = -2; i < turns; ++i) {
+            const int st = i & 1, t = i < 0 ? -1 : wide ? i >> 1 : i, next = i < 0 ? (wide ? 0 : st) : t + step;
+            const bool last_use = !wide || st == 1, more = next < tiles;
+            const uint32_t vslot = slot_of(order.v(t)), kslot = slot_of(order.k(next));
+            if (i >= 0 && !arrived(order.v(t))) return;
+            if (more && !arrived(order.k(next))) return;
+            if (i >= 0) {
+                const uint32_t turn = st ? ready[1]++ : ready[0]++;
+                if (!warp_wait(&c.weights[st], turn & 1, c, a.err)) return;
+            }
+            tmem_fence_after();
+            if (i >= 0) {
+                outputs(st, vslot, s.tile_pages(t), t >= step);
+                if (last_use) commit(&c.empty[vslot]);
+            }
+            if (more) {
+                scores(st, kslot, s.tile_pages(next));
+                if (last_use) commit(&c.empty[kslot]);
+            } else {
+                commit(&c.output[st]);
+            }
+        }
+        n0 += 2 * tiles;
     }
-    return m;
 }
 
-template <int D, class T>
-__device__ __forceinline__ void softmax_stream(const AttnArgs& a, const PlanHeader& h, Control& c, uint8_t* smem)
+// The segment's queries, by the softmax warps: 16-byte chunks of up to 256 rows into the tiles' swizzle, four loads of a thread
+// under way.
+template <int D>
+__device__ __forceinline__ void load_queries(const AttnArgs& a, const Segment& s, uint8_t* smem)
 {
     using G = Geo<D>;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, stream = warp >> 2, wq = warp & 3;
-    const int my = wq * 32 + lane;                        // row of the stream's tile
-    const uint32_t tm = c.tmem + ((uint32_t)wq << 21), ts = tm + stream * 128, to = tm + 256 + stream * 128;
-    Segments segs(a, h, blockIdx.x);
-    Segment s;
-    uint32_t n = 0, segment = 0, tile_no = 0;
-    const float sl = a.scale_log2;
-    while (segs.next(s)) {
-        // Queries: 16-byte chunks of up to 256 rows, in the tiles' swizzle.
-        if (segment > 0 && !warp_wait(&c.drained, (segment - 1) & 1, c, a.err)) return;
-        const int total = s.rows * a.G;
-        for (int i = threadIdx.x; i < total * (D / 8); i += 256) {
-            const int qr = i / (D / 8), ch = i % (D / 8), br = qr / a.G, g = qr - br * a.G;
-            const int tile = br >= s.rows0, r = qr - tile * s.rows0 * a.G;
-            const uint4 x = *reinterpret_cast<const uint4*>(a.q + (s.row0 + br) * a.q_stride + (int64_t)(s.head * a.G + g) * D + ch * 8);
-            *reinterpret_cast<uint4*>(smem + tile * G::kTileBytes + (ch >> 3) * G::kBlockBytes + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = x;
+    constexpr int kChunks = D / 8, kStep = 32 * kSoftmaxWarps / kChunks, kLoads = 4;   // chunks of a row; rows at a time
+    const int total = s.rows * a.G, ch = threadIdx.x % kChunks, first = threadIdx.x / kChunks, rows0 = s.rows0 * a.G;
+    const uint32_t by = (65536u + a.G - 1) / a.G;           // qr / G = qr * by >> 16 for qr < 256, G <= 8
+    const uint16_t* q = a.q + (int64_t)s.row0 * a.q_stride + (int64_t)s.head * a.G * D + ch * 8;
+#pragma unroll 1
+    for (int r0 = first; r0 < total; r0 += kLoads * kStep) {
+        uint4 x[kLoads];
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int qr = min(r0 + i * kStep, total - 1), br = (int)(qr * by >> 16);
+            x[i] = *reinterpret_cast<const uint4*>(q + br * a.q_stride + (int64_t)(qr - br * a.G) * D);
         }
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int qr = r0 + i * kStep, tile = qr >= rows0, r = qr - (tile ? rows0 : 0);
+            if (qr < total)
+                *reinterpret_cast<uint4*>(smem + tile * G::kTileBytes + (ch >> 3) * G::kBlockBytes + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = x[i];
+        }
+    }
+}
+
+// Bits of a page's 16 tokens that take part: none of a page that is not there, of the last page those before the prefix's end
+// (valid: the tile's tokens before it).
+__device__ __forceinline__ uint32_t token_bits(int page, uint32_t known, int valid)
+{
+    const int n = min(max(valid - page * kPageSize, 0), kPageSize);
+    return known >> page & 1u ? (1u << n) - 1u : 0u;
+}
+
+// A warp's scores of a tile: up to 4 pages of its rows, a row to a lane.
+struct Scores {
+    uint32_t at;       // in tensor memory
+    int first, pages;  // of the tile
+    bool whole;        // all tokens take part
+    uint32_t known;
+    int valid;
+    // Pages 2 i and 2 i + 1; of one that there is not, -infinity.
+    __device__ __forceinline__ void load(int i, uint32_t (&x)[32]) const
+    {
+        tmem_ld32(at + 32 * i, x);
+        tmem_wait_ld();
+        if (!whole || 2 * i + 2 > pages) {
+            const uint32_t bits = token_bits(first + 2 * i, known, valid) | (2 * i + 2 > pages ? 0u : token_bits(first + 2 * i + 1, known, valid) << 16);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) x[k] = bits >> k & 1u ? x[k] : 0xff800000u;
+        }
+    }
+};
+
+// A row's largest score.
+__device__ __forceinline__ float largest(const Scores& s)
+{
+    float mx = -INFINITY;
+#pragma unroll 1
+    for (int i = 0; 2 * i < s.pages; ++i) {
+        uint32_t x[32];
+        s.load(i, x);
+#pragma unroll
+        for (int k = 0; k < 32; k += 2) mx = fmaxf(mx, fmaxf(__uint_as_float(x[k]), __uint_as_float(x[k + 1])));
+    }
+    return mx;
+}
+
+// A row's weights 2^(s * sl - sub), two to a word, and their sum; the scores stay in tensor memory.
+template <class T>
+__device__ __forceinline__ float weigh(const Scores& s, float sl, float sub, uint32_t (&p)[2][16])
+{
+    const uint64_t sl2 = f2_pack(sl, sl), sub2 = f2_pack(-sub, -sub);
+    uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (2 * i < s.pages) {
+            uint32_t x[32];
+            s.load(i, x);
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                float u, v;
+                f2_unpack(f2_fma(f2_pack(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1])), sl2, sub2), u, v);
+                u = ex2(u);
+                v = ex2(v);
+                sum[k & 1] = f2_add(sum[k & 1], f2_pack(u, v));
+                p[i][k] = T::pack(u, v);
+            }
+        }
+    }
+    float u, v;
+    f2_unpack(f2_add(sum[0], sum[1]), u, v);
+    return u + v;
+}
+
+// What a row's weights in half a tile may add up to: fp16 holds each of them, and sums of 32 bits stay far from their end.
+// A reference that is the largest score leaves at most 64 times the weights' factor of 2^7.
+constexpr float kMostWeight = 32768.f;
+
+// Two warps share a row's tokens: the first half of a tile's pages and the second.  Weights are worked out with the
+// reference that there is; where the sum of either half says that it is too low (or there is none yet) both move to the
+// largest score of the tile and do it again.
+template <int D, class T>
+__device__ __forceinline__ void softmax_stream(const AttnArgs& a, Control& c, uint8_t* smem)
+{
+    using G = Geo<D>;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, stream = warp >> 3, half = warp >> 2 & 1, wq = warp & 3;
+    const int my = wq * 32 + lane;                        // row of the stream's tile
+    const uint32_t tm = c.tmem + ((uint32_t)wq << 21), ts = tm + stream * 128, to = tm + 256 + stream * 128 + half * (D / 2);
+    uint32_t n0 = 0, tile_no = 0, turn = 0, meetings = 0;
+    const float sl = a.scale_log2;
+    uint64_t* const pair = &c.pair[stream][wq];
+    auto meet = [&] {
+        __syncwarp();
+        if (lane == 0) arrive(pair);
+        return warp_wait(pair, meetings++ & 1, c, a.err);
+    };
+#pragma unroll 1
+    for (uint32_t segment = 0;; ++segment) {
+        if (!warp_wait(&c.told[segment % kSegments], segment / kSegments & 1, c, a.err)) return;
+        const Segment& s = c.segment[segment % kSegments];
+        if (s.pages == 0) return;
+        if (segment > 0 && !warp_wait(&c.drained, (segment - 1) & 1, c, a.err)) return;
+        load_queries<D>(a, s, smem);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) arrive(&c.queries);
-        const int qrows = (s.wide ? (stream == 0 ? s.rows0 : s.rows - s.rows0) : s.rows) * a.G;
+        const int tiles = s.tiles(), wide = s.wide;
+        const int qrows = (wide && stream == 1 ? s.rows - s.rows0 : s.rows0) * a.G;
         const bool works = wq * 32 < qrows;               // (the others have no row of the tile)
+        const Order order(tiles, wide);
         float ref = -INFINITY, l = 0.f;
         bool some = false;                                // products with V so far
-        const int tiles = s.tiles();
 #pragma unroll 1
-        for (int t = 0; t < tiles; ++t, ++tile_no, n += 2) {
-            const int np = tile_pages(s, t), pages = stream_pages(s, np, stream), first = stream_first(s, np, stream);
-            const uint32_t vslot = (n + 1) % G::kSlots;
-            if (!warp_wait(&c.scores[stream], tile_no & 1, c, a.err)) return;
+        for (int t = wide ? 0 : stream; t < tiles; t += wide ? 1 : 2, ++turn) {
+            const int pages = s.tile_pages(t), h0 = (pages + 1) / 2;
+            if (!warp_wait(&c.scores[stream], turn & 1, c, a.err)) return;
             tmem_fence_after();
-            const uint32_t known = (uint32_t)c.pages_known[tile_no % 8];
-            const int valid = s.r.len - (s.page + t * kTilePages) * kPageSize;
-            const bool whole = valid >= np * kPageSize && known == (1u << np) - 1u;
-            if (works && pages > 0) {
-                const int words = (pages + 1) / 2;
-                const bool plain = whole && (pages & 1) == 0;
-                float mx = -INFINITY;
+            Scores x;
+            x.known = (uint32_t)c.pages_known[(tile_no + t) % 8];
+            x.valid = s.valid - t * kTilePages * kPageSize;
+            x.whole = x.valid >= pages * kPageSize && x.known == (1u << pages) - 1u;
+            x.at = ts + (half ? h0 * 16 : 0);
+            x.first = half ? h0 : 0;
+            x.pages = half ? pages - h0 : h0;
+            if (works) {
+                uint32_t p[2][16];
+                float sum;
+                bool move = !some;
 #pragma unroll 1
-                for (int w = 0; w < words; ++w) {
-                    uint32_t x[32];
-                    tmem_ld32(ts + 32 * w, x);
-                    tmem_wait_ld();
-                    if (plain) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) mx = fmaxf(mx, __uint_as_float(x[i]));
-                    } else {
-                        const uint32_t bits = token_bits(w, first, pages, known, valid);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) mx = bits >> i & 1u ? fmaxf(mx, __uint_as_float(x[i])) : mx;
-                    }
-                }
-                mx *= sl;
-                const float top = fmaxf(ref, mx);
-                if (__any_sync(0xffffffffu, mx > ref + 8.f)) {
-                    if (some) {
-                        const float alpha = ref == top ? 1.f : ex2(ref - top);
-                        l *= alpha;
+                while (true) {
+                    if (move) {
+                        const float mx = largest(x) * sl;
+                        c.pair_value[stream][half][wq][lane] = mx;
+                        if (!meet()) return;
+                        const float top = my < qrows ? fmaxf(ref, fmaxf(mx, c.pair_value[stream][half ^ 1][wq][lane])) : 0.f;
+                        if (some) {
+                            const float alpha = ref == top ? 1.f : ex2(ref - top);
+                            l *= alpha;
 #pragma unroll 1
-                        for (int w = 0; w < D / 32; ++w) {
-                            uint32_t x[32];
-                            tmem_ld32(to + 32 * w, x);
-                            tmem_wait_ld();
+                            for (int w = 0; w < D / 32; ++w) {
+                                uint32_t o[16];
+                                tmem_ld16(to + 16 * w, o);
+                                tmem_wait_ld();
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * alpha);
-                            tmem_st32(to + 32 * w, x);
+                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                                tmem_st16(to + 16 * w, o);
+                            }
                         }
+                        ref = top;
                     }
-                    ref = top;
-                }
-                const float sub = (ref == -INFINITY ? 0.f : ref) - Weights<T>::kShift;
-                float sum = 0.f;
-#pragma unroll 1
-                for (int w = 0; w < words; ++w) {
-                    uint32_t x[32], p[16];
-                    tmem_ld32(ts + 32 * w, x);
-                    tmem_wait_ld();
-                    if (plain) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(ex2(fmaf(__uint_as_float(x[i]), sl, -sub)));
-                    } else {
-                        const uint32_t bits = token_bits(w, first, pages, known, valid);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) x[i] = bits >> i & 1u ? __float_as_uint(ex2(fmaf(__uint_as_float(x[i]), sl, -sub))) : 0u;
-                    }
-                    float part = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const float u = __uint_as_float(x[2 * i]), v = __uint_as_float(x[2 * i + 1]);
-                        part += u + v;
-                        p[i] = T::pack(u, v);
-                    }
-                    sum += part;
-                    tmem_st16(ts + 16 * w, p);
+                    sum = weigh<T>(x, sl, (ref == -INFINITY ? 0.f : ref) - Weights<T>::kShift, p);
+                    if (move) break;
+                    move = __any_sync(0xffffffffu, my < qrows && (sum > kMostWeight || ref == -INFINITY));
+                    if (lane == 0) c.pair_again[stream][half][wq] = move;
+                    if (!meet()) return;
+                    move |= c.pair_again[stream][half ^ 1][wq] != 0;
+                    if (!move) break;
                 }
                 l += sum;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (2 * i < x.pages) tmem_st16(x.at + 16 * i, p[i]);
                 tmem_wait_st();
             }
-            some |= pages > 0;
-            if (!whole) {   // rows of V that hold anything: zero, or 0 * NaN would reach the sums
-                if (!warp_wait(&c.full[vslot], (n + 1) / G::kSlots & 1, c, a.err)) return;
-                for (int r = first * kPageSize + wq; r < (first + pages) * kPageSize; r += 4)
-                    if (r >= valid || !(known >> (r / kPageSize) & 1u))
+            some = true;
+            if (!x.whole) {   // rows of V that hold anything: zero, or 0 * NaN would reach the sums
+                const uint32_t n = n0 + order.v(t), vslot = n % G::kSlots;
+                if (!warp_wait(&c.full[vslot], n / G::kSlots & 1, c, a.err)) return;
+#pragma unroll 1
+                for (int r = x.first * kPageSize + wq; r < (x.first + x.pages) * kPageSize; r += 4)
+                    if (r >= x.valid || !(x.known >> (r / kPageSize) & 1u))
                         for (int b = 0; b < G::kBlocks; ++b)
                             *reinterpret_cast<uint32_t*>(smem + G::kRing + vslot * G::kTileBytes + b * G::kBlockBytes + r * 128 + lane * 4) = 0u;
                 fence_proxy_async_smem();
@@ -436,30 +496,38 @@ __device__ __forceinline__ void softmax_stream(const AttnArgs& a, const PlanHead
             __syncwarp();
             if (lane == 0) arrive(&c.weights[stream]);
         }
+        n0 += 2 * tiles;
+        tile_no += tiles;
         if (!warp_wait(&c.output[stream], segment & 1, c, a.err)) return;
         tmem_fence_after();
         if (works) {
-            // Rows of 32 columns through shared memory (this warp's 4 KB of the query tiles, which all products
-            // have read by now), so that a row's columns are stored together.
-            const int64_t entry = run_entry(s.r, a.hkv, a.G, s.head, s.row0 - s.run, blockIdx.x) +
-                                  (int64_t)(stream == 0 ? 0 : (s.wide ? s.rows0 : s.rows) * a.G);
-            uint8_t* const mine = smem + warp * 4096;
-            if (my < qrows) a.view.run_ml[entry + my] = make_float2(some ? ref - Weights<T>::kShift : -INFINITY, some ? l : 0.f);
+            // Both halves' sums (the other has read the last tile's values: its weights have arrived).
+            c.pair_value[stream][half][wq][lane] = l;
+            if (!meet()) return;
+            // Columns through shared memory (this warp's part of the query tiles, which all products have read by now), so
+            // that those of a row are stored together.
+            constexpr int kCols = D / 4, kRowBytes = kCols * 4, kPieces = kRowBytes / 16;   // 32 at d = 128, else 16; 16-byte pieces
+            const int64_t entry = s.entry + (stream == 0 ? 0 : s.rows0 * a.G);
+            uint8_t* const mine = smem + warp * (32 * kRowBytes);
+            if (half == 0 && my < qrows)
+                a.view.run_ml[entry + my] = make_float2(some ? ref - Weights<T>::kShift : -INFINITY, some ? l + c.pair_value[stream][1][wq][lane] : 0.f);
 #pragma unroll 1
-            for (int w = 0; w < D / 32; ++w) {
-                uint32_t x[32];
-                tmem_ld32(to + 32 * w, x);
+            for (int w = 0; some && w < 2; ++w) {
+                uint32_t o[kCols];
+                if constexpr (D == 128) tmem_ld32(to + kCols * w, o);
+                else tmem_ld16(to + kCols * w, o);
                 tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    *reinterpret_cast<uint4*>(mine + lane * 128 + ((i ^ (lane & 7)) << 4)) =
-                        some ? make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]) : make_uint4(0, 0, 0, 0);
+                for (int i = 0; i < kPieces; ++i)
+                    *reinterpret_cast<uint4*>(mine + lane * kRowBytes + ((i ^ (lane & (kPieces - 1))) << 4)) =
+                        make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                 __syncwarp();
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int r = 4 * i + (lane >> 3), ch = lane & 7;
-                    const uint4 v = *reinterpret_cast<const uint4*>(mine + r * 128 + ((ch ^ (r & 7)) << 4));
-                    if (wq * 32 + r < qrows) *reinterpret_cast<uint4*>(a.view.run_o + (entry + wq * 32 + r) * D + w * 32 + ch * 4) = v;
+                for (int i = 0; i < kPieces; ++i) {
+                    const int r = (32 / kPieces) * i + lane / kPieces, ch = lane % kPieces;
+                    const uint4 v = *reinterpret_cast<const uint4*>(mine + r * kRowBytes + ((ch ^ (r & (kPieces - 1))) << 4));
+                    if (wq * 32 + r < qrows)
+                        *reinterpret_cast<uint4*>(a.view.run_o + (entry + wq * 32 + r) * D + half * (D / 2) + w * kCols + ch * 4) = v;
                 }
                 __syncwarp();
             }
@@ -467,7 +535,6 @@ __device__ __forceinline__ void softmax_stream(const AttnArgs& a, const PlanHead
         tmem_fence_before();
         __syncwarp();
         if (lane == 0) arrive(&c.drained);
-        ++segment;
     }
 }
 
@@ -497,7 +564,7 @@ struct Windows {
         head = s.head;
         page = s.page;
         left = count;
-        r = a.view.recs[rec];
+        r = s.r;
         fetch();
         shift();
     }
@@ -546,10 +613,12 @@ __device__ __forceinline__ void work_records(const AttnArgs& a, const PlanHeader
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ctas = a.grid - h.prefix_ctas;
     const int worker = warp * ctas + (int)blockIdx.x - h.prefix_ctas;   // (few workers: spread over the SMs)
     if (worker >= h.warps) return;
-    const int64_t u0 = share_start(worker, h.units, h.warps);
-    int left = (int)(share_start(worker + 1, h.units, h.warps) - u0);
     const WarpStart start = a.view.warp_starts[worker];
+    int left = start.count;
     uint8_t* const ring = smem + warp * G::kWarpRing;
+    if (lane < G::kStages) mbar_init(smem_addr(&c.stage[warp][lane]), 1);
+    fence_mbar_init();
+    __syncwarp();
     const uint64_t policy = l2_policy_evict_first();
 
     // The ring's side: a page's K and V by lanes of 64 columns each.
@@ -582,8 +651,8 @@ __device__ __forceinline__ void work_records(const AttnArgs& a, const PlanHeader
 
     int rec = start.rec, head = start.head, page = start.page, get = 0;
     bool fine = true;
+    Record r = start.r;
     while (left > 0 && fine) {
-        const Record r = a.view.recs[rec];
         const int stop = min(r.pages, page + left);
         // Queries as columns: B fragments, column lane / 4.
         const int cols = r.rows * a.G, col = lane >> 2;
@@ -684,7 +753,7 @@ __device__ __forceinline__ void work_records(const AttnArgs& a, const PlanHeader
             l0 += __shfl_xor_sync(0xffffffffu, l0, k);
             l1 += __shfl_xor_sync(0xffffffffu, l1, k);
         }
-        const int64_t entry = record_entry(r, a.hkv, a.G, head, worker);
+        const int64_t entry = record_entry(r.col, r.rows, a.hkv, a.G, head, worker);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const int cc = 2 * (lane & 3) + k;
@@ -702,8 +771,8 @@ __device__ __forceinline__ void work_records(const AttnArgs& a, const PlanHeader
             page = 0;
             if (++head == a.hkv) {
                 head = 0;
-                do ++rec;
-                while (a.view.recs[rec].pages == 0);
+                do r = a.view.recs[++rec];
+                while (r.pages == 0);
             }
         }
     }
@@ -719,57 +788,72 @@ template <int D, class T>
 __global__ void __launch_bounds__(kThreads, 1) attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                                                                 const __grid_constant__ AttnArgs a)
 {
-    extern __shared__ uint8_t raw[];
-    __shared__ Control c;
-    uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+    // (The kernel has no other shared memory: what it is given starts on 1024 bytes, as the swizzle wants it.)
+    extern __shared__ __align__(1024) uint8_t smem[];
+    Control& c = *reinterpret_cast<Control*>(smem + Geo<D>::kData);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    if (tid < 16) {
+    if (tid < 10) {
         mbar_init(smem_addr(&c.full[tid]), 1);
         mbar_init(smem_addr(&c.empty[tid]), 1);
     }
+    if (tid >= 64 && tid < 64 + kSegments) mbar_init(smem_addr(&c.told[tid - 64]), 1);
     if (tid < 2) {
         mbar_init(smem_addr(&c.scores[tid]), 2);
-        mbar_init(smem_addr(&c.weights[tid]), 4);
+        mbar_init(smem_addr(&c.weights[tid]), kSoftmaxWarps / 2);
         mbar_init(smem_addr(&c.output[tid]), 1);
     }
-    if (tid == 2) mbar_init(smem_addr(&c.queries), 8);
-    if (tid == 3) mbar_init(smem_addr(&c.drained), 8);
+    if (tid == 2) mbar_init(smem_addr(&c.queries), kSoftmaxWarps);
+    if (tid == 3) mbar_init(smem_addr(&c.drained), kSoftmaxWarps);
     if (tid == 4) c.gave_up = 0;
-    if (lane < 4) mbar_init(smem_addr(&c.stage[warp][lane]), 1);
+    if (tid >= 32 && tid < 40) mbar_init(smem_addr(&c.pair[0][0] + (tid - 32)), 2);
+    if (tid == 5) mbar_init(smem_addr(&c.last), 1);
     if (tid == 0) {
         prefetch_tensormap(&mk);
         prefetch_tensormap(&mv);
     }
-    fence_mbar_init();
-    __syncthreads();
-    griddep_wait();
-    griddep_launch_dependents();
-    const PlanHeader h = *a.view.header;
-    if (!plan_fits(h, a)) {
-        if (tid == 0 && blockIdx.x == 0) kv4_error(a.err, KVC_DEVERR_PLAN);
-        return;
-    }
-    if ((int)blockIdx.x >= h.prefix_ctas) {
-        work_records<D, T>(a, h, c, smem, &mk, &mv);
-        return;
-    }
+    // Tensor memory for all (it is given back at once where the CTA turns out to work on records): while the launch before
+    // finishes this costs nothing.
     if (warp == kMmaWarp) tmem_alloc(smem_addr(&c.tmem), 512);
+    fence_mbar_init();
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
-    if (warp < 8) {
-        softmax_stream<D, T>(a, h, c, smem);
-    } else if (warp == kLoadWarp) {
-        load_tiles<D>(a, h, c, smem, &mk, &mv, lane);
-    } else if (warp == kMmaWarp) {
-        if (lane == 0) {
-            issue_products<D, T>(a, h, c, smem);
-            if (*reinterpret_cast<volatile int32_t*>(&c.gave_up)) {   // what is under way ends before the memory is freed
-                mma_commit(smem_addr(&c.full[15]));
-                mbar_wait_bounded(smem_addr(&c.full[15]), 0, kLimitNs);
-            }
+    griddep_wait();
+    griddep_launch_dependents();
+    const PlanHeader h = *a.view.header;
+    CtaStart start;
+    if (warp == kLoadWarp) start = a.view.cta_starts[blockIdx.x];   // (of records' CTAs: not looked at)
+    const bool fits = plan_fits(h, a) && (smem_addr(smem) & 1023) == 0, records = (int)blockIdx.x >= h.prefix_ctas;
+    if (!fits || records) {
+        if (warp == kMmaWarp) tmem_dealloc(c.tmem, 512);
+        if (!fits) {
+            if (tid == 0 && blockIdx.x == 0) kv4_error(a.err, KVC_DEVERR_PLAN);
+            return;
         }
-        __syncwarp();
+        // (Registers: 96 a thread at launch; three groups of four warps take 144, the other two leave with 24.)
+        if (warp < kAttnWarps) {
+            asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
+            work_records<D, T>(a, h, c, smem, &mk, &mv);
+        } else {
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 24;");
+        }
+        return;
+    }
+    if (warp < kSoftmaxWarps) {   // (four groups of 104, one of 64)
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+        softmax_stream<D, T>(a, c, smem);
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if (warp == kLoadWarp) {
+            load_tiles<D>(a, start, c, smem, &mk, &mv);
+        } else if (warp == kMmaWarp) {
+            issue_products<D, T>(a, c, smem);
+            if (*reinterpret_cast<volatile int32_t*>(&c.gave_up) && lane == 0) {   // what is under way ends before the memory is freed
+                mma_commit(smem_addr(&c.last));
+                mbar_wait_bounded(smem_addr(&c.last), 0, kLimitNs);
+            }
+            __syncwarp();
+        }
     }
     tmem_fence_before();
     __syncthreads();
@@ -778,100 +862,114 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kernel(const __grid_con
 }
 
 // ---------------------------------------------------------------------- merge
-// A warp per (row, query head): the partial results of the row's own segments, then its prefix's, in their order.
+// A CTA of four warps per (row, query head): the partial results of the row's own segments, then its prefix's, in their order.
+// Each warp takes every fourth; with loads of eight under way, a unit of up to 32 segments is two trips to L2.
 template <int D, class T>
 __global__ void __launch_bounds__(128) merge_kernel(const __grid_constant__ AttnArgs a)
 {
     constexpr int N = D / 32;
+    using Vec = std::conditional_t<N == 4, float4, float2>;
+    __shared__ float s_o[4][D];
+    __shared__ float2 s_ml[4];
     griddep_wait();
     griddep_launch_dependents();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int head = blockIdx.x, row = blockIdx.y;
+    const int kv = (int)((uint32_t)head * ((65536u + a.G - 1) / a.G) >> 16), g = head - kv * a.G;   // (head < 8192, G <= 8)
+    const RowSources x = a.view.rows[row];
     const PlanHeader h = *a.view.header;
     if (!plan_fits(h, a)) return;
-    const int lane = threadIdx.x & 31;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    if (unit >= (int64_t)a.batch * a.hq) return;
-    const int row = (int)(unit / a.hq), head = (int)(unit - (int64_t)row * a.hq), kv = head / a.G, g = head - kv * a.G;
 
-    // Segments: workers first .. first + count - 1 of up to two sources.
-    struct Source {
-        int64_t entry;     // of worker `first`
-        int step, count;   // entries between workers; segments
-    };
-    Source src[2] = {{0, 0, 0}, {0, 0, 0}};
-    int halves = 1;        // streams that share the rows of the prefix's job
-    int64_t half_step = 0;
-    auto record = [&](int i, int col, Source& s) {
-        const Record r = a.view.recs[i];
-        if (r.pages == 0) return;
-        const int64_t u = (int64_t)r.unit + (int64_t)kv * r.pages;
-        const int64_t w0 = share_of(u, h.units, h.warps), w1 = share_of(u + r.pages - 1, h.units, h.warps);
-        s = {record_entry(r, a.hkv, a.G, kv, w0) + col, kRecordCols, (int)(w1 - w0) + 1};
-    };
-    record(2 * row + 1, g, src[0]);
-    const int run = a.view.row_run[row];
-    bool large = false;
-    if (run >= 0) {
-        const Run r = a.view.runs[run];
-        large = r.pages > 0;
-        if (large) {
-            const int each = chunk_rows(r.rows, r.chunks), chunk = (row - run) / each, row0 = chunk * each;
-            const int rows = min(each, r.rows - row0), w = page_cost(r.rows, r.chunks, a.G);
-            const int64_t first = r.cost + (int64_t)(kv * r.chunks + chunk) * r.pages * w;
-            const int64_t w0 = share_of(first, h.cost, h.prefix_ctas), w1 = share_of(first + (int64_t)(r.pages - 1) * w, h.cost, h.prefix_ctas);
-            halves = chunk_wide(rows, a.G) ? 1 : 2;
-            half_step = (int64_t)rows * a.G;
-            src[1] = {run_entry(r, a.hkv, a.G, kv, row0, w0) + (row - run - row0) * a.G + g, 4 * kTileRows, (int)(w1 - w0 + 1) * halves};
-        } else {
-            record(2 * run, (row - run) * a.G + g, src[1]);
-        }
-    }
+    // Workers of the row's own job and of its prefix's, the first and the last of each.
+    const bool run = x.kind == 2;
+    const int64_t own_unit = (int64_t)x.own_unit + (int64_t)kv * x.own_pages;
+    const int64_t pre_unit = run ? x.cost + kv * x.head_cost : (int64_t)x.place + (int64_t)kv * x.pages;
+    const int64_t pre_last = pre_unit + (int64_t)(x.pages - 1) * (run ? x.page_cost : 1);
+    const Shares shares = run ? h.cost : h.units;
+    const int own0 = h.units.worker(own_unit), own = x.own_pages > 0 ? h.units.worker(own_unit + x.own_pages - 1) - own0 + 1 : 0;
+    const int pre0 = shares.worker(pre_unit);
+    const int streams = run && !chunk_wide(x.crows, a.G) ? 2 : 1;      // that share the rows of the prefix's job
+    const int total = own + (x.kind ? (shares.worker(pre_last) - pre0 + 1) * streams : 0);
+    const int64_t own_entry = record_entry(x.own_col, 1, a.hkv, a.G, kv, own0) + g;
+    const int64_t pre_entry = run ? run_entry(x.place, x.rows, a.hkv, a.G, kv, x.row0, pre0) + (row - x.first - x.row0) * a.G + g
+                                  : record_entry(x.col, x.rows, a.hkv, a.G, kv, pre0) + (row - x.first) * a.G + g;
+    const int step = run ? 4 * kTileRows : kRecordCols, stream_step = x.crows * a.G;
+
     float m = -INFINITY, l = 0.f, o[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) o[i] = 0.f;
-    for (int k = 0; k < 2; ++k) {
-        const bool of_run = k == 1 && large;
-        const float2* ml = of_run ? a.view.run_ml : a.view.rec_ml;
-        const float* po = of_run ? a.view.run_o : a.view.rec_o;
-        for (int s0 = 0; s0 < src[k].count; s0 += 32) {
-            const int s = s0 + lane, n = min(32, src[k].count - s0), by = of_run ? halves : 1;
-            const int64_t e = src[k].entry + (int64_t)(s / by) * src[k].step + (s % by) * half_step;
-            const float2 x = s < src[k].count ? ml[e] : make_float2(-INFINITY, 0.f);
-            float top = x.y == 0.f ? -INFINITY : x.x;   // (a segment without tokens has no part)
+#pragma unroll 1
+    for (int s0 = warp; s0 < total; s0 += 128) {
+        // This lane's segment: its (m, l) and where its sums lie.
+        const int s = s0 + 4 * lane, n = min(32, (total - s0 + 3) / 4), p = s - own;
+        const bool in_run = run && p >= 0;
+        const int64_t e = p < 0 ? own_entry + (int64_t)s * kRecordCols
+                                : pre_entry + (int64_t)(streams == 2 ? p >> 1 : p) * step + (streams == 2 && (p & 1) ? stream_step : 0);
+        const float2 ml = lane < n ? (in_run ? a.view.run_ml : a.view.rec_ml)[e] : make_float2(-INFINITY, 0.f);
+        const uint64_t from = reinterpret_cast<uint64_t>((in_run ? a.view.run_o : a.view.rec_o) + e * D);
+        float top = ml.y == 0.f ? -INFINITY : ml.x;   // (a segment without tokens has no part)
 #pragma unroll
-            for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-            top = fmaxf(top, m);
-            const float old = m == top ? 1.f : ex2(m - top), mine = x.y == 0.f ? 0.f : x.x == top ? 1.f : ex2(x.x - top);
-            float sum = x.y * mine;
+        for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        top = fmaxf(top, m);
+        const float old = m == top ? 1.f : ex2(m - top), mine = ml.y == 0.f ? 0.f : ml.x == top ? 1.f : ex2(ml.x - top);
+        float sum = ml.y * mine;
 #pragma unroll
-            for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-            m = top;
-            l = l * old + sum;
+        for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        m = top;
+        l = l * old + sum;
 #pragma unroll
-            for (int i = 0; i < N; ++i) o[i] *= old;
-#pragma unroll 4
-            for (int j = 0; j < n; ++j) {
-                const float wj = __shfl_sync(0xffffffffu, mine, j);
-                const int64_t ej = __shfl_sync(0xffffffffu, e, j);
-                const float* p = po + ej * D + lane * N;
-                if constexpr (N == 4) {
-                    const float4 v = *reinterpret_cast<const float4*>(p);
-                    o[0] += wj * v.x;
-                    o[1] += wj * v.y;
-                    o[2] += wj * v.z;
-                    o[3] += wj * v.w;
-                } else {
-                    const float2 v = *reinterpret_cast<const float2*>(p);
-                    o[0] += wj * v.x;
-                    o[1] += wj * v.y;
+        for (int i = 0; i < N; ++i) o[i] *= old;
+        uint32_t parts = __ballot_sync(0xffffffffu, mine != 0.f);   // (what has no weight may hold anything)
+        while (parts) {
+            Vec v[8];
+            float f[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int k = parts ? __ffs(parts) - 1 : 0;
+                f[j] = __shfl_sync(0xffffffffu, mine, k);
+                if (!parts) f[j] = 0.f;
+                else v[j] = reinterpret_cast<const Vec*>(__shfl_sync(0xffffffffu, from, k))[lane];
+                parts &= parts - 1;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (f[j] != 0.f) {
+                    o[0] += f[j] * v[j].x;
+                    o[1] += f[j] * v[j].y;
+                    if constexpr (N == 4) {
+                        o[2] += f[j] * v[j].z;
+                        o[3] += f[j] * v[j].w;
+                    }
                 }
             }
         }
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int i = 0; i < N; ++i) s_o[warp][lane * N + i] = o[i];
+    if (lane == 0) s_ml[warp] = make_float2(m, l);
+    __syncthreads();
+    if (warp != 0) return;
+    float f[4], top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) top = fmaxf(top, s_ml[k].y == 0.f ? -INFINITY : s_ml[k].x);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float2 ml = s_ml[k];
+        f[k] = ml.y == 0.f ? 0.f : ml.x == top ? 1.f : ex2(ml.x - top);
+        sum += f[k] * ml.y;
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float y = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y += f[k] * s_o[k][lane * N + i];
+        o[i] = y * inv;
+    }
     uint16_t* const dst = a.out + (int64_t)row * a.out_stride + (int64_t)head * D + lane * N;
-    if constexpr (N == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(T::pack(o[0] * inv, o[1] * inv), T::pack(o[2] * inv, o[3] * inv));
-    else *reinterpret_cast<uint32_t*>(dst) = T::pack(o[0] * inv, o[1] * inv);
-    if (a.lse && lane == 0) a.lse[(int64_t)row * a.hq + head] = l == 0.f ? -INFINITY : m * 0.693147180559945309f + logf(l);
+    if constexpr (N == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(T::pack(o[0], o[1]), T::pack(o[2], o[3]));
+    else *reinterpret_cast<uint32_t*>(dst) = T::pack(o[0], o[1]);
+    if (a.lse && lane == 0) a.lse[(int64_t)row * a.hq + head] = sum == 0.f ? -INFINITY : top * 0.693147180559945309f + logf(sum);
 }
 
 PFN_cuTensorMapEncodeTiled_v12000 encoder()
@@ -903,12 +1001,22 @@ template <int D, class T>
 int launch_attention(const CUtensorMap& mk, const CUtensorMap& mv, const AttnArgs& a, cudaStream_t st)
 {
     static OncePerDevice once;
-    if (cudaError_t e = once.set_attribute(attention_kernel<D, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, Geo<D>::kSmem); e != cudaSuccess)
+    if (cudaError_t e = once.set_attribute(attention_kernel<D, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes<D>); e != cudaSuccess)
         return kv4_launch_result(e);
-    if (cudaError_t e = kv4_launch(attention_kernel<D, T>, dim3((unsigned)a.grid), kThreads, Geo<D>::kSmem, st, mk, mv, a); e != cudaSuccess)
+    // How its warps share registers holds for this number at launch.
+    int device = 0;
+    if (cudaError_t e = cudaGetDevice(&device); e != cudaSuccess) return kv4_launch_result(e);
+    static OncePerDevice registers;
+    if (cudaError_t e = registers(device, [] {
+            cudaFuncAttributes f;
+            const cudaError_t r = cudaFuncGetAttributes(&f, attention_kernel<D, T>);
+            return r != cudaSuccess ? r : f.numRegs == kRegisters ? cudaSuccess : cudaErrorInvalidKernelImage;
+        });
+        e != cudaSuccess)
         return kv4_launch_result(e);
-    const int64_t units = (int64_t)a.batch * a.hq;
-    return kv4_launch_result(kv4_launch(merge_kernel<D, T>, dim3((unsigned)((units + 3) / 4)), 128, 0, st, a));
+    if (cudaError_t e = kv4_launch(attention_kernel<D, T>, dim3((unsigned)a.grid), kThreads, kSharedBytes<D>, st, mk, mv, a); e != cudaSuccess)
+        return kv4_launch_result(e);
+    return kv4_launch_result(kv4_launch(merge_kernel<D, T>, dim3((unsigned)a.hq, (unsigned)a.batch), 128, 0, st, a));
 }
 
 }  // namespace

@@ -32,17 +32,29 @@ __device__ __forceinline__ Sums shuffle_up(const Sums& s, int n)
     return {__shfl_up_sync(0xffffffffu, s.units, n), __shfl_up_sync(0xffffffffu, s.cost, n), __shfl_up_sync(0xffffffffu, s.cols, n),
             __shfl_up_sync(0xffffffffu, s.rows, n)};
 }
+__device__ __forceinline__ Sums broadcast(const Sums& s, int from)
+{
+    return {__shfl_sync(0xffffffffu, s.units, from), __shfl_sync(0xffffffffu, s.cost, from), __shfl_sync(0xffffffffu, s.cols, from),
+            __shfl_sync(0xffffffffu, s.rows, from)};
+}
 struct Max {
     int32_t v;
 };
+__device__ __forceinline__ Max broadcast(const Max& s, int from) { return {__shfl_sync(0xffffffffu, s.v, from)}; }
 __device__ __forceinline__ Max operator+(const Max& a, const Max& b) { return {max(a.v, b.v)}; }
 __device__ __forceinline__ Max shuffle_up(const Max& s, int n) { return {__shfl_up_sync(0xffffffffu, s.v, n)}; }
 
 // Inclusive scan over the block's threads on top of `before`, which moves on by the total.
+// (By the first `warps` warps, which hold all rows; the others only keep the barriers.)
 template <class S>
-__device__ __forceinline__ S block_scan(S s, S* before, S* warp_sums)
+__device__ __forceinline__ S block_scan(S s, S* before, S* warp_sums, int warps)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (warp >= warps) {
+        __syncthreads();
+        __syncthreads();
+        return s;
+    }
 #pragma unroll 1
     for (int n = 1; n < 32; n <<= 1) {
         const S o = shuffle_up(s, n);
@@ -50,13 +62,17 @@ __device__ __forceinline__ S block_scan(S s, S* before, S* warp_sums)
     }
     if (lane == 31) warp_sums[warp] = s;
     __syncthreads();
-    S start = *before;
+    S t = warp_sums[lane < warps ? lane : warps - 1];
 #pragma unroll 1
-    for (int i = 0; i < warps; ++i) {
-        if (i == warp) s = start + s;
-        start = start + warp_sums[i];
+    for (int n = 1; n < warps; n <<= 1) {
+        const S o = shuffle_up(t, n);
+        if (lane >= n && lane < warps) t = o + t;
     }
-    *before = start;
+    const S start = *before;
+    s = start + s;
+    const S ahead = broadcast(t, max(warp - 1, 0));
+    if (warp > 0) s = ahead + s;
+    *before = start + broadcast(t, warps - 1);
     __syncthreads();
     return s;
 }
@@ -77,16 +93,35 @@ __device__ __forceinline__ int last_at(const I* first, int n, I x)
     return lo;
 }
 
+// Bytes of shared memory for each row.
+constexpr int kPlanRowBytes = 8 + 12 * 4;
+
 __global__ void __launch_bounds__(kPlanMaxThreads) plan_kernel(StepPlanArgs a)
 {
     extern __shared__ int64_t shared[];
-    int64_t* const s_cost = shared;                                   // [batch]
-    int32_t* const s_unit = reinterpret_cast<int32_t*>(s_cost + a.batch);   // [2 * batch]
-    int32_t* const s_pre = s_unit + 2 * a.batch;                      // [batch]: prefix, -1: none, of length 0 or refused
-    int32_t* const s_rows = s_pre + a.batch;                          // [batch]: rows of the run that starts there
+    const int B = a.batch;
+    int64_t* const s_cost = shared;                                   // by row: first cost unit of the run that starts there
+    int32_t* s_next = reinterpret_cast<int32_t*>(s_cost + B);
+    auto take = [&](int n) {
+        int32_t* const p = s_next;
+        s_next += n * B;
+        return p;
+    };
+    int32_t* const s_unit = take(2);     // by record: its first unit
+    int32_t* const s_col = take(2);      // query rows before it
+    int32_t* const s_req = take(1);      // the row's request
+    int32_t* const s_len = take(1);      // and its tokens
+    int32_t* const s_pre = take(1);      // prefix, -1: none, of length 0 or refused
+    int32_t* const s_plen = take(1);     // its tokens
+    int32_t* const s_rows = take(1);     // rows of the run that starts here
+    int32_t* const s_first = take(1);    // first row of the run that the row is in
+    int32_t* const s_before = take(1);   // rows in large runs before
+    int32_t* const s_pages = take(1);    // of the run that starts here; 0: none does
+    __shared__ PlanHeader s_header;
     __shared__ Sums sum_warps[kPlanMaxThreads / 32];
     __shared__ Max max_warps[kPlanMaxThreads / 32];
-    const int tid = threadIdx.x, threads = blockDim.x, B = a.batch, G = a.hq / a.hkv;
+    const int tid = threadIdx.x, threads = blockDim.x, G = a.hq / a.hkv;
+    const int warps_needed = min((B + 31) / 32, threads / 32);
     griddep_wait();
     griddep_launch_dependents();
 
@@ -104,21 +139,16 @@ __global__ void __launch_bounds__(kPlanMaxThreads) plan_kernel(StepPlanArgs a)
         return n;
     };
     bool any_bad = false;
-    // Own lengths go through the records, prefixes through shared memory.
 #pragma unroll 1
     for (int r = tid; r < B; r += threads) {
         const int req = a.seq_ids ? a.seq_ids[r] : r, pre = a.prefix_ids ? a.prefix_ids[r] : -1;
         bool bad = false;
         const int n = length(req, &bad), np = pre == -1 ? 0 : length(pre, &bad);
         any_bad |= bad;
+        s_req[r] = req;
+        s_len[r] = bad ? 0 : n;
         s_pre[r] = bad || np == 0 ? -1 : pre;
-        Record own{};
-        own.req = req;
-        own.len = bad ? 0 : n;
-        own.pages = bad ? 0 : pages_of(n);
-        own.row0 = r;
-        own.rows = 1;
-        a.view.recs[2 * r + 1] = own;
+        s_plen[r] = np;
     }
     if (any_bad) kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
     __syncthreads();
@@ -129,82 +159,78 @@ __global__ void __launch_bounds__(kPlanMaxThreads) plan_kernel(StepPlanArgs a)
         const int r = r0 + tid;
         const int pre = r < B ? s_pre[r] : -1;
         const bool starts = r < B && (r == 0 || s_pre[r - 1] != pre);
-        const Max at = block_scan(Max{starts ? r : -1}, &before_max, max_warps);
+        const Max at = block_scan(Max{starts ? r : -1}, &before_max, max_warps, warps_needed);
         if (r < B) {
-            a.view.row_run[r] = pre >= 0 ? at.v : -1;
+            s_first[r] = pre >= 0 ? at.v : -1;
             if (r + 1 == B || s_pre[r + 1] != pre) s_rows[at.v] = r + 1 - at.v;
         }
     }
     __syncthreads();
+    // A run's chunks.
+    auto chunks_of = [&](int rows) {
+        const int pair = 2 * (kTileRows / G), each = chunk_rows(rows, (rows + pair - 1) / pair);
+        return (rows + each - 1) / each;   // (nearly equal: the last ones might have been left without rows)
+    };
     // Places in the lines of work.
     Sums total{0, 0, 0, 0};
 #pragma unroll 1
     for (int r0 = 0; r0 < B; r0 += threads) {
         const int r = r0 + tid;
         Sums mine{0, 0, 0, 0};
-        Record own{}, small{};
         Run run{};
+        int small_pages = 0, rows = 0, pages = 0;
         if (r < B) {
-            own = a.view.recs[2 * r + 1];
-            const int pre = s_pre[r];
-            if (pre >= 0 && (r == 0 || s_pre[r - 1] != pre)) {
-                const int n = a.lens[pre], rows = s_rows[r], pages = pages_of(n);
+            if (s_first[r] == r) {
+                rows = s_rows[r];
+                pages = pages_of(s_plen[r]);
                 if (rows * G <= kRecordCols) {
-                    small.req = pre;
-                    small.len = n;
-                    small.pages = pages;
-                    small.row0 = r;
-                    small.rows = rows;
+                    small_pages = pages;
+                    mine.cols = rows * G;
                 } else {
-                    run.req = pre;
-                    run.len = n;
-                    run.pages = pages;
-                    run.rows = rows;
-                    const int pair = 2 * (kTileRows / G);
-                    run.chunks = (rows + pair - 1) / pair;
-                    // (nearly equal chunks: the last ones may be left without rows)
-                    const int each = chunk_rows(rows, run.chunks);
-                    run.chunks = (rows + each - 1) / each;
-                    mine.cost = (int64_t)pages * a.hkv * run.chunks * page_cost(rows, run.chunks, G);
+                    run.chunks = chunks_of(rows);
+                    const int cost = page_cost(rows, run.chunks, G);
+                    mine.cost = (int64_t)(pages + job_start(cost)) * a.hkv * run.chunks * cost;
                     mine.rows = rows;
                 }
             }
-            mine.units = (int64_t)(small.pages + own.pages) * a.hkv;
-            mine.cols = (small.rows + own.rows) * G;
+            mine.units = (int64_t)(small_pages + pages_of(s_len[r])) * a.hkv;
+            mine.cols += G;
         }
-        const Sums at = block_scan(mine, &total, sum_warps);
+        const Sums at = block_scan(mine, &total, sum_warps, warps_needed);
         if (r < B) {
             const int64_t unit = at.units - mine.units;
-            small.unit = (int32_t)unit;
-            own.unit = (int32_t)(unit + (int64_t)small.pages * a.hkv);
-            small.col = at.cols - mine.cols;
-            own.col = small.col + small.rows * G;
-            run.cost = at.cost - mine.cost;
-            run.rows_before = at.rows - mine.rows;
-            s_unit[2 * r] = small.unit;
-            s_unit[2 * r + 1] = own.unit;
-            s_cost[r] = run.cost;
-            a.view.recs[2 * r] = small;
-            a.view.recs[2 * r + 1] = own;
+            s_unit[2 * r] = (int32_t)unit;
+            s_unit[2 * r + 1] = (int32_t)(unit + (int64_t)small_pages * a.hkv);
+            s_col[2 * r] = at.cols - mine.cols;
+            s_col[2 * r + 1] = at.cols - G;
+            s_pages[r] = pages;
+            s_cost[r] = at.cost - mine.cost;
+            s_before[r] = at.rows - mine.rows;
+            run.req = s_pre[r];
+            run.len = s_plen[r];
+            run.pages = mine.cost ? pages : 0;
+            run.rows = rows;
+            run.cost = s_cost[r];
+            run.rows_before = s_before[r];
             a.view.runs[r] = run;
+            const int n = s_len[r];
+            a.view.recs[2 * r] = Record{s_pre[r], s_plen[r], small_pages, r, rows, s_unit[2 * r], s_col[2 * r], 0};
+            a.view.recs[2 * r + 1] = Record{s_req[r], n, pages_of(n), r, 1, s_unit[2 * r + 1], s_col[2 * r + 1], 0};
         }
     }
-    const bool fits = total.units < (int64_t)1 << 31 && total.cost < (int64_t)1 << 40;
-    // CTAs for large runs, the others for records: the cut at which the slower side is fastest.
-    int ctas = 0;
-    if (total.cost > 0) {
-        const double c = (double)total.cost, u = (double)total.units * kRecordCost;
-        ctas = a.grid;
-        if (total.units > 0) {
-            const int f = min(max((int)(a.grid * c / (c + u)), 1), a.grid - 1), g = min(f + 1, a.grid - 1);
-            ctas = max(c / f, u / (a.grid - f)) <= max(c / g, u / (a.grid - g)) ? f : g;
-        }
-        const int64_t enough = total.cost / (2 * kWideCost);   // every worker has a page of each kind
-        if (ctas > enough) ctas = (int)max(enough, (int64_t)1);
-    }
-    const int64_t slots = (int64_t)(a.grid - ctas) * kAttnWarps;
-    const int64_t warps = min(slots, total.units);
     if (tid == 0) {
+        // CTAs for large runs, the others for records: the cut at which the slower side is fastest.
+        const bool fits = total.units < (int64_t)1 << 31 && total.cost < (int64_t)1 << 40;
+        int ctas = 0;
+        if (total.cost > 0) {
+            const float c = (float)total.cost, u = (float)total.units * kRecordCost;   // (64-bit floating point is far slower here)
+            ctas = a.grid;
+            if (total.units > 0) {
+                const int f = min(max((int)(a.grid * c / (c + u)), 1), a.grid - 1), g = min(f + 1, a.grid - 1);
+                ctas = max(c / f, u / (a.grid - f)) <= max(c / g, u / (a.grid - g)) ? f : g;
+            }
+            if (total.cost < (int64_t)ctas * kLeastRunPages * kWideCost) ctas = max((int)total.cost / (kLeastRunPages * kWideCost), 1);
+        }
         if (!fits) kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
         PlanHeader h{};
         h.magic = fits ? kPlanMagic : 0;
@@ -216,30 +242,71 @@ __global__ void __launch_bounds__(kPlanMaxThreads) plan_kernel(StepPlanArgs a)
         h.max_seqs = a.max_seqs;
         h.max_pages = a.max_pages;
         h.prefix_ctas = ctas;
-        h.warps = (int)warps;
-        h.units = total.units;
-        h.cost = total.cost;
+        h.warps = (int)min((int64_t)(a.grid - ctas) * kAttnWarps, (total.units + kLeastRecordPages - 1) / kLeastRecordPages);
+        if (fits) {
+            h.units = make_shares(total.units, h.warps);
+            h.cost = make_shares(total.cost, ctas);
+        }
         *a.view.header = h;
+        s_header = h;
     }
     __syncthreads();
-    if (!fits) return;
+    if (s_header.magic == 0) return;
+    // Where workers start.
+    const Shares units = s_header.units, costs = s_header.cost;
 #pragma unroll 1
-    for (int w = tid; w < warps; w += threads) {
-        const int32_t u = (int32_t)share_start(w, total.units, warps);
-        const int i = last_at(s_unit, 2 * B, u);
-        const int pages = a.view.recs[i].pages, off = u - s_unit[i];
-        const int head = off / pages;
-        a.view.warp_starts[w] = WarpStart{i, head, off - head * pages, 0};
+    for (int w = tid; w < units.n; w += threads) {
+        const int32_t u = (int32_t)units.start(w);
+        const int i = last_at(s_unit, 2 * B, u), r = i >> 1;
+        const bool own = i & 1;
+        const int len = own ? s_len[r] : s_plen[r], pages = pages_of(len), off = u - s_unit[i], head = (int)divide(off, pages);
+        a.view.warp_starts[w] = WarpStart{i, head, off - head * pages, (int32_t)units.start(w + 1) - u,
+                                          Record{own ? s_req[r] : s_pre[r], len, pages, r, own ? 1 : s_rows[r], s_unit[i], s_col[i], 0}};
     }
 #pragma unroll 1
-    for (int c = tid; c < ctas; c += threads) {
-        const int64_t at = share_start(c, total.cost, ctas);
-        int i = last_at(s_cost, B, at);
-        const Run run = a.view.runs[i];
-        const int w = page_cost(run.rows, run.chunks, G);
-        const int64_t page = (at - run.cost + w - 1) / w;      // the first page that starts at or after the share
-        const int64_t job = page / run.pages;
-        a.view.cta_starts[c] = CtaStart{i, (int32_t)job, (int32_t)(page - job * run.pages), 0};   // (job: may be one past the run's last)
+    for (int c = threads - 1 - tid; c < costs.n; c += threads) {   // (the last threads: the first have more of the others)
+        const int64_t at = costs.start(c), end = costs.start(c + 1);
+        const int i = last_at(s_cost, B, at), rows = s_rows[i], chunks = chunks_of(rows);
+        const Run run{s_pre[i], s_plen[i], s_pages[i], rows, s_cost[i], s_before[i], chunks};
+        const int w = page_cost(rows, chunks, G), start = job_start(w);
+        // The first page that starts at or after the share; the segment may be of the run's next job, or of none.
+        const int64_t page = pages_at(at - run.cost, w);
+        int job = (int)divide(page, run.pages + start), p = max((int)(page - (int64_t)job * (run.pages + start)) - start, 0);
+        Segment s{};
+        if (p < run.pages && job < chunks * a.hkv) s = make_segment(run, i, job, p, end, a.hkv, G, c);
+        if (s.pages > 0 || p > 0) ++job;
+        a.view.cta_starts[c] = CtaStart{i, job, end, run, s};
+    }
+    // What the merge reads of a row.
+#pragma unroll 1
+    for (int r = tid; r < B; r += threads) {
+        RowSources x{};
+        x.own_unit = s_unit[2 * r + 1];
+        x.own_pages = pages_of(s_len[r]);
+        x.own_col = s_col[2 * r + 1];
+        const int first = s_first[r];
+        if (first >= 0) {
+            const int rows = s_rows[first];
+            x.first = first;
+            x.pages = pages_of(s_plen[r]);
+            x.rows = rows;
+            if (rows * G <= kRecordCols) {
+                x.kind = 1;
+                x.place = s_unit[2 * first];
+                x.col = s_col[2 * first];
+            } else {
+                const int chunks = chunks_of(rows), each = chunk_rows(rows, chunks), chunk = (r - first) / each;
+                const int cost = page_cost(rows, chunks, G), opens = job_start(cost);
+                x.kind = 2;
+                x.place = s_before[first];
+                x.cost = s_cost[first] + ((int64_t)chunk * (x.pages + opens) + opens) * cost;
+                x.head_cost = (int64_t)chunks * (x.pages + opens) * cost;
+                x.row0 = chunk * each;
+                x.crows = min(each, rows - x.row0);
+                x.page_cost = cost;
+            }
+        }
+        a.view.rows[r] = x;
     }
 }
 
@@ -275,11 +342,9 @@ extern "C" KVC_API int kv16_plan(const kv16_pool* pool, const kv_tables* tables,
     a.dim = pool->head_dim;
     a.grid = sms;
     a.err = device_error;
-    constexpr int kRowBytes = 8 + 4 * 4;
     static OncePerDevice once;
-    if (cudaError_t e = once.set_attribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowBytes * kKv16MaxBatch);
+    if (cudaError_t e = once.set_attribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPlanRowBytes * kKv16MaxBatch);
         e != cudaSuccess)
         return kv4_launch_result(e);
-    const int threads = batch <= 256 ? 256 : kPlanMaxThreads;   // (few rows: shorter scans and barriers)
-    return kv4_launch_result(kv4_launch(plan_kernel, dim3(1), threads, (size_t)kRowBytes * batch, static_cast<cudaStream_t>(stream), a));
+    return kv4_launch_result(kv4_launch(plan_kernel, dim3(1), kPlanMaxThreads, (size_t)kPlanRowBytes * batch, static_cast<cudaStream_t>(stream), a));
 }

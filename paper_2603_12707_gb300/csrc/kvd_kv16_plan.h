@@ -17,18 +17,48 @@
 
 namespace kvd {
 
-constexpr int kAttnWarps = 12;          // of a CTA; the workers of records
+constexpr int kAttnWarps = 12;          // of a CTA that work on records
 constexpr int kRecordCols = 8;          // query rows of a record's job at most
 constexpr int kTileRows = 128;          // query rows of one of a CTA's two streams
+constexpr int kTilePages = 8;           // of a tile of a large run: 128 tokens
 constexpr uint32_t kPlanMagic = 0x16a77e41u;
+
+// Cost of a page of a large run's job, with both streams on rows of their own or taking turns, and what opening and
+// closing a job costs beside, in such pages; a record's page costs kRecordCost.
+constexpr int kRecordCost = 16, kWideCost = 20, kNarrowCost = 10, kWideStart = 15, kNarrowStart = 30;
+// Shares are not made smaller than this (pages): every segment is one more result to merge.
+constexpr int kLeastRunPages = 8, kLeastRecordPages = 4;
+
+// `total` units cut into n shares; worker w's starts at w * total / n, as far as 20 bits after the point go (rounded up, so
+// that the last one ends at the total).
+struct Shares {
+    int64_t each;       // in 2^-20 units
+    float inverse;      // workers a unit
+    int32_t n;
+    __host__ __device__ int64_t start(int w) const { return w * each >> 20; }
+    // The worker whose share holds unit u: an estimate that is one off at most, mended.
+    __host__ __device__ int worker(int64_t u) const
+    {
+        int w = (int)((float)u * inverse);
+        w = w < n - 1 ? w : n - 1;
+        w -= w > 0 && start(w) > u;
+        w += w + 1 < n && start(w + 1) <= u;
+        return w;
+    }
+};
+__host__ __device__ inline Shares make_shares(int64_t total, int n)   // total < 2^40
+{
+    if (n == 0 || total == 0) return {0, 0.f, 0};
+    return {((total << 20) + n - 1) / n, (float)n / (float)total, n};
+}
 
 struct PlanHeader {
     uint32_t magic;
     int32_t batch, hq, hkv, dim, grid, max_seqs, max_pages;   // what it was made for
     int32_t prefix_ctas;        // CTAs 0 .. are the workers of large runs
     int32_t warps;              // workers of records
-    int64_t units;              // pages x KV heads of all records
-    int64_t cost;               // of all large runs
+    Shares units;               // pages x KV heads of all records
+    Shares cost;                // of all large runs
 };
 
 struct Record {
@@ -46,23 +76,53 @@ struct Run {                    // by its first row; pages 0 in the other rows
     int32_t chunks;             // row chunks of a KV head
 };
 
-struct WarpStart {              // where a worker of records starts
-    int32_t rec, head, page, pad;
+// A worker's part of a large run's job.
+struct Segment {
+    int32_t pages;               // 0: no more segments
+    int32_t valid;               // tokens from its first page to the prefix's end
+    int32_t wide;                // the streams have rows of their own (else they take turns at the tiles)
+    int32_t head, row0, rows;    // KV head, first batch row, batch rows
+    int32_t rows0;               // batch rows of stream 0's tile
+    int32_t first;               // its first page
+    int64_t entry;               // of its results
+    __host__ __device__ int tiles() const { return (pages + kTilePages - 1) / kTilePages; }
+    __host__ __device__ int tile_pages(int t) const
+    {
+        const int left = pages - t * kTilePages;
+        return left < kTilePages ? left : kTilePages;
+    }
 };
 
-struct CtaStart {               // where a worker of large runs starts
-    int32_t run, job, page, pad;
+struct WarpStart {              // where a worker of records starts, and what it does
+    int32_t rec, head, page, count;
+    Record r;
 };
 
-// Cost of a page of a large run's job: with both streams on rows of their own, or on halves of a tile's tokens.
-// A record's page costs kRecordCost.
-constexpr int kRecordCost = 16, kWideCost = 13, kNarrowCost = 7;
+struct CtaStart {               // where a worker of large runs starts, and the end of its share
+    int32_t run, job;           // the job after the first segment
+    int64_t end;
+    Run r;
+    Segment s;                  // the first segment
+};
+
+// What the merge has to know of a row: its own tokens' job and its prefix's.
+struct RowSources {
+    int32_t own_unit, own_pages, own_col;
+    int32_t kind;               // of the prefix: 0 none, 1 a record, 2 a large run
+    int32_t first;              // first row of the run
+    int32_t pages, rows;
+    int32_t place;              // a record's unit, or a run's rows_before
+    int64_t cost;               // of a large run: of its row chunk's first page for KV head 0
+    int64_t head_cost;          // from one KV head to the next
+    int32_t row0, crows, page_cost;   // of the chunk: first row in the run, rows
+    int32_t col;                // of a record
+};
 
 struct PlanView {
     PlanHeader* header;
     Record* recs;               // [2 * batch]: 2 r the small run that starts in row r, 2 r + 1 row r's own tokens
     Run* runs;                  // [batch]
-    int32_t* row_run;           // [batch]: first row of the run that row r is in, -1: none
+    RowSources* rows;           // [batch]
     WarpStart* warp_starts;     // [grid * kAttnWarps]
     CtaStart* cta_starts;       // [grid]
     float* rec_o;               // partial results of records: [entries][dim], and (m, l)
@@ -88,7 +148,7 @@ __host__ __device__ inline PlanView plan_view(void* base, int batch, int hq, int
     v.header = reinterpret_cast<PlanHeader*>(take(sizeof(PlanHeader)));
     v.recs = reinterpret_cast<Record*>(take((int64_t)sizeof(Record) * 2 * batch));
     v.runs = reinterpret_cast<Run*>(take((int64_t)sizeof(Run) * batch));
-    v.row_run = reinterpret_cast<int32_t*>(take((int64_t)4 * batch));
+    v.rows = reinterpret_cast<RowSources*>(take((int64_t)sizeof(RowSources) * batch));
     v.warp_starts = reinterpret_cast<WarpStart*>(take((int64_t)sizeof(WarpStart) * grid * kAttnWarps));
     v.cta_starts = reinterpret_cast<CtaStart*>(take((int64_t)sizeof(CtaStart) * grid));
     // Entries of a record's segment: its query rows; segments are jobs and cuts between workers.
@@ -103,9 +163,14 @@ __host__ __device__ inline PlanView plan_view(void* base, int batch, int hq, int
     return v;
 }
 
-// Start of worker w's share of `total` units among n workers, and the worker whose share holds unit u.
-__host__ __device__ inline int64_t share_start(int64_t w, int64_t total, int64_t n) { return w * total / n; }
-__host__ __device__ inline int64_t share_of(int64_t u, int64_t total, int64_t n) { return ((u + 1) * n - 1) / total; }
+// x / d for x >= 0 and a quotient below 2^22.
+__host__ __device__ inline int64_t divide(int64_t x, int32_t d)
+{
+    int64_t q = (int64_t)((float)x / (float)d);
+    while (q * d > x) --q;
+    while ((q + 1) * d <= x) ++q;
+    return q;
+}
 
 // Chunks of a large run's rows: nearly equal, of up to 2 * (128 / G) batch rows.
 __host__ __device__ inline int chunk_rows(int rows, int chunks) { return (rows + chunks - 1) / chunks; }
@@ -114,15 +179,42 @@ __host__ __device__ inline int page_cost(int rows, int chunks, int G)
 {
     return chunk_wide(chunk_rows(rows, chunks), G) ? kWideCost : kNarrowCost;
 }
+__host__ __device__ inline int job_start(int cost) { return cost == kWideCost ? kWideStart : kNarrowStart; }
+// x / cost rounded up, x >= 0, by either cost of a page.
+__host__ __device__ inline int64_t pages_at(int64_t x, int cost) { return cost == kWideCost ? (x + kWideCost - 1) / kWideCost : (x + kNarrowCost - 1) / kNarrowCost; }
 
 // First entries of partial results.
-__host__ __device__ inline int64_t record_entry(const Record& r, int hkv, int G, int head, int64_t worker)
+__host__ __device__ inline int64_t record_entry(int col, int rows, int hkv, int G, int head, int worker)
 {
-    return (int64_t)r.col * hkv + (int64_t)head * r.rows * G + kRecordCols * worker;
+    return (int64_t)col * hkv + (int64_t)head * rows * G + kRecordCols * worker;
 }
-__host__ __device__ inline int64_t run_entry(const Run& r, int hkv, int G, int head, int row_in_run, int64_t worker)
+__host__ __device__ inline int64_t run_entry(int rows_before, int rows, int hkv, int G, int head, int row_in_run, int worker)
 {
-    return (int64_t)2 * G * ((int64_t)r.rows_before * hkv + (int64_t)head * r.rows + row_in_run) + 4 * kTileRows * worker;
+    return (int64_t)2 * G * ((int64_t)rows_before * hkv + (int64_t)head * rows + row_in_run) + 4 * kTileRows * worker;
+}
+
+// The segment of a worker whose share ends at `end`: job `job` of the run from page `page` on.  pages 0: the share ends
+// before it.
+__host__ __device__ inline Segment make_segment(const Run& r, int run, int job, int page, int64_t end, int hkv, int G, int worker)
+{
+    Segment s{};
+    const int each = chunk_rows(r.rows, r.chunks), cost = chunk_wide(each, G) ? kWideCost : kNarrowCost, opens = job_start(cost);
+    const int64_t left = end - (r.cost + (int64_t)job * (r.pages + opens) * cost);
+    if (left <= 0) return s;
+    int64_t stop = pages_at(left, cost) - opens;
+    if (stop > r.pages) stop = r.pages;
+    if (stop <= page) return s;
+    s.head = job / r.chunks;
+    const int first = (job - s.head * r.chunks) * each;
+    s.pages = (int)stop - page;
+    s.valid = r.len - page * kPageSize;
+    s.row0 = run + first;
+    s.rows = each < r.rows - first ? each : r.rows - first;
+    s.wide = chunk_wide(s.rows, G);
+    s.rows0 = s.wide ? (s.rows + 1) / 2 : s.rows;
+    s.first = page;
+    s.entry = run_entry(r.rows_before, r.rows, hkv, G, s.head, first, worker);
+    return s;
 }
 
 }  // namespace kvd
