@@ -32,18 +32,19 @@ namespace {
 
 constexpr uint64_t kLimitNs = 1000000000ull;       // of waits for copies before leaving
 constexpr long long kLimitCycles = 2000000000ll;   // of all others: a second
-constexpr int kSoftmaxWarps = 16;                  // two streams of two halves of four
+constexpr int kSoftmaxWarps = 8;                   // two streams of four
 constexpr int kThreads = 32 * (kSoftmaxWarps + 4);
-constexpr int kRegisters = 96;                     // of a thread at launch
 constexpr int kLoadWarp = kSoftmaxWarps, kMmaWarp = kSoftmaxWarps + 1;
 
 template <int D>
 struct Geo {
     static constexpr int kBlocks = D / 64;                        // blocks of 64 columns (128 bytes)
-    static constexpr int kBlockBytes = kTileRows * 128;           // of a tile of 128 rows
+    static constexpr int kQueryBlock = kTileRows * 128;           // bytes of a block of a tile of queries
+    static constexpr int kQueryTile = kBlocks * kQueryBlock;
+    static constexpr int kBlockBytes = kTilePages * kPageSize * 128;   // of a block of a tile of K or V
     static constexpr int kTileBytes = kBlocks * kBlockBytes;
     static constexpr int kSlots = D == 128 ? 5 : 9;               // tiles of K or V in the ring
-    static constexpr int kRing = 2 * kTileBytes;                  // after two tiles of queries
+    static constexpr int kRing = 2 * kQueryTile;                  // after two tiles of queries
     static constexpr int kPageBytes = kPageSize * D * 2;          // K, or V, of a page and KV head
     static constexpr int kStages = D == 128 ? 2 : 4;              // of a record warp's ring: K and V of a page each
     static constexpr int kWarpRing = kStages * 2 * kPageBytes;
@@ -74,19 +75,19 @@ struct AttnArgs {
     int32_t* err;
 };
 
-constexpr int kSegments = 8;         // told ahead: a tile at least each, so the ring ends it at five
+constexpr int kSegments = 8;         // told ahead: the ring has room for K and V of less than five tiles
 
 struct Control {                     // in shared memory
-    uint64_t full[10], empty[10];    // ring slots of large runs
+    // The ring's slots.  Copies end in any order, and a stream that takes turns passes over slots of the other's tiles: the tile
+    // before may still be on its way to a slot when this stream comes to wait for the next.  So a slot has two barriers, for every
+    // other tile; the tile two before has been used (the loading warp found it so before it loaded what the stream saw last).
+    uint64_t full[18], empty[9];
     uint64_t told[kSegments];
-    uint64_t scores[2], weights[2], output[2], queries, drained;   // by stream
-    uint64_t pair[2][4];             // of a stream's two warps with the same rows
-    int32_t pair_again[2][2][4];     // [stream][half][rows]: its weights want a higher reference
-    float pair_value[2][2][4][32];   // a row's largest score, or its sum of weights
-    int32_t pages_known[8];          // by tile: bits of its pages that are there (a tile's are read before the eighth after it is loaded)
+    uint64_t scores[2], weights[2][2], half[2], queries, drained;   // by stream; weights by half of a tile
+    int32_t pages_known[8];          // by tile: bits of its pages that are there (read before the eighth after it is loaded)
     uint32_t tmem;
     int32_t gave_up;                 // a wait ran out: everybody leaves
-    uint64_t last;                   // what was issued before leaving so
+    uint64_t last[2];                // what was issued before leaving so
     union {
         Segment segment[kSegments];
         uint64_t stage[kAttnWarps][4];   // rings of record warps
@@ -121,6 +122,11 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, Contro
     }
 }
 
+__device__ __forceinline__ void arrive(uint64_t* bar, uint32_t count)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(bar)), "r"(count) : "memory");
+}
+
 __device__ __forceinline__ void arrive(uint64_t* bar)
 {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
@@ -135,6 +141,9 @@ struct Order {
     __device__ __forceinline__ int k(int j) const { return j < ahead ? j : 2 * j - ahead + 1; }
     __device__ __forceinline__ int v(int n) const { return min(ahead + 2 * n, tiles + n); }
 };
+// A stream's tiles: how many, and its j-th.
+__device__ __forceinline__ int stream_tiles(int tiles, bool wide, int stream) { return wide ? tiles : (tiles + 1 - stream) >> 1; }
+__device__ __forceinline__ int stream_tile(bool wide, int stream, int j) { return wide ? j : 2 * j + stream; }
 
 // The loading warp: goes through the worker's share segment by segment, tells the others of each and loads its tiles.
 template <int D>
@@ -142,7 +151,8 @@ __device__ __forceinline__ void load_tiles(const AttnArgs& a, const CtaStart& st
                                            const CUtensorMap* mv)
 {
     using G = Geo<D>;
-    const int lane = threadIdx.x & 31, p = lane % kTilePages, block = lane / kTilePages;
+    const int lane = threadIdx.x & 31;
+    const bool one = elect_one();
     const uint64_t policy = l2_policy_evict_first();
     uint32_t n = 0, tile_no = 0, told = 0;                // tiles of K and V so far; of both; segments
     auto tell = [&](const Segment& s) {
@@ -175,33 +185,47 @@ __device__ __forceinline__ void load_tiles(const AttnArgs& a, const CtaStart& st
         const int32_t* row = a.table + (int64_t)r.req * a.max_pages + s.first;
         const int tiles = s.tiles();
         const Order order(tiles, s.wide);
-        // Page ids of the next tile of K, and those of the tiles of which V is still to come (one or two).
-        auto ids_of = [&](int t) { return t < tiles && p < s.tile_pages(t) ? row[t * kTilePages + p] : -1; };
-        int next = ids_of(0), even = -1, odd = -1, kt = 0, vt = 0;
+        // Page ids: a lane has a page of a window of four tiles, and of the one before it (V comes up to two later).
+        auto ids_of = [&](int window) {
+            const int page = window * 32 + lane;
+            return page < s.pages ? row[page] : -1;
+        };
+        int next = ids_of(0), now = -1, before = -1, kt = 0, vt = 0;
 #pragma unroll 1
         for (int i = 0; i < 2 * tiles; ++i, ++n) {
             const bool of_k = kt < tiles && i == order.k(kt);
-            const int t = of_k ? kt++ : vt++;
-            int id = t & 1 ? odd : even;
-            if (of_k) {
-                id = next;
-                next = ids_of(kt);
-                even = t & 1 ? even : id;
-                odd = t & 1 ? id : odd;
+            if (of_k && kt % 4 == 0) {
+                before = now;
+                now = next;
+                next = ids_of(kt / 4 + 1);
             }
-            const int np = s.tile_pages(t), slot = n % G::kSlots;
-            const bool known = p < np && id >= 0 && id < a.num_pages;
-            const uint32_t mask = __ballot_sync(0xffffffffu, known) & 0xffu, bar = smem_addr(&c.full[slot]);
+            const int t = of_k ? kt++ : vt++;
+            // (One lane issues the tile's copies, with operands in uniform registers: lanes with a copy each would be served one
+            // after the other, some 130 cycles each, which bounded the whole kernel.)
+            const int np = s.tile_pages(t), slot = n % G::kSlots, held = (kt - 1) / 4 == t / 4 ? now : before;
+            const uint32_t bar = smem_addr(&c.full[n % (2 * G::kSlots)]), dst = smem_addr(smem + G::kRing + slot * G::kTileBytes);
+            int rows[kTilePages];
+            uint32_t mask = 0;
+#pragma unroll
+            for (int p = 0; p < kTilePages; ++p) {
+                const int id = __shfl_sync(0xffffffffu, held, (t % 4) * kTilePages + p);
+                mask |= (p < np && id >= 0 && id < a.num_pages ? 1u : 0u) << p;
+                rows[p] = (id * a.hkv + s.head) * kPageSize;
+            }
             if (!(fine = warp_wait(&c.empty[slot], (n / G::kSlots & 1) ^ 1, c, a.err))) break;
-            if (lane == 0) {
+            if (one) {
                 if (of_k) c.pages_known[(tile_no + t) % 8] = (int32_t)mask;
                 if (mask != (1u << np) - 1u) kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
                 mbar_arrive_expect_tx(bar, __popc(mask) * (uint32_t)G::kPageBytes);
+                const CUtensorMap* const map = of_k ? mk : mv;
+#pragma unroll
+                for (int p = 0; p < kTilePages; ++p)
+                    if (mask >> p & 1u) {
+#pragma unroll
+                        for (int b = 0; b < G::kBlocks; ++b) tma_load_3d(dst + b * G::kBlockBytes + p * 2048, map, 0, rows[p], b, bar, policy);
+                    }
             }
             __syncwarp();
-            if (known && block < G::kBlocks)
-                tma_load_3d(smem_addr(smem + G::kRing + slot * G::kTileBytes + block * G::kBlockBytes + p * 2048), of_k ? mk : mv, 0,
-                            (id * a.hkv + s.head) * kPageSize, block, bar, policy);
         }
         tile_no += tiles;
         s.pages = 0;
@@ -210,86 +234,76 @@ __device__ __forceinline__ void load_tiles(const AttnArgs& a, const CtaStart& st
     // Where others gave up: what is under way arrives before the CTA leaves.
     if (*reinterpret_cast<volatile int32_t*>(&c.gave_up))
         for (uint32_t i = n > G::kSlots ? n - G::kSlots : 0; i < n; ++i)
-            mbar_wait_bounded(smem_addr(&c.full[i % G::kSlots]), i / G::kSlots & 1, kLimitNs);
+            mbar_wait_bounded(smem_addr(&c.full[i % (2 * G::kSlots)]), i / (2 * G::kSlots) & 1, kLimitNs);
 }
 
-// The issuing warp.  (All of it goes along, so that addresses and descriptors stay in uniform registers; one lane issues.)
+// A stream's issuing warp: a tile's weights against V, in halves as they come, then the stream's next tile of K against its
+// queries.  (All of the warp goes along, so that addresses and descriptors stay in uniform registers; one lane issues.  Two warps, since what one does
+// between its products takes as long as those.)
 template <int D, class T>
-__device__ __forceinline__ void issue_products(const AttnArgs& a, Control& c, uint8_t* smem)
+__device__ __forceinline__ void issue_products(const AttnArgs& a, Control& c, uint8_t* smem, int stream)
 {
     using G = Geo<D>;
     constexpr bool kBf16 = std::is_same_v<T, Bf16>;
-    const uint32_t base = smem_addr(smem), tm = c.tmem;
+    const uint32_t base = smem_addr(smem), ring = base + G::kRing, ts = c.tmem + stream * 128, to = c.tmem + 256 + stream * 128;
     const bool one = elect_one();
-    uint32_t n0 = 0, ready[2] = {0, 0};
-    bool wide = false;
-    // K of a tile against a stream's queries.
-    auto scores = [&](int stream, uint32_t slot, int pages) {
-        const uint64_t q = smem_desc(base + (wide ? stream * G::kTileBytes : 0), 16, 1024);
-        const uint64_t k = smem_desc(base + G::kRing + slot * G::kTileBytes, 16, 1024);
-        const uint32_t idesc = mma_desc(kBf16, false, kTileRows, pages * kPageSize), d = tm + stream * 128;
-        if (one) {
-#pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) {
-                const uint32_t off = ((ks / 4) * G::kBlockBytes + (ks % 4) * 32) >> 4;
-                mma_ss(d, q + off, k + off, idesc, ks > 0);
-            }
-            mma_commit(smem_addr(&c.scores[stream]));
-            arrive(&c.scores[stream]);       // (what the loading warp has said of the tile comes along)
-        }
-        __syncwarp();
-    };
-    // A stream's weights against V; a half's weights lie where its scores were.
-    auto outputs = [&](int stream, uint32_t slot, int pages, bool add) {
-        const int half = (pages + 1) / 2;
-        const uint64_t v = smem_desc(base + G::kRing + slot * G::kTileBytes, G::kBlockBytes, 1024);
-        const uint32_t idesc = mma_desc(kBf16, true, kTileRows, D), d = tm + 256 + stream * 128, w = tm + stream * 128;
-        if (one) {
-#pragma unroll
-            for (int kk = 0; kk < kTilePages; ++kk)
-                if (kk < pages) mma_ts(d, w + kk * 8 + (kk < half ? 0 : half * 8), v + kk * (2048 >> 4), idesc, add || kk > 0);
-        }
-        __syncwarp();
-    };
-    auto commit = [&](uint64_t* bar) {
-        if (one) mma_commit(smem_addr(bar));
-        __syncwarp();
-    };
-    auto slot_of = [&](int at) { return (n0 + at) % G::kSlots; };
-    auto arrived = [&](int at) { return warp_wait(&c.full[slot_of(at)], (n0 + at) / G::kSlots & 1, c, a.err); };
+    uint32_t n0 = 0, first_halves = 0, second_halves = 0;
 #pragma unroll 1
     for (uint32_t segment = 0;; ++segment) {
         if (!warp_wait(&c.told[segment % kSegments], segment / kSegments & 1, c, a.err)) return;
         const Segment s = c.segment[segment % kSegments];
         if (s.pages == 0) return;
-        wide = s.wide;
-        const int tiles = s.tiles(), step = wide ? 1 : 2;
+        const bool wide = s.wide;
+        const int tiles = s.tiles(), mine = stream_tiles(tiles, wide, stream);
         const Order order(tiles, wide);
+        const uint64_t q = smem_desc(base + (wide ? stream * G::kQueryTile : 0), 16, 1024);
+        const uint32_t vdesc = mma_desc(kBf16, true, kTileRows, D);
+        auto arrived = [&](int at) { return warp_wait(&c.full[(n0 + at) % (2 * G::kSlots)], (n0 + at) / (2 * G::kSlots) & 1, c, a.err); };
         if (!warp_wait(&c.queries, segment & 1, c, a.err)) return;
-        // The streams' first tiles, then turns: a tile's weights against its V, the stream's next tile of K against its queries.
-        const int turns = wide ? 2 * tiles : tiles;
 #pragma unroll 1
-        for (int i = -2; i < turns; ++i) {
-            const int st = i & 1, t = i < 0 ? -1 : wide ? i >> 1 : i, next = i < 0 ? (wide ? 0 : st) : t + step;
-            const bool last_use = !wide || st == 1, more = next < tiles;
-            const uint32_t vslot = slot_of(order.v(t)), kslot = slot_of(order.k(next));
-            if (i >= 0 && !arrived(order.v(t))) return;
-            if (more && !arrived(order.k(next))) return;
-            if (i >= 0) {
-                const uint32_t turn = st ? ready[1]++ : ready[0]++;
-                if (!warp_wait(&c.weights[st], turn & 1, c, a.err)) return;
+        for (int j = -1; j < mine; ++j) {
+            const int t = stream_tile(wide, stream, j), next = stream_tile(wide, stream, j + 1);
+            const int vat = order.v(t), kat = order.k(next), pages = s.tile_pages(t);
+            const bool more = j + 1 < mine;
+            const uint64_t v = smem_desc(ring + (n0 + vat) % G::kSlots * G::kTileBytes, G::kBlockBytes, 1024);
+            const uint64_t k = smem_desc(ring + (n0 + kat) % G::kSlots * G::kTileBytes, 16, 1024);
+            const uint32_t kdesc = mma_desc(kBf16, false, kTileRows, s.tile_pages(next) * kPageSize);
+            if (j >= 0) {
+                if (!arrived(vat)) return;
+                if (!warp_wait(&c.weights[stream][0], first_halves++ & 1, c, a.err)) return;
+                tmem_fence_after();
+                if (one) {                        // (weights lie where their scores were, those of each half by themselves)
+#pragma unroll
+                    for (int kk = 0; kk < kTilePages / 2; ++kk)
+                        if (kk < pages) mma_ts(to, ts + kk * 8, v + kk * (2048 >> 4), vdesc, j > 0 || kk > 0);
+                    if (pages > kTilePages / 2) mma_commit(smem_addr(&c.half[stream]));
+                }
+                __syncwarp();
+                if (more && !arrived(kat)) return;
+                if (pages > kTilePages / 2 && !warp_wait(&c.weights[stream][1], second_halves++ & 1, c, a.err)) return;
+            } else if (more && !arrived(kat)) {
+                return;
             }
             tmem_fence_after();
-            if (i >= 0) {
-                outputs(st, vslot, s.tile_pages(t), t >= step);
-                if (last_use) commit(&c.empty[vslot]);
+            if (one) {
+                if (j >= 0) {
+#pragma unroll
+                    for (int kk = kTilePages / 2; kk < kTilePages; ++kk)
+                        if (kk < pages) mma_ts(to, ts + kk * 8 + 32, v + kk * (2048 >> 4), vdesc, true);
+                }
+                if (more) {
+#pragma unroll
+                    for (int ks = 0; ks < D / 16; ++ks)
+                        mma_ss(ts, q + (((ks / 4) * G::kQueryBlock + (ks % 4) * 32) >> 4), k + (((ks / 4) * G::kBlockBytes + (ks % 4) * 32) >> 4),
+                               kdesc, ks > 0);
+                }
+                // Scores are there, and what came before is done (or there is nothing to do).  One commit for each group of
+                // products, right behind it: who reads the scores frees the slots.
+                if (j >= 0 || more) mma_commit(smem_addr(&c.scores[stream]));
+                else if (mine == 0) arrive(&c.scores[stream]);
+                if (j >= 0 || more || mine == 0) arrive(&c.scores[stream]);   // (what the loading warp has said of the tile comes along)
             }
-            if (more) {
-                scores(st, kslot, s.tile_pages(next));
-                if (last_use) commit(&c.empty[kslot]);
-            } else {
-                commit(&c.output[st]);
-            }
+            __syncwarp();
         }
         n0 += 2 * tiles;
     }
@@ -317,7 +331,7 @@ __device__ __forceinline__ void load_queries(const AttnArgs& a, const Segment& s
         for (int i = 0; i < kLoads; ++i) {
             const int qr = r0 + i * kStep, tile = qr >= rows0, r = qr - (tile ? rows0 : 0);
             if (qr < total)
-                *reinterpret_cast<uint4*>(smem + tile * G::kTileBytes + (ch >> 3) * G::kBlockBytes + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = x[i];
+                *reinterpret_cast<uint4*>(smem + tile * G::kQueryTile + (ch >> 3) * G::kQueryBlock + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = x[i];
         }
     }
 }
@@ -330,89 +344,16 @@ __device__ __forceinline__ uint32_t token_bits(int page, uint32_t known, int val
     return known >> page & 1u ? (1u << n) - 1u : 0u;
 }
 
-// A warp's scores of a tile: up to 4 pages of its rows, a row to a lane.
-struct Scores {
-    uint32_t at;       // in tensor memory
-    int first, pages;  // of the tile
-    bool whole;        // all tokens take part
-    uint32_t known;
-    int valid;
-    // Pages 2 i and 2 i + 1; of one that there is not, -infinity.
-    __device__ __forceinline__ void load(int i, uint32_t (&x)[32]) const
-    {
-        tmem_ld32(at + 32 * i, x);
-        tmem_wait_ld();
-        if (!whole || 2 * i + 2 > pages) {
-            const uint32_t bits = token_bits(first + 2 * i, known, valid) | (2 * i + 2 > pages ? 0u : token_bits(first + 2 * i + 1, known, valid) << 16);
-#pragma unroll
-            for (int k = 0; k < 32; ++k) x[k] = bits >> k & 1u ? x[k] : 0xff800000u;
-        }
-    }
-};
-
-// A row's largest score.
-__device__ __forceinline__ float largest(const Scores& s)
-{
-    float mx = -INFINITY;
-#pragma unroll 1
-    for (int i = 0; 2 * i < s.pages; ++i) {
-        uint32_t x[32];
-        s.load(i, x);
-#pragma unroll
-        for (int k = 0; k < 32; k += 2) mx = fmaxf(mx, fmaxf(__uint_as_float(x[k]), __uint_as_float(x[k + 1])));
-    }
-    return mx;
-}
-
-// A row's weights 2^(s * sl - sub), two to a word, and their sum; the scores stay in tensor memory.
-template <class T>
-__device__ __forceinline__ float weigh(const Scores& s, float sl, float sub, uint32_t (&p)[2][16])
-{
-    const uint64_t sl2 = f2_pack(sl, sl), sub2 = f2_pack(-sub, -sub);
-    uint64_t sum[2] = {0ull, 0ull};
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        if (2 * i < s.pages) {
-            uint32_t x[32];
-            s.load(i, x);
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                float u, v;
-                f2_unpack(f2_fma(f2_pack(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1])), sl2, sub2), u, v);
-                u = ex2(u);
-                v = ex2(v);
-                sum[k & 1] = f2_add(sum[k & 1], f2_pack(u, v));
-                p[i][k] = T::pack(u, v);
-            }
-        }
-    }
-    float u, v;
-    f2_unpack(f2_add(sum[0], sum[1]), u, v);
-    return u + v;
-}
-
-// What a row's weights in half a tile may add up to: fp16 holds each of them, and sums of 32 bits stay far from their end.
-// A reference that is the largest score leaves at most 64 times the weights' factor of 2^7.
-constexpr float kMostWeight = 32768.f;
-
-// Two warps share a row's tokens: the first half of a tile's pages and the second.  Weights are worked out with the
-// reference that there is; where the sum of either half says that it is too low (or there is none yet) both move to the
-// largest score of the tile and do it again.
+// A stream's softmax: a thread owns a row of the tile, whose scores are all in its registers at once.
 template <int D, class T>
 __device__ __forceinline__ void softmax_stream(const AttnArgs& a, Control& c, uint8_t* smem)
 {
     using G = Geo<D>;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, stream = warp >> 3, half = warp >> 2 & 1, wq = warp & 3;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, stream = warp >> 2, wq = warp & 3;
     const int my = wq * 32 + lane;                        // row of the stream's tile
-    const uint32_t tm = c.tmem + ((uint32_t)wq << 21), ts = tm + stream * 128, to = tm + 256 + stream * 128 + half * (D / 2);
-    uint32_t n0 = 0, tile_no = 0, turn = 0, meetings = 0;
+    const uint32_t tm = c.tmem + ((uint32_t)wq << 21), ts = tm + stream * 128, to = tm + 256 + stream * 128;
+    uint32_t n0 = 0, tile_no = 0, phase = 0, halves = 0;  // phase: of the next scores; halves: first halves so far
     const float sl = a.scale_log2;
-    uint64_t* const pair = &c.pair[stream][wq];
-    auto meet = [&] {
-        __syncwarp();
-        if (lane == 0) arrive(pair);
-        return warp_wait(pair, meetings++ & 1, c, a.err);
-    };
 #pragma unroll 1
     for (uint32_t segment = 0;; ++segment) {
         if (!warp_wait(&c.told[segment % kSegments], segment / kSegments & 1, c, a.err)) return;
@@ -423,100 +364,131 @@ __device__ __forceinline__ void softmax_stream(const AttnArgs& a, Control& c, ui
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) arrive(&c.queries);
-        const int tiles = s.tiles(), wide = s.wide;
+        const int tiles = s.tiles(), wide = s.wide, mine = stream_tiles(tiles, wide, stream);
         const int qrows = (wide && stream == 1 ? s.rows - s.rows0 : s.rows0) * a.G;
         const bool works = wq * 32 < qrows;               // (the others have no row of the tile)
         const Order order(tiles, wide);
+        // (A slot is free when both streams have used its tile.)
+        auto free_slot = [&](int at) { arrive(&c.empty[(n0 + at) % G::kSlots], wide ? 1 : 2); };
         float ref = -INFINITY, l = 0.f;
-        bool some = false;                                // products with V so far
 #pragma unroll 1
-        for (int t = wide ? 0 : stream; t < tiles; t += wide ? 1 : 2, ++turn) {
-            const int pages = s.tile_pages(t), h0 = (pages + 1) / 2;
-            if (!warp_wait(&c.scores[stream], turn & 1, c, a.err)) return;
+        for (int j = 0; j < mine; ++j) {
+            const int t = stream_tile(wide, stream, j), pages = s.tile_pages(t), valid = s.valid - t * kTilePages * kPageSize;
+            if (!warp_wait(&c.scores[stream], phase++ & 1, c, a.err)) return;
             tmem_fence_after();
-            Scores x;
-            x.known = (uint32_t)c.pages_known[(tile_no + t) % 8];
-            x.valid = s.valid - t * kTilePages * kPageSize;
-            x.whole = x.valid >= pages * kPageSize && x.known == (1u << pages) - 1u;
-            x.at = ts + (half ? h0 * 16 : 0);
-            x.first = half ? h0 : 0;
-            x.pages = half ? pages - h0 : h0;
-            if (works) {
-                uint32_t p[2][16];
-                float sum;
-                bool move = !some;
+            if (wq == 0 && lane == 0) {   // the tile of K has been used, and the stream's last one of V
+                free_slot(order.k(t));
+                if (j > 0) free_slot(order.v(stream_tile(wide, stream, j - 1)));
+            }
+            const uint32_t known = (uint32_t)c.pages_known[(tile_no + t) % 8];
+            const bool whole = valid >= kTilePages * kPageSize && known == (1u << kTilePages) - 1u;
+            const int parts = pages > kTilePages / 2 ? 2 : 1;
+            // A half of the tile's tokens at a time: the first's product with V runs while the second is worked.
 #pragma unroll 1
-                while (true) {
-                    if (move) {
-                        const float mx = largest(x) * sl;
-                        c.pair_value[stream][half][wq][lane] = mx;
-                        if (!meet()) return;
-                        const float top = my < qrows ? fmaxf(ref, fmaxf(mx, c.pair_value[stream][half ^ 1][wq][lane])) : 0.f;
-                        if (some) {
-                            const float alpha = ref == top ? 1.f : ex2(ref - top);
+            for (int h = 0; h < parts; ++h) {
+                const uint32_t sc = ts + h * 64;
+                if (works) {
+                    uint32_t x[2][32];
+                    tmem_ld32(sc, x[0]);
+                    tmem_ld32(sc + 32, x[1]);
+                    tmem_wait_ld();
+                    tmem_loaded(x[0]);
+                    tmem_loaded(x[1]);
+                    if (!whole) {
+#pragma unroll
+                        for (int w = 0; w < 2; ++w) {
+                            const uint32_t bits = token_bits(4 * h + 2 * w, known, valid) | token_bits(4 * h + 2 * w + 1, known, valid) << 16;
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) x[w][i] = bits >> i & 1u ? x[w][i] : 0xff800000u;
+                        }
+                    }
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) mx = fmaxf(mx, fmaxf(__uint_as_float(x[0][i]), __uint_as_float(x[1][i])));
+                    mx *= sl;
+                    // The reference moves where a score exceeds it by more than 8 (see the top); no row looks at another's.
+                    const bool moves = my < qrows && mx > ref + 8.f;
+                    if (__any_sync(0xffffffffu, moves)) {
+                        if (j > 0 || h > 0) {
+                            // (Scores that have come were issued after the products of the tile before; the first half's say so.)
+                            if (h > 0) {
+                                if (!warp_wait(&c.half[stream], halves & 1, c, a.err)) return;
+                                tmem_fence_after();
+                            }
+                            const float alpha = moves ? ex2(ref - mx) : 1.f;
                             l *= alpha;
 #pragma unroll 1
-                            for (int w = 0; w < D / 32; ++w) {
+                            for (int w = 0; w < D / 16; ++w) {
                                 uint32_t o[16];
                                 tmem_ld16(to + 16 * w, o);
                                 tmem_wait_ld();
+                                tmem_loaded(o);
 #pragma unroll
                                 for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
                                 tmem_st16(to + 16 * w, o);
                             }
                         }
-                        ref = top;
+                        ref = moves ? mx : ref;
                     }
-                    sum = weigh<T>(x, sl, (ref == -INFINITY ? 0.f : ref) - Weights<T>::kShift, p);
-                    if (move) break;
-                    move = __any_sync(0xffffffffu, my < qrows && (sum > kMostWeight || ref == -INFINITY));
-                    if (lane == 0) c.pair_again[stream][half][wq] = move;
-                    if (!meet()) return;
-                    move |= c.pair_again[stream][half ^ 1][wq] != 0;
-                    if (!move) break;
-                }
-                l += sum;
+                    const float sub = (ref == -INFINITY ? 0.f : ref) - Weights<T>::kShift;
+                    const uint64_t sl2 = f2_pack(sl, sl), sub2 = f2_pack(-sub, -sub);
+                    uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    if (2 * i < x.pages) tmem_st16(x.at + 16 * i, p[i]);
-                tmem_wait_st();
-            }
-            some = true;
-            if (!x.whole) {   // rows of V that hold anything: zero, or 0 * NaN would reach the sums
-                const uint32_t n = n0 + order.v(t), vslot = n % G::kSlots;
-                if (!warp_wait(&c.full[vslot], n / G::kSlots & 1, c, a.err)) return;
+                    for (int w = 0; w < 2; ++w) {
+                        uint32_t p[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            float u, v;
+                            f2_unpack(f2_fma(f2_pack(__uint_as_float(x[w][2 * i]), __uint_as_float(x[w][2 * i + 1])), sl2, sub2), u, v);
+                            u = ex2(u);
+                            v = ex2(v);
+                            sum[i & 1] = f2_add(sum[i & 1], f2_pack(u, v));
+                            p[i] = T::pack(u, v);
+                        }
+                        tmem_st16(sc + 16 * w, p);
+                    }
+                    float u, v;
+                    f2_unpack(f2_add(sum[0], sum[1]), u, v);
+                    l += u + v;
+                    tmem_wait_st();
+                }
+                if (!whole) {   // rows of V that hold anything: zero, or 0 * NaN would reach the sums
+                    const uint32_t n = n0 + order.v(t), vslot = n % G::kSlots;
+                    if (!warp_wait(&c.full[n % (2 * G::kSlots)], n / (2 * G::kSlots) & 1, c, a.err)) return;
 #pragma unroll 1
-                for (int r = x.first * kPageSize + wq; r < (x.first + x.pages) * kPageSize; r += 4)
-                    if (r >= x.valid || !(x.known >> (r / kPageSize) & 1u))
-                        for (int b = 0; b < G::kBlocks; ++b)
-                            *reinterpret_cast<uint32_t*>(smem + G::kRing + vslot * G::kTileBytes + b * G::kBlockBytes + r * 128 + lane * 4) = 0u;
-                fence_proxy_async_smem();
+                    for (int r = h * (kTilePages / 2) * kPageSize + wq; r < min(pages, (h + 1) * (kTilePages / 2)) * kPageSize; r += 4)
+                        if (r >= valid || !(known >> (r / kPageSize) & 1u))
+                            for (int b = 0; b < G::kBlocks; ++b)
+                                *reinterpret_cast<uint32_t*>(smem + G::kRing + vslot * G::kTileBytes + b * G::kBlockBytes + r * 128 + lane * 4) = 0u;
+                    fence_proxy_async_smem();
+                }
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) arrive(&c.weights[stream][h]);
             }
-            tmem_fence_before();
-            __syncwarp();
-            if (lane == 0) arrive(&c.weights[stream]);
+            halves += parts - 1;
         }
+        const bool some = mine > 0;
+        if (!warp_wait(&c.scores[stream], phase++ & 1, c, a.err)) return;   // (the last products are done)
+        if (some && wq == 0 && lane == 0) free_slot(order.v(stream_tile(wide, stream, mine - 1)));
         n0 += 2 * tiles;
         tile_no += tiles;
-        if (!warp_wait(&c.output[stream], segment & 1, c, a.err)) return;
         tmem_fence_after();
         if (works) {
-            // Both halves' sums (the other has read the last tile's values: its weights have arrived).
-            c.pair_value[stream][half][wq][lane] = l;
-            if (!meet()) return;
-            // Columns through shared memory (this warp's part of the query tiles, which all products have read by now), so
-            // that those of a row are stored together.
-            constexpr int kCols = D / 4, kRowBytes = kCols * 4, kPieces = kRowBytes / 16;   // 32 at d = 128, else 16; 16-byte pieces
+            // Some columns at a time through shared memory, so that those of a row are stored together: in the stream's own
+            // tile of queries, which its products have read by now, or in the second one where both streams work on the first.
+            constexpr int kCols = D / 4, kRowBytes = kCols * 4, kPieces = kRowBytes / 16;   // pieces of 16 bytes
             const int64_t entry = s.entry + (stream == 0 ? 0 : s.rows0 * a.G);
-            uint8_t* const mine = smem + warp * (32 * kRowBytes);
-            if (half == 0 && my < qrows)
-                a.view.run_ml[entry + my] = make_float2(some ? ref - Weights<T>::kShift : -INFINITY, some ? l + c.pair_value[stream][1][wq][lane] : 0.f);
+            uint8_t* const mine = smem + (wide ? stream * G::kQueryTile + wq * 32 * kRowBytes : G::kQueryTile + warp * 32 * kRowBytes);
+            static_assert(kSoftmaxWarps * 32 * kRowBytes <= G::kQueryTile);
+            if (my < qrows) a.view.run_ml[entry + my] = make_float2(some ? ref - Weights<T>::kShift : -INFINITY, some ? l : 0.f);
 #pragma unroll 1
-            for (int w = 0; some && w < 2; ++w) {
+            for (int w = 0; some && w < 4; ++w) {
                 uint32_t o[kCols];
                 if constexpr (D == 128) tmem_ld32(to + kCols * w, o);
                 else tmem_ld16(to + kCols * w, o);
                 tmem_wait_ld();
+                tmem_loaded(o);
 #pragma unroll
                 for (int i = 0; i < kPieces; ++i)
                     *reinterpret_cast<uint4*>(mine + lane * kRowBytes + ((i ^ (lane & (kPieces - 1))) << 4)) =
@@ -526,8 +498,7 @@ __device__ __forceinline__ void softmax_stream(const AttnArgs& a, Control& c, ui
                 for (int i = 0; i < kPieces; ++i) {
                     const int r = (32 / kPieces) * i + lane / kPieces, ch = lane % kPieces;
                     const uint4 v = *reinterpret_cast<const uint4*>(mine + r * kRowBytes + ((ch ^ (r & (kPieces - 1))) << 4));
-                    if (wq * 32 + r < qrows)
-                        *reinterpret_cast<uint4*>(a.view.run_o + (entry + wq * 32 + r) * D + half * (D / 2) + w * kCols + ch * 4) = v;
+                    if (wq * 32 + r < qrows) *reinterpret_cast<uint4*>(a.view.run_o + (entry + wq * 32 + r) * D + w * kCols + ch * 4) = v;
                 }
                 __syncwarp();
             }
@@ -625,6 +596,7 @@ __device__ __forceinline__ void work_records(const AttnArgs& a, const PlanHeader
     Windows win(a, start, left);
     uint32_t skipped = 0, phase = 0;                 // bits by stage: a page that is not there; the barrier's parity
     int put = 0, staged = 0;
+    const bool one = elect_one();
     auto load = [&] {
         if (win.done()) return;
         const int id = win.id();
@@ -632,13 +604,17 @@ __device__ __forceinline__ void work_records(const AttnArgs& a, const PlanHeader
         const uint32_t bar = smem_addr(&c.stage[warp][put]);
         if (known) {
             skipped &= ~(1u << put);
-            if (lane == 0) mbar_arrive_expect_tx(bar, 2 * G::kPageBytes);
-            __syncwarp();
-            if (lane < 2 * G::kBlocks) {
-                const int side = lane / G::kBlocks, block = lane % G::kBlocks;
-                tma_load_3d(smem_addr(ring + (put * 2 + side) * G::kPageBytes + block * 2048), side ? mv : mk, 0,
-                            (id * a.hkv + win.cur_head) * kPageSize, block, bar, policy);
+            if (one) {
+                const uint32_t dst = smem_addr(ring + put * 2 * G::kPageBytes);
+                const int row = (id * a.hkv + win.cur_head) * kPageSize;
+                mbar_arrive_expect_tx(bar, 2 * G::kPageBytes);
+#pragma unroll
+                for (int b = 0; b < G::kBlocks; ++b) {
+                    tma_load_3d(dst + b * 2048, mk, 0, row, b, bar, policy);
+                    tma_load_3d(dst + G::kPageBytes + b * 2048, mv, 0, row, b, bar, policy);
+                }
             }
+            __syncwarp();
         } else {
             skipped |= 1u << put;
             if (lane == 0) kv4_error(a.err, KVC_DEVERR_PAGE_RANGE);
@@ -791,22 +767,19 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kernel(const __grid_con
     // (The kernel has no other shared memory: what it is given starts on 1024 bytes, as the swizzle wants it.)
     extern __shared__ __align__(1024) uint8_t smem[];
     Control& c = *reinterpret_cast<Control*>(smem + Geo<D>::kData);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    if (tid < 10) {
-        mbar_init(smem_addr(&c.full[tid]), 1);
-        mbar_init(smem_addr(&c.empty[tid]), 1);
-    }
+    const int tid = threadIdx.x, warp = tid >> 5;
+    if (tid < 18) mbar_init(smem_addr(&c.full[tid]), 1);
+    if (tid < 9) mbar_init(smem_addr(&c.empty[tid]), 2);
     if (tid >= 64 && tid < 64 + kSegments) mbar_init(smem_addr(&c.told[tid - 64]), 1);
     if (tid < 2) {
         mbar_init(smem_addr(&c.scores[tid]), 2);
-        mbar_init(smem_addr(&c.weights[tid]), kSoftmaxWarps / 2);
-        mbar_init(smem_addr(&c.output[tid]), 1);
+        mbar_init(smem_addr(&c.half[tid]), 1);
     }
+    if (tid < 4) mbar_init(smem_addr(&c.weights[0][0] + tid), 4);
     if (tid == 2) mbar_init(smem_addr(&c.queries), kSoftmaxWarps);
     if (tid == 3) mbar_init(smem_addr(&c.drained), kSoftmaxWarps);
     if (tid == 4) c.gave_up = 0;
-    if (tid >= 32 && tid < 40) mbar_init(smem_addr(&c.pair[0][0] + (tid - 32)), 2);
-    if (tid == 5) mbar_init(smem_addr(&c.last), 1);
+    if (tid == 5 || tid == 6) mbar_init(smem_addr(&c.last[tid - 5]), 1);
     if (tid == 0) {
         prefetch_tensormap(&mk);
         prefetch_tensormap(&mv);
@@ -830,27 +803,20 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kernel(const __grid_con
             if (tid == 0 && blockIdx.x == 0) kv4_error(a.err, KVC_DEVERR_PLAN);
             return;
         }
-        // (Registers: 96 a thread at launch; three groups of four warps take 144, the other two leave with 24.)
-        if (warp < kAttnWarps) {
-            asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
-            work_records<D, T>(a, h, c, smem, &mk, &mv);
-        } else {
-            asm volatile("setmaxnreg.dec.sync.aligned.u32 24;");
-        }
+        if (warp < kAttnWarps) work_records<D, T>(a, h, c, smem, &mk, &mv);
         return;
     }
-    if (warp < kSoftmaxWarps) {   // (four groups of 104, one of 64)
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+    if (warp < kSoftmaxWarps) {
         softmax_stream<D, T>(a, c, smem);
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == kLoadWarp) {
             load_tiles<D>(a, start, c, smem, &mk, &mv);
-        } else if (warp == kMmaWarp) {
-            issue_products<D, T>(a, c, smem);
-            if (*reinterpret_cast<volatile int32_t*>(&c.gave_up) && lane == 0) {   // what is under way ends before the memory is freed
-                mma_commit(smem_addr(&c.last));
-                mbar_wait_bounded(smem_addr(&c.last), 0, kLimitNs);
+        } else if (warp < kMmaWarp + 2) {
+            issue_products<D, T>(a, c, smem, warp - kMmaWarp);
+            if (*reinterpret_cast<volatile int32_t*>(&c.gave_up) && elect_one()) {   // what is under way ends before the memory is freed
+                uint64_t* const last = &c.last[warp - kMmaWarp];
+                mma_commit(smem_addr(last));
+                mbar_wait_bounded(smem_addr(last), 0, kLimitNs);
             }
             __syncwarp();
         }
@@ -1002,17 +968,6 @@ int launch_attention(const CUtensorMap& mk, const CUtensorMap& mv, const AttnArg
 {
     static OncePerDevice once;
     if (cudaError_t e = once.set_attribute(attention_kernel<D, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes<D>); e != cudaSuccess)
-        return kv4_launch_result(e);
-    // How its warps share registers holds for this number at launch.
-    int device = 0;
-    if (cudaError_t e = cudaGetDevice(&device); e != cudaSuccess) return kv4_launch_result(e);
-    static OncePerDevice registers;
-    if (cudaError_t e = registers(device, [] {
-            cudaFuncAttributes f;
-            const cudaError_t r = cudaFuncGetAttributes(&f, attention_kernel<D, T>);
-            return r != cudaSuccess ? r : f.numRegs == kRegisters ? cudaSuccess : cudaErrorInvalidKernelImage;
-        });
-        e != cudaSuccess)
         return kv4_launch_result(e);
     if (cudaError_t e = kv4_launch(attention_kernel<D, T>, dim3((unsigned)a.grid), kThreads, kSharedBytes<D>, st, mk, mv, a); e != cudaSuccess)
         return kv4_launch_result(e);

@@ -1,5 +1,5 @@
 // kv16_plan: the plan of a decode step over shared prefixes (kvd_kv16_plan.h),
-// made by one CTA from the lengths on the device.  Runs of rows with one prefix come from a scan of maxima
+// made from the lengths on the device.  Every CTA finds the places of all rows and writes a part of the plan.  Runs of rows with one prefix come from a scan of maxima
 // over their first rows, places in the two lines of work from scans of sums, each worker's start from a
 // binary search.
 #include "kvd_kv16_plan.h"
@@ -122,6 +122,7 @@ __global__ void __launch_bounds__(kPlanMaxThreads) plan_kernel(StepPlanArgs a)
     __shared__ Max max_warps[kPlanMaxThreads / 32];
     const int tid = threadIdx.x, threads = blockDim.x, G = a.hq / a.hkv;
     const int warps_needed = min((B + 31) / 32, threads / 32);
+    const bool speaks = blockIdx.x == 0;       // one CTA writes and reports what all find
     griddep_wait();
     griddep_launch_dependents();
 
@@ -150,7 +151,7 @@ __global__ void __launch_bounds__(kPlanMaxThreads) plan_kernel(StepPlanArgs a)
         s_pre[r] = bad || np == 0 ? -1 : pre;
         s_plen[r] = np;
     }
-    if (any_bad) kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
+    if (any_bad && speaks) kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
     __syncthreads();
     // Runs.
     Max before_max{-1};
@@ -206,16 +207,18 @@ __global__ void __launch_bounds__(kPlanMaxThreads) plan_kernel(StepPlanArgs a)
             s_pages[r] = pages;
             s_cost[r] = at.cost - mine.cost;
             s_before[r] = at.rows - mine.rows;
-            run.req = s_pre[r];
-            run.len = s_plen[r];
-            run.pages = mine.cost ? pages : 0;
-            run.rows = rows;
-            run.cost = s_cost[r];
-            run.rows_before = s_before[r];
-            a.view.runs[r] = run;
-            const int n = s_len[r];
-            a.view.recs[2 * r] = Record{s_pre[r], s_plen[r], small_pages, r, rows, s_unit[2 * r], s_col[2 * r], 0};
-            a.view.recs[2 * r + 1] = Record{s_req[r], n, pages_of(n), r, 1, s_unit[2 * r + 1], s_col[2 * r + 1], 0};
+            if (speaks) {
+                run.req = s_pre[r];
+                run.len = s_plen[r];
+                run.pages = mine.cost ? pages : 0;
+                run.rows = rows;
+                run.cost = s_cost[r];
+                run.rows_before = s_before[r];
+                a.view.runs[r] = run;
+                const int n = s_len[r];
+                a.view.recs[2 * r] = Record{s_pre[r], s_plen[r], small_pages, r, rows, s_unit[2 * r], s_col[2 * r], 0};
+                a.view.recs[2 * r + 1] = Record{s_req[r], n, pages_of(n), r, 1, s_unit[2 * r + 1], s_col[2 * r + 1], 0};
+            }
         }
     }
     if (tid == 0) {
@@ -231,7 +234,7 @@ __global__ void __launch_bounds__(kPlanMaxThreads) plan_kernel(StepPlanArgs a)
             }
             if (total.cost < (int64_t)ctas * kLeastRunPages * kWideCost) ctas = max((int)total.cost / (kLeastRunPages * kWideCost), 1);
         }
-        if (!fits) kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
+        if (!fits && speaks) kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
         PlanHeader h{};
         h.magic = fits ? kPlanMagic : 0;
         h.batch = B;
@@ -247,15 +250,16 @@ __global__ void __launch_bounds__(kPlanMaxThreads) plan_kernel(StepPlanArgs a)
             h.units = make_shares(total.units, h.warps);
             h.cost = make_shares(total.cost, ctas);
         }
-        *a.view.header = h;
+        if (speaks) *a.view.header = h;
         s_header = h;
     }
     __syncthreads();
     if (s_header.magic == 0) return;
-    // Where workers start.
+    // Where workers start, and what the merge reads of a row, by all CTAs' threads.
+    const int all = threads * gridDim.x, at0 = blockIdx.x * threads + tid;
     const Shares units = s_header.units, costs = s_header.cost;
 #pragma unroll 1
-    for (int w = tid; w < units.n; w += threads) {
+    for (int w = at0; w < units.n; w += all) {
         const int32_t u = (int32_t)units.start(w);
         const int i = last_at(s_unit, 2 * B, u), r = i >> 1;
         const bool own = i & 1;
@@ -264,7 +268,7 @@ __global__ void __launch_bounds__(kPlanMaxThreads) plan_kernel(StepPlanArgs a)
                                           Record{own ? s_req[r] : s_pre[r], len, pages, r, own ? 1 : s_rows[r], s_unit[i], s_col[i], 0}};
     }
 #pragma unroll 1
-    for (int c = threads - 1 - tid; c < costs.n; c += threads) {   // (the last threads: the first have more of the others)
+    for (int c = all - 1 - at0; c < costs.n; c += all) {   // (the last threads: the first have more of the others)
         const int64_t at = costs.start(c), end = costs.start(c + 1);
         const int i = last_at(s_cost, B, at), rows = s_rows[i], chunks = chunks_of(rows);
         const Run run{s_pre[i], s_plen[i], s_pages[i], rows, s_cost[i], s_before[i], chunks};
@@ -277,9 +281,8 @@ __global__ void __launch_bounds__(kPlanMaxThreads) plan_kernel(StepPlanArgs a)
         if (s.pages > 0 || p > 0) ++job;
         a.view.cta_starts[c] = CtaStart{i, job, end, run, s};
     }
-    // What the merge reads of a row.
 #pragma unroll 1
-    for (int r = tid; r < B; r += threads) {
+    for (int r = at0; r < B; r += all) {
         RowSources x{};
         x.own_unit = s_unit[2 * r + 1];
         x.own_pages = pages_of(s_len[r]);
@@ -346,5 +349,7 @@ extern "C" KVC_API int kv16_plan(const kv16_pool* pool, const kv_tables* tables,
     if (cudaError_t e = once.set_attribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kPlanRowBytes * kKv16MaxBatch);
         e != cudaSuccess)
         return kv4_launch_result(e);
-    return kv4_launch_result(kv4_launch(plan_kernel, dim3(1), kPlanMaxThreads, (size_t)kPlanRowBytes * batch, static_cast<cudaStream_t>(stream), a));
+    // Few rows: small blocks, whose scans and barriers are shorter.
+    const int threads = batch <= 256 ? 256 : kPlanMaxThreads;
+    return kv4_launch_result(kv4_launch(plan_kernel, dim3(batch <= 256 ? 16 : 4), threads, (size_t)kPlanRowBytes * batch, static_cast<cudaStream_t>(stream), a));
 }

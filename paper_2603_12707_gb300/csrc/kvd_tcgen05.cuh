@@ -22,6 +22,15 @@ __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// Registers that a load before tmem_wait_ld wrote: no use of them moves ahead of this (and so of the wait).
+template <int N>
+__device__ __forceinline__ void tmem_loaded(uint32_t (&r)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; i += 8)
+        asm volatile("" : "+r"(r[i]), "+r"(r[i + 1]), "+r"(r[i + 2]), "+r"(r[i + 3]), "+r"(r[i + 4]), "+r"(r[i + 5]), "+r"(r[i + 6]), "+r"(r[i + 7]));
+}
+
 // 32 columns of this warp's 32 lanes; a lane is a row.  (What is loaded is there after tmem_wait_ld.)
 __device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t (&r)[32])
 {
