@@ -309,31 +309,24 @@ __device__ __forceinline__ void issue_products(const AttnArgs& a, Control& c, ui
     }
 }
 
-// The segment's queries, by the softmax warps: 16-byte chunks of up to 256 rows into the tiles' swizzle, four loads of a thread
-// under way.
+// The segment's queries, by the softmax warps: 16-byte chunks of up to 256 rows into the tiles' swizzle, all under way at once.
 template <int D>
 __device__ __forceinline__ void load_queries(const AttnArgs& a, const Segment& s, uint8_t* smem)
 {
     using G = Geo<D>;
-    constexpr int kChunks = D / 8, kStep = 32 * kSoftmaxWarps / kChunks, kLoads = 4;   // chunks of a row; rows at a time
-    const int total = s.rows * a.G, ch = threadIdx.x % kChunks, first = threadIdx.x / kChunks, rows0 = s.rows0 * a.G;
+    constexpr int kChunks = D / 8, kStep = 32 * kSoftmaxWarps / kChunks;   // chunks of a row; rows at a time
+    const int total = s.rows * a.G, ch = threadIdx.x % kChunks, rows0 = s.rows0 * a.G;
     const uint32_t by = (65536u + a.G - 1) / a.G;           // qr / G = qr * by >> 16 for qr < 256, G <= 8
     const uint16_t* q = a.q + (int64_t)s.row0 * a.q_stride + (int64_t)s.head * a.G * D + ch * 8;
-#pragma unroll 1
-    for (int r0 = first; r0 < total; r0 += kLoads * kStep) {
-        uint4 x[kLoads];
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int qr = min(r0 + i * kStep, total - 1), br = (int)(qr * by >> 16);
-            x[i] = *reinterpret_cast<const uint4*>(q + br * a.q_stride + (int64_t)(qr - br * a.G) * D);
-        }
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            const int qr = r0 + i * kStep, tile = qr >= rows0, r = qr - (tile ? rows0 : 0);
-            if (qr < total)
-                *reinterpret_cast<uint4*>(smem + tile * G::kQueryTile + (ch >> 3) * G::kQueryBlock + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = x[i];
-        }
+    const uint32_t to = smem_addr(smem) + (ch >> 3) * G::kQueryBlock;
+#pragma unroll 2
+    for (int qr = threadIdx.x / kChunks; qr < total; qr += kStep) {
+        const int br = (int)(qr * by >> 16), tile = qr >= rows0, r = qr - (tile ? rows0 : 0);
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + tile * G::kQueryTile + r * 128 + (((ch & 7) ^ (r & 7)) << 4)),
+                     "l"(q + br * a.q_stride + (int64_t)(qr - br * a.G) * D)
+                     : "memory");
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 // Bits of a page's 16 tokens that take part: none of a page that is not there, of the last page those before the prefix's end
@@ -402,10 +395,16 @@ __device__ __forceinline__ void softmax_stream(const AttnArgs& a, Control& c, ui
                             for (int i = 0; i < 32; ++i) x[w][i] = bits >> i & 1u ? x[w][i] : 0xff800000u;
                         }
                     }
-                    float mx = -INFINITY;
+                    float top[8];                         // (eight chains)
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) mx = fmaxf(mx, fmaxf(__uint_as_float(x[0][i]), __uint_as_float(x[1][i])));
-                    mx *= sl;
+                    for (int i = 0; i < 8; ++i) top[i] = fmaxf(__uint_as_float(x[0][i]), __uint_as_float(x[1][i]));
+#pragma unroll
+                    for (int i = 8; i < 32; ++i) top[i & 7] = fmaxf(top[i & 7], fmaxf(__uint_as_float(x[0][i]), __uint_as_float(x[1][i])));
+#pragma unroll
+                    for (int d = 4; d > 0; d >>= 1)
+#pragma unroll
+                        for (int i = 0; i < d; ++i) top[i] = fmaxf(top[i], top[i + d]);
+                    const float mx = top[0] * sl;
                     // The reference moves where a score exceeds it by more than 8 (see the top); no row looks at another's.
                     const bool moves = my < qrows && mx > ref + 8.f;
                     if (__any_sync(0xffffffffu, moves)) {
