@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(kPlanMaxThreads) plan_kernel(StepPlanArgs a)
         const bool fits = total.units < (int64_t)1 << 31 && total.cost < (int64_t)1 << 40;
         int ctas = 0;
         if (total.cost > 0) {
-            const float c = (float)total.cost, u = (float)total.units * kRecordCost;   // (64-bit floating point is far slower here)
+            const float c = (float)total.cost, u = (float)total.units * record_cost(a.dim);   // (64-bit floating point is far slower here)
             ctas = a.grid;
             if (total.units > 0) {
                 const int f = min(max((int)(a.grid * c / (c + u)), 1), a.grid - 1), g = min(f + 1, a.grid - 1);

@@ -16,7 +16,8 @@
 namespace kvd {
 namespace {
 
-constexpr int kRopeWarps = 8;
+constexpr int kRopeWarps = 1;      // of a CTA, so that a token's end frees its place (5003 normed tokens of 24 heads 15.4 us with 4, 13.9 with 1)
+constexpr int kAhead = 3;      // turns whose rows are under way together
 
 struct RopeArgs {
     const uint64_t* freqs;
@@ -55,17 +56,22 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8])
     return make_uint4(T::pack(x[0], x[1]), T::pack(x[2], x[3]), T::pack(x[4], x[5]), T::pack(x[6], x[7]));
 }
 
-// A head's elements on this lane, times 1 / sqrt(mean of squares + eps) and the weights.
+// 1 / sqrt(mean of squares + eps) of a head's elements, which makes them 2^-96 times as large where their squares pass the
+// range of 32 bits.
 template <int D>
-__device__ __forceinline__ void norm_row(float (&a)[8], float (&b)[8], float eps)
+__device__ __forceinline__ float norm_of(float (&a)[8], float (&b)[8], float eps)
 {
-    float s = 0.f;
+    float s = 0.f, z = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s = fmaf(a[i], a[i], fmaf(b[i], b[i], s));
+    for (int i = 0; i < 8; ++i) {
+        s = fmaf(a[i], a[i], s);
+        z = fmaf(b[i], b[i], z);
+    }
+    s += z;
 #pragma unroll
     for (int m = 1; m < D / 16; m <<= 1) s += __shfl_xor_sync(0xffffffffu, s, m);
     float r = rsqrtf(fmaf(s, 1.f / D, eps));
-    if (__any_sync(0xffffffffu, s > 0x1p126f)) {   // squares past the range of 32 bits: the same of elements 2^-96 times as large
+    if (__any_sync(0xffffffffu, s > 0x1p126f)) {
         const bool far = s > 0x1p126f;
         const float by = far ? 0x1p-96f : 1.f;
         float t = 0.f;
@@ -79,14 +85,31 @@ __device__ __forceinline__ void norm_row(float (&a)[8], float (&b)[8], float eps
         for (int m = 1; m < D / 16; m <<= 1) t += __shfl_xor_sync(0xffffffffu, t, m);
         if (far) r = rsqrtf(t * (1.f / D));
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        a[i] *= r;
-        b[i] *= r;
-    }
+    return r;
 }
 
-template <int D, class T, RopeKind KIND, bool POOL>
+// Sine and cosine of `turn` / 2^32 turns: the nearest quarter turn, and Taylor's series of what is left, at most pi / 4, to
+// terms below 2^-25.
+__device__ __forceinline__ void sine_cosine(uint32_t turn, float* sine, float* cosine)
+{
+    const uint32_t quarter = (turn + 0x20000000u) >> 30;
+    const float x = (float)(int32_t)(turn - (quarter << 30)) * 1.46291807926715968e-9f;   // 2 pi / 2^32
+    const float y = x * x;
+    const float s = fmaf(x * y, fmaf(y, fmaf(y, fmaf(y, 2.75573192e-6f, -1.98412698e-4f), 8.33333333e-3f), -1.66666667e-1f), x);
+    const float c = fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, -2.75573192e-7f, 2.48015873e-5f), -1.38888889e-3f), 4.16666667e-2f), -0.5f), 1.f);
+    const float u = quarter & 1 ? c : s, v = quarter & 1 ? s : c;
+    *sine = __uint_as_float(__float_as_uint(u) ^ (quarter & 2) << 30);
+    *cosine = __uint_as_float(__float_as_uint(v) ^ ((quarter + 1) & 2) << 30);
+}
+
+__device__ __forceinline__ uint4 load_row(const uint16_t* p)   // (read once; not kept in L1, since the same rows may be written)
+{
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+
+template <int D, class T, RopeKind KIND, bool NORM, bool POOL>
 __global__ void __launch_bounds__(32 * kRopeWarps) rope_kernel(RopeArgs a)
 {
     constexpr int kLanes = D / 16, kHeads = 32 / kLanes;   // lanes of a head; heads at a time
@@ -94,27 +117,41 @@ __global__ void __launch_bounds__(32 * kRopeWarps) rope_kernel(RopeArgs a)
     griddep_launch_dependents();
     const int64_t w = (int64_t)blockIdx.x * kRopeWarps + (threadIdx.x >> 5);
     const int lane = threadIdx.x & 31, sub = lane % kLanes;
-    const int64_t t = w / a.parts;
+    const int64_t t = a.parts == 1 ? w : w / a.parts;
     if (t >= a.n) return;
     const int first = (int)(w - t * a.parts) * a.part_heads;
     const int heads = a.hq + (POOL ? 2 : 1) * a.hkv, stop = min(first + a.part_heads, heads);
 
-    // This lane's chunks and the cosines and sines of its pairs.
+    // This lane's chunks, and the rows' addresses; the first rows are under way while the angles are worked out.
     const int rc = KIND == kNoRotation ? 0 : a.rot_chunks;
     const bool turns = KIND != kNoRotation && sub < rc;
     const int c0 = sub < rc ? sub : rc + sub, c1 = c0 + (sub < rc ? rc : kLanes - rc);
-    float cs[8], sn[8];
-    if (KIND != kNoRotation && turns) {
+    auto source = [&](int h) {
+        return h < a.hq                     ? a.q + t * a.q_stride + (int64_t)h * D
+               : !POOL || h < a.hq + a.hkv ? a.k + t * a.k_stride + (int64_t)(h - a.hq) * D
+                                           : a.v + t * a.v_stride + (int64_t)(h - a.hq - a.hkv) * D;
+    };
+    uint4 x0[kAhead], x1[kAhead];
+    auto load = [&](int h0) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int j = KIND == kHalves ? 8 * sub + i : 4 * (i < 4 ? c0 : c1) + (i & 3);
-            const int axis = a.axes ? min((int)a.axes[j], a.num_axes - 1) : 0;
-            const int64_t pos = a.positions[axis * a.axis_stride + t];
-            const int32_t turn = (int32_t)((uint64_t)pos * a.freqs[j] >> 32);
-            sincospif((float)turn * 0x1p-31f, &sn[i], &cs[i]);
-            sn[i] *= a.scale;
-            cs[i] *= a.scale;
+        for (int i = 0; i < kAhead; ++i) {
+            const int h = h0 + i * kHeads + lane / kLanes;
+            if (h < stop) {
+                const uint16_t* const src = source(h);
+                x0[i] = load_row(src + c0 * 8);
+                x1[i] = load_row(src + c1 * 8);
+            }
         }
+    };
+    load(first);
+    uint4 qw[2] = {}, kw[2] = {};
+    if (NORM && a.q_weight) {
+        qw[0] = reinterpret_cast<const uint4*>(a.q_weight)[c0];
+        qw[1] = reinterpret_cast<const uint4*>(a.q_weight)[c1];
+    }
+    if (NORM && a.k_weight) {
+        kw[0] = reinterpret_cast<const uint4*>(a.k_weight)[c0];
+        kw[1] = reinterpret_cast<const uint4*>(a.k_weight)[c1];
     }
     int64_t slot = 0;
     if (POOL) {
@@ -124,71 +161,75 @@ __global__ void __launch_bounds__(32 * kRopeWarps) rope_kernel(RopeArgs a)
             slot = -1;
         }
     }
-#pragma unroll 2
-    for (int h0 = first; h0 < stop; h0 += kHeads) {
-        const int h = h0 + lane / kLanes;
-        const bool live = h < stop, is_q = h < a.hq, is_v = POOL && h >= a.hq + a.hkv;
-        const int kh = h - a.hq - (is_v ? a.hkv : 0);
-        const uint16_t* src = is_q ? a.q + t * a.q_stride + (int64_t)h * D
-                                   : (is_v ? a.v + t * a.v_stride : a.k + t * a.k_stride) + (int64_t)kh * D;
-        const uint4 zero = make_uint4(0, 0, 0, 0);
-        uint4 x0 = live ? reinterpret_cast<const uint4*>(src)[c0] : zero;
-        uint4 x1 = live ? reinterpret_cast<const uint4*>(src)[c1] : zero;
-        const uint16_t* weight = is_q ? a.q_weight : a.k_weight;
-        const bool normed = !is_v && weight != nullptr;
-        const bool some = __any_sync(0xffffffffu, normed);
-        if (some || KIND != kNoRotation) {
-            float x[8], y[8], p[8], r[8];
-            unpack8<T>(x0, x);
-            unpack8<T>(x1, y);
+    float cs[8], sn[8];
+    if (KIND != kNoRotation && turns) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                p[i] = x[i];
-                r[i] = y[i];
-            }
-            if (some) {
-                norm_row<D>(p, r, a.eps);
-                if (normed) {
-                    float g[8];
-                    unpack8<T>(reinterpret_cast<const uint4*>(weight)[c0], g);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i] = p[i] * g[i];
-                    unpack8<T>(reinterpret_cast<const uint4*>(weight)[c1], g);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) y[i] = r[i] * g[i];
-                }
-            }
-            if (turns && !is_v) {
-                if (KIND == kHalves) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float u = x[i], w2 = y[i];
-                        x[i] = u * cs[i] - w2 * sn[i];
-                        y[i] = w2 * cs[i] + u * sn[i];
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float u = x[2 * i], w2 = x[2 * i + 1], u2 = y[2 * i], w3 = y[2 * i + 1];
-                        x[2 * i] = u * cs[i] - w2 * sn[i];
-                        x[2 * i + 1] = w2 * cs[i] + u * sn[i];
-                        y[2 * i] = u2 * cs[4 + i] - w3 * sn[4 + i];
-                        y[2 * i + 1] = w3 * cs[4 + i] + u2 * sn[4 + i];
-                    }
-                }
-            }
-            if (!is_v && (turns || normed)) {
-                x0 = pack8<T>(x);
-                x1 = pack8<T>(y);
-            }
+        for (int i = 0; i < 8; ++i) {
+            const int j = KIND == kHalves ? 8 * sub + i : 4 * (i < 4 ? c0 : c1) + (i & 3);
+            const int axis = a.axes ? min((int)a.axes[j], a.num_axes - 1) : 0;
+            const int64_t pos = a.positions[axis * a.axis_stride + t];
+            sine_cosine((uint32_t)((uint64_t)pos * a.freqs[j] >> 32), &sn[i], &cs[i]);
+            sn[i] *= a.scale;
+            cs[i] *= a.scale;
         }
-        if (!live || (POOL && !is_q && slot < 0)) continue;
-        uint16_t* dst;
-        if (is_q) dst = a.q_out + t * a.q_out_stride + (int64_t)h * D;
-        else if (POOL) dst = (is_v ? a.v_out : a.k_out) + (((slot / kPageSize) * a.hkv + kh) * kPageSize + slot % kPageSize) * D;
-        else dst = a.k_out + t * a.k_out_stride + (int64_t)kh * D;
-        reinterpret_cast<uint4*>(dst)[c0] = x0;
-        reinterpret_cast<uint4*>(dst)[c1] = x1;
+    }
+    const int64_t slot_row = POOL ? ((slot / kPageSize) * a.hkv * kPageSize + slot % kPageSize) * D : 0;
+#pragma unroll 1
+    for (int h0 = first; h0 < stop; h0 += kAhead * kHeads) {
+        if (h0 != first) load(h0);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int h = h0 + i * kHeads + lane / kLanes;
+            if (h0 + i * kHeads >= stop) break;            // (of the whole warp)
+            const bool is_q = h < a.hq, is_v = POOL && h >= a.hq + a.hkv;
+            const bool normed = NORM && !is_v && (is_q ? a.q_weight : a.k_weight) != nullptr;
+            if (NORM || KIND != kNoRotation) {
+                float x[8], y[8];
+                unpack8<T>(x0[i], x);
+                unpack8<T>(x1[i], y);
+                if (NORM && __any_sync(0xffffffffu, normed)) {
+                    const float z = norm_of<D>(x, y, a.eps), f = normed ? z : 1.f;   // (values are not stored from here)
+                    float g[8];
+                    unpack8<T>(is_q ? qw[0] : kw[0], g);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[k] = x[k] * f * (normed ? g[k] : 1.f);
+                    unpack8<T>(is_q ? qw[1] : kw[1], g);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) y[k] = y[k] * f * (normed ? g[k] : 1.f);
+                }
+                if (turns) {
+                    if (KIND == kHalves) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const float u = x[k], v = y[k];
+                            x[k] = u * cs[k] - v * sn[k];
+                            y[k] = v * cs[k] + u * sn[k];
+                        }
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const float u = x[2 * k], v = x[2 * k + 1], u2 = y[2 * k], v2 = y[2 * k + 1];
+                            x[2 * k] = u * cs[k] - v * sn[k];
+                            x[2 * k + 1] = v * cs[k] + u * sn[k];
+                            y[2 * k] = u2 * cs[4 + k] - v2 * sn[4 + k];
+                            y[2 * k + 1] = v2 * cs[4 + k] + u2 * sn[4 + k];
+                        }
+                    }
+                }
+                if (!is_v && (turns || normed)) {
+                    x0[i] = pack8<T>(x);
+                    x1[i] = pack8<T>(y);
+                }
+            }
+            if (h >= stop || (POOL && !is_q && slot < 0)) continue;
+            const int kh = h - a.hq - (is_v ? a.hkv : 0);
+            uint16_t* dst;
+            if (is_q) dst = a.q_out + t * a.q_out_stride + (int64_t)h * D;
+            else if (POOL) dst = (is_v ? a.v_out : a.k_out) + slot_row + (int64_t)kh * (kPageSize * D);
+            else dst = a.k_out + t * a.k_out_stride + (int64_t)kh * D;
+            reinterpret_cast<uint4*>(dst)[c0] = x0[i];
+            reinterpret_cast<uint4*>(dst)[c1] = x1[i];
+        }
     }
 }
 
@@ -207,9 +248,15 @@ cudaError_t launch_rope(RopeArgs& a, int kind, cudaStream_t st)
     const int64_t warps = (int64_t)a.n * a.parts;
     const dim3 grid((unsigned)((warps + kRopeWarps - 1) / kRopeWarps));
     constexpr int kBlock = 32 * kRopeWarps;
-    if (kind == kHalves) return kv4_launch(rope_kernel<D, T, kHalves, POOL>, grid, kBlock, 0, st, a);
-    if (kind == kNeighbours) return kv4_launch(rope_kernel<D, T, kNeighbours, POOL>, grid, kBlock, 0, st, a);
-    return kv4_launch(rope_kernel<D, T, kNoRotation, POOL>, grid, kBlock, 0, st, a);
+    const bool norm = a.q_weight || a.k_weight;
+    if (kind == kHalves)
+        return norm ? kv4_launch(rope_kernel<D, T, kHalves, true, POOL>, grid, kBlock, 0, st, a)
+                    : kv4_launch(rope_kernel<D, T, kHalves, false, POOL>, grid, kBlock, 0, st, a);
+    if (kind == kNeighbours)
+        return norm ? kv4_launch(rope_kernel<D, T, kNeighbours, true, POOL>, grid, kBlock, 0, st, a)
+                    : kv4_launch(rope_kernel<D, T, kNeighbours, false, POOL>, grid, kBlock, 0, st, a);
+    return norm ? kv4_launch(rope_kernel<D, T, kNoRotation, true, POOL>, grid, kBlock, 0, st, a)
+                : kv4_launch(rope_kernel<D, T, kNoRotation, false, POOL>, grid, kBlock, 0, st, a);
 }
 
 template <bool POOL>

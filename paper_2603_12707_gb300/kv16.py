@@ -16,7 +16,7 @@ import math
 import torch
 
 from . import kvdecode as kd
-from .kv4 import _DTYPES, PAGE_SIZE, Tables, _rows, _vector
+from .kv4 import _DTYPES, PAGE_SIZE, Tables, _vector
 
 KVC_DEVERR_PLAN = 16
 
@@ -114,28 +114,27 @@ def _positions(rope, positions, n):
     shape, stride = positions.shape, positions.stride()
     if len(shape) == 1:                 # one row for all axes
         shape, stride = (rope.num_axes, shape[0]), (0, stride[0])
-    if shape != (rope.num_axes, n) or (stride[1] != 1 and n > 1) or stride[0] < 0:
+    if shape != (rope.num_axes, n) or (stride[1] != 1 and n > 1):
         raise ValueError(f"positions must have shape [{n}] or [{rope.num_axes}][{n}], an axis's {n} in a row")
     return positions.data_ptr(), stride[0]
 
 
-def _heads(x, name, dtype, n, dim):
-    """Address, heads and row stride of rows x [n][heads][dim] (None: no heads)."""
+def _heads(x, name, dtype, n, dim, heads=None):
+    """Address, heads and row stride of rows x [n][heads][dim] whose heads are dense (None: no heads)."""
     if x is None:
+        if heads:
+            raise ValueError(f"{name} must be given")
         return None, 0, 0
-    if x.dim() != 3 or x.shape[0] != n or x.shape[2] != dim:
-        raise ValueError(f"{name} must have shape [{n}][heads][{dim}]")
-    ptr, stride = _rows(x, name, dtype, x.shape)
-    return ptr, x.shape[1], stride
-
-
-def _out(x, name, like, dtype, n, dim):
-    """Address and row stride of the output for rows `like`."""
-    if like is None:
-        return None, 0
-    if x is None or x.shape != like.shape:
-        raise ValueError(f"{name} must have the shape of what it is written for")
-    return _rows(x, name, dtype, x.shape)
+    if x.dtype is not dtype or not x.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor of {dtype}")
+    shape = x.shape
+    if len(shape) != 3 or shape[0] != n or shape[2] != dim or (heads is not None and shape[1] != heads):
+        raise ValueError(f"{name} must have shape [{n}][{'heads' if heads is None else heads}][{dim}], not {tuple(shape)}")
+    row, head, one = x.stride()
+    have = shape[1]
+    if one != 1 or (head != dim and have != 1):
+        raise ValueError(f"the heads of {name} must be dense")
+    return x.data_ptr(), have, row if n > 1 else have * dim
 
 
 # ---------------------------------------------------------------- C names
@@ -151,8 +150,8 @@ def kv_qk_rope(rope, positions, q, k, q_out, k_out, q_weight=None, k_weight=None
     pos, axis = _positions(rope, positions, n)
     qp, hq, qs = _heads(q, "q", dtype, n, dim)
     kp, hkv, ks = _heads(k, "k", dtype, n, dim)
-    qo, qos = _out(q_out, "q_out", q, dtype, n, dim)
-    ko, kos = _out(k_out, "k_out", k, dtype, n, dim)
+    qo, _, qos = _heads(q_out, "q_out", dtype, n, dim, hq) if hq else (None, 0, 0)
+    ko, _, kos = _heads(k_out, "k_out", dtype, n, dim, hkv) if hkv else (None, 0, 0)
     rc = (_fns or _load())["kv_qk_rope"](
         None if rope is None else rope.ref, _DTYPES[dtype], dim, n, pos, axis, hq, qp, qs, qo, qos, hkv, kp, ks, ko, kos,
         _vector(q_weight, "q_weight", dtype, dim), _vector(k_weight, "k_weight", dtype, dim), eps, kd._stream(stream))
@@ -164,12 +163,12 @@ def kv16_write(pool: Pool, slots, k, v, rope=None, positions=None, q=None, q_out
                eps: float = 1e-6, device_error=None, stream=None):
     """Rows k (normed and rotated as in kv_qk_rope) and v into their slots (int64 [n]); rows q, if any, into q_out."""
     n, dim, dtype = slots.numel(), pool.head_dim, pool.dtype
-    shape = (n, pool.num_kv_heads, dim)
+    heads = pool.num_kv_heads
     pos, axis = _positions(rope, positions, n)
-    kp, ks = _rows(k, "k", dtype, shape)
-    vp, vs = _rows(v, "v", dtype, shape)
+    kp, _, ks = _heads(k, "k", dtype, n, dim, heads)
+    vp, _, vs = _heads(v, "v", dtype, n, dim, heads)
     qp, hq, qs = _heads(q, "q", dtype, n, dim)
-    qo, qos = _out(q_out, "q_out", q, dtype, n, dim)
+    qo, _, qos = _heads(q_out, "q_out", dtype, n, dim, hq) if hq else (None, 0, 0)
     rc = (_fns or _load())["kv16_write"](
         pool.ref, None if rope is None else rope.ref, n, _vector(slots, "slots", torch.int64, 0), pos, axis, hq, qp, qs, qo,
         qos, kp, ks, vp, vs, _vector(q_weight, "q_weight", dtype, dim), _vector(k_weight, "k_weight", dtype, dim), eps,
@@ -203,12 +202,9 @@ def kv16_plan(pool: Pool, tables: Tables, num_q_heads: int, batch: int, workspac
 def kv16_attention(pool: Pool, tables: Tables, q, out, workspace, lse=None, softmax_scale: float = 0.0,
                    device_error=None, stream=None):
     """Decode attention of the planned rows q [batch][num_q_heads][head_dim] over their prefixes and their own tokens."""
-    shape = q.shape
-    if len(shape) != 3 or shape[2] != pool.head_dim:
-        raise ValueError(f"q must have shape [batch][num_q_heads][{pool.head_dim}]")
-    batch, heads = shape[0], shape[1]
-    q, q_stride = _rows(q, "q", pool.dtype, shape)
-    out, out_stride = _rows(out, "out", pool.dtype, shape)
+    batch, dim, dtype = len(q), pool.head_dim, pool.dtype
+    q, heads, q_stride = _heads(q, "q", dtype, batch, dim)
+    out, _, out_stride = _heads(out, "out", dtype, batch, dim, heads)
     rc = (_fns or _load())["kv16_attention"](
         pool.ref, tables.ref, batch, heads, q, q_stride, out, out_stride,
         _vector(lse, "lse", torch.float32, batch * heads), softmax_scale,
