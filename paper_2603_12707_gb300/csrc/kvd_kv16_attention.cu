@@ -34,6 +34,7 @@ constexpr uint64_t kLimitNs = 1000000000ull;       // of waits for copies before
 constexpr long long kLimitCycles = 2000000000ll;   // of all others: a second
 constexpr int kSoftmaxWarps = 8;                   // two streams of four
 constexpr int kThreads = 32 * (kSoftmaxWarps + 4);
+static_assert(kThreads == 32 * kAttnWarps);
 constexpr int kLoadWarp = kSoftmaxWarps, kMmaWarp = kSoftmaxWarps + 1;
 
 template <int D>
@@ -575,15 +576,14 @@ struct Windows {
 };
 
 template <int D, class T>
-__device__ __forceinline__ void work_records(const AttnArgs& a, const PlanHeader& h, Control& c, uint8_t* smem, const CUtensorMap* mk,
+__device__ __forceinline__ void work_records(const AttnArgs& a, const WarpStart& start, Control& c, uint8_t* smem, const CUtensorMap* mk,
                                              const CUtensorMap* mv)
 {
     using G = Geo<D>;
     constexpr int KS = D / 16;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, ctas = a.grid - h.prefix_ctas;
-    const int worker = warp * ctas + (int)blockIdx.x - h.prefix_ctas;   // (few workers: spread over the SMs)
-    if (worker >= h.warps) return;
-    const WarpStart start = a.view.warp_starts[worker];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (start.count == 0) return;
+    const int worker = start.worker;
     int left = start.count;
     uint8_t* const ring = smem + warp * G::kWarpRing;
     if (lane < G::kStages) mbar_init(smem_addr(&c.stage[warp][lane]), 1);
@@ -793,8 +793,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kernel(const __grid_con
     griddep_wait();
     griddep_launch_dependents();
     const PlanHeader h = *a.view.header;
+    // (What either kind of CTA starts with comes along with the header; the other's is not looked at.)
+    const WarpStart mine = a.view.warp_starts[blockIdx.x * kAttnWarps + warp];
     CtaStart start;
-    if (warp == kLoadWarp) start = a.view.cta_starts[blockIdx.x];   // (of records' CTAs: not looked at)
+    if (warp == kLoadWarp) start = a.view.cta_starts[blockIdx.x];
     const bool fits = plan_fits(h, a) && (smem_addr(smem) & 1023) == 0, records = (int)blockIdx.x >= h.prefix_ctas;
     if (!fits || records) {
         if (warp == kMmaWarp) tmem_dealloc(c.tmem, 512);
@@ -802,7 +804,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kernel(const __grid_con
             if (tid == 0 && blockIdx.x == 0) kv4_error(a.err, KVC_DEVERR_PLAN);
             return;
         }
-        if (warp < kAttnWarps) work_records<D, T>(a, h, c, smem, &mk, &mv);
+        work_records<D, T>(a, mine, c, smem, &mk, &mv);
         return;
     }
     if (warp < kSoftmaxWarps) {
@@ -841,24 +843,11 @@ __global__ void __launch_bounds__(128) merge_kernel(const __grid_constant__ Attn
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int head = blockIdx.x, row = blockIdx.y;
     const int kv = (int)((uint32_t)head * ((65536u + a.G - 1) / a.G) >> 16), g = head - kv * a.G;   // (head < 8192, G <= 8)
-    const RowSources x = a.view.rows[row];
+    const RowSources x = a.view.rows[(int64_t)row * a.hkv + kv];
     const PlanHeader h = *a.view.header;
     if (!plan_fits(h, a)) return;
-
-    // Workers of the row's own job and of its prefix's, the first and the last of each.
-    const bool run = x.kind == 2;
-    const int64_t own_unit = (int64_t)x.own_unit + (int64_t)kv * x.own_pages;
-    const int64_t pre_unit = run ? x.cost + kv * x.head_cost : (int64_t)x.place + (int64_t)kv * x.pages;
-    const int64_t pre_last = pre_unit + (int64_t)(x.pages - 1) * (run ? x.page_cost : 1);
-    const Shares shares = run ? h.cost : h.units;
-    const int own0 = h.units.worker(own_unit), own = x.own_pages > 0 ? h.units.worker(own_unit + x.own_pages - 1) - own0 + 1 : 0;
-    const int pre0 = shares.worker(pre_unit);
-    const int streams = run && !chunk_wide(x.crows, a.G) ? 2 : 1;      // that share the rows of the prefix's job
-    const int total = own + (x.kind ? (shares.worker(pre_last) - pre0 + 1) * streams : 0);
-    const int64_t own_entry = record_entry(x.own_col, 1, a.hkv, a.G, kv, own0) + g;
-    const int64_t pre_entry = run ? run_entry(x.place, x.rows, a.hkv, a.G, kv, x.row0, pre0) + (row - x.first - x.row0) * a.G + g
-                                  : record_entry(x.col, x.rows, a.hkv, a.G, kv, pre0) + (row - x.first) * a.G + g;
-    const int step = run ? 4 * kTileRows : kRecordCols, stream_step = x.crows * a.G;
+    const int own = x.own_count, total = own + x.prefix_count;
+    const bool run = x.stream_step >= 0;
 
     float m = -INFINITY, l = 0.f, o[N];
 #pragma unroll
@@ -868,8 +857,9 @@ __global__ void __launch_bounds__(128) merge_kernel(const __grid_constant__ Attn
         // This lane's segment: its (m, l) and where its sums lie.
         const int s = s0 + 4 * lane, n = min(32, (total - s0 + 3) / 4), p = s - own;
         const bool in_run = run && p >= 0;
-        const int64_t e = p < 0 ? own_entry + (int64_t)s * kRecordCols
-                                : pre_entry + (int64_t)(streams == 2 ? p >> 1 : p) * step + (streams == 2 && (p & 1) ? stream_step : 0);
+        const int64_t e = g + (p < 0                 ? x.own + (int64_t)s * kRecordCols
+                               : x.stream_step > 0 ? x.prefix + (int64_t)(p >> 1) * x.step + (p & 1 ? x.stream_step : 0)
+                                                   : x.prefix + (int64_t)p * x.step);
         const float2 ml = lane < n ? (in_run ? a.view.run_ml : a.view.rec_ml)[e] : make_float2(-INFINITY, 0.f);
         const uint64_t from = reinterpret_cast<uint64_t>((in_run ? a.view.run_o : a.view.rec_o) + e * D);
         float top = ml.y == 0.f ? -INFINITY : ml.x;   // (a segment without tokens has no part)

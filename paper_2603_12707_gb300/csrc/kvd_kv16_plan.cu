@@ -258,17 +258,31 @@ __global__ void __launch_bounds__(kPlanMaxThreads) plan_kernel(StepPlanArgs a)
     // Where workers start, and what the merge reads of a row, by all CTAs' threads.
     const int all = threads * gridDim.x, at0 = blockIdx.x * threads + tid;
     const Shares units = s_header.units, costs = s_header.cost;
+    // Workers of records lie over the CTAs by turns, so that few of them are on different SMs.
+    const int rec_ctas = a.grid - costs.n;
 #pragma unroll 1
-    for (int w = at0; w < units.n; w += all) {
-        const int32_t u = (int32_t)units.start(w);
-        const int i = last_at(s_unit, 2 * B, u), r = i >> 1;
-        const bool own = i & 1;
-        const int len = own ? s_len[r] : s_plen[r], pages = pages_of(len), off = u - s_unit[i], head = (int)divide(off, pages);
-        a.view.warp_starts[w] = WarpStart{i, head, off - head * pages, (int32_t)units.start(w + 1) - u,
-                                          Record{own ? s_req[r] : s_pre[r], len, pages, r, own ? 1 : s_rows[r], s_unit[i], s_col[i], 0}};
+    for (int i = at0; i < rec_ctas * kAttnWarps; i += all) {
+        const int w = i, warp = w / rec_ctas, cta = costs.n + w - warp * rec_ctas;
+        WarpStart* const to = &a.view.warp_starts[cta * kAttnWarps + warp];
+        if (w >= units.n) {
+            to->count = 0;
+        } else {
+            WarpStart x{};
+            x.worker = w;
+            const int32_t u = (int32_t)units.start(w);
+            const int k = last_at(s_unit, 2 * B, u), r = k >> 1;
+            const bool own = k & 1;
+            const int len = own ? s_len[r] : s_plen[r], pages = pages_of(len), off = u - s_unit[k];
+            x.rec = k;
+            x.head = (int)divide(off, pages);
+            x.page = off - x.head * pages;
+            x.count = (int32_t)units.start(w + 1) - u;
+            x.r = Record{own ? s_req[r] : s_pre[r], len, pages, r, own ? 1 : s_rows[r], s_unit[k], s_col[k], 0};
+            *to = x;
+        }
     }
 #pragma unroll 1
-    for (int c = all - 1 - at0; c < costs.n; c += all) {   // (the last threads: the first have more of the others)
+    for (int c = all - 1 - at0; c < costs.n; c += all) {
         const int64_t at = costs.start(c), end = costs.start(c + 1);
         const int i = last_at(s_cost, B, at), rows = s_rows[i], chunks = chunks_of(rows);
         const Run run{s_pre[i], s_plen[i], s_pages[i], rows, s_cost[i], s_before[i], chunks};
@@ -282,34 +296,40 @@ __global__ void __launch_bounds__(kPlanMaxThreads) plan_kernel(StepPlanArgs a)
         a.view.cta_starts[c] = CtaStart{i, job, end, run, s};
     }
 #pragma unroll 1
-    for (int r = at0; r < B; r += all) {
+    for (int i = at0 < all / 2 ? at0 + all / 2 : at0 - all / 2; i < B * a.hkv; i += all) {   // (other threads first)
+        const int r = i / a.hkv, kv = i - r * a.hkv, first = s_first[r], pages = pages_of(s_len[r]);
         RowSources x{};
-        x.own_unit = s_unit[2 * r + 1];
-        x.own_pages = pages_of(s_len[r]);
-        x.own_col = s_col[2 * r + 1];
-        const int first = s_first[r];
+        auto segments = [](const Shares& s, int64_t u, int64_t last, int* w0) {
+            *w0 = s.worker(u);
+            return s.worker(last) - *w0 + 1;
+        };
+        int w0;
+        if (pages > 0) {
+            const int64_t u = (int64_t)s_unit[2 * r + 1] + (int64_t)kv * pages;
+            x.own_count = segments(units, u, u + pages - 1, &w0);
+            x.own = record_entry(s_col[2 * r + 1], 1, a.hkv, G, kv, w0);
+        }
         if (first >= 0) {
-            const int rows = s_rows[first];
-            x.first = first;
-            x.pages = pages_of(s_plen[r]);
-            x.rows = rows;
+            const int rows = s_rows[first], ppages = pages_of(s_plen[r]);
             if (rows * G <= kRecordCols) {
-                x.kind = 1;
-                x.place = s_unit[2 * first];
-                x.col = s_col[2 * first];
+                const int64_t u = (int64_t)s_unit[2 * first] + (int64_t)kv * ppages;
+                x.prefix_count = segments(units, u, u + ppages - 1, &w0);
+                x.prefix = record_entry(s_col[2 * first], rows, a.hkv, G, kv, w0) + (r - first) * G;
+                x.step = kRecordCols;
+                x.stream_step = -1;
             } else {
-                const int chunks = chunks_of(rows), each = chunk_rows(rows, chunks), chunk = (r - first) / each;
-                const int cost = page_cost(rows, chunks, G), opens = job_start(cost);
-                x.kind = 2;
-                x.place = s_before[first];
-                x.cost = s_cost[first] + ((int64_t)chunk * (x.pages + opens) + opens) * cost;
-                x.head_cost = (int64_t)chunks * (x.pages + opens) * cost;
-                x.row0 = chunk * each;
-                x.crows = min(each, rows - x.row0);
-                x.page_cost = cost;
+                const int chunks = chunks_of(rows), each = chunk_rows(rows, chunks), chunk = (r - first) / each, row0 = chunk * each;
+                const int crows = min(each, rows - row0), cost = page_cost(rows, chunks, G), opens = job_start(cost);
+                const int64_t u = s_cost[first] + ((int64_t)(kv * chunks + chunk) * (ppages + opens) + opens) * cost;
+                const int n = segments(costs, u, u + (int64_t)(ppages - 1) * cost, &w0);
+                const bool wide = chunk_wide(crows, G);
+                x.prefix_count = wide ? n : 2 * n;
+                x.prefix = run_entry(s_before[first], rows, a.hkv, G, kv, row0, w0) + (r - first - row0) * G;
+                x.step = 4 * kTileRows;
+                x.stream_step = wide ? 0 : crows * G;
             }
         }
-        a.view.rows[r] = x;
+        a.view.rows[i] = x;
     }
 }
 

@@ -47,10 +47,13 @@ struct Shares {
         return w;
     }
 };
-__host__ __device__ inline Shares make_shares(int64_t total, int n)   // total < 2^40
+__host__ __device__ inline Shares make_shares(int64_t total, int n)   // total < 2^40, n < 2^12
 {
     if (n == 0 || total == 0) return {0, 0.f, 0};
-    return {((total << 20) + n - 1) / n, (float)n / (float)total, n};
+    // total * 2^20 / n in steps of 32 bits (a division of 64 takes the plan a microsecond)
+    const uint32_t d = (uint32_t)n, high = (uint32_t)(total >> 16), q1 = high / d;
+    const uint32_t low = (high - q1 * d) << 16 | (uint32_t)(total & 0xffff), q2 = low / d, rest = low - q2 * d;
+    return {((((int64_t)q1 << 16) + q2) << 20) + ((rest << 20) + d - 1) / d, (float)n / (float)total, n};
 }
 
 struct PlanHeader {
@@ -94,9 +97,11 @@ struct Segment {
     }
 };
 
-struct WarpStart {              // where a worker of records starts, and what it does
-    int32_t rec, head, page, count;
+struct WarpStart {              // by CTA and warp: what a worker of records does
+    int32_t worker;
+    int32_t rec, head, page, count;   // where it starts; pages (0: it has none)
     Record r;
+    int32_t pad[3];
 };
 
 struct CtaStart {               // where a worker of large runs starts, and the end of its share
@@ -106,24 +111,20 @@ struct CtaStart {               // where a worker of large runs starts, and the 
     Segment s;                  // the first segment
 };
 
-// What the merge has to know of a row: its own tokens' job and its prefix's.
+// What the merge has to know of a row and KV head: the segments of its own tokens' job and of its prefix's, and where the results
+// of their first query head lie.
 struct RowSources {
-    int32_t own_unit, own_pages, own_col;
-    int32_t kind;               // of the prefix: 0 none, 1 a record, 2 a large run
-    int32_t first;              // first row of the run
-    int32_t pages, rows;
-    int32_t place;              // a record's unit, or a run's rows_before
-    int64_t cost;               // of a large run: of its row chunk's first page for KV head 0
-    int64_t head_cost;          // from one KV head to the next
-    int32_t row0, crows, page_cost;   // of the chunk: first row in the run, rows
-    int32_t col;                // of a record
+    int64_t own, prefix;        // first entries
+    int32_t own_count, prefix_count;   // segments; of the prefix, both streams' where they share rows
+    int32_t step;               // entries from one of the prefix's segments to the next
+    int32_t stream_step;        // to the second stream's; 0: there is none.  -1: the prefix is a record
 };
 
 struct PlanView {
     PlanHeader* header;
     Record* recs;               // [2 * batch]: 2 r the small run that starts in row r, 2 r + 1 row r's own tokens
     Run* runs;                  // [batch]
-    RowSources* rows;           // [batch]
+    RowSources* rows;           // [batch][hkv]
     WarpStart* warp_starts;     // [grid * kAttnWarps]
     CtaStart* cta_starts;       // [grid]
     float* rec_o;               // partial results of records: [entries][dim], and (m, l)
@@ -149,7 +150,7 @@ __host__ __device__ inline PlanView plan_view(void* base, int batch, int hq, int
     v.header = reinterpret_cast<PlanHeader*>(take(sizeof(PlanHeader)));
     v.recs = reinterpret_cast<Record*>(take((int64_t)sizeof(Record) * 2 * batch));
     v.runs = reinterpret_cast<Run*>(take((int64_t)sizeof(Run) * batch));
-    v.rows = reinterpret_cast<RowSources*>(take((int64_t)sizeof(RowSources) * batch));
+    v.rows = reinterpret_cast<RowSources*>(take((int64_t)sizeof(RowSources) * batch * hkv));
     v.warp_starts = reinterpret_cast<WarpStart*>(take((int64_t)sizeof(WarpStart) * grid * kAttnWarps));
     v.cta_starts = reinterpret_cast<CtaStart*>(take((int64_t)sizeof(CtaStart) * grid));
     // Entries of a record's segment: its query rows; segments are jobs and cuts between workers.
