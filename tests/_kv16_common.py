@@ -53,8 +53,8 @@ def assert_rows(got, ref, dtype, what=""):
     assert (err <= lim).all(), (what, float((err - lim).max()), torch.nonzero(err > lim)[:4].tolist())
 
 
-def attention(k, v, table, lens, seq_ids, prefix_ids, q, scale, dtype, pages_left_out=()):
-    """64-bit attention of q [B, Hq, d] over pools k, v [pages, Hkv, 16, d] (torch, CPU): (out, lse, bound, lse bound).
+def attention(k, v, table, lens, seq_ids, prefix_ids, q, scale, dtype):
+    """64-bit attention of q [B, Hq, d] over pools k, v [pages, Hkv, 16, d] (torch, one device): (out, lse, bound, lse bound).
 
     Scores: fp32 sums of d products, each step rounded or truncated at 2^-23 of the running sum: eps <= d 2^-22 times the
     largest sum of |q k| scale (the factor 2 covers the few operations after it).  A relative error e^eps - 1 of every
@@ -64,16 +64,17 @@ def attention(k, v, table, lens, seq_ids, prefix_ids, q, scale, dtype, pages_lef
     b, hq, d = q.shape
     hkv = k.shape[1]
     g = hq // hkv
-    out, lse = torch.zeros((b, hq, d), dtype=torch.float64), torch.full((b, hq), -math.inf, dtype=torch.float64)
-    bound, lse_bound = torch.zeros((b, hq, 1), dtype=torch.float64), torch.zeros((b, hq), dtype=torch.float64)
+    f64 = dict(dtype=torch.float64, device=q.device)
+    out, lse = torch.zeros((b, hq, d), **f64), torch.full((b, hq), -math.inf, **f64)
+    bound, lse_bound = torch.zeros((b, hq, 1), **f64), torch.zeros((b, hq), **f64)
     cache = {}
 
     def tokens(req):
         if req not in cache:
             n = int(lens[req])
-            pg = torch.as_tensor(np.asarray(table[req][:pages_of(n)]), dtype=torch.int64)
-            there = torch.tensor([int(p) not in pages_left_out and 0 <= int(p) < k.shape[0] for p in pg]).repeat_interleave(P)[:n]
-            pg = pg.clamp(0, k.shape[0] - 1)
+            ids = [int(p) for p in table[req][:pages_of(n)]]
+            there = torch.tensor([0 <= p < k.shape[0] for p in ids], device=k.device).repeat_interleave(P)[:n]
+            pg = torch.tensor(ids, device=k.device).clamp(0, k.shape[0] - 1)
             cache[req] = [x[pg].double().permute(1, 0, 2, 3).reshape(hkv, -1, d)[:, :n][:, there] for x in (k, v)]
         return cache[req]
 
@@ -111,13 +112,13 @@ def attention(k, v, table, lens, seq_ids, prefix_ids, q, scale, dtype, pages_lef
 
 def assert_attention(out, lse, ref, dtype, what=""):
     r_out, r_lse, bound, lse_bound = ref
-    got = out.double().cpu()
+    got = out.double().to(r_out.device)
     assert torch.isfinite(got).all(), (what, "not finite")
     err = (got - r_out).abs()
     lim = UNIT[dtype] * r_out.abs() + (1 + UNIT[dtype]) * bound + TINY[dtype]
     assert (err <= lim).all(), (what, float((err - lim).max()), torch.nonzero(err > lim)[:4].tolist())
     if lse is not None:
-        got = lse.double().cpu()
+        got = lse.double().to(r_lse.device)
         empty = torch.isinf(r_lse)
         assert (got[empty] == -math.inf).all(), what
         err = (got[~empty] - r_lse[~empty]).abs()

@@ -204,7 +204,7 @@ def run(kv16, kv4, lens, seq_ids, prefix_ids, hq, hkv, d, dtype, seed=0, scale=0
         assert torch.equal(first.view(torch.int16), out.view(torch.int16)), "two calls differ"
         if strided:
             assert (wide_o[:, hq:] == -3.0).all()
-        ref = attention(k, v, table, lens, seq_ids, prefix_ids, q, scale if scale > 0 else d ** -0.5, dtype)
+        ref = attention(pool.k, pool.v, table, lens, seq_ids, prefix_ids, dq, scale if scale > 0 else d ** -0.5, dtype)
         if check:
             assert_attention(out, lse, ref, dtype, (hq, hkv, d, layer))
         results.append((out, lse, ref))
@@ -228,3 +228,326 @@ def test_own_tokens_only(kv16, kv4, hq, hkv, d, dtype):
 def test_one_prefix_for_all(kv16, kv4, hq, hkv, d, dtype, plen):
     own = [0, 1, 17, 64, 5, 0, 300, 33, 16, 2, 90]
     run(kv16, kv4, own + [plen], list(range(11)), [11] * 11, hq, hkv, d, dtype, seed=plen)
+
+
+# Several groups: prefixes of one row, of few rows (records), of many; one that comes again later; an empty one; rows
+# without; own requests that repeat; a prefix that is a row's own request too.
+def mixed(seed, plens=(300, 17, 0, 129, 1000, 64)):
+    rng = np.random.default_rng(seed)
+    rows = [(0, 9), (1, 1), (-1, 3), (2, 4), (3, 2), (0, 5), (4, 30), (5, 3), (-1, 1)]
+    own, pre = [], []
+    for g, n in rows:
+        for _ in range(n):
+            own.append(int(rng.choice([0, 1, 15, 16, 33, 100, 260])))
+            pre.append(g)
+    b = len(own)
+    ids = list(range(b))
+    ids[5] = ids[4]
+    ids[20] = b + 1                                  # its own tokens are a prefix of others
+    return own + list(plens), ids, [g if g < 0 else b + g for g in pre]
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv", [(3, 3), (28, 4), (8, 1), (10, 5), (6, 2)])
+def test_groups_of_every_size(kv16, kv4, hq, hkv, d, dtype):
+    lens, ids, pre = mixed(hq)
+    run(kv16, kv4, lens, ids, pre, hq, hkv, d, dtype, seed=hq + d, strided=True, layers=2, scale=0.07)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq,hkv,batch", [(7, 1, 120), (2, 2, 700), (8, 1, 300), (5, 1, 52), (24, 3, 33), (1, 1, 257), (4, 1, 4096)])
+def test_more_rows_than_a_tile_holds(kv16, kv4, hq, hkv, d, batch):
+    """Chunks of rows, the last of them with fewer; one row more than two tiles hold."""
+    own = [(7 * i) % 40 for i in range(batch)]
+    run(kv16, kv4, own + [333], list(range(batch)), [batch] * batch, hq, hkv, d, BF, seed=batch, with_lse=False)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("hq,hkv,d,plen,batch", [(28, 4, 128, 20011, 40), (14, 2, 64, 30000, 150), (8, 8, 128, 9999, 20), (16, 1, 64, 50001, 11)])
+def test_long_prefixes(kv16, kv4, hq, hkv, d, plen, batch, dtype):
+    own = [(13 * i) % 90 for i in range(batch)]
+    if hq // hkv > 8:
+        hkv = 2
+    (out, lse, ref), = run(kv16, kv4, own + [plen], list(range(batch)), [batch] * batch, hq, hkv, d, dtype, seed=plen, poisoned=False)
+    # The roundings of weights and of the output are spread evenly: together sqrt(2) of the output's own, which is UNIT / sqrt(3) at most.
+    rel = float((out.double() - ref[0]).norm() / ref[0].norm())
+    assert rel <= 1.25 * 2 ** 0.5 * UNIT[dtype] / 3 ** 0.5, rel
+
+
+@pytest.mark.parametrize("d,hkv,batch,plen", [(128, 16, 20, 300), (64, 16, 24, 700), (128, 24, 40, 100), (128, 8, 150, 130), (64, 32, 17, 129)])
+def test_many_jobs_of_few_workers(kv16, kv4, d, hkv, batch, plen):
+    """Long own tokens take most of the GPU: each worker of the prefix goes through many short jobs, with one tile and more."""
+    own = [1500 + 40 * i % 700 for i in range(batch)]
+    run(kv16, kv4, own + [plen], list(range(batch)), [batch] * batch, hkv, hkv, d, BF, seed=plen, poisoned=False)
+
+
+@pytest.mark.parametrize("d,hq,hkv,batch,plen,olen", [(128, 32, 32, 64, 701, 400), (64, 14, 2, 150, 4000, 100), (128, 28, 4, 70, 9000, 30)])
+def test_every_call_gives_the_same(kv16, kv4, d, hq, hkv, batch, plen, olen):
+    """Copies that end in another order, streams that run apart: 400 calls, bit for bit."""
+    lens = [olen + i % 50 for i in range(batch)] + [plen]
+    table, pages = make_tables(lens, 5)
+    tabs = kv4.Tables(torch.from_numpy(table).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    pool = kv16.Pool(*(torch.randn((pages, hkv, P, d), device="cuda", generator=torch.Generator("cuda").manual_seed(s)).to(BF) for s in (1, 2)))
+    q = rows(batch, hq, d, BF, 3).cuda()
+    work, err = kv16.kv16_workspace(pool, hq, batch), err_word()
+    kv16.kv16_plan(pool, tabs, hq, batch, work, prefix_ids=torch.full((batch,), batch, dtype=torch.int32, device="cuda"), device_error=err)
+    first = None
+    for _ in range(400):
+        out = torch.full((batch, hq, d), float("nan"), dtype=BF, device="cuda")
+        kv16.kv16_attention(pool, tabs, q, out, work, device_error=err)
+        first = out if first is None else first
+        assert torch.equal(first.view(torch.int16), out.view(torch.int16))
+    assert int(err) == 0
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("q_scale", [0.0, 6.0, 60.0])
+def test_flat_and_sharp_scores(kv16, kv4, dtype, q_scale):
+    """Weights that are all equal; references that move often; one token that takes all."""
+    run(kv16, kv4, [0, 40, 7] * 10 + [1500], list(range(30)), [30] * 30, 8, 2, 128, dtype, seed=4, q_scale=q_scale, v_mean=1.0)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("d,batch", [(64, 40), (128, 40), (128, 3)])
+def test_scores_that_rise(kv16, kv4, dtype, d, batch):
+    """Keys grow along the prefix, so every tile, and every half of one, moves the reference, by 2 to 40 in log2 units."""
+    plen, hq, hkv = 900, 4, 2
+    lens = [3] * batch + [plen]
+    table, pages = make_tables(lens, 9)
+    k, v = make_pool(pages, hkv, d, dtype, 1, table, lens)
+    t = np.arange(plen)
+    direction = torch.randn(d, generator=torch.Generator().manual_seed(0))
+    at = table[batch][t // P].astype(np.int64)
+    for step in (0.02, 0.3):
+        k[at, :, t % P] = (direction * torch.tensor(t * step, dtype=torch.float32)[:, None])[:, None].to(dtype).expand(-1, hkv, -1)
+        pool = kv16.Pool(k.cuda(), v.cuda())
+        tabs = kv4.Tables(torch.from_numpy(table).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"))
+        q = (direction + 0.1 * torch.randn((batch, hq, d), generator=torch.Generator().manual_seed(1))).to(dtype).cuda()
+        work, err, ids = kv16.kv16_workspace(pool, hq, batch), err_word(), torch.full((batch,), batch, dtype=torch.int32, device="cuda")
+        out, lse = torch.empty_like(q), torch.empty((batch, hq), device="cuda")
+        kv16.kv16_plan(pool, tabs, hq, batch, work, prefix_ids=ids, device_error=err)
+        kv16.kv16_attention(pool, tabs, q, out, work, lse=lse, device_error=err)
+        assert int(err) == 0
+        ref = attention(pool.k, pool.v, table, lens, None, [batch] * batch, q, d ** -0.5, dtype)
+        assert_attention(out, lse, ref, dtype, step)
+
+
+def test_values_that_are_not_finite(kv16, kv4):
+    """A NaN or an infinity in a token's V reaches the rows that attend to it, in its element; a query that is none, its own head."""
+    d, hq, hkv, batch = 64, 4, 2, 20
+    lens = [20] * batch + [200]
+    table, pages = make_tables(lens, 2)
+    k, v = make_pool(pages, hkv, d, BF, 1, table, lens)
+    v[int(table[3][0]), 1, 5, 7] = float("nan")            # row 3's own token, KV head 1, element 7
+    v[int(table[batch][2]), 0, 1, 9] = float("inf")        # the prefix, KV head 0, element 9
+    q = rows(batch, hq, d, BF, 1)
+    q[11, 2, 0] = float("nan")
+    pool = kv16.Pool(k.cuda(), v.cuda())
+    tabs = kv4.Tables(torch.from_numpy(table).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    work = kv16.kv16_workspace(pool, hq, batch)
+    out = torch.empty((batch, hq, d), dtype=BF, device="cuda")
+    kv16.kv16_plan(pool, tabs, hq, batch, work, prefix_ids=torch.full((batch,), batch, dtype=torch.int32, device="cuda"))
+    kv16.kv16_attention(pool, tabs, q.cuda(), out, work)
+    got = out.cpu()
+    want = torch.ones((batch, hq, d), dtype=torch.bool)
+    want[3, 2:, 7] = want[:, :2, 9] = want[11, 2] = False
+    assert torch.equal(torch.isfinite(got), want)
+    assert torch.isinf(got[0, 0, 9]) and torch.isnan(got[3, 2, 7]) and torch.isnan(got[11, 2]).all()
+
+
+def test_page_ids_outside_the_pool_are_left_out(kv16, kv4):
+    d, hq, hkv, batch = 128, 8, 4, 30
+    lens = [50 + i for i in range(batch)] + [700]
+    table, pages = make_tables(lens, 3)
+    table[batch][3], table[batch][20], table[batch][43], table[4][1] = -5, pages, 2 ** 31 - 1, pages + 7
+    k, v = make_pool(pages, hkv, d, BF, 1)
+    pool = kv16.Pool(k.cuda(), v.cuda())
+    tabs = kv4.Tables(torch.from_numpy(table).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    q = rows(batch, hq, d, BF, 1).cuda()
+    work, err = kv16.kv16_workspace(pool, hq, batch), err_word()
+    out, lse = torch.empty_like(q), torch.empty((batch, hq), device="cuda")
+    kv16.kv16_plan(pool, tabs, hq, batch, work, prefix_ids=torch.full((batch,), batch, dtype=torch.int32, device="cuda"), device_error=err)
+    assert int(err) == 0
+    kv16.kv16_attention(pool, tabs, q, out, work, lse=lse, device_error=err)
+    assert int(err) == 1
+    assert_attention(out, lse, attention(pool.k, pool.v, table, lens, None, [batch] * batch, q, d ** -0.5, BF), BF)
+
+
+def test_rows_that_are_refused(kv16, kv4):
+    """An unknown request, a length past the table: zeros, the bit, and all other rows as ever."""
+    d, hq, hkv, batch = 64, 6, 3, 26
+    lens = [30 + i for i in range(batch)] + [260, 999999, -4]
+    good = [n if 0 <= n <= 400 else 0 for n in lens]
+    table, pages = make_tables(good, 3)
+    k, v = make_pool(pages, hkv, d, FP, 1, table, good)
+    pool = kv16.Pool(k.cuda(), v.cuda())
+    tabs = kv4.Tables(torch.from_numpy(table).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    ids, pre = list(range(batch)), [batch] * batch
+    ids[2], ids[9], pre[12], pre[13], pre[17], ids[20] = -1, len(lens), len(lens) + 5, batch + 1, -2, batch + 2
+    bad = [2, 9, 12, 13, 17, 20]
+    q = rows(batch, hq, d, FP, 1).cuda()
+    work, err = kv16.kv16_workspace(pool, hq, batch), err_word()
+    out, lse = torch.full_like(q, 5.0), torch.full((batch, hq), 5.0, device="cuda")
+    dev = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    kv16.kv16_plan(pool, tabs, hq, batch, work, seq_ids=dev(ids), prefix_ids=dev(pre), device_error=err)
+    assert int(err) == 4
+    kv16.kv16_attention(pool, tabs, q, out, work, lse=lse)
+    assert (out[bad] == 0).all() and (lse[bad] == -math.inf).all()
+    fine = [i for i in range(batch) if i not in bad]
+    ref = attention(pool.k, pool.v, table, good, [ids[i] for i in fine], [pre[i] for i in fine], q[fine], d ** -0.5, FP)
+    assert_attention(out[fine], lse[fine], ref, FP)
+
+
+def test_a_workspace_without_this_plan(kv16, kv4):
+    d, hq, hkv, batch = 64, 4, 2, 5
+    lens = [20] * batch + [100]
+    table, pages = make_tables(lens, 3)
+    pool = kv16.Pool.empty(pages, hkv, d)
+    tabs = kv4.Tables(torch.from_numpy(table).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    work = kv16.kv16_workspace(pool, 8, batch)
+    work.zero_()
+    q = rows(batch, hq, d, BF, 1).cuda()
+
+    def attend(q, tabs=tabs, pool=pool):
+        out, err = torch.full_like(q, 5.0), err_word()
+        kv16.kv16_attention(pool, tabs, q, out, work, device_error=err)
+        return int(err), bool((out == 5.0).all())
+
+    assert attend(q) == (16, True)                                   # no plan at all
+    kv16.kv16_plan(pool, tabs, hq, batch, work)
+    assert attend(q)[0] == 0
+    assert attend(q[:4]) == (16, True)                               # of another batch
+    assert attend(rows(batch, 2, d, BF, 1).cuda()) == (16, True)     # other heads
+    wide = torch.cat([torch.from_numpy(table).cuda()] * 2, 1).contiguous()
+    assert attend(q, kv4.Tables(wide, tabs.lens)) == (16, True)      # other tables
+    kv16.kv16_plan(pool, tabs, 8, batch, work)
+    assert attend(q) == (16, True)
+
+
+def test_calls_that_the_binding_refuses(kv16, kv4):
+    d, hkv = 64, 2
+    pool = kv16.Pool.empty(4, hkv, d)
+    tabs = kv4.Tables.empty(4, 2, 2)
+    x = torch.zeros((3, 4, d), dtype=BF, device="cuda")
+    k = torch.zeros((3, hkv, d), dtype=BF, device="cuda")
+    slots = torch.zeros(3, dtype=torch.int64, device="cuda")
+    rope = kv16.Rope([1.0] * 32, num_axes=3)
+    pos = torch.zeros((3, 3), dtype=torch.int32, device="cuda")
+    bad = [lambda: kv16.kv_qk_rope(rope, pos.long(), x, k, x, k), lambda: kv16.kv_qk_rope(rope, pos[:2], x, k, x, k),
+           lambda: kv16.kv_qk_rope(rope, None, x, k, x, k), lambda: kv16.kv_qk_rope(rope, pos.t()[:, :2], x, k, x, k),
+           lambda: kv16.kv_qk_rope(rope, pos, x, k[:2], x, k), lambda: kv16.kv_qk_rope(rope, pos, x, k.half(), x, k),
+           lambda: kv16.kv_qk_rope(rope, pos, x, k, x, None), lambda: kv16.kv_qk_rope(rope, pos, x, k, x[:, :3], k),
+           lambda: kv16.kv_qk_rope(rope, pos, x, k, x, k, q_weight=torch.zeros(d, device="cuda")),
+           lambda: kv16.kv_qk_rope(rope, pos, x, k, x, k, q_weight=torch.zeros(d - 1, dtype=BF, device="cuda")),
+           lambda: kv16.kv_qk_rope(rope, pos, x.transpose(1, 2), k, x, k), lambda: kv16.kv_qk_rope(rope, pos, x.cpu(), k, x, k),
+           lambda: kv16.kv16_write(pool, slots.int(), k, k), lambda: kv16.kv16_write(pool, slots, x, k),
+           lambda: kv16.kv16_write(pool, slots[:2], k, k), lambda: kv16.kv16_write(pool, slots, k, k, q=x),
+           lambda: kv16.kv16_plan(pool, tabs, 4, 2, torch.zeros(16, device="cuda")),
+           lambda: kv16.kv16_plan(pool, tabs, 4, 2, kv16.kv16_workspace(pool, 4, 2), seq_ids=slots[:2].int()[:1]),
+           lambda: kv16.kv16_attention(pool, tabs, x[:2], x[:1], kv16.kv16_workspace(pool, 4, 2)),
+           lambda: kv16.Pool(pool.k, pool.v[:2]), lambda: kv16.Pool(pool.k, pool.v.half()), lambda: kv16.Pool(pool.k[:, :, :8], pool.v[:, :, :8])]
+    for call in bad:
+        with pytest.raises(ValueError):
+            call()
+    small = kv16.kv16_workspace(pool, 4, 1)[:-256]
+    with pytest.raises(kv16.kd.KVDecodeError, match="workspace"):
+        kv16.kv16_plan(pool, tabs, 4, 1, small)
+    kv16.kv_qk_rope(rope, torch.zeros(3, dtype=torch.int32, device="cuda"), x, k, x, k)    # one row of positions for all axes
+
+
+# ------------------------------------------------------ graphs, streams, devices
+def test_a_captured_step_follows_the_lengths(kv16, kv4):
+    """Tables, rotation and write, plan and two layers of attention captured once and replayed while the requests grow."""
+    d, hq, hkv, batch, plen = 128, 8, 2, 12, 333
+    lens = [17 * i % 60 for i in range(batch)] + [plen]
+    pages = sum(pages_of(n + 40) for n in lens)
+    tabs = kv4.Tables.empty(pages, batch + 1, max(pages_of(n + 40) for n in lens))
+    slots = torch.empty(sum(lens), dtype=torch.int64, device="cuda")
+    kv4.kv_tables_step(tabs, None, torch.tensor(lens, dtype=torch.int32, device="cuda"), slots)
+    pools = [kv16.Pool(*(torch.randn((pages, hkv, P, d), device="cuda").to(BF) for _ in range(2))) for _ in range(2)]
+    rope = kv16.Rope(inv_freq(d // 2))
+    side = torch.cuda.Stream()
+    ids = torch.arange(batch, dtype=torch.int32, device="cuda")
+    pre = torch.full((batch,), batch, dtype=torch.int32, device="cuda")
+    ones = torch.ones(batch, dtype=torch.int32, device="cuda")
+    new, pos = torch.empty(batch, dtype=torch.int64, device="cuda"), torch.empty(batch, dtype=torch.int32, device="cuda")
+    x = [torch.empty((batch, hq + 2 * hkv, d), dtype=BF, device="cuda") for _ in pools]
+    qr, out = ([torch.empty((batch, hq, d), dtype=BF, device="cuda") for _ in pools] for _ in range(2))
+    lse = [torch.empty((batch, hq), device="cuda") for _ in pools]
+    work, err = kv16.kv16_workspace(pools[0], hq, batch), err_word()
+
+    def step(s):
+        kv4.kv_tables_step(tabs, ids, ones, new, pos, device_error=err, stream=s)
+        kv16.kv16_plan(pools[0], tabs, hq, batch, work, seq_ids=ids, prefix_ids=pre, device_error=err, stream=s)
+        for i, pool in enumerate(pools):
+            q, k, v = x[i][:, :hq], x[i][:, hq:hq + hkv], x[i][:, hq + hkv:]
+            kv16.kv16_write(pool, new, k, v, rope=rope, positions=pos, q=q, q_out=qr[i], device_error=err, stream=s)
+            kv16.kv16_attention(pool, tabs, qr[i], out[i], work, lse=lse[i], device_error=err, stream=s)
+
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side), torch.cuda.graph(g, stream=side):
+        step(side)
+    for it in range(6):
+        with torch.cuda.stream(side):
+            for i in range(2):
+                x[i].copy_(rows(batch, hq + 2 * hkv, d, BF, 100 * it + i))
+            g.replay()
+        side.synchronize()
+        lens = [n + 1 for n in lens[:-1]] + [plen]
+        assert int(err) == 0 and tabs.lens.tolist() == lens
+        table = tabs.block_table.cpu().numpy()
+        for i, pool in enumerate(pools):
+            assert_rows(qr[i], turned(x[i][:, :hq].cpu(), [[n - 1 for n in lens[:-1]]], inv_freq(d // 2), None), BF)
+            ref = attention(pool.k, pool.v, table, lens, None, [batch] * batch, qr[i], d ** -0.5, BF)
+            assert_attention(out[i], lse[i], ref, BF, (it, i))
+
+
+def test_a_step_on_a_stream_of_its_own(kv16, kv4):
+    """Beside slow work on the default stream, with a raw handle for the stream."""
+    lens, ids, pre = mixed(1)
+    b = len(ids)
+    table, pages = make_tables(lens, 1)
+    k, v = make_pool(pages, 4, 128, BF, 2, table, lens)
+    q = rows(b, 8, 128, BF, 1)
+    side = torch.cuda.Stream()
+    dev = lambda t: torch.tensor(t, dtype=torch.int32, device="cuda")  # noqa: E731
+    with torch.cuda.stream(side):
+        pool, dq = kv16.Pool(k.cuda(), v.cuda()), q.cuda()
+        tabs, work = kv4.Tables(torch.from_numpy(table).cuda(), dev(lens)), kv16.kv16_workspace(pool, 8, b)
+        dids, dpre, out = dev(ids), dev(pre), torch.empty_like(dq)
+    side.synchronize()
+    torch.cuda._sleep(40_000_000)
+    kv16.kv16_plan(pool, tabs, 8, b, work, seq_ids=dids, prefix_ids=dpre, stream=side.cuda_stream)
+    kv16.kv16_attention(pool, tabs, dq, out, work, stream=side.cuda_stream)
+    side.synchronize()
+    assert_attention(out, None, attention(pool.k, pool.v, table, lens, ids, pre, dq, 128 ** -0.5, BF), BF)
+
+
+def test_two_graphs_share_a_workspace(kv16, kv4):
+    """Each holds its own plan call: replayed by turns they give what they gave alone."""
+    graphs = []
+    work = torch.zeros(64 << 20, dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    for hq, hkv, d, batch, plen in ((8, 2, 128, 30, 700), (6, 6, 64, 9, 2000)):
+        lens = [5 * i % 70 for i in range(batch)] + [plen]
+        table, pages = make_tables(lens, batch)
+        pool = kv16.Pool(*(x.cuda() for x in make_pool(pages, hkv, d, BF, 1, table, lens)))
+        tabs = kv4.Tables(torch.from_numpy(table).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"))
+        q, pre = rows(batch, hq, d, BF, 1).cuda(), torch.full((batch,), batch, dtype=torch.int32, device="cuda")
+        out = torch.empty_like(q)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(side), torch.cuda.graph(g, stream=side):
+            kv16.kv16_plan(pool, tabs, hq, batch, work, prefix_ids=pre, stream=side)
+            kv16.kv16_attention(pool, tabs, q, out, work, stream=side)
+        ref = attention(pool.k, pool.v, table, lens, None, [batch] * batch, q, d ** -0.5, BF)
+        graphs.append((g, out, ref, (pool, tabs, q, pre)))
+    for i in (0, 1, 1, 0, 0, 1):
+        g, out, ref, _ = graphs[i]
+        with torch.cuda.stream(side):
+            out.fill_(float("nan"))
+            g.replay()
+        side.synchronize()
+        assert_attention(out, None, ref, BF, i)
