@@ -1,5 +1,6 @@
 """Drive a decode session of a workload through the C ABI: over the bf16 cache
-(``DecodeSession``) or over the 4-bit one (``Kv4Session``).
+(``DecodeSession``), over the 4-bit one (``Kv4Session``) or over 16-bit pools in
+which requests share prefixes (``SharedPrefixSession``).
 
 Sets up a cache for a ``WorkloadConfig`` (pool sized for the prefix plus
 ``extra_tokens`` decode steps, page order and reservation order from the
@@ -12,7 +13,7 @@ from __future__ import annotations
 
 import numpy as np
 
-from . import kv4
+from . import kv4, kv16
 from . import kvdecode as kd
 from . import workloads as wl
 
@@ -90,6 +91,14 @@ class DecodeSession:
         self.close()
 
 
+def _on_stream(s):
+    """torch's work and memory on stream s: a block that is freed is handed out again behind what reads it."""
+    from torch import cuda
+    if not isinstance(s, cuda.Stream):
+        s = cuda.ExternalStream(int(s)) if s else cuda.default_stream()
+    return cuda.stream(s)
+
+
 class Kv4Session:
     """The same session over a 4-bit cache: every step's block tables and slot
     map are built on the device from the requests' lengths, new K and V are
@@ -125,11 +134,7 @@ class Kv4Session:
             self.workspace = kv4.kv4_workspace(self.pools[0], cfg.num_q_heads)
 
     def _on_stream(self):
-        """torch's work and memory on the session's stream: a block that is freed is handed out again behind what reads it."""
-        cuda, s = self._torch.cuda, self.stream
-        if not isinstance(s, cuda.Stream):
-            s = cuda.ExternalStream(int(s)) if s else cuda.default_stream()
-        return cuda.stream(s)
+        return _on_stream(self.stream)
 
     def grow(self, new_lens):
         """Requests grow by new_lens tokens (host sequence), or give -n back; returns the new tokens' slots."""
@@ -164,6 +169,125 @@ class Kv4Session:
     def attend(self, layer: int, q, out, scale: float = 0.0, lse=None):
         kv4.kv4_decode_attention(self.pools[self.phys(layer)], self.tables, q, out, self.workspace, lse=lse,
                                  softmax_scale=scale, device_error=self.error, stream=self.stream)
+
+    def check(self):
+        """Wait for the session's stream and raise if a call has found something wrong."""
+        with self._on_stream():
+            bits = int(self.error.item())
+        if bits:
+            raise RuntimeError(f"device error bits {bits:#x}")
+
+
+class SharedPrefixSession:
+    """A decode session in which requests continue shared prefixes (an image and its prompt, a system prompt), each held
+    once: request i of the workload holds its own tokens only and continues prefix ``prefix_of[i]`` (-1: none), whose
+    ``prefix_lens`` tokens are a request of their own, row ``cfg.batch + prefix_of[i]`` of the block tables.
+
+    A step: ``begin_step`` (slots, positions and the attention plan, on the device), then per layer ``append`` (queries
+    and keys normed and rotated, K and V written into their slots) and ``attend``.  ``rope`` None: no rotation.  A token's position
+    is its index behind the prefix; ``first_positions`` (a sequence) gives a request's first own token another than the
+    length of its prefix, as where an image takes fewer positions than tokens.
+
+    Ordered on its stream as ``Kv4Session`` is: ``begin_step``, ``append`` and ``attend`` only enqueue."""
+
+    def __init__(self, cfg: wl.WorkloadConfig, prefix_lens, prefix_of, rope=None, q_weight=None, k_weight=None, eps: float = 1e-6,
+                 first_positions=None, extra_tokens: int = 8, dtype=None, device="cuda", stream=None, lens=None, slack_pages: int = 8):
+        import torch
+        self.cfg, self.rope, self.stream, self._torch = cfg, rope, stream, torch
+        self.q_weight, self.k_weight, self.eps = q_weight, k_weight, eps
+        self._i32 = dict(dtype=torch.int32, device=device)
+        own = np.array(wl.context_lengths(cfg) if lens is None else lens, dtype=np.int64)
+        self.lens0 = np.concatenate([own, np.array(prefix_lens, dtype=np.int64)])
+        self.lens = np.zeros_like(self.lens0)      # held so far: fill_prefix admits requests and prefixes
+        self.prefix_of = [int(g) for g in prefix_of]
+        if len(self.prefix_of) != cfg.batch or len(own) != cfg.batch:
+            raise ValueError("prefix_of and lens must have an entry for each request")
+        if not all(-1 <= g < len(prefix_lens) for g in self.prefix_of):
+            raise ValueError("prefix_of must name one of prefix_lens, or -1")
+        if first_positions is None:
+            first_positions = [int(prefix_lens[g]) if g >= 0 else 0 for g in self.prefix_of]
+        if len(first_positions) != cfg.batch:
+            raise ValueError("first_positions must have an entry for each request")
+        self.first_positions = [int(p) for p in first_positions]
+        dtype = torch.bfloat16 if dtype is None else dtype
+        P = kv4.PAGE_SIZE
+        room = self.lens0 + np.array([extra_tokens] * cfg.batch + [0] * len(prefix_lens), dtype=np.int64)
+        num_pages = int(((room + P - 1) // P).sum()) + slack_pages
+        with self._on_stream():
+            self.pools = [kv16.Pool.empty(num_pages, cfg.num_kv_heads, cfg.head_dim, dtype, device=device)
+                          for _ in range(cfg.phys_layers)]
+            self.tables = kv4.Tables.empty(num_pages, len(room), max(1, int((room.max() + P - 1) // P)), device=device)
+            order = wl.page_order(cfg, num_pages)
+            if order is not None:
+                self.tables.free_ring.copy_(torch.from_numpy(order))
+            self.error = torch.zeros(1, **self._i32)
+            self.ones = torch.ones(cfg.batch, **self._i32)
+            self.ids = torch.arange(cfg.batch, **self._i32)
+            self.prefix_ids = torch.tensor([cfg.batch + g if g >= 0 else -1 for g in self.prefix_of], **self._i32)
+            self.first = torch.tensor(self.first_positions, **self._i32)
+            self.index, self.positions = torch.empty(cfg.batch, **self._i32), torch.empty(cfg.batch, **self._i32)
+            self.step_slots = torch.empty(cfg.batch, dtype=torch.int64, device=device)
+            self.workspace = kv16.kv16_workspace(self.pools[0], cfg.num_q_heads, cfg.batch)
+
+    def _on_stream(self):
+        return _on_stream(self.stream)
+
+    def grow(self, new_lens):
+        """Requests, then prefixes, grow by new_lens tokens (host sequence), or give -n back; returns the new tokens' slots
+        and positions.  A prefix may grow or be dropped only while no request that continues it takes a step."""
+        new = np.array([int(n) for n in new_lens], dtype=np.int64)
+        added = int(np.maximum(new, 0).sum())
+        with self._on_stream():
+            dev = self._torch.tensor(new, **self._i32)
+            slots = self._torch.empty(added, dtype=self._torch.int64, device=dev.device)
+            index = self._torch.empty(added, **self._i32)
+            kv4.kv_tables_step(self.tables, None, dev, slots, index, device_error=self.error, stream=self.stream)
+            first = np.repeat(np.array(self.first_positions + [0] * (len(new) - self.cfg.batch)), np.maximum(new, 0))
+            index += self._torch.from_numpy(first.astype(np.int32)).to(dev.device)
+        self.lens += new
+        return slots, index
+
+    def write(self, layer: int, slots, positions, k, v):
+        """Prompt tokens' K, normed and rotated, and V into their slots."""
+        kv16.kv16_write(self.pools[self.phys(layer)], slots, k, v, rope=self.rope, positions=positions if self.rope else None,
+                        k_weight=self.k_weight, eps=self.eps, device_error=self.error, stream=self.stream)
+
+    def fill_prefix(self, layers=None):
+        """Admit every request and prefix and write their cached tokens into the given layer pools."""
+        cfg = self.cfg
+        slots, positions = self.grow(self.lens0)
+        with self._on_stream():
+            for l in range(cfg.phys_layers) if layers is None else layers:
+                k, v, _ = wl.packed_prefix(cfg, [l], self.lens0, slots.device)
+                self.write(l, slots, positions, *(x[0].to(self.pools[l].dtype) for x in (k, v)))
+                del k, v
+
+    def begin_step(self):
+        kv4.kv_tables_step(self.tables, self.ids, self.ones, self.step_slots, self.index, device_error=self.error,
+                           stream=self.stream)
+        with self._on_stream():
+            self._torch.add(self.index, self.first, out=self.positions)
+        kv16.kv16_plan(self.pools[0], self.tables, self.cfg.num_q_heads, self.cfg.batch, self.workspace, seq_ids=self.ids,
+                       prefix_ids=self.prefix_ids, device_error=self.error, stream=self.stream)
+        self.lens[:self.cfg.batch] += 1
+
+    def phys(self, layer: int) -> int:
+        return layer % self.cfg.phys_layers
+
+    def append(self, layer: int, q, k_new, v_new, q_out, positions=None):
+        """The new tokens' K and V into their slots; queries for ``attend`` into q_out (which may be q).  positions: others than
+        the step's, for instance one row for each axis."""
+        if self.rope is None:
+            positions = None
+        elif positions is None:
+            positions = self.positions
+        kv16.kv16_write(self.pools[self.phys(layer)], self.step_slots, k_new, v_new, rope=self.rope, positions=positions, q=q,
+                        q_out=q_out, q_weight=self.q_weight, k_weight=self.k_weight, eps=self.eps, device_error=self.error,
+                        stream=self.stream)
+
+    def attend(self, layer: int, q, out, scale: float = 0.0, lse=None):
+        kv16.kv16_attention(self.pools[self.phys(layer)], self.tables, q, out, self.workspace, lse=lse, softmax_scale=scale,
+                            device_error=self.error, stream=self.stream)
 
     def check(self):
         """Wait for the session's stream and raise if a call has found something wrong."""

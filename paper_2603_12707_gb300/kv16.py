@@ -10,7 +10,6 @@ are on the device that is current.
 from __future__ import annotations
 
 import ctypes
-import fractions
 import math
 
 import torch
@@ -94,8 +93,9 @@ class Rope:
         if axes is not None and (len(axes) != len(inv_freq) or not all(0 <= int(a) < num_axes for a in axes)):
             raise ValueError("axes must name an axis below num_axes for each of inv_freq")
         # turns per position, modulo 1, in units of 2^-64
-        turn = fractions.Fraction(314159265358979323846264338327950288419716939937510, 10 ** 50) * 2
-        words = [round(fractions.Fraction(f) / turn * 2 ** 64) % 2 ** 64 for f in inv_freq]
+        turn, words = 2 * 314159265358979323846264338327950288419716939937510, []    # (2 pi in units of 10^-50)
+        for num, den in map(float.as_integer_ratio, inv_freq):
+            words.append((num * 10 ** 50 * 2 ** 65 + den * turn) // (2 * den * turn) % 2 ** 64)
         self.frequencies = torch.tensor([w - 2 ** 64 if w >= 2 ** 63 else w for w in words], dtype=torch.int64, device=device)
         self.axes = None if axes is None else torch.tensor([int(a) for a in axes], dtype=torch.uint8, device=device)
         self.num_axes, self.rotary_dim = num_axes, 2 * len(inv_freq)
