@@ -456,10 +456,13 @@ __device__ __forceinline__ void softmax_stream(const AttnArgs& a, Control& c, ui
                     const uint32_t n = n0 + order.v(t), vslot = n % G::kSlots;
                     if (!warp_wait(&c.full[n % (2 * G::kSlots)], n / (2 * G::kSlots) & 1, c, a.err)) return;
 #pragma unroll 1
-                    for (int r = h * (kTilePages / 2) * kPageSize + wq; r < min(pages, (h + 1) * (kTilePages / 2)) * kPageSize; r += 4)
-                        if (r >= valid || !(known >> (r / kPageSize) & 1u))
+                    for (int page = h * (kTilePages / 2); page < min(pages, (h + 1) * (kTilePages / 2)); ++page) {
+                        const int from = known >> page & 1u ? valid - page * kPageSize : 0;   // (a thread has 16 bytes of each block)
+                        if (my >> 3 >= from)
                             for (int b = 0; b < G::kBlocks; ++b)
-                                *reinterpret_cast<uint32_t*>(smem + G::kRing + vslot * G::kTileBytes + b * G::kBlockBytes + r * 128 + lane * 4) = 0u;
+                                *reinterpret_cast<uint4*>(smem + G::kRing + vslot * G::kTileBytes + b * G::kBlockBytes + page * 2048 + my * 16) =
+                                    make_uint4(0u, 0u, 0u, 0u);
+                    }
                     fence_proxy_async_smem();
                 }
                 tmem_fence_before();

@@ -25,8 +25,8 @@ constexpr uint32_t kPlanMagic = 0x16a77e41u;
 
 // Cost of a page of a large run's job, with both streams on rows of their own or taking turns, and what opening and
 // closing a job costs beside, in such pages; a record's page, which costs what its bytes take.
-__host__ __device__ inline int record_cost(int dim) { return dim / 8; }
-constexpr int kWideCost = 24, kNarrowCost = 12, kWideStart = 20, kNarrowStart = 60;
+__host__ __device__ inline int record_cost(int dim) { return dim / 16; }
+constexpr int kWideCost = 24, kNarrowCost = 12, kWideStart = 20, kNarrowStart = 30;
 // Shares are not made smaller than this (pages): every segment is one more result to merge.
 constexpr int kLeastRunPages = 8, kLeastRecordPages = 4;
 
