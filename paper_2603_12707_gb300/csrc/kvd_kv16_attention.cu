@@ -35,7 +35,10 @@ constexpr long long kLimitCycles = 2000000000ll;   // of all others: a second
 constexpr int kSoftmaxWarps = 8;                   // two streams of four
 constexpr int kThreads = 32 * (kSoftmaxWarps + 4);
 static_assert(kThreads == 32 * kAttnWarps);
+constexpr int kRegisters = 168, kSoftmaxRegisters = 208, kOtherRegisters = 88;   // of a thread: at launch, then by what a warp does
+static_assert(kSoftmaxWarps * kSoftmaxRegisters + 4 * kOtherRegisters <= (kSoftmaxWarps + 4) * kRegisters);
 constexpr int kLoadWarp = kSoftmaxWarps, kMmaWarp = kSoftmaxWarps + 1;
+constexpr int kOut = 256;                          // first column of the sums in tensor memory
 
 template <int D>
 struct Geo {
@@ -84,7 +87,7 @@ struct Control {                     // in shared memory
     // other tile; the tile two before has been used (the loading warp found it so before it loaded what the stream saw last).
     uint64_t full[18], empty[9];
     uint64_t told[kSegments];
-    uint64_t scores[2], weights[2][2], half[2], queries, drained;   // by stream; weights by half of a tile
+    uint64_t scores[2], taken[2], weights[2][2], half[2], done[2], queries, drained;   // by stream; weights by half of a tile
     int32_t pages_known[8];          // by tile: bits of its pages that are there (read before the eighth after it is loaded)
     uint32_t tmem;
     int32_t gave_up;                 // a wait ran out: everybody leaves
@@ -134,17 +137,22 @@ __device__ __forceinline__ void arrive(uint64_t* bar)
 }
 
 // ------------------------------------------------------------ large runs, tcgen05
-// Both streams work on every tile (wide), or they take turns.  Tiles of K run ahead of those of V by one for each tile that is
-// in work, so the ring's order within a segment is K 0 .. A - 1, then V n, K n + A, as far as there are any: where a tile lies in it.
+// Both streams work on every tile (wide), or they take turns.  Tiles of K run ahead of those of V by two, so the ring's order within a segment is
+// K 0 .. A - 1, then V n, K n + A, as far as there are any: where a tile lies in it.
 struct Order {
     int ahead, tiles;
-    __device__ __forceinline__ Order(int n, bool wide) : ahead(min(wide ? 1 : 2, n)), tiles(n) {}
+    __device__ __forceinline__ explicit Order(int n) : ahead(min(2, n)), tiles(n) {}
     __device__ __forceinline__ int k(int j) const { return j < ahead ? j : 2 * j - ahead + 1; }
     __device__ __forceinline__ int v(int n) const { return min(ahead + 2 * n, tiles + n); }
 };
 // A stream's tiles: how many, and its j-th.
 __device__ __forceinline__ int stream_tiles(int tiles, bool wide, int stream) { return wide ? tiles : (tiles + 1 - stream) >> 1; }
 __device__ __forceinline__ int stream_tile(bool wide, int stream, int j) { return wide ? j : 2 * j + stream; }
+
+// Where a stream's scores lie in tensor memory, and its weights.  Wide: both streams' scores in the same 128 columns, so that those of the next
+// tile can be made while this one's are worked (a softmax warp holds them in registers).  Else each has 128, and weights lie over scores.
+__device__ __forceinline__ uint32_t scores_at(const Control& c, bool wide, int stream) { return c.tmem + (wide ? 0 : stream * 128); }
+__device__ __forceinline__ uint32_t weights_at(const Control& c, bool wide, int stream) { return c.tmem + stream * (wide ? 64 : 128) + (wide ? 128 : 0); }
 
 // The loading warp: goes through the worker's share segment by segment, tells the others of each and loads its tiles.
 template <int D>
@@ -185,7 +193,7 @@ __device__ __forceinline__ void load_tiles(const AttnArgs& a, const CtaStart& st
 
         const int32_t* row = a.table + (int64_t)r.req * a.max_pages + s.first;
         const int tiles = s.tiles();
-        const Order order(tiles, s.wide);
+        const Order order(tiles);
         // Page ids: a lane has a page of a window of four tiles, and of the one before it (V comes up to two later).
         auto ids_of = [&](int window) {
             const int page = window * 32 + lane;
@@ -238,74 +246,80 @@ __device__ __forceinline__ void load_tiles(const AttnArgs& a, const CtaStart& st
             mbar_wait_bounded(smem_addr(&c.full[i % (2 * G::kSlots)]), i / (2 * G::kSlots) & 1, kLimitNs);
 }
 
-// A stream's issuing warp: a tile's weights against V, in halves as they come, then the stream's next tile of K against its
-// queries.  (All of the warp goes along, so that addresses and descriptors stay in uniform registers; one lane issues.  Two warps, since what one does
-// between its products takes as long as those.)
-template <int D, class T>
+// A stream's issuing warp: the scores of its next tile, as soon as the other stream has taken its own from the columns that they share, then the
+// weights of the tile before against V, in halves as they come.  (All of the warp goes along, so that addresses and descriptors stay in uniform
+// registers; one lane issues.  Two warps, since what one does between its products takes as long as those.)
+template <int D, class T, bool kWide>
 __device__ __forceinline__ void issue_products(const AttnArgs& a, Control& c, uint8_t* smem, int stream)
 {
     using G = Geo<D>;
     constexpr bool kBf16 = std::is_same_v<T, Bf16>;
-    const uint32_t base = smem_addr(smem), ring = base + G::kRing, ts = c.tmem + stream * 128, to = c.tmem + 256 + stream * 128;
+    const uint32_t base = smem_addr(smem), ring = base + G::kRing, to = c.tmem + kOut + stream * 128;
     const bool one = elect_one();
-    uint32_t n0 = 0, first_halves = 0, second_halves = 0;
+    uint32_t n0 = 0, before = 0, others = 0, second_halves = 0;   // tiles of both; of this stream; of the other
 #pragma unroll 1
     for (uint32_t segment = 0;; ++segment) {
         if (!warp_wait(&c.told[segment % kSegments], segment / kSegments & 1, c, a.err)) return;
         const Segment s = c.segment[segment % kSegments];
         if (s.pages == 0) return;
-        const bool wide = s.wide;
+        const bool wide = kWide && s.wide;
         const int tiles = s.tiles(), mine = stream_tiles(tiles, wide, stream);
-        const Order order(tiles, wide);
+        const Order order(tiles);
         const uint64_t q = smem_desc(base + (wide ? stream * G::kQueryTile : 0), 16, 1024);
         const uint32_t vdesc = mma_desc(kBf16, true, kTileRows, D);
         auto arrived = [&](int at) { return warp_wait(&c.full[(n0 + at) % (2 * G::kSlots)], (n0 + at) / (2 * G::kSlots) & 1, c, a.err); };
         if (!warp_wait(&c.queries, segment & 1, c, a.err)) return;
-#pragma unroll 1
-        for (int j = -1; j < mine; ++j) {
-            const int t = stream_tile(wide, stream, j), next = stream_tile(wide, stream, j + 1);
-            const int vat = order.v(t), kat = order.k(next), pages = s.tile_pages(t);
-            const bool more = j + 1 < mine;
-            const uint64_t v = smem_desc(ring + (n0 + vat) % G::kSlots * G::kTileBytes, G::kBlockBytes, 1024);
-            const uint64_t k = smem_desc(ring + (n0 + kat) % G::kSlots * G::kTileBytes, 16, 1024);
-            const uint32_t kdesc = mma_desc(kBf16, false, kTileRows, s.tile_pages(next) * kPageSize);
-            if (j >= 0) {
-                if (!arrived(vat)) return;
-                if (!warp_wait(&c.weights[stream][0], first_halves++ & 1, c, a.err)) return;
+        const uint32_t ts = scores_at(c, wide, stream), tp = weights_at(c, wide, stream);
+        int j = 0, n = 0;                 // tiles whose scores, and whose products with V, have been issued
+        while (n < mine) {
+            if (j < mine && j <= n + wide) {
+                const int t = stream_tile(wide, stream, j), at = order.k(t);
+                const uint64_t k = smem_desc(ring + (n0 + at) % G::kSlots * G::kTileBytes, 16, 1024);
+                const uint32_t kdesc = mma_desc(kBf16, false, kTileRows, s.tile_pages(t) * kPageSize);
+                if (!arrived(at)) return;
+                // (Where the streams share the columns their scores follow one another by turns; a segment's first find them free.)
+                if (wide && (stream == 1 || j > 0) && !warp_wait(&c.taken[stream ^ 1], (others + j - (stream == 0)) & 1, c, a.err)) return;
                 tmem_fence_after();
-                if (one) {                        // (weights lie where their scores were, those of each half by themselves)
-#pragma unroll
-                    for (int kk = 0; kk < kTilePages / 2; ++kk)
-                        if (kk < pages) mma_ts(to, ts + kk * 8, v + kk * (2048 >> 4), vdesc, j > 0 || kk > 0);
-                    if (pages > kTilePages / 2) mma_commit(smem_addr(&c.half[stream]));
-                }
-                __syncwarp();
-                if (more && !arrived(kat)) return;
-                if (pages > kTilePages / 2 && !warp_wait(&c.weights[stream][1], second_halves++ & 1, c, a.err)) return;
-            } else if (more && !arrived(kat)) {
-                return;
-            }
-            tmem_fence_after();
-            if (one) {
-                if (j >= 0) {
-#pragma unroll
-                    for (int kk = kTilePages / 2; kk < kTilePages; ++kk)
-                        if (kk < pages) mma_ts(to, ts + kk * 8 + 32, v + kk * (2048 >> 4), vdesc, true);
-                }
-                if (more) {
+                if (one) {
 #pragma unroll
                     for (int ks = 0; ks < D / 16; ++ks)
                         mma_ss(ts, q + (((ks / 4) * G::kQueryBlock + (ks % 4) * 32) >> 4), k + (((ks / 4) * G::kBlockBytes + (ks % 4) * 32) >> 4),
                                kdesc, ks > 0);
+                    mma_commit(smem_addr(&c.scores[stream]));
+                    arrive(&c.scores[stream]);   // (what the loading warp has said of the tile comes along)
                 }
-                // Scores are there, and what came before is done (or there is nothing to do).  One commit for each group of
-                // products, right behind it: who reads the scores frees the slots.
-                if (j >= 0 || more) mma_commit(smem_addr(&c.scores[stream]));
-                else if (mine == 0) arrive(&c.scores[stream]);
-                if (j >= 0 || more || mine == 0) arrive(&c.scores[stream]);   // (what the loading warp has said of the tile comes along)
+                ++j;
+            } else {
+                const int t = stream_tile(wide, stream, n), at = order.v(t), pages = s.tile_pages(t);
+                const uint64_t v = smem_desc(ring + (n0 + at) % G::kSlots * G::kTileBytes, G::kBlockBytes, 1024);
+                if (!arrived(at)) return;
+                if (!warp_wait(&c.weights[stream][0], (before + n) & 1, c, a.err)) return;
+                tmem_fence_after();
+                if (one) {
+#pragma unroll
+                    for (int kk = 0; kk < kTilePages / 2; ++kk)
+                        if (kk < pages) mma_ts(to, tp + kk * 8, v + kk * (2048 >> 4), vdesc, n > 0 || kk > 0);
+                    if (!kWide && pages > kTilePages / 2) mma_commit(smem_addr(&c.half[stream]));
+                }
+                __syncwarp();
+                if (pages > kTilePages / 2) {
+                    if (!warp_wait(&c.weights[stream][1], second_halves++ & 1, c, a.err)) return;
+                    tmem_fence_after();
+                }
+                if (one) {
+#pragma unroll
+                    for (int kk = kTilePages / 2; kk < kTilePages; ++kk)
+                        if (kk < pages) mma_ts(to, tp + kk * 8, v + kk * (2048 >> 4), vdesc, true);
+                    mma_commit(smem_addr(&c.done[stream]));
+                }
+                ++n;
             }
             __syncwarp();
         }
+        if (mine == 0 && one) arrive(&c.done[stream]);   // (the stream's softmax goes on with its issuing warp)
+        __syncwarp();
+        before += mine;
+        others += stream_tiles(tiles, wide, stream ^ 1);
         n0 += 2 * tiles;
     }
 }
@@ -338,15 +352,98 @@ __device__ __forceinline__ uint32_t token_bits(int page, uint32_t known, int val
     return known >> page & 1u ? (1u << n) - 1u : 0u;
 }
 
-// A stream's softmax: a thread owns a row of the tile, whose scores are all in its registers at once.
+__device__ __forceinline__ float max3(uint32_t a, uint32_t b, uint32_t c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(__uint_as_float(a)), "f"(__uint_as_float(b)), "f"(__uint_as_float(c)));
+    return d;
+}
+
+// The softmax of a thread's row over N x 32 tokens whose scores are x.
 template <int D, class T>
+struct RowSoftmax {
+    float ref = -INFINITY, l = 0.f;   // reference, in log2 units; the sum of weights
+
+    // Tokens that do not take part: bits of 16 for each page.
+    template <int N>
+    static __device__ __forceinline__ void mask(uint32_t (&x)[N][32], int page, uint32_t known, int valid)
+    {
+#pragma unroll
+        for (int w = 0; w < N; ++w) {
+            const uint32_t bits = token_bits(page + 2 * w, known, valid) | token_bits(page + 2 * w + 1, known, valid) << 16;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[w][i] = bits >> i & 1u ? x[w][i] : 0xff800000u;
+        }
+    }
+    // Whether the reference has to move, and where to: a score exceeds it by more than 8 (see the top).
+    template <int N>
+    __device__ __forceinline__ bool exceeds(const uint32_t (&x)[N][32], float sl, float* to) const
+    {
+        float top[8];                                     // (eight chains)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top[i] = fmaxf(__uint_as_float(x[0][i]), __uint_as_float(x[1][i]));
+#pragma unroll
+        for (int i = 8; i < 32; ++i) top[i & 7] = max3(__float_as_uint(top[i & 7]), x[0][i], x[1][i]);
+#pragma unroll
+        for (int w = 2; w < N; w += 2)
+#pragma unroll
+            for (int i = 0; i < 32; ++i) top[i & 7] = max3(__float_as_uint(top[i & 7]), x[w][i], x[w + 1][i]);
+#pragma unroll
+        for (int d = 4; d > 0; d >>= 1)
+#pragma unroll
+            for (int i = 0; i < d; ++i) top[i] = fmaxf(top[i], top[i + d]);
+        *to = top[0] * sl;
+        return *to > ref + 8.f;
+    }
+    // It moves, and with it the sums so far, in whose columns nothing is under way (none: there are no sums yet).
+    __device__ __forceinline__ void move(bool moves, float to, bool none, uint32_t out)
+    {
+        if (!none) {
+            const float alpha = moves ? ex2(ref - to) : 1.f;
+            l *= alpha;
+#pragma unroll 1
+            for (int w = 0; w < D / 16; ++w) {
+                uint32_t o[16];
+                tmem_ld16(out + 16 * w, o);
+                tmem_wait_ld();
+                tmem_loaded(o);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                tmem_st16(out + 16 * w, o);
+            }
+        }
+        ref = moves ? to : ref;
+    }
+    // Weights of 32 tokens, in the pool's type, and their sum.
+    __device__ __forceinline__ void weigh(const uint32_t (&x)[32], float sl, uint32_t (&p)[16])
+    {
+        const float sub = (ref == -INFINITY ? 0.f : ref) - Weights<T>::kShift;
+        const uint64_t sl2 = f2_pack(sl, sl), sub2 = f2_pack(-sub, -sub);
+        uint64_t sum[2] = {0ull, 0ull};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float u, v;
+            f2_unpack(f2_fma(f2_pack(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), sl2, sub2), u, v);
+            u = ex2(u);
+            v = ex2(v);
+            sum[i & 1] = f2_add(sum[i & 1], f2_pack(u, v));
+            p[i] = T::pack(u, v);
+        }
+        float u, v;
+        f2_unpack(f2_add(sum[0], sum[1]), u, v);
+        l += u + v;
+    }
+};
+
+// A stream's softmax: a thread owns a row of the tile.
+template <int D, class T, bool kWide>
 __device__ __forceinline__ void softmax_stream(const AttnArgs& a, Control& c, uint8_t* smem)
 {
     using G = Geo<D>;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, stream = warp >> 2, wq = warp & 3;
     const int my = wq * 32 + lane;                        // row of the stream's tile
-    const uint32_t tm = c.tmem + ((uint32_t)wq << 21), ts = tm + stream * 128, to = tm + 256 + stream * 128;
-    uint32_t n0 = 0, tile_no = 0, phase = 0, halves = 0;  // phase: of the next scores; halves: first halves so far
+    const uint32_t quarter = (uint32_t)wq << 21, to = c.tmem + quarter + kOut + stream * 128;
+    uint32_t n0 = 0, tile_no = 0, scored = 0, halves = 0, used = 0;   // phases of the stream's scores, half and done
     const float sl = a.scale_log2;
 #pragma unroll 1
     for (uint32_t segment = 0;; ++segment) {
@@ -358,103 +455,32 @@ __device__ __forceinline__ void softmax_stream(const AttnArgs& a, Control& c, ui
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) arrive(&c.queries);
-        const int tiles = s.tiles(), wide = s.wide, mine = stream_tiles(tiles, wide, stream);
+        const bool wide = kWide && s.wide;
+        const int tiles = s.tiles(), mine = stream_tiles(tiles, wide, stream);
         const int qrows = (wide && stream == 1 ? s.rows - s.rows0 : s.rows0) * a.G;
         const bool works = wq * 32 < qrows;               // (the others have no row of the tile)
-        const Order order(tiles, wide);
+        const Order order(tiles);
         // (A slot is free when both streams have used its tile.)
-        auto free_slot = [&](int at) { arrive(&c.empty[(n0 + at) % G::kSlots], wide ? 1 : 2); };
-        float ref = -INFINITY, l = 0.f;
+        auto free_slot = [&](int at) {
+            if (wq == 0 && lane == 0) arrive(&c.empty[(n0 + at) % G::kSlots], wide ? 1 : 2);
+        };
+        const uint32_t ts = scores_at(c, wide, stream) + quarter, tp = weights_at(c, wide, stream) + quarter;
+        RowSoftmax<D, T> row;
 #pragma unroll 1
         for (int j = 0; j < mine; ++j) {
             const int t = stream_tile(wide, stream, j), pages = s.tile_pages(t), valid = s.valid - t * kTilePages * kPageSize;
-            if (!warp_wait(&c.scores[stream], phase++ & 1, c, a.err)) return;
+            if (!warp_wait(&c.scores[stream], scored++ & 1, c, a.err)) return;
             tmem_fence_after();
-            if (wq == 0 && lane == 0) {   // the tile of K has been used, and the stream's last one of V
-                free_slot(order.k(t));
-                if (j > 0) free_slot(order.v(stream_tile(wide, stream, j - 1)));
-            }
             const uint32_t known = (uint32_t)c.pages_known[(tile_no + t) % 8];
             const bool whole = valid >= kTilePages * kPageSize && known == (1u << kTilePages) - 1u;
+            free_slot(order.k(t));
+            if (!kWide && j > 0) free_slot(order.v(t - 2));
+            // Weights of a half are handed on at once: the first half's product with V runs while the second is worked.
             const int parts = pages > kTilePages / 2 ? 2 : 1;
-            // A half of the tile's tokens at a time: the first's product with V runs while the second is worked.
-#pragma unroll 1
-            for (int h = 0; h < parts; ++h) {
-                const uint32_t sc = ts + h * 64;
-                if (works) {
-                    uint32_t x[2][32];
-                    tmem_ld32(sc, x[0]);
-                    tmem_ld32(sc + 32, x[1]);
-                    tmem_wait_ld();
-                    tmem_loaded(x[0]);
-                    tmem_loaded(x[1]);
-                    if (!whole) {
-#pragma unroll
-                        for (int w = 0; w < 2; ++w) {
-                            const uint32_t bits = token_bits(4 * h + 2 * w, known, valid) | token_bits(4 * h + 2 * w + 1, known, valid) << 16;
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) x[w][i] = bits >> i & 1u ? x[w][i] : 0xff800000u;
-                        }
-                    }
-                    float top[8];                         // (eight chains)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) top[i] = fmaxf(__uint_as_float(x[0][i]), __uint_as_float(x[1][i]));
-#pragma unroll
-                    for (int i = 8; i < 32; ++i) top[i & 7] = fmaxf(top[i & 7], fmaxf(__uint_as_float(x[0][i]), __uint_as_float(x[1][i])));
-#pragma unroll
-                    for (int d = 4; d > 0; d >>= 1)
-#pragma unroll
-                        for (int i = 0; i < d; ++i) top[i] = fmaxf(top[i], top[i + d]);
-                    const float mx = top[0] * sl;
-                    // The reference moves where a score exceeds it by more than 8 (see the top); no row looks at another's.
-                    const bool moves = my < qrows && mx > ref + 8.f;
-                    if (__any_sync(0xffffffffu, moves)) {
-                        if (j > 0 || h > 0) {
-                            // (Scores that have come were issued after the products of the tile before; the first half's say so.)
-                            if (h > 0) {
-                                if (!warp_wait(&c.half[stream], halves & 1, c, a.err)) return;
-                                tmem_fence_after();
-                            }
-                            const float alpha = moves ? ex2(ref - mx) : 1.f;
-                            l *= alpha;
-#pragma unroll 1
-                            for (int w = 0; w < D / 16; ++w) {
-                                uint32_t o[16];
-                                tmem_ld16(to + 16 * w, o);
-                                tmem_wait_ld();
-                                tmem_loaded(o);
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                                tmem_st16(to + 16 * w, o);
-                            }
-                        }
-                        ref = moves ? mx : ref;
-                    }
-                    const float sub = (ref == -INFINITY ? 0.f : ref) - Weights<T>::kShift;
-                    const uint64_t sl2 = f2_pack(sl, sl), sub2 = f2_pack(-sub, -sub);
-                    uint64_t sum[2] = {0ull, 0ull};
-#pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        uint32_t p[16];
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            float u, v;
-                            f2_unpack(f2_fma(f2_pack(__uint_as_float(x[w][2 * i]), __uint_as_float(x[w][2 * i + 1])), sl2, sub2), u, v);
-                            u = ex2(u);
-                            v = ex2(v);
-                            sum[i & 1] = f2_add(sum[i & 1], f2_pack(u, v));
-                            p[i] = T::pack(u, v);
-                        }
-                        tmem_st16(sc + 16 * w, p);
-                    }
-                    float u, v;
-                    f2_unpack(f2_add(sum[0], sum[1]), u, v);
-                    l += u + v;
-                    tmem_wait_st();
-                }
+            auto hand_on = [&](int h) {
                 if (!whole) {   // rows of V that hold anything: zero, or 0 * NaN would reach the sums
                     const uint32_t n = n0 + order.v(t), vslot = n % G::kSlots;
-                    if (!warp_wait(&c.full[n % (2 * G::kSlots)], n / (2 * G::kSlots) & 1, c, a.err)) return;
+                    if (!warp_wait(&c.full[n % (2 * G::kSlots)], n / (2 * G::kSlots) & 1, c, a.err)) return false;
 #pragma unroll 1
                     for (int page = h * (kTilePages / 2); page < min(pages, (h + 1) * (kTilePages / 2)); ++page) {
                         const int from = known >> page & 1u ? valid - page * kPageSize : 0;   // (a thread has 16 bytes of each block)
@@ -468,12 +494,92 @@ __device__ __forceinline__ void softmax_stream(const AttnArgs& a, Control& c, ui
                 tmem_fence_before();
                 __syncwarp();
                 if (lane == 0) arrive(&c.weights[stream][h]);
+                return true;
+            };
+            if constexpr (kWide) {
+                // All of the tile's scores into registers, and the columns are the other stream's.
+                uint32_t x[4][32], p[16];
+                float mx;
+                if (works) {
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) tmem_ld32(ts + 32 * w, x[w]);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) tmem_loaded(x[w]);
+                }
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) arrive(&c.taken[stream]);
+                if (works) {
+                    if (!whole) row.mask(x, 0, known, valid);
+                    const bool moves = my < qrows && row.exceeds(x, sl, &mx);   // (no row looks at another's)
+                    if (__any_sync(0xffffffffu, moves)) {
+                        if (j > 0) {
+                            if (!warp_wait(&c.done[stream], used & 1, c, a.err)) return;
+                            tmem_fence_after();
+                        }
+                        row.move(moves, mx, j == 0, to);
+                    }
+                    row.weigh(x[0], sl, p);
+                }
+                // Weights lie where those of the tile before did, when these have met V (where the streams take turns, before these
+                // scores were made).
+                if (wide && j > 0) {
+                    if (!warp_wait(&c.done[stream], used & 1, c, a.err)) return;
+                    tmem_fence_after();
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (h == parts) break;
+                    if (works) {
+                        if (h > 0) row.weigh(x[2], sl, p);
+                        tmem_st16(tp + 32 * h, p);
+                        row.weigh(x[2 * h + 1], sl, p);
+                        tmem_st16(tp + 32 * h + 16, p);
+                        tmem_wait_st();
+                    }
+                    if (!hand_on(h)) return;
+                }
+            } else {
+                // A half at a time all along: fewer instructions to fetch, and weights sooner, where there are few tiles.  (Scores that
+                // have come were made after the products of the tile before.)
+#pragma unroll 1
+                for (int h = 0; h < parts; ++h) {
+                    if (works) {
+                        uint32_t x[2][32], p[16];
+                        float mx;
+                        tmem_ld32(ts + 64 * h, x[0]);
+                        tmem_ld32(ts + 64 * h + 32, x[1]);
+                        tmem_wait_ld();
+                        tmem_loaded(x[0]);
+                        tmem_loaded(x[1]);
+                        if (!whole) row.mask(x, 4 * h, known, valid);
+                        const bool moves = my < qrows && row.exceeds(x, sl, &mx);
+                        if (__any_sync(0xffffffffu, moves)) {
+                            if (h > 0) {
+                                if (!warp_wait(&c.half[stream], halves & 1, c, a.err)) return;
+                                tmem_fence_after();
+                            }
+                            row.move(moves, mx, j == 0 && h == 0, to);
+                        }
+                        row.weigh(x[0], sl, p);
+                        tmem_st16(tp + 32 * h, p);
+                        row.weigh(x[1], sl, p);
+                        tmem_st16(tp + 32 * h + 16, p);
+                        tmem_wait_st();
+                    }
+                    if (!hand_on(h)) return;
+                }
+                halves += parts - 1;
             }
-            halves += parts - 1;
+            if (j > 0) {
+                if (kWide) free_slot(order.v(stream_tile(wide, stream, j - 1)));
+                ++used;
+            }
         }
         const bool some = mine > 0;
-        if (!warp_wait(&c.scores[stream], phase++ & 1, c, a.err)) return;   // (the last products are done)
-        if (some && wq == 0 && lane == 0) free_slot(order.v(stream_tile(wide, stream, mine - 1)));
+        if (!warp_wait(&c.done[stream], used++ & 1, c, a.err)) return;   // (the last products are in)
+        if (some) free_slot(order.v(stream_tile(wide, stream, mine - 1)));
         n0 += 2 * tiles;
         tile_no += tiles;
         tmem_fence_after();
@@ -484,7 +590,7 @@ __device__ __forceinline__ void softmax_stream(const AttnArgs& a, Control& c, ui
             const int64_t entry = s.entry + (stream == 0 ? 0 : s.rows0 * a.G);
             uint8_t* const mine = smem + (wide ? stream * G::kQueryTile + wq * 32 * kRowBytes : G::kQueryTile + warp * 32 * kRowBytes);
             static_assert(kSoftmaxWarps * 32 * kRowBytes <= G::kQueryTile);
-            if (my < qrows) a.view.run_ml[entry + my] = make_float2(some ? ref - Weights<T>::kShift : -INFINITY, some ? l : 0.f);
+            if (my < qrows) a.view.run_ml[entry + my] = make_float2(some ? row.ref - Weights<T>::kShift : -INFINITY, some ? row.l : 0.f);
 #pragma unroll 1
             for (int w = 0; some && w < 4; ++w) {
                 uint32_t o[kCols];
@@ -762,7 +868,8 @@ __device__ __forceinline__ void work_records(const AttnArgs& a, const WarpStart&
         }
 }
 
-template <int D, class T>
+// kWide: for batches of more than 128 query rows of a KV head, whose runs may have more than a stream holds.
+template <int D, class T, bool kWide>
 __global__ void __launch_bounds__(kThreads, 1) attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                                                                 const __grid_constant__ AttnArgs a)
 {
@@ -776,6 +883,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kernel(const __grid_con
     if (tid < 2) {
         mbar_init(smem_addr(&c.scores[tid]), 2);
         mbar_init(smem_addr(&c.half[tid]), 1);
+        mbar_init(smem_addr(&c.taken[tid]), 4);
+        mbar_init(smem_addr(&c.done[tid]), 1);
     }
     if (tid < 4) mbar_init(smem_addr(&c.weights[0][0] + tid), 4);
     if (tid == 2) mbar_init(smem_addr(&c.queries), kSoftmaxWarps);
@@ -811,12 +920,14 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kernel(const __grid_con
         return;
     }
     if (warp < kSoftmaxWarps) {
-        softmax_stream<D, T>(a, c, smem);
+        if constexpr (kWide) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegisters));
+        softmax_stream<D, T, kWide>(a, c, smem);
     } else {
+        if constexpr (kWide) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegisters));
         if (warp == kLoadWarp) {
             load_tiles<D>(a, start, c, smem, &mk, &mv);
         } else if (warp < kMmaWarp + 2) {
-            issue_products<D, T>(a, c, smem, warp - kMmaWarp);
+            issue_products<D, T, kWide>(a, c, smem, warp - kMmaWarp);
             if (*reinterpret_cast<volatile int32_t*>(&c.gave_up) && elect_one()) {   // what is under way ends before the memory is freed
                 uint64_t* const last = &c.last[warp - kMmaWarp];
                 mma_commit(smem_addr(last));
@@ -955,15 +1066,29 @@ CUresult encode_pages(PFN_cuTensorMapEncodeTiled_v12000 encode, CUtensorMap* map
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
+template <int D, class T, bool kWide>
+int launch_attention(const CUtensorMap& mk, const CUtensorMap& mv, const AttnArgs& a, cudaStream_t st)
+{
+    const auto kernel = attention_kernel<D, T, kWide>;
+    static OncePerDevice once;
+    if (cudaError_t e = once.set_attribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes<D>); e != cudaSuccess)
+        return kv4_launch_result(e);
+    if (kWide) {   // (threads that ask for more registers than the block was launched with would wait for them forever)
+        static const int registers = [&] {
+            cudaFuncAttributes f{};
+            return cudaFuncGetAttributes(&f, kernel) == cudaSuccess ? f.numRegs : 0;
+        }();
+        if (registers != kRegisters) return kv4_fail(KVC_ERR_CUDA, "kv16_attention: the kernel was built with other registers than it moves");
+    }
+    if (cudaError_t e = kv4_launch(kernel, dim3((unsigned)a.grid), kThreads, kSharedBytes<D>, st, mk, mv, a); e != cudaSuccess)
+        return kv4_launch_result(e);
+    return kv4_launch_result(kv4_launch(merge_kernel<D, T>, dim3((unsigned)a.hq, (unsigned)a.batch), 128, 0, st, a));
+}
+
 template <int D, class T>
 int launch_attention(const CUtensorMap& mk, const CUtensorMap& mv, const AttnArgs& a, cudaStream_t st)
 {
-    static OncePerDevice once;
-    if (cudaError_t e = once.set_attribute(attention_kernel<D, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes<D>); e != cudaSuccess)
-        return kv4_launch_result(e);
-    if (cudaError_t e = kv4_launch(attention_kernel<D, T>, dim3((unsigned)a.grid), kThreads, kSharedBytes<D>, st, mk, mv, a); e != cudaSuccess)
-        return kv4_launch_result(e);
-    return kv4_launch_result(kv4_launch(merge_kernel<D, T>, dim3((unsigned)a.hq, (unsigned)a.batch), 128, 0, st, a));
+    return a.batch * a.G > kTileRows ? launch_attention<D, T, true>(mk, mv, a, st) : launch_attention<D, T, false>(mk, mv, a, st);
 }
 
 }  // namespace

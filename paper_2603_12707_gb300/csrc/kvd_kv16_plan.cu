@@ -232,6 +232,12 @@ __global__ void __launch_bounds__(kPlanMaxThreads) plan_kernel(StepPlanArgs a)
                 const int f = min(max((int)(a.grid * c / (c + u)), 1), a.grid - 1), g = min(f + 1, a.grid - 1);
                 ctas = max(c / f, u / (a.grid - f)) <= max(c / g, u / (a.grid - g)) ? f : g;
             }
+            // One run whose rows come in chunks: the same number of CTAs for each of its jobs, so that the chunks' CTAs read the same
+            // pages at about the same time, from L2 but for the first.
+            if (total.rows * G > 2 * kTileRows) {
+                const int r = last_at(s_cost, B, (int64_t)0), chunks = chunks_of(s_rows[r]), jobs = a.hkv * chunks;
+                if (s_rows[r] == total.rows && chunks > 1 && ctas % jobs * 8 <= ctas) ctas -= ctas % jobs;
+            }
             if (total.cost < (int64_t)ctas * kLeastRunPages * kWideCost) ctas = max((int)total.cost / (kLeastRunPages * kWideCost), 1);
         }
         if (!fits && speaks) kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
