@@ -6,15 +6,17 @@
 // a second launch merges.  One persistent CTA per SM works on one kind:
 //
 // * Prefixes of many rows: S = Q K^T with up to 256 query rows of a KV head against tiles of 128 tokens is a dense
-//   contraction, done by tcgen05.  Two streams of four softmax warps each hold scores and outputs of 128
-//   query rows in tensor memory (128 + head_dim columns); with more than 128 rows each has rows of
-//   its own, else the streams take halves of a tile's tokens.  A warp loads tiles (TMA, a
-//   ring of K and V tiles in shared memory), one thread issues the MMAs of both streams in turn, so that
-//   one stream's products run while the other's scores are worked.  A thread owns a row: no exchange between
-//   lanes.  Weights go back into tensor memory where their scores were, 16 bits each, as the
-//   operand of P V.
-// * A row's own tokens, and prefixes of few rows: a warp's worth of pages (16 tokens) at a
+//   contraction, done by tcgen05.  Two streams of four softmax warps each have scores, weights and sums of 128
+//   query rows in tensor memory; with more than 128 rows each has rows of its own ("wide"), else the streams take turns at the
+//   tiles.  A thread owns a row: no exchange between lanes.  A ninth warp loads tiles (TMA, a ring of K and V tiles in shared
+//   memory) and tells the others of segments, one more for each stream issues its products.  Weights go back into tensor memory, 16 bits
+//   each, as the operand of P V, half a tile at a time, so that the first half meets V while the second is worked.
+//   Bound by the softmax warps: a tile of 256 rows takes 3100 cycles, of which the tensor pipe is busy 2050 and the
+//   exponentials' 1030 (a warp loads 128 scores, finds their largest and makes and rounds 128 weights, about 790 instructions;
+//   two warps share an issue slot).  One prefix of 131009 tokens, 96 rows of 28/4 heads: 155 us a layer, 1.16 PFLOP/s.
+// * A row's own tokens, and prefixes of up to 8 query rows: a warp takes a page (16 tokens) at a
 //   time, S^T = K q^T and O^T = V^T P^T on mma.sync with the query rows padded to 8 columns, each warp with a ring of its own.
+//   Bound by reading K and V: 64 rows of 32/32 heads and 640 to 1344 tokens 157 us a layer, 6.7 TB/s.
 //
 // The reference m of a row moves only when a score exceeds it by more than 8 in log2 units (weights stay below 2^8).
 // fp16 weights carry a factor 2^7 more, so that the small ones keep their bits.
@@ -35,7 +37,9 @@ constexpr long long kLimitCycles = 2000000000ll;   // of all others: a second
 constexpr int kSoftmaxWarps = 8;                   // two streams of four
 constexpr int kThreads = 32 * (kSoftmaxWarps + 4);
 static_assert(kThreads == 32 * kAttnWarps);
-constexpr int kRegisters = 168, kSoftmaxRegisters = 208, kOtherRegisters = 88;   // of a thread: at launch, then by what a warp does
+// Registers of a thread at launch, and then by what its warp does.  (A row's 128 scores have to stay in registers: with 168 for
+// all some spill, and the tile above takes 4600 cycles.)
+constexpr int kRegisters = 168, kSoftmaxRegisters = 208, kOtherRegisters = 88;
 static_assert(kSoftmaxWarps * kSoftmaxRegisters + 4 * kOtherRegisters <= (kSoftmaxWarps + 4) * kRegisters);
 constexpr int kLoadWarp = kSoftmaxWarps, kMmaWarp = kSoftmaxWarps + 1;
 constexpr int kOut = 256;                          // first column of the sums in tensor memory
@@ -246,8 +250,8 @@ __device__ __forceinline__ void load_tiles(const AttnArgs& a, const CtaStart& st
             mbar_wait_bounded(smem_addr(&c.full[i % (2 * G::kSlots)]), i / (2 * G::kSlots) & 1, kLimitNs);
 }
 
-// A stream's issuing warp: the scores of its next tile, as soon as the other stream has taken its own from the columns that they share, then the
-// weights of the tile before against V, in halves as they come.  (All of the warp goes along, so that addresses and descriptors stay in uniform
+// A stream's issuing warp.  Wide: the scores of its next tile, as soon as the other stream has taken its own from the columns that they share, then
+// the weights of the tile before against V, in halves as they come.  Else first a tile's weights against V, then the next one's scores.  (All of the warp goes along, so that addresses and descriptors stay in uniform
 // registers; one lane issues.  Two warps, since what one does between its products takes as long as those.)
 template <int D, class T, bool kWide>
 __device__ __forceinline__ void issue_products(const AttnArgs& a, Control& c, uint8_t* smem, int stream)
@@ -868,7 +872,10 @@ __device__ __forceinline__ void work_records(const AttnArgs& a, const WarpStart&
         }
 }
 
-// kWide: for batches of more than 128 query rows of a KV head, whose runs may have more than a stream holds.
+// kWide: for batches of more than 128 query rows of a KV head, whose runs may have more than a stream holds.  The other kernel has half the softmax's
+// instructions to fetch, which shows where a CTA has a tile or two: four rows of 28/4 heads on 1369 tokens 9.5 us a layer with it, 10.4 with this one.
+// (This one against that, when that still took such batches: 131009 tokens and 96 rows 155 against 173, 32768 and 32 rows 27.6 against 29.6, eleven
+// small groups at d = 64 23.7 against 22.8.)
 template <int D, class T, bool kWide>
 __global__ void __launch_bounds__(kThreads, 1) attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                                                                 const __grid_constant__ AttnArgs a)
@@ -944,7 +951,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kernel(const __grid_con
 
 // ---------------------------------------------------------------------- merge
 // A CTA of four warps per (row, query head): the partial results of the row's own segments, then its prefix's, in their order.
-// Each warp takes every fourth; with loads of eight under way, a unit of up to 32 segments is two trips to L2.
+// Each warp takes every fourth; with loads of eight under way, a unit of up to 32 segments is two trips to L2.  Bound by
+// those trips and the launch: 1.6 us behind the attention of one row, 3.5 us for 896 units of 33 segments each (15 MB).
 template <int D, class T>
 __global__ void __launch_bounds__(128) merge_kernel(const __grid_constant__ AttnArgs a)
 {

@@ -24,7 +24,9 @@ constexpr int kTilePages = 8;           // of a tile of a large run: 128 tokens
 constexpr uint32_t kPlanMagic = 0x16a77e41u;
 
 // Cost of a page of a large run's job, with both streams on rows of their own or taking turns, and what opening and
-// closing a job costs beside, in such pages; a record's page, which costs what its bytes take.
+// closing a job costs beside, in such pages; a record's page.  (In units of some 20 cycles of an SM; the minima are flat: with records at
+// twice this, 64 rows of 32 heads on 701 tokens take 82.7 us a layer instead of 76.5; with 60 pages for opening a narrow job,
+// 16 rows of 32 heads on 1000 tokens 14.3 instead of 13.2.)
 __host__ __device__ inline int record_cost(int dim) { return dim / 16; }
 constexpr int kWideCost = 24, kNarrowCost = 12, kWideStart = 20, kNarrowStart = 30;
 // Shares are not made smaller than this (pages): every segment is one more result to merge.

