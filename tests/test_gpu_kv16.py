@@ -303,13 +303,14 @@ def test_every_call_gives_the_same(kv16, kv4, d, hq, hkv, batch, plen, olen):
 
 @pytest.mark.parametrize("dtype", [BF, FP])
 @pytest.mark.parametrize("q_scale", [0.0, 6.0, 60.0])
-def test_flat_and_sharp_scores(kv16, kv4, dtype, q_scale):
+@pytest.mark.parametrize("batch,d", [(30, 128), (63, 128), (99, 64)])     # 120, 252 and 396 query rows of a KV head
+def test_flat_and_sharp_scores(kv16, kv4, dtype, q_scale, batch, d):
     """Weights that are all equal; references that move often; one token that takes all."""
-    run(kv16, kv4, [0, 40, 7] * 10 + [1500], list(range(30)), [30] * 30, 8, 2, 128, dtype, seed=4, q_scale=q_scale, v_mean=1.0)
+    run(kv16, kv4, [0, 40, 7] * (batch // 3) + [1500], list(range(batch)), [batch] * batch, 8, 2, d, dtype, seed=4, q_scale=q_scale, v_mean=1.0)
 
 
 @pytest.mark.parametrize("dtype", [BF, FP])
-@pytest.mark.parametrize("d,batch", [(64, 40), (128, 40), (128, 3)])
+@pytest.mark.parametrize("d,batch", [(64, 40), (128, 40), (128, 3), (64, 100), (128, 100), (128, 300)])
 def test_scores_that_rise(kv16, kv4, dtype, d, batch):
     """Keys grow along the prefix, so every tile, and every half of one, moves the reference, by 2 to 40 in log2 units."""
     plen, hq, hkv = 900, 4, 2
@@ -333,9 +334,10 @@ def test_scores_that_rise(kv16, kv4, dtype, d, batch):
         assert_attention(out, lse, ref, dtype, step)
 
 
-def test_values_that_are_not_finite(kv16, kv4):
+@pytest.mark.parametrize("d,batch", [(64, 20), (64, 110), (128, 75)])
+def test_values_that_are_not_finite(kv16, kv4, d, batch):
     """A NaN or an infinity in a token's V reaches the rows that attend to it, in its element; a query that is none, its own head."""
-    d, hq, hkv, batch = 64, 4, 2, 20
+    hq, hkv = 4, 2
     lens = [20] * batch + [200]
     table, pages = make_tables(lens, 2)
     k, v = make_pool(pages, hkv, d, BF, 1, table, lens)
@@ -356,8 +358,9 @@ def test_values_that_are_not_finite(kv16, kv4):
     assert torch.isinf(got[0, 0, 9]) and torch.isnan(got[3, 2, 7]) and torch.isnan(got[11, 2]).all()
 
 
-def test_page_ids_outside_the_pool_are_left_out(kv16, kv4):
-    d, hq, hkv, batch = 128, 8, 4, 30
+@pytest.mark.parametrize("d,batch", [(128, 30), (128, 70), (64, 140)])
+def test_page_ids_outside_the_pool_are_left_out(kv16, kv4, d, batch):
+    hq, hkv = 8, 4
     lens = [50 + i for i in range(batch)] + [700]
     table, pages = make_tables(lens, 3)
     table[batch][3], table[batch][20], table[batch][43], table[4][1] = -5, pages, 2 ** 31 - 1, pages + 7
@@ -374,9 +377,10 @@ def test_page_ids_outside_the_pool_are_left_out(kv16, kv4):
     assert_attention(out, lse, attention(pool.k, pool.v, table, lens, None, [batch] * batch, q, d ** -0.5, BF), BF)
 
 
-def test_rows_that_are_refused(kv16, kv4):
+@pytest.mark.parametrize("d,batch", [(64, 26), (128, 90)])
+def test_rows_that_are_refused(kv16, kv4, d, batch):
     """An unknown request, a length past the table: zeros, the bit, and all other rows as ever."""
-    d, hq, hkv, batch = 64, 6, 3, 26
+    hq, hkv = 6, 3
     lens = [30 + i for i in range(batch)] + [260, 999999, -4]
     good = [n if 0 <= n <= 400 else 0 for n in lens]
     table, pages = make_tables(good, 3)
@@ -551,3 +555,101 @@ def test_two_graphs_share_a_workspace(kv16, kv4):
             g.replay()
         side.synchronize()
         assert_attention(out, None, ref, BF, i)
+
+
+def test_two_streams_at_once(kv16, kv4):
+    """Plans and attention of two batches on two streams, each with a workspace of its own, without order between them."""
+    jobs = []
+    for seed, (hq, hkv, d, batch, plen) in enumerate(((8, 2, 128, 50, 3000), (14, 2, 64, 60, 2000))):
+        lens = [9 * i % 80 for i in range(batch)] + [plen]
+        table, pages = make_tables(lens, seed)
+        pool = kv16.Pool(*(x.cuda() for x in make_pool(pages, hkv, d, BF, seed, table, lens)))
+        tabs = kv4.Tables(torch.from_numpy(table).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"))
+        q, pre = rows(batch, hq, d, BF, seed).cuda(), torch.full((batch,), batch, dtype=torch.int32, device="cuda")
+        ref = attention(pool.k, pool.v, table, lens, None, [batch] * batch, q, d ** -0.5, BF)
+        jobs.append((torch.cuda.Stream(), pool, tabs, q, pre, kv16.kv16_workspace(pool, hq, batch), [torch.empty_like(q) for _ in range(40)], ref))
+    torch.cuda.synchronize()
+    for i in range(40):
+        for stream, pool, tabs, q, pre, work, outs, _ in jobs:
+            kv16.kv16_plan(pool, tabs, q.shape[1], len(q), work, prefix_ids=pre, stream=stream)
+            kv16.kv16_attention(pool, tabs, q, outs[i], work, stream=stream)
+    torch.cuda.synchronize()
+    for *_, outs, ref in jobs:
+        assert_attention(outs[0], None, ref, BF)
+        assert all(torch.equal(outs[0].view(torch.int16), o.view(torch.int16)) for o in outs[1:])
+
+
+def test_offsets_past_32_bits(kv16, kv4):
+    """A pool of more than 2^31 elements a side, and rows of queries that far apart."""
+    d, hkv, hq, batch, plen, pages = 128, 1, 8, 33, 400, 1_200_000
+    pool = kv16.Pool.empty(pages, hkv, d)
+    assert pool.k.numel() > 2 ** 31
+    lens = [1 + 5 * i % 50 for i in range(batch)] + [plen]
+    table, used = make_tables(lens, 3)
+    table[table >= 0] += pages - used                     # the pool's last pages
+    tabs = kv4.Tables(torch.from_numpy(table).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    slots = torch.tensor([int(table[r][t // P]) * P + t % P for r, n in enumerate(lens) for t in range(n)], device="cuda")
+    assert int(slots.max()) * d > 2 ** 31
+    k, v = (rows(len(slots), hkv, d, BF, seed).cuda() for seed in (1, 2))
+    far = torch.zeros(batch << 26, dtype=BF, device="cuda")
+    q, out = (torch.as_strided(far, (batch, hq, d), (1 << 26, d, 1), at) for at in (0, hq * d))
+    assert (batch - 1) << 26 > 2 ** 30 and far.numel() > 2 ** 31
+    err = err_word()
+    kv16.kv16_write(pool, slots, k, v, device_error=err)
+    kv16.kv_qk_rope(kv16.Rope(inv_freq(d // 2)), torch.arange(batch, dtype=torch.int32, device="cuda"), rows(batch, hq, d, BF, 5).cuda(), None, q, None)
+    assert_rows(q, turned(rows(batch, hq, d, BF, 5), [list(range(batch))], inv_freq(d // 2), None), BF)
+    work = kv16.kv16_workspace(pool, hq, batch)
+    kv16.kv16_plan(pool, tabs, hq, batch, work, prefix_ids=torch.full((batch,), batch, dtype=torch.int32, device="cuda"), device_error=err)
+    kv16.kv16_attention(pool, tabs, q, out, work, device_error=err)
+    assert int(err) == 0
+    at = slots[:3]
+    assert torch.equal(pool.k[at // P, 0, at % P], k[:3, 0]) and torch.equal(pool.v[at // P, 0, at % P], v[:3, 0])
+    assert_attention(out, None, attention(pool.k, pool.v, table, lens, None, [batch] * batch, q, d ** -0.5, BF), BF)
+
+
+def test_one_row_of_queries_for_all(kv16, kv4):
+    """Stride 0: every row asks the same of its own tokens."""
+    lens = [40, 1, 0, 33, 200]
+    table, pages = make_tables(lens, 1)
+    pool = kv16.Pool(*(x.cuda() for x in make_pool(pages, 2, 64, BF, 1, table, lens)))
+    tabs = kv4.Tables(torch.from_numpy(table).cuda(), torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    q = rows(1, 4, 64, BF, 1).cuda().expand(5, 4, 64)
+    out, work = torch.empty((5, 4, 64), dtype=BF, device="cuda"), kv16.kv16_workspace(pool, 4, 5)
+    kv16.kv16_plan(pool, tabs, 4, 5, work)
+    kv16.kv16_attention(pool, tabs, q, out, work)
+    assert_attention(out, None, attention(pool.k, pool.v, table, lens, None, None, q, 64 ** -0.5, BF), BF)
+
+
+@pytest.mark.parametrize("batch", [4, 40])
+def test_the_first_call_is_captured(kvlib, batch):
+    """In a process whose first use of these kernels is under capture."""
+    import subprocess
+    import sys
+    code = f"""
+import torch
+from paper_2603_12707_gb300 import kv4, kv16
+hq, hkv, d, batch = 28, 4, 128, {batch}
+pool = kv16.Pool(*(torch.randn((batch + 9, hkv, 16, d), device="cuda").bfloat16() for _ in range(2)))
+tabs = kv4.Tables(torch.arange(batch + 1, dtype=torch.int32, device="cuda")[:, None] * torch.ones(8, dtype=torch.int32, device="cuda"),
+                  torch.tensor([16] * batch + [16], dtype=torch.int32, device="cuda"))
+pre = torch.full((batch,), batch, dtype=torch.int32, device="cuda")
+q = torch.randn((batch, hq, d), device="cuda").bfloat16()
+out, again, work = torch.empty_like(q), torch.empty_like(q), kv16.kv16_workspace(pool, hq, batch)
+rope, pos = kv16.Rope([1.0] * 64), torch.zeros(batch, dtype=torch.int32, device="cuda")
+slots = torch.full((batch,), -1, dtype=torch.int64, device="cuda")
+new = torch.zeros((batch, hkv, d), dtype=torch.bfloat16, device="cuda")
+torch.cuda.synchronize()
+s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+with torch.cuda.stream(s), torch.cuda.graph(g, stream=s):
+    kv16.kv16_plan(pool, tabs, hq, batch, work, prefix_ids=pre, stream=s)
+    kv16.kv16_write(pool, slots, new, new, rope=rope, positions=pos, q=q, q_out=q, stream=s)
+    kv16.kv16_attention(pool, tabs, q, out, work, stream=s)
+with torch.cuda.stream(s):
+    g.replay()
+s.synchronize()
+kv16.kv16_attention(pool, tabs, q, again, work)
+assert torch.isfinite(out).all() and torch.equal(out, again)
+print("fine")
+"""
+    got = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=120)
+    assert got.returncode == 0 and "fine" in got.stdout, got.stdout + got.stderr
