@@ -61,10 +61,10 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8])
     return make_uint4(T::pack(x[0], x[1]), T::pack(x[2], x[3]), T::pack(x[4], x[5]), T::pack(x[6], x[7]));
 }
 
-// 1 / sqrt(mean of squares + eps) of a head's elements, which makes them 2^-96 times as large where their squares pass the
-// range of 32 bits.
+// 1 / sqrt(mean of squares + eps) of a head's elements, which makes them 2^-96 times as large where they are normed and their
+// squares pass the range of 32 bits.
 template <int D>
-__device__ __forceinline__ float norm_of(float (&a)[8], float (&b)[8], float eps)
+__device__ __forceinline__ float norm_of(float (&a)[8], float (&b)[8], float eps, bool normed)
 {
     float s = 0.f, z = 0.f;
 #pragma unroll
@@ -76,8 +76,8 @@ __device__ __forceinline__ float norm_of(float (&a)[8], float (&b)[8], float eps
 #pragma unroll
     for (int m = 1; m < D / 16; m <<= 1) s += __shfl_xor_sync(0xffffffffu, s, m);
     float r = rsqrtf(fmaf(s, 1.f / D, eps));
-    if (__any_sync(0xffffffffu, s > 0x1p126f)) {
-        const bool far = s > 0x1p126f;
+    const bool far = normed && s > 0x1p126f;
+    if (__any_sync(0xffffffffu, far)) {
         const float by = far ? 0x1p-96f : 1.f;
         float t = 0.f;
 #pragma unroll
@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(32 * kRopeWarps) rope_kernel(RopeArgs a)
                 unpack8<T>(x0[i], x);
                 unpack8<T>(x1[i], y);
                 if (NORM && __any_sync(0xffffffffu, normed)) {
-                    const float z = norm_of<D>(x, y, a.eps), f = normed ? z : 1.f;   // (values are not stored from here)
+                    const float z = norm_of<D>(x, y, a.eps, normed), f = normed ? z : 1.f;   // (values are not stored from here)
                     float g[8];
                     unpack8<T>(is_q ? qw[0] : kw[0], g);
 #pragma unroll

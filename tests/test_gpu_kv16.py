@@ -126,6 +126,21 @@ def test_norms_alone_and_of_extreme_rows(kv16):
     assert torch.isnan(got[6, 1]).all() and torch.isfinite(got[6, 0]).all() and torch.isfinite(got[5, 1]).all()
 
 
+@pytest.mark.parametrize("of_q", [True, False])
+def test_huge_rows_beside_normed_ones(kv16, of_q):
+    """Only queries, or only keys, are normed; the others' squares pass the range of 32 bits and they are only turned."""
+    n, d, freq = 9, 128, inv_freq(64)
+    q, k = rows(n, 5, d, BF, 1), rows(n, 6, d, BF, 2)
+    big = k if of_q else q
+    big[::2] = (big[::2].float() * 2.0 ** 90).to(BF)
+    w = rows(1, 1, d, BF, 3).reshape(d)
+    out = torch.empty_like(q).cuda(), torch.empty_like(k).cuda()
+    kv16.kv_qk_rope(kv16.Rope(freq), torch.arange(n, dtype=torch.int32, device="cuda"), q.cuda(), k.cuda(), *out,
+                    **{"q_weight" if of_q else "k_weight": w.cuda()})
+    for got, x, weight in zip(out, (q, k), (w, None) if of_q else (None, w)):
+        assert_rows(got, turned(x, [list(range(n))], freq, None, weight=weight), BF, weight is None)
+
+
 @pytest.mark.parametrize("dtype", [BF, FP])
 @pytest.mark.parametrize("n,hq,hkv,d,rotated,normed", [(1, 28, 4, 128, True, False), (64, 32, 32, 128, True, True), (531, 14, 2, 64, True, False),
                                                        (33, 0, 5, 128, False, False), (77, 8, 8, 64, False, True), (3000, 4, 2, 128, True, True)])
