@@ -338,6 +338,14 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
     return r;
 }
 
+// d = a * b on both lanes, round to nearest.
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
 // d = a + b on both lanes, round to nearest.
 __device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b)
 {

@@ -10,8 +10,8 @@
 // the upper 32 bits go into the sine.
 //
 // Bound by memory where there are many rows: 49152 tokens of 28 + 4 heads, in and out, 121 us (6.6 TB/s), 40960 tokens of
-// 32 + 2 x 32 heads into pages 311 us (6.5 TB/s).  A chunk of 5003 normed tokens of 24 heads takes 13.9 us (4.4 TB/s: one wave of warps, each two
-// trips to memory long), 32 tokens 2.0 us (the launch and those trips).  A warp goes over a part of its token's heads, kAhead
+// 32 + 2 x 32 heads into pages 311 us (6.5 TB/s).  A chunk of 5003 normed tokens of 24 heads takes 12.6 us (4.9 TB/s: a wave of warps and a
+// part of one, each two trips to memory long, a third of the time instructions), 32 tokens 2.0 us (the launch and those trips).  A warp goes over a part of its token's heads, kAhead
 // turns of rows under way; few tokens are shared among more warps.
 #include <string>
 
@@ -21,8 +21,8 @@
 namespace kvd {
 namespace {
 
-constexpr int kRopeWarps = 1;      // of a CTA, so that a token's end frees its place (5003 normed tokens of 24 heads 15.4 us with 4, 13.9 with 1)
-constexpr int kAhead = 3;      // turns whose rows are under way together
+constexpr int kRopeWarps = 1;      // of a CTA, so that a token's end frees its place (5003 normed tokens of 24 heads 13.1 us with 4, 12.6 with 1)
+constexpr int kAhead = 3;      // turns whose rows are under way together (2: that chunk 13.1 us; 4: 12.3, but 64 tokens into pages 3.1 instead of 2.95)
 
 struct RopeArgs {
     const uint64_t* freqs;
@@ -66,12 +66,15 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8])
 template <int D>
 __device__ __forceinline__ float norm_of(float (&a)[8], float (&b)[8], float eps, bool normed)
 {
-    float s = 0.f, z = 0.f;
+    uint64_t u = 0ull, v = 0ull;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        s = fmaf(a[i], a[i], s);
-        z = fmaf(b[i], b[i], z);
+    for (int i = 0; i < 8; i += 2) {
+        const uint64_t p = f2_pack(a[i], a[i + 1]), q = f2_pack(b[i], b[i + 1]);
+        u = f2_fma(p, p, u);
+        v = f2_fma(q, q, v);
     }
+    float s, z;
+    f2_unpack(f2_add(u, v), s, z);
     s += z;
 #pragma unroll
     for (int m = 1; m < D / 16; m <<= 1) s += __shfl_xor_sync(0xffffffffu, s, m);
@@ -149,15 +152,7 @@ __global__ void __launch_bounds__(32 * kRopeWarps) rope_kernel(RopeArgs a)
         }
     };
     load(first);
-    uint4 qw[2] = {}, kw[2] = {};
-    if (NORM && a.q_weight) {
-        qw[0] = reinterpret_cast<const uint4*>(a.q_weight)[c0];
-        qw[1] = reinterpret_cast<const uint4*>(a.q_weight)[c1];
-    }
-    if (NORM && a.k_weight) {
-        kw[0] = reinterpret_cast<const uint4*>(a.k_weight)[c0];
-        kw[1] = reinterpret_cast<const uint4*>(a.k_weight)[c1];
-    }
+    constexpr uint32_t kOnes = std::is_same_v<T, Bf16> ? 0x3f803f80u : 0x3c003c00u;   // (where only one of the two is normed)
     int64_t slot = 0;
     if (POOL) {
         slot = a.slots[t];
@@ -194,21 +189,38 @@ __global__ void __launch_bounds__(32 * kRopeWarps) rope_kernel(RopeArgs a)
                 unpack8<T>(x1[i], y);
                 if (NORM && __any_sync(0xffffffffu, normed)) {
                     const float z = norm_of<D>(x, y, a.eps, normed), f = normed ? z : 1.f;   // (values are not stored from here)
+                    const uint64_t f2 = f2_pack(f, f);
+                    const uint4* const weight = reinterpret_cast<const uint4*>(is_q ? a.q_weight : a.k_weight);
+                    uint4 w0 = make_uint4(kOnes, kOnes, kOnes, kOnes), w1 = w0;
+                    if (normed) {
+                        w0 = __ldg(weight + c0);
+                        w1 = __ldg(weight + c1);
+                    }
                     float g[8];
-                    unpack8<T>(is_q ? qw[0] : kw[0], g);
+                    unpack8<T>(w0, g);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) x[k] = x[k] * f * (normed ? g[k] : 1.f);
-                    unpack8<T>(is_q ? qw[1] : kw[1], g);
+                    for (int k = 0; k < 4; ++k) f2_unpack(f2_mul(f2_mul(f2_pack(x[2 * k], x[2 * k + 1]), f2), f2_pack(g[2 * k], g[2 * k + 1])), x[2 * k], x[2 * k + 1]);
+                    unpack8<T>(w1, g);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) y[k] = y[k] * f * (normed ? g[k] : 1.f);
+                    for (int k = 0; k < 4; ++k) f2_unpack(f2_mul(f2_mul(f2_pack(y[2 * k], y[2 * k + 1]), f2), f2_pack(g[2 * k], g[2 * k + 1])), y[2 * k], y[2 * k + 1]);
                 }
                 if (turns) {
                     if (KIND == kHalves) {
+                        if constexpr (NORM) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const uint64_t u = f2_pack(x[2 * k], x[2 * k + 1]), v = f2_pack(y[2 * k], y[2 * k + 1]);
+                            const uint64_t c = f2_pack(cs[2 * k], cs[2 * k + 1]), z = f2_pack(sn[2 * k], sn[2 * k + 1]);
+                            f2_unpack(f2_fma(u, c, f2_mul(v, f2_pack(-sn[2 * k], -sn[2 * k + 1]))), x[2 * k], x[2 * k + 1]);
+                            f2_unpack(f2_fma(v, c, f2_mul(u, z)), y[2 * k], y[2 * k + 1]);
+                        }
+                        } else {
 #pragma unroll
                         for (int k = 0; k < 8; ++k) {
                             const float u = x[k], v = y[k];
                             x[k] = u * cs[k] - v * sn[k];
                             y[k] = v * cs[k] + u * sn[k];
+                        }
                         }
                     } else {
 #pragma unroll
