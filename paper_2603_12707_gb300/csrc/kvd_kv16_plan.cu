@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(kPlanMaxThreads) plan_kernel(StepPlanArgs a)
             s_pages[r] = pages;
             s_cost[r] = at.cost - mine.cost;
             s_before[r] = at.rows - mine.rows;
-            if (speaks) {
+            if (blockIdx.x == 1) {             // (others than the one that writes the header)
                 run.req = s_pre[r];
                 run.len = s_plen[r];
                 run.pages = mine.cost ? pages : 0;
@@ -216,22 +216,25 @@ __global__ void __launch_bounds__(kPlanMaxThreads) plan_kernel(StepPlanArgs a)
                 run.cost = s_cost[r];
                 run.rows_before = s_before[r];
                 a.view.runs[r] = run;
+            }
+            if (blockIdx.x == 2) {
                 const int n = s_len[r];
                 a.view.recs[2 * r] = Record{s_pre[r], s_plen[r], small_pages, r, rows, s_unit[2 * r], s_col[2 * r], 0};
                 a.view.recs[2 * r + 1] = Record{s_req[r], n, pages_of(n), r, 1, s_unit[2 * r + 1], s_col[2 * r + 1], 0};
             }
         }
     }
-    if (tid == 0) {
-        // CTAs for large runs, the others for records: the cut at which the slower side is fastest.
+    if (tid < 32) {
+        // CTAs for large runs, the others for records: the cut at which the slower side is fastest.  (All lanes alike, but for the
+        // shares, of which each other lane makes the other kind's.  Quotients are within two steps of 2^-24; 64-bit floating point is far slower.)
         const bool fits = total.units < (int64_t)1 << 31 && total.cost < (int64_t)1 << 40;
         int ctas = 0;
         if (total.cost > 0) {
-            const float c = (float)total.cost, u = (float)total.units * record_cost(a.dim);   // (64-bit floating point is far slower here)
+            const float c = (float)total.cost, u = (float)total.units * record_cost(a.dim);
             ctas = a.grid;
             if (total.units > 0) {
-                const int f = min(max((int)(a.grid * c / (c + u)), 1), a.grid - 1), g = min(f + 1, a.grid - 1);
-                ctas = max(c / f, u / (a.grid - f)) <= max(c / g, u / (a.grid - g)) ? f : g;
+                const int f = min(max((int)__fdividef(a.grid * c, c + u), 1), a.grid - 1), g = min(f + 1, a.grid - 1);
+                ctas = max(__fdividef(c, (float)f), __fdividef(u, (float)(a.grid - f))) <= max(__fdividef(c, (float)g), __fdividef(u, (float)(a.grid - g))) ? f : g;
             }
             // One run whose rows come in chunks: the same number of CTAs for each of its jobs, so that the chunks' CTAs read the same
             // pages at about the same time, from L2 but for the first.
@@ -241,24 +244,31 @@ __global__ void __launch_bounds__(kPlanMaxThreads) plan_kernel(StepPlanArgs a)
             }
             if (total.cost < (int64_t)ctas * kLeastRunPages * kWideCost) ctas = max((int)total.cost / (kLeastRunPages * kWideCost), 1);
         }
-        if (!fits && speaks) kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
-        PlanHeader h{};
-        h.magic = fits ? kPlanMagic : 0;
-        h.batch = B;
-        h.hq = a.hq;
-        h.hkv = a.hkv;
-        h.dim = a.dim;
-        h.grid = a.grid;
-        h.max_seqs = a.max_seqs;
-        h.max_pages = a.max_pages;
-        h.prefix_ctas = ctas;
-        h.warps = (int)min((int64_t)(a.grid - ctas) * kAttnWarps, (total.units + kLeastRecordPages - 1) / kLeastRecordPages);
-        if (fits) {
-            h.units = make_shares(total.units, h.warps);
-            h.cost = make_shares(total.cost, ctas);
+        if (!fits && speaks && tid == 0) kv4_error(a.err, KVC_DEVERR_SEQ_RANGE);
+        const int warps = (int)min((int64_t)(a.grid - ctas) * kAttnWarps, (total.units + kLeastRecordPages - 1) / kLeastRecordPages);
+        if (tid < 2) {
+            Shares shares{};
+            if (fits) shares = make_shares(tid ? total.cost : total.units, tid ? ctas : warps);
+            PlanHeader h{};
+            h.magic = fits ? kPlanMagic : 0;
+            h.batch = B;
+            h.hq = a.hq;
+            h.hkv = a.hkv;
+            h.dim = a.dim;
+            h.grid = a.grid;
+            h.max_seqs = a.max_seqs;
+            h.max_pages = a.max_pages;
+            h.prefix_ctas = ctas;
+            h.warps = warps;
+            if (tid == 1) s_header.cost = shares;
+            __syncwarp(3u);
+            if (tid == 0) {
+                h.units = shares;
+                h.cost = s_header.cost;
+                s_header = h;
+                if (speaks) *a.view.header = h;
+            }
         }
-        if (speaks) *a.view.header = h;
-        s_header = h;
     }
     __syncthreads();
     if (s_header.magic == 0) return;
