@@ -259,7 +259,6 @@ __global__ void __launch_bounds__(kPlanMaxThreads) plan_kernel(StepPlanArgs a)
             h.max_seqs = a.max_seqs;
             h.max_pages = a.max_pages;
             h.prefix_ctas = ctas;
-            h.warps = warps;
             if (tid == 1) s_header.cost = shares;
             __syncwarp(3u);
             if (tid == 0) {

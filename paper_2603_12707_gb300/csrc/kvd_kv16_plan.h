@@ -62,7 +62,7 @@ struct PlanHeader {
     uint32_t magic;
     int32_t batch, hq, hkv, dim, grid, max_seqs, max_pages;   // what it was made for
     int32_t prefix_ctas;        // CTAs 0 .. are the workers of large runs
-    int32_t warps;              // workers of records
+    int32_t pad;
     Shares units;               // pages x KV heads of all records
     Shares cost;                // of all large runs
 };
