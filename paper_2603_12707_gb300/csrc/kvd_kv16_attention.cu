@@ -11,9 +11,10 @@
 //   tiles.  A thread owns a row: no exchange between lanes.  A ninth warp loads tiles (TMA, a ring of K and V tiles in shared
 //   memory) and tells the others of segments, one more for each stream issues its products.  Weights go back into tensor memory, 16 bits
 //   each, as the operand of P V, half a tile at a time, so that the first half meets V while the second is worked.
-//   Bound by the softmax warps: a tile of 256 rows takes 3100 cycles, of which the tensor pipe is busy 2050 and the
-//   exponentials' 1030 (a warp loads 128 scores, finds their largest and makes and rounds 128 weights, about 790 instructions;
-//   two warps share an issue slot).  One prefix of 131009 tokens, 96 rows of 28/4 heads: 155 us a layer, 1.16 PFLOP/s.
+//   A tile of 256 rows takes 3000 cycles, of which the tensor pipe is busy 2050.  Bound by the columns that both streams' scores
+//   pass through by turns: 512 cycles of products, 490 until four warps have them in registers, some 360 for the two hand-overs, twice
+//   a tile (half of the exponentials, no search for the largest score or no rounding change its time by 2 % at most).  One prefix of
+//   131009 tokens, 96 rows of 28/4 heads: 151 us a layer, 1.19 PFLOP/s.
 // * A row's own tokens, and prefixes of up to 8 query rows: a warp takes a page (16 tokens) at a
 //   time, S^T = K q^T and O^T = V^T P^T on mma.sync with the query rows padded to 8 columns, each warp with a ring of its own.
 //   Bound by reading K and V: 64 rows of 32/32 heads and 640 to 1344 tokens 157 us a layer, 6.7 TB/s.
@@ -130,11 +131,6 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, Contro
     }
 }
 
-__device__ __forceinline__ void arrive(uint64_t* bar, uint32_t count)
-{
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(bar)), "r"(count) : "memory");
-}
-
 __device__ __forceinline__ void arrive(uint64_t* bar)
 {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
@@ -244,6 +240,8 @@ __device__ __forceinline__ void load_tiles(const AttnArgs& a, const CtaStart& st
         s.pages = 0;
     }
     if (fine) tell(s);
+    // The CTA does not leave before its slots have been told to be free.
+    for (uint32_t i = n > G::kSlots ? n - G::kSlots : 0; fine && i < n; ++i) fine = warp_wait(&c.empty[i % G::kSlots], i / G::kSlots & 1, c, a.err);
     // Where others gave up: what is under way arrives before the CTA leaves.
     if (*reinterpret_cast<volatile int32_t*>(&c.gave_up))
         for (uint32_t i = n > G::kSlots ? n - G::kSlots : 0; i < n; ++i)
@@ -272,6 +270,12 @@ __device__ __forceinline__ void issue_products(const AttnArgs& a, Control& c, ui
         const uint64_t q = smem_desc(base + (wide ? stream * G::kQueryTile : 0), 16, 1024);
         const uint32_t vdesc = mma_desc(kBf16, true, kTileRows, D);
         auto arrived = [&](int at) { return warp_wait(&c.full[(n0 + at) % (2 * G::kSlots)], (n0 + at) / (2 * G::kSlots) & 1, c, a.err); };
+        // A slot is free when the products that both streams, or the one that has the tile, issued with it are done.
+        auto free_slot = [&](int at) {
+            uint64_t* const slot = &c.empty[(n0 + at) % G::kSlots];
+            mma_commit(smem_addr(slot));
+            if (!wide) arrive(slot);
+        };
         if (!warp_wait(&c.queries, segment & 1, c, a.err)) return;
         const uint32_t ts = scores_at(c, wide, stream), tp = weights_at(c, wide, stream);
         int j = 0, n = 0;                 // tiles whose scores, and whose products with V, have been issued
@@ -291,6 +295,7 @@ __device__ __forceinline__ void issue_products(const AttnArgs& a, Control& c, ui
                                kdesc, ks > 0);
                     mma_commit(smem_addr(&c.scores[stream]));
                     arrive(&c.scores[stream]);   // (what the loading warp has said of the tile comes along)
+                    free_slot(at);
                 }
                 ++j;
             } else {
@@ -315,6 +320,7 @@ __device__ __forceinline__ void issue_products(const AttnArgs& a, Control& c, ui
                     for (int kk = kTilePages / 2; kk < kTilePages; ++kk)
                         if (kk < pages) mma_ts(to, tp + kk * 8, v + kk * (2048 >> 4), vdesc, true);
                     mma_commit(smem_addr(&c.done[stream]));
+                    free_slot(at);
                 }
                 ++n;
             }
@@ -464,10 +470,6 @@ __device__ __forceinline__ void softmax_stream(const AttnArgs& a, Control& c, ui
         const int qrows = (wide && stream == 1 ? s.rows - s.rows0 : s.rows0) * a.G;
         const bool works = wq * 32 < qrows;               // (the others have no row of the tile)
         const Order order(tiles);
-        // (A slot is free when both streams have used its tile.)
-        auto free_slot = [&](int at) {
-            if (wq == 0 && lane == 0) arrive(&c.empty[(n0 + at) % G::kSlots], wide ? 1 : 2);
-        };
         const uint32_t ts = scores_at(c, wide, stream) + quarter, tp = weights_at(c, wide, stream) + quarter;
         RowSoftmax<D, T> row;
 #pragma unroll 1
@@ -475,10 +477,22 @@ __device__ __forceinline__ void softmax_stream(const AttnArgs& a, Control& c, ui
             const int t = stream_tile(wide, stream, j), pages = s.tile_pages(t), valid = s.valid - t * kTilePages * kPageSize;
             if (!warp_wait(&c.scores[stream], scored++ & 1, c, a.err)) return;
             tmem_fence_after();
+            uint32_t x[kWide ? 4 : 1][32];
+            if constexpr (kWide) {
+                // All of the tile's scores into registers, and the columns are the other stream's.
+                if (works) {
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) tmem_ld32(ts + 32 * w, x[w]);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) tmem_loaded(x[w]);
+                }
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) arrive(&c.taken[stream]);
+            }
             const uint32_t known = (uint32_t)c.pages_known[(tile_no + t) % 8];
             const bool whole = valid >= kTilePages * kPageSize && known == (1u << kTilePages) - 1u;
-            free_slot(order.k(t));
-            if (!kWide && j > 0) free_slot(order.v(t - 2));
             // Weights of a half are handed on at once: the first half's product with V runs while the second is worked.
             const int parts = pages > kTilePages / 2 ? 2 : 1;
             auto hand_on = [&](int h) {
@@ -501,19 +515,8 @@ __device__ __forceinline__ void softmax_stream(const AttnArgs& a, Control& c, ui
                 return true;
             };
             if constexpr (kWide) {
-                // All of the tile's scores into registers, and the columns are the other stream's.
-                uint32_t x[4][32], p[16];
+                uint32_t p[16];
                 float mx;
-                if (works) {
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) tmem_ld32(ts + 32 * w, x[w]);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) tmem_loaded(x[w]);
-                }
-                tmem_fence_before();
-                __syncwarp();
-                if (lane == 0) arrive(&c.taken[stream]);
                 if (works) {
                     if (!whole) row.mask(x, 0, known, valid);
                     const bool moves = my < qrows && row.exceeds(x, sl, &mx);   // (no row looks at another's)
@@ -576,14 +579,10 @@ __device__ __forceinline__ void softmax_stream(const AttnArgs& a, Control& c, ui
                 }
                 halves += parts - 1;
             }
-            if (j > 0) {
-                if (kWide) free_slot(order.v(stream_tile(wide, stream, j - 1)));
-                ++used;
-            }
+            used += j > 0;
         }
         const bool some = mine > 0;
         if (!warp_wait(&c.done[stream], used++ & 1, c, a.err)) return;   // (the last products are in)
-        if (some) free_slot(order.v(stream_tile(wide, stream, mine - 1)));
         n0 += 2 * tiles;
         tile_no += tiles;
         tmem_fence_after();
@@ -874,8 +873,8 @@ __device__ __forceinline__ void work_records(const AttnArgs& a, const WarpStart&
 
 // kWide: for batches of more than 128 query rows of a KV head, whose runs may have more than a stream holds.  The other kernel has half the softmax's
 // instructions to fetch, which shows where a CTA has a tile or two: four rows of 28/4 heads on 1369 tokens 9.5 us a layer with it, 10.4 with this one.
-// (This one against that, when that still took such batches: 131009 tokens and 96 rows 155 against 173, 32768 and 32 rows 27.6 against 29.6, eleven
-// small groups at d = 64 23.7 against 22.8.)
+// (This one against that, when that still took such batches: 131009 tokens and 96 rows 151 against 173, 32768 and 32 rows 27.1 against 29.6, eleven
+// small groups at d = 64 24.2 against 22.8.)
 template <int D, class T, bool kWide>
 __global__ void __launch_bounds__(kThreads, 1) attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                                                                 const __grid_constant__ AttnArgs a)
