@@ -950,8 +950,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kernel(const __grid_con
 
 // ---------------------------------------------------------------------- merge
 // A CTA of four warps per (row, query head): the partial results of the row's own segments, then its prefix's, in their order.
-// Each warp takes every fourth; with loads of eight under way, a unit of up to 32 segments is two trips to L2.  Bound by
-// those trips and the launch: 1.6 us behind the attention of one row, 3.5 us for 896 units of 33 segments each (15 MB).
+// Each warp takes every fourth; with loads of eight under way, a unit of up to 32 segments is one trip to L2 after its sources.  Bound by
+// those trips and the launch: 1.3 us behind the attention of one row, 3.5 us for 896 units of 33 segments each (15 MB).
 template <int D, class T>
 __global__ void __launch_bounds__(128) merge_kernel(const __grid_constant__ AttnArgs a)
 {
@@ -983,6 +983,11 @@ __global__ void __launch_bounds__(128) merge_kernel(const __grid_constant__ Attn
                                                    : x.prefix + (int64_t)p * x.step);
         const float2 ml = lane < n ? (in_run ? a.view.run_ml : a.view.rec_ml)[e] : make_float2(-INFINITY, 0.f);
         const uint64_t from = reinterpret_cast<uint64_t>((in_run ? a.view.run_o : a.view.rec_o) + e * D);
+        // The first eight's sums come along with them.
+        Vec v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) v[j] = reinterpret_cast<const Vec*>(__shfl_sync(0xffffffffu, from, j))[lane];
         float top = ml.y == 0.f ? -INFINITY : ml.x;   // (a segment without tokens has no part)
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
@@ -995,18 +1000,8 @@ __global__ void __launch_bounds__(128) merge_kernel(const __grid_constant__ Attn
         l = l * old + sum;
 #pragma unroll
         for (int i = 0; i < N; ++i) o[i] *= old;
-        uint32_t parts = __ballot_sync(0xffffffffu, mine != 0.f);   // (what has no weight may hold anything)
-        while (parts) {
-            Vec v[8];
-            float f[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int k = parts ? __ffs(parts) - 1 : 0;
-                f[j] = __shfl_sync(0xffffffffu, mine, k);
-                if (!parts) f[j] = 0.f;
-                else v[j] = reinterpret_cast<const Vec*>(__shfl_sync(0xffffffffu, from, k))[lane];
-                parts &= parts - 1;
-            }
+        float f[8];
+        auto add = [&] {                              // (what has no weight may hold anything)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 if (f[j] != 0.f) {
@@ -1018,6 +1013,21 @@ __global__ void __launch_bounds__(128) merge_kernel(const __grid_constant__ Attn
                     }
                 }
             }
+        };
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = __shfl_sync(0xffffffffu, mine, j);
+        add();
+        uint32_t parts = __ballot_sync(0xffffffffu, mine != 0.f) & ~0xffu;
+        while (parts) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int k = parts ? __ffs(parts) - 1 : 0;
+                f[j] = __shfl_sync(0xffffffffu, mine, k);
+                if (!parts) f[j] = 0.f;
+                else v[j] = reinterpret_cast<const Vec*>(__shfl_sync(0xffffffffu, from, k))[lane];
+                parts &= parts - 1;
+            }
+            add();
         }
     }
 #pragma unroll
