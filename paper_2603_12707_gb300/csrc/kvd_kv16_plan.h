@@ -29,8 +29,9 @@ constexpr uint32_t kPlanMagic = 0x16a77e41u;
 // 16 rows of 32 heads on 1000 tokens 14.3 instead of 13.2.)
 __host__ __device__ inline int record_cost(int dim) { return dim / 16; }
 constexpr int kWideCost = 24, kNarrowCost = 12, kWideStart = 20, kNarrowStart = 30;
-// Shares are not made smaller than this (pages): every segment is one more result to merge.
-constexpr int kLeastRunPages = 8, kLeastRecordPages = 4;
+// Shares are not made smaller than this (pages): every segment is one more result to merge.  (Records, a layer with 4, 2 and 1: one row of 16
+// tokens, 28/4 heads, 9.7, 6.9 and 5.8 us; four of 1369 9.4, 9.45 and 11.0.  Runs with 4, 8 and 12: four rows on 1369 tokens 9.5, 9.6 and 10.9.)
+constexpr int kLeastRunPages = 8, kLeastRecordPages = 2;
 
 // `total` units cut into n shares; worker w's starts at w * total / n, as far as 20 bits after the point go (rounded up, so
 // that the last one ends at the total).
