@@ -583,41 +583,32 @@ __device__ __forceinline__ void softmax_stream(const AttnArgs& a, Control& c, ui
         }
         const bool some = mine > 0;
         if (!warp_wait(&c.done[stream], used++ & 1, c, a.err)) return;   // (the last products are in)
+        if (lane == 0) arrive(&c.drained);                              // (this stream's products need the queries no more)
         n0 += 2 * tiles;
         tile_no += tiles;
         tmem_fence_after();
         if (works) {
-            // Some columns at a time through shared memory, so that those of a row are stored together: in the stream's own
-            // tile of queries, which its products have read by now, or in the second one where both streams work on the first.
-            constexpr int kCols = D / 4, kRowBytes = kCols * 4, kPieces = kRowBytes / 16;   // pieces of 16 bytes
+            // A row's results, 32 bytes (a sector) of each at a time.  (By way of shared memory, so that a row's columns leave together: d = 64 4 %
+            // longer, four rows on an image 9.2 us a layer instead of 8.8, one prefix of 32768 tokens 27.1 instead of 27.5.)
             const int64_t entry = s.entry + (stream == 0 ? 0 : s.rows0 * a.G);
-            uint8_t* const mine = smem + (wide ? stream * G::kQueryTile + wq * 32 * kRowBytes : G::kQueryTile + warp * 32 * kRowBytes);
-            static_assert(kSoftmaxWarps * 32 * kRowBytes <= G::kQueryTile);
             if (my < qrows) a.view.run_ml[entry + my] = make_float2(some ? row.ref - Weights<T>::kShift : -INFINITY, some ? row.l : 0.f);
+            float* const row_o = a.view.run_o + (entry + my) * D;
 #pragma unroll 1
-            for (int w = 0; some && w < 4; ++w) {
-                uint32_t o[kCols];
-                if constexpr (D == 128) tmem_ld32(to + kCols * w, o);
-                else tmem_ld16(to + kCols * w, o);
+            for (int w = 0; some && w < D / 32; ++w) {
+                uint32_t o[32];
+                tmem_ld32(to + 32 * w, o);
                 tmem_wait_ld();
                 tmem_loaded(o);
+                if (my < qrows) {
 #pragma unroll
-                for (int i = 0; i < kPieces; ++i)
-                    *reinterpret_cast<uint4*>(mine + lane * kRowBytes + ((i ^ (lane & (kPieces - 1))) << 4)) =
-                        make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-                __syncwarp();
-#pragma unroll
-                for (int i = 0; i < kPieces; ++i) {
-                    const int r = (32 / kPieces) * i + lane / kPieces, ch = lane % kPieces;
-                    const uint4 v = *reinterpret_cast<const uint4*>(mine + r * kRowBytes + ((ch ^ (r & (kPieces - 1))) << 4));
-                    if (wq * 32 + r < qrows) *reinterpret_cast<uint4*>(a.view.run_o + (entry + wq * 32 + r) * D + w * kCols + ch * 4) = v;
+                    for (int i = 0; i < 4; ++i)
+                        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(row_o + 32 * w + 8 * i), "r"(o[8 * i]), "r"(o[8 * i + 1]),
+                                     "r"(o[8 * i + 2]), "r"(o[8 * i + 3]), "r"(o[8 * i + 4]), "r"(o[8 * i + 5]), "r"(o[8 * i + 6]), "r"(o[8 * i + 7])
+                                     : "memory");
                 }
-                __syncwarp();
             }
         }
         tmem_fence_before();
-        __syncwarp();
-        if (lane == 0) arrive(&c.drained);
     }
 }
 
@@ -872,9 +863,9 @@ __device__ __forceinline__ void work_records(const AttnArgs& a, const WarpStart&
 }
 
 // kWide: for batches of more than 128 query rows of a KV head, whose runs may have more than a stream holds.  The other kernel has half the softmax's
-// instructions to fetch, which shows where a CTA has a tile or two: four rows of 28/4 heads on 1369 tokens 9.5 us a layer with it, 10.4 with this one.
+// instructions to fetch, which shows where a CTA has a tile or two: four rows of 28/4 heads on 1369 tokens took 9.5 us a layer with it, 10.4 with this one.
 // (This one against that, when that still took such batches: 131009 tokens and 96 rows 151 against 173, 32768 and 32 rows 27.1 against 29.6, eleven
-// small groups at d = 64 24.2 against 22.8.)
+// small groups at d = 64 23.7 against 22.8.)
 template <int D, class T, bool kWide>
 __global__ void __launch_bounds__(kThreads, 1) attention_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ CUtensorMap mv,
                                                                 const __grid_constant__ AttnArgs a)
