@@ -224,6 +224,7 @@ __global__ void __launch_bounds__(kPlanMaxThreads) plan_kernel(StepPlanArgs a)
             }
         }
     }
+    __syncthreads();                       // (the search for the first large run below reads all rows' places)
     if (tid < 32) {
         // CTAs for large runs, the others for records: the cut at which the slower side is fastest.  (All lanes alike, but for the
         // shares, of which each other lane makes the other kind's.  Quotients are within two steps of 2^-24; 64-bit floating point is far slower.)
