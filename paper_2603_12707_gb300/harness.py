@@ -186,7 +186,12 @@ class SharedPrefixSession:
     A step: ``begin_step`` (slots, positions and the attention plan, on the device), then per layer ``append`` (queries
     and keys normed and rotated, K and V written into their slots) and ``attend``.  ``rope`` None: no rotation.  A token's position
     is its index behind the prefix; ``first_positions`` (a sequence) gives a request's first own token another than the
-    length of its prefix, as where an image takes fewer positions than tokens.
+    length of its prefix, as where an image takes fewer positions than tokens.  Those stay until ``grow`` is given others.
+
+    Where a session with a ``rope`` was not given any, requests' first positions follow their prefix: one that has been shortened, or
+    has outgrown ``prefix_lens``, counts with the length that it has (before that, and while it is held in part, with the length in
+    ``prefix_lens``).  A request that holds tokens turned for another length is not continued: ``grow`` refuses such a change.
+    (Without a ``rope`` nothing is turned, and first positions stay as they were made.)
 
     Ordered on its stream as ``Kv4Session`` is: ``begin_step``, ``append`` and ``attend`` only enqueue."""
 
@@ -204,11 +209,12 @@ class SharedPrefixSession:
             raise ValueError("prefix_of and lens must have an entry for each request")
         if not all(-1 <= g < len(prefix_lens) for g in self.prefix_of):
             raise ValueError("prefix_of must name one of prefix_lens, or -1")
+        self._follows = rope is not None and first_positions is None
+        self._counts = {g: int(n) for g, n in enumerate(prefix_lens)}      # tokens that a prefix counts for its requests' positions
+        self._moved = set()                                               # prefixes that have been shortened or have outgrown prefix_lens
         if first_positions is None:
-            first_positions = [int(prefix_lens[g]) if g >= 0 else 0 for g in self.prefix_of]
-        if len(first_positions) != cfg.batch:
-            raise ValueError("first_positions must have an entry for each request")
-        self.first_positions = [int(p) for p in first_positions]
+            first_positions = [self._counts[g] if g >= 0 else 0 for g in self.prefix_of]
+        self.first_positions = self._first_positions(first_positions)
         dtype = torch.bfloat16 if dtype is None else dtype
         P = kv4.PAGE_SIZE
         room = self.lens0 + np.array([extra_tokens] * cfg.batch + [0] * len(prefix_lens), dtype=np.int64)
@@ -232,12 +238,47 @@ class SharedPrefixSession:
     def _on_stream(self):
         return _on_stream(self.stream)
 
-    def grow(self, new_lens):
+    def _first_positions(self, given):
+        if len(given) != self.cfg.batch:
+            raise ValueError("first_positions must have an entry for each request")
+        return [int(p) for p in given]
+
+    def _follow(self, new):
+        """What prefixes count, which of them have moved, and first positions, once requests and prefixes have grown by new."""
+        batch, counts, moved, first = self.cfg.batch, dict(self._counts), set(self._moved), list(self.first_positions)
+        if not new[batch:].any():
+            return counts, moved, first
+        with self._on_stream():
+            before = np.array(self.tables.lens.tolist(), dtype=np.int64)      # (of the device: steps of graphs count there)
+        for g in (int(i) for i in np.flatnonzero(new[batch:])):
+            n = int((before + new)[batch + g])
+            if new[batch + g] < 0 or n > counts[g]:
+                moved.add(g)
+            if g in moved and n > 0:             # (a prefix that is gone may come again as it was)
+                counts[g] = n
+        for i, g in enumerate(self.prefix_of):
+            if g >= 0 and first[i] != counts[g]:
+                if before[i] > 0 and before[i] + new[i] > 0:
+                    raise ValueError(f"request {i} holds tokens turned as behind {first[i]} of prefix {g}, which would be {counts[g]}: "
+                                     "close it first, or give first_positions")
+                first[i] = counts[g]
+        return counts, moved, first
+
+    def grow(self, new_lens, first_positions=None):
         """Requests, then prefixes, grow by new_lens tokens (host sequence), or give -n back; returns the new tokens' slots
-        and positions.  A prefix may grow or be dropped only while no request that continues it takes a step."""
+        and positions.  A prefix may grow or be dropped only while no request that continues it takes a step.
+        first_positions: the requests' first positions from now on."""
         new = np.array([int(n) for n in new_lens], dtype=np.int64)
         added = int(np.maximum(new, 0).sum())
+        first = self.first_positions
+        if first_positions is not None:
+            first, self._follows = self._first_positions(first_positions), False
+        elif self._follows:
+            self._counts, self._moved, first = self._follow(new)
         with self._on_stream():
+            if first != self.first_positions:
+                self.first_positions = first
+                self.first.copy_(self._torch.tensor(first, dtype=self.first.dtype))
             dev = self._torch.tensor(new, **self._i32)
             slots = self._torch.empty(added, dtype=self._torch.int64, device=dev.device)
             index = self._torch.empty(added, **self._i32)
