@@ -85,7 +85,9 @@ KVC_API int kv_qk_rope(const kv_rope *rope, int32_t dtype, int32_t head_dim, int
 /* The same for n new tokens of a paged cache: normed and rotated keys, and the
  * values as they are, go to the tokens' slots (device int64 [n], page * 16 +
  * position % 16, distinct, as kv_tables_step gives them), the queries (or none:
- * num_q_heads 0) to q_out.  A slot of -1 is skipped, another one outside the pool
+ * num_q_heads 0) to q_out, which may be q as above.  The positions that kv_tables_step
+ * gives count a request's own tokens: where it continues a prefix (kv16_plan), the
+ * caller adds the first position behind that.  A slot of -1 is skipped, another one outside the pool
  * is skipped and sets KVC_DEVERR_PAGE_RANGE; the token's queries are written in
  * either case.  Without rope and weights it is a plain write. */
 KVC_API int kv16_write(const kv16_pool *pool, const kv_rope *rope, int32_t n, const int64_t *slots,
@@ -105,7 +107,9 @@ KVC_API int64_t kv16_workspace_bytes(const kv16_pool *pool, int32_t num_q_heads,
  *   prefix_ids  device [batch]: the request whose tokens row r attends to before
  *               its own, -1: none; NULL: none for all.  A prefix is a request of
  *               the same tables.  Rows that share one should follow one another: each
- *               run of neighbours with the same prefix reads it once
+ *               run of neighbours with the same prefix reads it once.  (Keys are in the
+ *               pool as they were turned: positions of own tokens behind a prefix are
+ *               the caller's, see kv16_write)
  *   workspace   device, 256-byte aligned, workspace_bytes >= kv16_workspace_bytes()
  *               for this batch.  It holds this plan until the next one, and serves
  *               calls that are ordered on one stream
