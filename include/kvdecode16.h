@@ -133,8 +133,10 @@ KVC_API int kv16_plan(const kv16_pool *pool, const kv_tables *tables, int32_t nu
  * tokens gives zeros and lse = -infinity.  The tokens of a page id outside the
  * pool are left out, with KVC_DEVERR_PAGE_RANGE.  A workspace without a plan
  * of this batch, num_q_heads and pool shape sets KVC_DEVERR_PLAN, and nothing is
- * written.  Scores, softmax statistics and sums are held in 32 bits; weights
- * meet V in the pool's type, at most half a step of it off.  The result of a call
+ * written.  Scores, softmax statistics and sums are held in 32 bits: scores of any
+ * size that are numbers there give weights that are.  Weights
+ * meet V in the pool's type, at most half a step of it off (fp16: weights below 2^-21 of the
+ * largest, 2^-32 of that).  The result of a call
  * does not depend on timing: partial results are merged in a fixed order. */
 KVC_API int kv16_attention(const kv16_pool *pool, const kv_tables *tables, int32_t batch, int32_t num_q_heads,
                            const void *q, int64_t q_stride, void *out, int64_t out_stride, float *lse,

@@ -19,8 +19,10 @@
 //   time, S^T = K q^T and O^T = V^T P^T on mma.sync with the query rows padded to 8 columns, each warp with a ring of its own.
 //   Bound by reading K and V: 64 rows of 32/32 heads and 640 to 1344 tokens 157 us a layer, 6.7 TB/s.
 //
-// The reference m of a row moves only when a score exceeds it by more than 8 in log2 units (weights stay below 2^8).
-// fp16 weights carry a factor 2^7 more, so that the small ones keep their bits.
+// The reference m of a row moves only when a score exceeds it by more than 8 in log2 units (weights stay at or below 2^8).
+// fp16 weights carry a factor 2^7 more, so that the small ones keep their bits; m does not, since sums and denominators both do.
+// Differences to the reference are taken before anything is added to them: far out, where the numbers of 32 bits are 2 apart and more,
+// m - 7 and m + 8 would be rounded to others, and weights with them past 2^16.
 #include <cudaTypedefs.h>
 #include <math.h>
 
@@ -83,6 +85,8 @@ struct AttnArgs {
     int64_t num_pages;
     int32_t* err;
 };
+
+constexpr float kFar = 0x1p20f;      // references from here on, in log2 units: half a unit in their last place is 2^-4 and more
 
 constexpr int kSegments = 8;         // told ahead: the ring has room for K and V of less than five tiles
 
@@ -372,7 +376,13 @@ __device__ __forceinline__ float max3(uint32_t a, uint32_t b, uint32_t c)
 // The softmax of a thread's row over N x 32 tokens whose scores are x.
 template <int D, class T>
 struct RowSoftmax {
-    float ref = -INFINITY, l = 0.f;   // reference, in log2 units; the sum of weights
+    float top = -INFINITY, l = 0.f;   // reference, as a score; the sum of weights
+    float sub = -Weights<T>::kShift;  // what weigh() takes off scores in log2 units
+    bool far = false;                 // a row of this warp's is far out
+
+    // The reference in log2 units, and whether it is far out.
+    __device__ __forceinline__ float reference(float sl) const { return __fmul_rn(top, sl); }
+    __device__ __forceinline__ bool is_far(float sl) const { return fabsf(reference(sl)) >= kFar && top != -INFINITY; }
 
     // Tokens that do not take part: bits of 16 for each page.
     template <int N>
@@ -385,31 +395,32 @@ struct RowSoftmax {
             for (int i = 0; i < 32; ++i) x[w][i] = bits >> i & 1u ? x[w][i] : 0xff800000u;
         }
     }
-    // Whether the reference has to move, and where to: a score exceeds it by more than 8 (see the top).
+    // Whether the reference has to move, and where to: a score exceeds it by more than 8 in log2 units (see the top).
     template <int N>
     __device__ __forceinline__ bool exceeds(const uint32_t (&x)[N][32], float sl, float* to) const
     {
-        float top[8];                                     // (eight chains)
+        float y[8];                                       // (eight chains)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top[i] = fmaxf(__uint_as_float(x[0][i]), __uint_as_float(x[1][i]));
+        for (int i = 0; i < 8; ++i) y[i] = fmaxf(__uint_as_float(x[0][i]), __uint_as_float(x[1][i]));
 #pragma unroll
-        for (int i = 8; i < 32; ++i) top[i & 7] = max3(__float_as_uint(top[i & 7]), x[0][i], x[1][i]);
+        for (int i = 8; i < 32; ++i) y[i & 7] = max3(__float_as_uint(y[i & 7]), x[0][i], x[1][i]);
 #pragma unroll
         for (int w = 2; w < N; w += 2)
 #pragma unroll
-            for (int i = 0; i < 32; ++i) top[i & 7] = max3(__float_as_uint(top[i & 7]), x[w][i], x[w + 1][i]);
+            for (int i = 0; i < 32; ++i) y[i & 7] = max3(__float_as_uint(y[i & 7]), x[w][i], x[w + 1][i]);
 #pragma unroll
         for (int d = 4; d > 0; d >>= 1)
 #pragma unroll
-            for (int i = 0; i < d; ++i) top[i] = fmaxf(top[i], top[i + d]);
-        *to = top[0] * sl;
-        return *to > ref + 8.f;
+            for (int i = 0; i < d; ++i) y[i] = fmaxf(y[i], y[i + d]);
+        *to = y[0];
+        return (y[0] - top) * sl > 8.f;
     }
     // It moves, and with it the sums so far, in whose columns nothing is under way (none: there are no sums yet).
-    __device__ __forceinline__ void move(bool moves, float to, bool none, uint32_t out)
+    __device__ __forceinline__ void move(bool moves, float to, float sl, bool none, uint32_t out)
     {
         if (!none) {
-            const float alpha = moves ? ex2(ref - to) : 1.f;
+            const float is = __fmul_rn(to, sl);
+            const float alpha = moves ? ex2(fabsf(is) >= kFar ? (top - to) * sl : reference(sl) - is) : 1.f;
             l *= alpha;
 #pragma unroll 1
             for (int w = 0; w < D / 16; ++w) {
@@ -422,12 +433,24 @@ struct RowSoftmax {
                 tmem_st16(out + 16 * w, o);
             }
         }
-        ref = moves ? to : ref;
+        top = moves ? to : top;
+        sub = (is_far(sl) || top == -INFINITY ? 0.f : reference(sl)) - Weights<T>::kShift;
+        far = __any_sync(0xffffffffu, is_far(sl));
+    }
+    // Weights come from one fused multiply-add of score, scale and the reference in log2 units, whose rounding is the same for all weights
+    // and for m.  Far out, where it counts, the reference is taken off the scores first.
+    template <int N>
+    __device__ __forceinline__ void approach(uint32_t (&x)[N][32], float sl) const
+    {
+        const float by = is_far(sl) ? top : 0.f;
+#pragma unroll
+        for (int w = 0; w < N; ++w)
+#pragma unroll
+            for (int i = 0; i < 32; ++i) x[w][i] = __float_as_uint(__uint_as_float(x[w][i]) - by);
     }
     // Weights of 32 tokens, in the pool's type, and their sum.
     __device__ __forceinline__ void weigh(const uint32_t (&x)[32], float sl, uint32_t (&p)[16])
     {
-        const float sub = (ref == -INFINITY ? 0.f : ref) - Weights<T>::kShift;
         const uint64_t sl2 = f2_pack(sl, sl), sub2 = f2_pack(-sub, -sub);
         uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
@@ -525,8 +548,9 @@ __device__ __forceinline__ void softmax_stream(const AttnArgs& a, Control& c, ui
                             if (!warp_wait(&c.done[stream], used & 1, c, a.err)) return;
                             tmem_fence_after();
                         }
-                        row.move(moves, mx, j == 0, to);
+                        row.move(moves, mx, sl, j == 0, to);
                     }
+                    if (__builtin_expect(row.far, false)) row.approach(x, sl);
                     row.weigh(x[0], sl, p);
                 }
                 // Weights lie where those of the tile before did, when these have met V (where the streams take turns, before these
@@ -567,8 +591,9 @@ __device__ __forceinline__ void softmax_stream(const AttnArgs& a, Control& c, ui
                                 if (!warp_wait(&c.half[stream], halves & 1, c, a.err)) return;
                                 tmem_fence_after();
                             }
-                            row.move(moves, mx, j == 0 && h == 0, to);
+                            row.move(moves, mx, sl, j == 0 && h == 0, to);
                         }
+                        if (__builtin_expect(row.far, false)) row.approach(x, sl);
                         row.weigh(x[0], sl, p);
                         tmem_st16(tp + 32 * h, p);
                         row.weigh(x[1], sl, p);
@@ -591,7 +616,7 @@ __device__ __forceinline__ void softmax_stream(const AttnArgs& a, Control& c, ui
             // A row's results, 32 bytes (a sector) of each at a time.  (By way of shared memory, so that a row's columns leave together: d = 64 4 %
             // longer, four rows on an image 9.2 us a layer instead of 8.8, one prefix of 32768 tokens 27.1 instead of 27.5.)
             const int64_t entry = s.entry + (stream == 0 ? 0 : s.rows0 * a.G);
-            if (my < qrows) a.view.run_ml[entry + my] = make_float2(some ? row.ref - Weights<T>::kShift : -INFINITY, some ? row.l : 0.f);
+            if (my < qrows) a.view.run_ml[entry + my] = make_float2(some ? row.reference(sl) : -INFINITY, some ? row.l : 0.f);
             float* const row_o = a.view.run_o + (entry + my) * D;
 #pragma unroll 1
             for (int w = 0; some && w < D / 32; ++w) {
@@ -768,7 +793,7 @@ __device__ __forceinline__ void work_records(const AttnArgs& a, const WarpStart&
                 }
                 float sc[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) sc[k] = (acc[0][k] + acc[1][k]) * a.scale_log2;
+                for (int k = 0; k < 4; ++k) sc[k] = __fmul_rn(acc[0][k] + acc[1][k], a.scale_log2);   // (not fused with the difference below)
                 // Lane: tokens lane / 4 and + 8, columns 2 (lane % 4) and + 1.
                 const int t0 = lane >> 2;
                 if (valid < kPageSize) {
@@ -776,7 +801,7 @@ __device__ __forceinline__ void work_records(const AttnArgs& a, const WarpStart&
                     if (t0 + 8 >= valid) sc[2] = sc[3] = -INFINITY;
                 }
                 const float x0 = fmaxf(sc[0], sc[2]), x1 = fmaxf(sc[1], sc[3]);
-                if (__any_sync(0xffffffffu, x0 > m0 + 8.f || x1 > m1 + 8.f)) {
+                if (__any_sync(0xffffffffu, x0 - m0 > 8.f || x1 - m1 > 8.f)) {
                     float y0 = x0, y1 = x1;
 #pragma unroll
                     for (int k = 4; k < 32; k <<= 1) {
@@ -798,8 +823,9 @@ __device__ __forceinline__ void work_records(const AttnArgs& a, const WarpStart&
                         o[i][3] *= f1;
                     }
                 }
-                const float s0 = (m0 == -INFINITY ? 0.f : m0) - Weights<T>::kShift, s1 = (m1 == -INFINITY ? 0.f : m1) - Weights<T>::kShift;
-                const float p0 = ex2(sc[0] - s0), p1 = ex2(sc[1] - s1), p2 = ex2(sc[2] - s0), p3 = ex2(sc[3] - s1);
+                constexpr float kShift = Weights<T>::kShift;
+                const float s0 = m0 == -INFINITY ? 0.f : m0, s1 = m1 == -INFINITY ? 0.f : m1;
+                const float p0 = ex2(sc[0] - s0 + kShift), p1 = ex2(sc[1] - s1 + kShift), p2 = ex2(sc[2] - s0 + kShift), p3 = ex2(sc[3] - s1 + kShift);
                 l0 += p0 + p2;
                 l1 += p1 + p3;
                 // P^T as B fragments: [token][column] to [column][token].
@@ -842,7 +868,7 @@ __device__ __forceinline__ void work_records(const AttnArgs& a, const WarpStart&
                 dst[16 * i] = o[i][k];
                 dst[16 * i + 8] = o[i][k + 2];
             }
-            if (lane < 4) a.view.rec_ml[entry + cc] = make_float2((k ? m1 : m0) - Weights<T>::kShift, k ? l1 : l0);
+            if (lane < 4) a.view.rec_ml[entry + cc] = make_float2(k ? m1 : m0, k ? l1 : l0);
         }
         // The next job.
         if (left > 0) {
@@ -1046,7 +1072,7 @@ __global__ void __launch_bounds__(128) merge_kernel(const __grid_constant__ Attn
     uint16_t* const dst = a.out + (int64_t)row * a.out_stride + (int64_t)head * D + lane * N;
     if constexpr (N == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(T::pack(o[0], o[1]), T::pack(o[2], o[3]));
     else *reinterpret_cast<uint32_t*>(dst) = T::pack(o[0], o[1]);
-    if (a.lse && lane == 0) a.lse[(int64_t)row * a.hq + head] = sum == 0.f ? -INFINITY : top * 0.693147180559945309f + logf(sum);
+    if (a.lse && lane == 0) a.lse[(int64_t)row * a.hq + head] = sum == 0.f ? -INFINITY : top * 0.693147180559945309f + logf(sum * exp2f(-Weights<T>::kShift));
 }
 
 PFN_cuTensorMapEncodeTiled_v12000 encoder()
