@@ -136,7 +136,9 @@ KVC_API int kv16_plan(const kv16_pool *pool, const kv_tables *tables, int32_t nu
  * written.  Scores, softmax statistics and sums are held in 32 bits: scores of any
  * size that are numbers there give weights that are.  Weights
  * meet V in the pool's type, at most half a step of it off (fp16: weights below 2^-21 of the
- * largest, 2^-32 of that).  The result of a call
+ * largest, 2^-32 of that).  Outputs that would round to an infinity are the type's
+ * largest number; sums of weights up to 2^8 times V have to be numbers of 32 bits (bf16:
+ * V below 2^88 always is).  The result of a call
  * does not depend on timing: partial results are merged in a fixed order. */
 KVC_API int kv16_attention(const kv16_pool *pool, const kv_tables *tables, int32_t batch, int32_t num_q_heads,
                            const void *q, int64_t q_stride, void *out, int64_t out_stride, float *lse,

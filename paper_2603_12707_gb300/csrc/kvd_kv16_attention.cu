@@ -63,12 +63,12 @@ struct Geo {
 };
 
 template <class T>
-struct Weights {   // weights in the pool's type: log2 of the factor that they carry
-    static constexpr float kShift = 0.f;
+struct Weights {   // weights in the pool's type: log2 of the factor that they carry; and the type's largest number
+    static constexpr float kShift = 0.f, kMost = 0x1.fep127f;
 };
 template <>
 struct Weights<Fp16> {
-    static constexpr float kShift = 7.f;
+    static constexpr float kShift = 7.f, kMost = 65504.f;
 };
 
 struct AttnArgs {
@@ -1067,7 +1067,9 @@ __global__ void __launch_bounds__(128) merge_kernel(const __grid_constant__ Attn
         float y = 0.f;
 #pragma unroll
         for (int k = 0; k < 4; ++k) y += f[k] * s_o[k][lane * N + i];
-        o[i] = y * inv;
+        // (An average of numbers at the end of the range, taken with rounded weights, may pass it.)
+        y *= inv;
+        o[i] = fabsf(y) < INFINITY ? fminf(fmaxf(y, -Weights<T>::kMost), Weights<T>::kMost) : y;
     }
     uint16_t* const dst = a.out + (int64_t)row * a.out_stride + (int64_t)head * D + lane * N;
     if constexpr (N == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(T::pack(o[0], o[1]), T::pack(o[2], o[3]));

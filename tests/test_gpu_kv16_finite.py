@@ -90,3 +90,33 @@ def test_far_scores_that_rise(kvlib, dtype, on_prefix, hq, hkv, base):
     assert (err <= (UNIT[dtype] * (1 + UNIT[dtype]) * 1.001 + UNIT[dtype]) * mag + 2.0 ** -14 * vd.abs().max()).all(), float(err.max())
     top = (base + step) * math.log(2)
     assert ((lse - top - math.log(w.sum())).abs() <= 2.0 ** -21 * top + 2.0 ** -14).all()
+
+
+@pytest.mark.parametrize("on_prefix,hq,hkv", SHAPES)
+def test_values_at_the_end_of_the_range(kvlib, on_prefix, hq, hkv):
+    """V is 65504 or its negative in all tokens of an element.  The tokens that count for most follow, in nearly all of a worker's shares, others that
+    set the reference 7 lower; their weights, 2^14.0007, are rounded up by 2^-11.1.  An average of equal numbers stays among the type's numbers."""
+    n, d, batch = 100000, 64, on_prefix or 6
+    score = torch.full((n,), -20.0)
+    score[::128], score[1000::2048] = 0.0, 7.0
+    k = torch.zeros((n, hkv, d), dtype=FP)
+    k[..., 0], k[1000::2048, :, 1] = score.to(FP)[:, None], 0.76
+    v = torch.full((n, hkv, d), 65504.0, dtype=FP)
+    v[..., 1::2] *= -1
+    q = torch.zeros((batch, hq, d), dtype=FP)
+    q[..., 0], q[..., 1] = 1.0, 2.0 ** -10
+    out, lse = attend(kvlib, k, v, q, on_prefix, LN2)
+    assert torch.isfinite(out).all()
+    assert ((out - v[0].double().repeat_interleave(hq // hkv, 0)).abs() <= 65504 * 2.0 ** -10).all()
+    exact = score.double() + k[:, 0, 1].double() * 2.0 ** -10
+    assert ((lse - math.log(torch.exp2(exact).sum())).abs() <= 2.0 ** -14).all()
+
+
+def test_infinite_values_stay_infinite(kvlib):
+    n, d = 40, 64
+    v = torch.zeros((n, 2, d), dtype=FP)
+    v[3, 0, 5], v[7, 1, 9] = math.inf, -math.inf
+    out, _ = attend(kvlib, torch.zeros((n, 2, d), dtype=FP), v, torch.ones((20, 4, d), dtype=FP), 20, 1.0)
+    assert (out[:, :2, 5] == math.inf).all() and (out[:, 2:, 9] == -math.inf).all()
+    out[:, :2, 5] = out[:, 2:, 9] = 0
+    assert (out == 0).all()
