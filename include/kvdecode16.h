@@ -133,7 +133,8 @@ KVC_API int kv16_plan(const kv16_pool *pool, const kv_tables *tables, int32_t nu
  * tokens gives zeros and lse = -infinity.  The tokens of a page id outside the
  * pool are left out, with KVC_DEVERR_PAGE_RANGE.  A workspace without a plan
  * of this batch, num_q_heads and pool shape sets KVC_DEVERR_PLAN, and nothing is
- * written.  Scores, softmax statistics and sums are held in 32 bits: scores of any
+ * written.  Waits in the kernel end after a second or so: should one run out, the call and
+ * those that follow by the same plan set KVC_DEVERR_WAIT_TIMEOUT, and outputs are NaN.  Scores, softmax statistics and sums are held in 32 bits: scores of any
  * size that are numbers there give weights that are.  Weights
  * meet V in the pool's type, at most half a step of it off (fp16: weights below 2^-21 of the
  * largest, 2^-32 of that).  Outputs that would round to an infinity are the type's

@@ -111,9 +111,9 @@ template <int D>
 constexpr int kSharedBytes = Geo<D>::kData + (int)sizeof(Control);
 static_assert(kSharedBytes<128> <= 232448 && kSharedBytes<64> <= 232448, "shared memory of a CTA");
 
-__device__ __forceinline__ bool plan_fits(const PlanHeader& h, const AttnArgs& a)
+__device__ __forceinline__ bool plan_fits(const PlanHeader& h, const AttnArgs& a, uint32_t magic = kPlanMagic)
 {
-    return h.magic == kPlanMagic && h.batch == a.batch && h.hq == a.hq && h.hkv == a.hkv && h.dim == a.dim && h.grid == a.grid &&
+    return h.magic == magic && h.batch == a.batch && h.hq == a.hq && h.hkv == a.hkv && h.dim == a.dim && h.grid == a.grid &&
            h.max_seqs == a.max_seqs && h.max_pages == a.max_pages;
 }
 
@@ -936,10 +936,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kernel(const __grid_con
     if (!fits || records) {
         if (warp == kMmaWarp) tmem_dealloc(c.tmem, 512);
         if (!fits) {
-            if (tid == 0 && blockIdx.x == 0) kv4_error(a.err, KVC_DEVERR_PLAN);
+            if (tid == 0 && blockIdx.x == 0) kv4_error(a.err, plan_fits(h, a, kPlanGaveUp) ? KVC_DEVERR_WAIT_TIMEOUT : KVC_DEVERR_PLAN);
             return;
         }
         work_records<D, T>(a, mine, c, smem, &mk, &mv);
+        if (*reinterpret_cast<volatile int32_t*>(&c.gave_up)) a.view.header->magic = kPlanGaveUp;
         return;
     }
     if (warp < kSoftmaxWarps) {
@@ -963,6 +964,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_kernel(const __grid_con
     __syncthreads();
     tmem_fence_after();
     if (warp == kMmaWarp) tmem_dealloc(c.tmem, 512);
+    if (tid == 0 && c.gave_up) a.view.header->magic = kPlanGaveUp;
 }
 
 // ---------------------------------------------------------------------- merge
@@ -983,7 +985,13 @@ __global__ void __launch_bounds__(128) merge_kernel(const __grid_constant__ Attn
     const int kv = (int)((uint32_t)head * ((65536u + a.G - 1) / a.G) >> 16), g = head - kv * a.G;   // (head < 8192, G <= 8)
     const RowSources x = a.view.rows[(int64_t)row * a.hkv + kv];
     const PlanHeader h = *a.view.header;
-    if (!plan_fits(h, a)) return;
+    if (!plan_fits(h, a)) {
+        if (plan_fits(h, a, kPlanGaveUp)) {           // partial results are not all there, or those of another call
+            for (int i = threadIdx.x; i < D; i += 128) a.out[(int64_t)row * a.out_stride + (int64_t)head * D + i] = (uint16_t)T::pack(NAN, NAN);
+            if (a.lse && threadIdx.x == 0) a.lse[(int64_t)row * a.hq + head] = NAN;
+        }
+        return;
+    }
     const int own = x.own_count, total = own + x.prefix_count;
     const bool run = x.stream_step >= 0;
 

@@ -22,6 +22,7 @@ constexpr int kRecordCols = 8;          // query rows of a record's job at most
 constexpr int kTileRows = 128;          // query rows of one of a CTA's two streams
 constexpr int kTilePages = 8;           // of a tile of a large run: 128 tokens
 constexpr uint32_t kPlanMagic = 0x16a77e41u;
+constexpr uint32_t kPlanGaveUp = 0x16a77e42u;   // of a plan by which attention gave up a wait: it serves no call any more, and outputs become NaN
 
 // Cost of a page of a large run's job, with both streams on rows of their own or taking turns, and what opening and
 // closing a job costs beside, in such pages; a record's page.  (In units of some 20 cycles of an SM; the minima are flat: with records at

@@ -10,7 +10,7 @@ _record = [(n, "<i4") for n in ("req", "len", "pages", "row0", "rows", "unit", "
 _run = [("req", "<i4"), ("len", "<i4"), ("pages", "<i4"), ("rows", "<i4"), ("cost", "<i8"), ("rows_before", "<i4"), ("chunks", "<i4")]
 _segment = [(n, "<i4") for n in ("pages", "valid", "wide", "head", "row0", "rows", "rows0", "first")] + [("entry", "<i8")]
 _shares = [("each", "<i8"), ("inverse", "<f4"), ("n", "<i4")]
-HEADER = np.dtype([(n, "<i4") for n in ("magic", "batch", "hq", "hkv", "dim", "grid", "max_seqs", "max_pages", "prefix_ctas", "gave_up")]
+HEADER = np.dtype([(n, "<i4") for n in ("magic", "batch", "hq", "hkv", "dim", "grid", "max_seqs", "max_pages", "prefix_ctas", "pad")]
                   + [("units", _shares), ("cost", _shares)])
 RECORD, RUN = np.dtype(_record), np.dtype(_run)
 ROW = np.dtype([("own", "<i8"), ("prefix", "<i8")] + [(n, "<i4") for n in ("own_count", "prefix_count", "step", "stream_step")])
