@@ -808,11 +808,10 @@ __device__ __forceinline__ void work_records(const AttnArgs& a, const WarpStart&
                         y0 = fmaxf(y0, __shfl_xor_sync(0xffffffffu, y0, k));
                         y1 = fmaxf(y1, __shfl_xor_sync(0xffffffffu, y1, k));
                     }
-                    y0 = fmaxf(y0, m0);
-                    y1 = fmaxf(y1, m1);
-                    const float f0 = y0 == m0 ? 1.f : ex2(m0 - y0), f1 = y1 == m1 ? 1.f : ex2(m1 - y1);
-                    m0 = y0;
-                    m1 = y1;
+                    const bool moves0 = y0 - m0 > 8.f, moves1 = y1 - m1 > 8.f;   // (no column looks at another's)
+                    const float f0 = moves0 ? ex2(m0 - y0) : 1.f, f1 = moves1 ? ex2(m1 - y1) : 1.f;
+                    m0 = moves0 ? y0 : m0;
+                    m1 = moves1 ? y1 : m1;
                     l0 *= f0;
                     l1 *= f1;
 #pragma unroll
