@@ -313,6 +313,17 @@ struct OncePerDevice {
     }
 };
 
+// Threads of a kernel that asks for more registers than its block was launched with wait for them forever.  Success where blocks of `warps` get
+// `needed` (a lane of each warp's, added up); `ask` writes the kernel's registers a thread, which are handed out in eights, and its failure
+// is the result's.
+template <class Ask>
+cudaError_t enough_registers(int warps, int needed, Ask ask)
+{
+    int registers = 0;
+    if (cudaError_t e = ask(&registers); e != cudaSuccess) return e;
+    return (registers + 7) / 8 * 8 * warps >= needed ? cudaSuccess : cudaErrorLaunchOutOfResources;
+}
+
 int32_t noalloc_chunk_cap(bool gqa, int num_kv_heads, int64_t warps, int64_t rows, int64_t pages, int64_t max_pages,
                           int32_t T);
 

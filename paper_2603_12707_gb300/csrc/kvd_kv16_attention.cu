@@ -43,7 +43,8 @@ static_assert(kThreads == 32 * kAttnWarps);
 // Registers of a thread at launch, and then by what its warp does.  (A row's 128 scores have to stay in registers: with 168 for
 // all some spill, and the tile above takes 4600 cycles.)
 constexpr int kRegisters = 168, kSoftmaxRegisters = 208, kOtherRegisters = 88;
-static_assert(kSoftmaxWarps * kSoftmaxRegisters + 4 * kOtherRegisters <= (kSoftmaxWarps + 4) * kRegisters);
+constexpr int kMovedRegisters = kSoftmaxWarps * kSoftmaxRegisters + 4 * kOtherRegisters;   // of a lane of each warp
+static_assert(kMovedRegisters <= (kSoftmaxWarps + 4) * kRegisters);
 constexpr int kLoadWarp = kSoftmaxWarps, kMmaWarp = kSoftmaxWarps + 1;
 constexpr int kOut = 256;                          // first column of the sums in tensor memory
 
@@ -1113,16 +1114,20 @@ template <int D, class T, bool kWide>
 int launch_attention(const CUtensorMap& mk, const CUtensorMap& mv, const AttnArgs& a, cudaStream_t st)
 {
     const auto kernel = attention_kernel<D, T, kWide>;
-    static OncePerDevice once;
-    if (cudaError_t e = once.set_attribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes<D>); e != cudaSuccess)
-        return kv4_launch_result(e);
-    if (kWide) {   // (threads that ask for more registers than the block was launched with would wait for them forever)
-        static const int registers = [&] {
+    static OncePerDevice once;                        // (what fails is tried again by the next call)
+    int device = 0;
+    if (cudaError_t e = cudaGetDevice(&device); e != cudaSuccess) return kv4_launch_result(e);
+    const cudaError_t ready = once(device, [&] {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedBytes<D>);
+        if (e != cudaSuccess || !kWide) return e;
+        return enough_registers(kSoftmaxWarps + 4, kMovedRegisters, [&](int* n) {
             cudaFuncAttributes f{};
-            return cudaFuncGetAttributes(&f, kernel) == cudaSuccess ? f.numRegs : 0;
-        }();
-        if (registers != kRegisters) return kv4_fail(KVC_ERR_CUDA, "kv16_attention: the kernel was built with other registers than it moves");
-    }
+            const cudaError_t asked = cudaFuncGetAttributes(&f, kernel);
+            *n = f.numRegs;
+            return asked;
+        });
+    });
+    if (ready != cudaSuccess) return kv4_launch_result(ready);
     if (cudaError_t e = kv4_launch(kernel, dim3((unsigned)a.grid), kThreads, kSharedBytes<D>, st, mk, mv, a); e != cudaSuccess)
         return kv4_launch_result(e);
     return kv4_launch_result(kv4_launch(merge_kernel<D, T>, dim3((unsigned)a.hq, (unsigned)a.batch), 128, 0, st, a));
