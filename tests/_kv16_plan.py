@@ -1,10 +1,17 @@
 """What a plan of kv16_plan says, checked as a whole: every page of every record and every large run is one worker's, and the
 merge looks for partial results where those workers put them.  Worked out here from the lengths and the two numbers of
 workers that the plan's header holds; works on a workspace's bytes, wherever they were made."""
+import os
+import re
+
 import numpy as np
 
-P, WARPS, COLS, TILE = 16, 12, 8, 128
-WIDE, NARROW, OPENS = 24, 12, {24: 20, 12: 30}    # cost of a page, and pages that opening a job counts
+_text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2603_12707_gb300", "csrc", "kvd_kv16_plan.h")).read()
+_consts = {n: int(v.rstrip("u"), 0) for n, v in re.findall(r"\b(k\w+) = (0x[0-9a-f]+u|\d+)\b", _text)}
+P, WARPS, COLS, TILE = 16, _consts["kAttnWarps"], _consts["kRecordCols"], _consts["kTileRows"]
+WIDE, NARROW = _consts["kWideCost"], _consts["kNarrowCost"]                      # cost of a page,
+OPENS = {WIDE: _consts["kWideStart"], NARROW: _consts["kNarrowStart"]}           # and pages that opening a job counts
+MADE, GAVE_UP = _consts["kPlanMagic"], _consts["kPlanGaveUp"]
 
 _record = [(n, "<i4") for n in ("req", "len", "pages", "row0", "rows", "unit", "col", "pad")]
 _run = [("req", "<i4"), ("len", "<i4"), ("pages", "<i4"), ("rows", "<i4"), ("cost", "<i8"), ("rows_before", "<i4"), ("chunks", "<i4")]
@@ -35,7 +42,7 @@ def check_plan(workspace, lens, seq_ids, prefix_ids, hq, hkv, dim, grid):
     batch, g = len(prefix_ids), hq // hkv
     header, recs, runs, rows, warps, ctas = parts(workspace, batch, hkv, grid)
     h = header[0]
-    assert h["magic"] == 0x16a77e41 and (h["batch"], h["hq"], h["hkv"], h["dim"], h["grid"]) == (batch, hq, hkv, dim, grid)
+    assert h["magic"] == MADE and (h["batch"], h["hq"], h["hkv"], h["dim"], h["grid"]) == (batch, hq, hkv, dim, grid)
     prefix = [int(p) if p >= 0 and lens[p] > 0 else -1 for p in prefix_ids]
 
     # Records and runs.

@@ -4,11 +4,11 @@ import pytest
 import torch
 
 from _kv16_common import assert_attention, attention, make_pool, make_tables
+from _kv16_plan import GAVE_UP, MADE
 
 pytestmark = pytest.mark.gpu
 
 TIMEOUT, PLAN = 2, 16      # KVC_DEVERR_*
-MADE, GAVE_UP = 0x16a77e41, 0x16a77e42
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
