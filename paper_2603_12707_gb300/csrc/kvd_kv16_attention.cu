@@ -17,7 +17,7 @@
 //   131009 tokens, 96 rows of 28/4 heads: 151 us a layer, 1.19 PFLOP/s.
 // * A row's own tokens, and prefixes of up to 8 query rows: a warp takes a page (16 tokens) at a
 //   time, S^T = K q^T and O^T = V^T P^T on mma.sync with the query rows padded to 8 columns, each warp with a ring of its own.
-//   Bound by reading K and V: 64 rows of 32/32 heads and 640 to 1344 tokens 157 us a layer, 6.7 TB/s.
+//   Bound by reading K and V: 64 rows of 32/32 heads and 640 to 1344 tokens 155 us a layer, 6.7 TB/s.
 //
 // The reference m of a row moves only when a score exceeds it by more than 8 in log2 units (weights stay at or below 2^8).
 // fp16 weights carry a factor 2^7 more, so that the small ones keep their bits; m does not, since sums and denominators both do.
@@ -889,7 +889,7 @@ __device__ __forceinline__ void work_records(const AttnArgs& a, const WarpStart&
 }
 
 // kWide: for batches of more than 128 query rows of a KV head, whose runs may have more than a stream holds.  The other kernel has half the softmax's
-// instructions to fetch, which shows where a CTA has a tile or two: four rows of 28/4 heads on 1369 tokens took 9.5 us a layer with it, 10.4 with this one.
+// instructions to fetch, which shows where a CTA has a tile or two: four rows of 28/4 heads on 1369 tokens take 9.0 us a layer with it, 9.2 with this one.
 // (This one against that, when that still took such batches: 131009 tokens and 96 rows 151 against 173, 32768 and 32 rows 27.1 against 29.6, eleven
 // small groups at d = 64 23.7 against 22.8.)
 template <int D, class T, bool kWide>

@@ -256,7 +256,7 @@ cudaError_t launch_rope(RopeArgs& a, int kind, cudaStream_t st)
     constexpr int kHeads = 32 / (D / 16);
     const int heads = a.hq + (POOL ? 2 : 1) * a.hkv;
     // A warp goes over all heads of its token, whose angles it works out once; with few tokens the heads are
-    // shared among more warps.
+    // shared among more warps.  (152 SMs of a GB300, with up to 32 warps each; nothing but this split depends on the number.)
     const int most = (heads + kHeads - 1) / kHeads;
     int64_t parts = ((int64_t)152 * 32 + a.n - 1) / a.n;
     parts = parts < 1 ? 1 : parts < most ? parts : most;

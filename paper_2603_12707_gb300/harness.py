@@ -188,6 +188,8 @@ class SharedPrefixSession:
     is its index behind the prefix; ``first_positions`` (a sequence) gives a request's first own token another than the
     length of its prefix, as where an image takes fewer positions than tokens.  Those stay until ``grow`` is given others.
 
+    Requests that share a prefix read it once where they are neighbours in the workload: ``prefix_of`` is best ordered by prefix.
+
     Where a session with a ``rope`` was not given any, requests' first positions follow their prefix: one that has been shortened, or
     has outgrown ``prefix_lens``, counts with the length that it has (before that, and while it is held in part, with the length in
     ``prefix_lens``).  A request that holds tokens turned for another length is not continued: ``grow`` refuses such a change.
